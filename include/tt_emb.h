@@ -598,6 +598,105 @@ int tt_emb_debug_dedup(const tt_shape_t *shape, const int64_t *indices, int64_t 
  * call that follows must be made under the same value. */
 int tt_emb_debug_set_fast_path(int mode);
 
+/*
+ * ---- Operators at a language model's way in: token embedding, dropout, residual addition + RMS norm ----
+ *
+ * They work on arrays of rows in 32- and 16-bit types.  Every sum, mean square and gradient is held in 32 bits; a value is
+ * rounded once, when it is stored.  Arrays need no more alignment than their elements; rows may be parts of wider ones (odd
+ * strides included), and an array that is only read may repeat one row (ld = 0).  Unless a comment says otherwise no output
+ * overlaps another array.  Sizes: less than 2^31 rows and 2^20 columns (32,768 in the norms), element offsets of 64 bits.
+ * The results are bit-identical from run to run.  n_rows == 0 or L == 0 is valid.
+ */
+enum {
+    TT_F32 = 0,
+    TT_BF16 = 1,
+    TT_F16 = 2,
+    TT_E4M3 = 3          /* 8 bits, 4 of exponent and 3 of mantissa, no infinities, largest value 448 */
+};
+
+/* Rows of an array: row r begins at data + r * ld elements.  The struct is host memory, data is device memory. */
+typedef struct tt_rows_t {
+    void *data;
+    int64_t ld;
+    int32_t type;
+} tt_rows_t;
+
+/* L tokens of 32 or 64 bits (signed), one after the other.  Host struct, device data.  A token outside [0, num_rows) is no
+ * token (padding): its row is zero and it has no gradient. */
+typedef struct tt_tokens_t {
+    const void *data;
+    int64_t L;
+    int32_t bits;
+} tt_tokens_t;
+
+/*
+ * Dropout whose mask is never stored: whether an element is kept depends on its row, its column, `site` and the two device
+ * words `state` alone, so that the backward pass finds the same elements again, and a recorded graph new ones when the program
+ * has changed the words.  Generator: Philox4x32-10 (Salmon et al., SC 2011), key = state[0] (seed), counter = (block low, block
+ * high, site, low 32 bits of state[1] (step)) with block = row * ceil(N / 8) + column / 8; column c of the block has 16 bits,
+ * half c & 1 (low first) of word (c & 7) / 2.  Kept iff they are at least q = round(65536 p), and multiplied by
+ * 65536 / (65536 - q); dropped elements are 0, whatever they were.  q == 0 drops nothing, p == 1 everything.
+ * site: the dropout's number within the model.  Host struct.
+ */
+typedef struct tt_dropout_t {
+    const int64_t *state;
+    uint32_t site;
+    float p;
+} tt_dropout_t;
+
+/* output[t][:] = dropout(scale * table[token t][:]); dropout == NULL: none.  The table's and the output's types are free. */
+int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_tokens_t *tokens, float scale,
+                 const tt_dropout_t *dropout, const tt_rows_t *output, void *stream);
+
+/*
+ * Gradient of the table: row v is scale * (sum over the positions t of token v, of grad_output[t][:], dropped out as in the
+ * forward pass).  The positions are sorted by token and every row is written once.  accumulate == 0: all num_rows rows are
+ * written, zeros where no token is; else the sums are added to grad_table, whose other rows are not touched.
+ * tt_token_bwd_sgd: table -= lr * gradient in place, rows in use only.
+ * workspace: tt_token_bwd_workspace_bytes(L, N) bytes, 16-byte aligned (enough for fewer tokens too).  L < 2^28.
+ */
+size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t N);
+int tt_token_bwd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
+                 const tt_rows_t *grad_table, int64_t num_rows, int64_t N, int accumulate,
+                 void *workspace, size_t workspace_bytes, void *stream);
+int tt_token_bwd_sgd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
+                     const tt_rows_t *table, int64_t num_rows, int64_t N, float lr,
+                     void *workspace, size_t workspace_bytes, void *stream);
+
+/* output = dropout(x) + residual (NULL: none) and its gradient grad_x = dropout(grad_output) (the residual's is grad_output
+ * itself).  All arrays have one type.  output may be x or residual, grad_x may be grad_output. */
+int tt_dropout_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_dropout_t *dropout, const tt_rows_t *output,
+                   int64_t n_rows, int64_t N, void *stream);
+int tt_dropout_bwd(const tt_rows_t *grad_output, const tt_dropout_t *dropout, const tt_rows_t *grad_x, int64_t n_rows, int64_t N, void *stream);
+
+/*
+ * h = residual + dropout(x);  rstd = 1 / sqrt(mean of h^2 over the row + eps);  y = h * rstd * weight.
+ * residual, dropout, weight: NULL for none.  sum: h, stored (NULL: not).  rstd: fp32 [n_rows] or NULL; it and y come from the
+ * unrounded h.  Types: x any of 32 or 16 bits; residual and sum x's or 32 bits; weight any, N values; output x's, or TT_E4M3.
+ * TT_E4M3: output = y / s rounded to the nearest even, s = max |y| / 448 over the row (group == 0) or over each group of
+ * 32, 64 or 128 columns; scales: fp32 rows of 1 or ceil(N / group) values.  A scale below 2^-126 is stored as 0, with values 0.
+ * NaN in y makes its scale and all values under that scale NaN.  scales == NULL and group == 0 for other types.
+ * output may be x, and sum may be residual.
+ */
+int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_dropout_t *dropout, const void *weight, int32_t weight_type,
+                        float eps, const tt_rows_t *sum, const tt_rows_t *output, float *rstd, const tt_rows_t *scales, int32_t group,
+                        int64_t n_rows, int64_t N, void *stream);
+
+/*
+ * Gradients, from the stored h and rstd.  With g = grad_output * weight:
+ *   dh = rstd * (g - h * rstd^2 * mean(g * h)) + grad_sum,   grad_residual = dh,   grad_x = dropout(dh),
+ *   grad_weight = sum over the rows of grad_output * h * rstd.
+ * grad_sum: the gradient that reaches h through the residual stream, NULL for none.  grad_x, grad_residual, grad_weight: any of
+ * them may be NULL.  Types: grad_output and grad_x one, any of 32 or 16 bits; h, grad_sum and grad_residual one, that or 32 bits;
+ * weight and grad_weight any.  accumulate != 0 adds to grad_weight.  grad_x may be grad_output, grad_residual may be grad_sum.
+ * workspace: tt_add_rms_norm_bwd_workspace_bytes(n_rows, N) bytes, 16-byte aligned, if grad_weight is asked for.
+ */
+size_t tt_add_rms_norm_bwd_workspace_bytes(int64_t n_rows, int64_t N);
+int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const float *rstd, const void *weight, int32_t weight_type,
+                        const tt_rows_t *grad_sum, const tt_dropout_t *dropout, const tt_rows_t *grad_x, const tt_rows_t *grad_residual,
+                        void *grad_weight, int32_t grad_weight_type, int accumulate, int64_t n_rows, int64_t N,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import torch
 
@@ -33,7 +33,9 @@ EXPORTS = ("tt_last_error", "tt_cache_table_capacity", "tt_emb_workspace_bytes",
            "tt_emb_mean_weights", "tt_init_sampled_gaussian", "tt_embd_fwd", "tt_embd_bwd", "tt_embd_sgd_update", "tt_freq_reset", "tt_freq_update", "tt_freq_export", "tt_dense_bag_fwd", "tt_dense_bag_bwd_sgd", "tt_dense_bag_bwd_sgd_merged", "tt_dense_bag_bwd_workspace_bytes",
            "tt_emb_validate", "tt_emb_debug_launch_probe", "tt_emb_kept_bytes", "tt_emb_kept_has_lists", "tt_emb_kept_prepare", "tt_emb_fwd_keep", "tt_emb_bwd_kept", "tt_emb_bwd_sgd_kept", "tt_emb_debug_kept_lists", "tt_emb_bwd_sgd_static", "tt_emb_static_scratch_bytes", "tt_emb_fwd_keep_t0", "tt_emb_bwd_t0", "tt_emb_bwd_sgd_t0", "tt_emb_bwd_prepare", "tt_emb_fwd_prepared", "tt_emb_fwd_uses_lists", "tt_emb_bwd_sgd_prepared", "tt_emb_bwd_has_prepass", "tt_emb_bwd_two_calls_group_earlier",
            "tt_emb_fwd", "tt_emb_bwd", "tt_emb_bwd_sgd", "tt_emb_sgd_update", "tt_cache_build", "tt_cache_lookup",
-           "tt_emb_debug_decode", "tt_emb_debug_decode_as", "tt_emb_debug_dedup", "tt_emb_debug_set_fast_path")
+           "tt_emb_debug_decode", "tt_emb_debug_decode_as", "tt_emb_debug_dedup", "tt_emb_debug_set_fast_path",
+           "tt_token_fwd", "tt_token_bwd_workspace_bytes", "tt_token_bwd", "tt_token_bwd_sgd", "tt_dropout_fwd", "tt_dropout_bwd",
+           "tt_add_rms_norm_fwd", "tt_add_rms_norm_bwd_workspace_bytes", "tt_add_rms_norm_bwd")
 
 
 class TTShape(C.Structure):
@@ -124,6 +126,17 @@ def lib():
         l.tt_emb_debug_decode_as.argtypes = [vp, vp, i64, C.c_int, vp, vp, vp, vp]
         l.tt_emb_debug_dedup.argtypes = [vp, vp, i64, vp, C.c_int, vp, vp, vp, vp, vp, C.c_size_t, vp]
         l.tt_emb_debug_set_fast_path.argtypes = [C.c_int]
+        l.tt_token_fwd.argtypes = [vp, i64, i64, vp, f32, vp, vp, vp]
+        l.tt_token_bwd_workspace_bytes.restype = C.c_size_t
+        l.tt_token_bwd_workspace_bytes.argtypes = [i64, i64]
+        l.tt_token_bwd.argtypes = [vp, vp, f32, vp, vp, i64, i64, C.c_int, vp, C.c_size_t, vp]
+        l.tt_token_bwd_sgd.argtypes = [vp, vp, f32, vp, vp, i64, i64, f32, vp, C.c_size_t, vp]
+        l.tt_dropout_fwd.argtypes = [vp, vp, vp, vp, i64, i64, vp]
+        l.tt_dropout_bwd.argtypes = [vp, vp, vp, i64, i64, vp]
+        l.tt_add_rms_norm_fwd.argtypes = [vp, vp, vp, vp, C.c_int32, f32, vp, vp, vp, vp, C.c_int32, i64, i64, vp]
+        l.tt_add_rms_norm_bwd_workspace_bytes.restype = C.c_size_t
+        l.tt_add_rms_norm_bwd_workspace_bytes.argtypes = [i64, i64]
+        l.tt_add_rms_norm_bwd.argtypes = [vp, vp, vp, vp, C.c_int32, vp, vp, vp, vp, vp, C.c_int32, C.c_int, i64, i64, vp, C.c_size_t, vp]
         _lib = l
     return _lib
 
@@ -598,3 +611,101 @@ def tt_embd_sgd_update(shape: TTShapeD, cores: Sequence[torch.Tensor], grad_core
                        zero_grad: bool = False) -> None:
     _check(lib().tt_embd_sgd_update(C.byref(shape), _ptr_array_d(cores), _ptr_array_d(grad_cores), C.c_float(lr),
                                     int(zero_grad), _stream()))
+
+
+# ---- operators at a language model's way in -------------------------------------------------------------------------
+# Arrays are tensors of rows, [..., N]: float32, bfloat16 or float16, the last dimension dense, the others evenly spaced (parts
+# of wider arrays and, for what is only read, expanded rows among them).  They allocate nothing but scratch memory, where the
+# workspace is left out (not under capture: a recorded call needs its workspace).
+
+
+class TTRows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("type", C.c_int32)]
+
+
+class TTTokens(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("L", C.c_int64), ("bits", C.c_int32)]
+
+
+class TTDropout(C.Structure):
+    _fields_ = [("state", C.c_void_p), ("site", C.c_uint32), ("p", C.c_float)]
+
+
+class Dropout(NamedTuple):
+    """p: the share that is dropped.  state: int64 [2] on the device, (seed, step); the backward pass of a step must see the words
+    of its forward pass.  site: the dropout's number within the model.  A plain tuple (p, state, site) will do as well."""
+    p: float
+    state: torch.Tensor
+    site: int = 0
+
+
+def tt_token_fwd(table: torch.Tensor, tokens: torch.Tensor, output: torch.Tensor, scale: float = 1.0,
+                 dropout: Optional[Dropout] = None) -> torch.Tensor:
+    """output[t] = dropout(scale * table[tokens[t]]); tokens int64 or int32, those outside [0, rows of the table) give zeros."""
+    rc = _call.token_fwd(table, tokens, output, scale, dropout)
+    if rc:
+        _check(rc)
+    return output
+
+
+def token_bwd_workspace_bytes(L: int, N: int) -> int:
+    return int(lib().tt_token_bwd_workspace_bytes(int(L), int(N)))
+
+
+def tt_token_bwd(tokens: torch.Tensor, grad_output: torch.Tensor, grad_table: torch.Tensor, scale: float = 1.0,
+                 dropout: Optional[Dropout] = None, accumulate: bool = False, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The table's gradient: all of its rows are written, or, with accumulate, the sums are added to the rows in use."""
+    rc = _call.token_bwd(tokens, grad_output, grad_table, scale, dropout, workspace, accumulate)
+    if rc:
+        _check(rc)
+    return grad_table
+
+
+def tt_token_bwd_sgd(tokens: torch.Tensor, grad_output: torch.Tensor, table: torch.Tensor, lr: float, scale: float = 1.0,
+                     dropout: Optional[Dropout] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """table -= lr * gradient, in place, on the rows in use."""
+    rc = _call.token_bwd_sgd(tokens, grad_output, table, scale, dropout, workspace, lr)
+    if rc:
+        _check(rc)
+    return table
+
+
+def tt_dropout_fwd(x: torch.Tensor, output: torch.Tensor, dropout: Dropout, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """output = dropout(x) + residual."""
+    rc = _call.dropout_fwd(x, output, dropout, residual)
+    if rc:
+        _check(rc)
+    return output
+
+
+def tt_dropout_bwd(grad_output: torch.Tensor, grad_x: torch.Tensor, dropout: Dropout) -> torch.Tensor:
+    rc = _call.dropout_bwd(grad_output, grad_x, dropout)
+    if rc:
+        _check(rc)
+    return grad_x
+
+
+def tt_add_rms_norm_fwd(x: torch.Tensor, weight: Optional[torch.Tensor], output: torch.Tensor, residual: Optional[torch.Tensor] = None,
+                        sum_out: Optional[torch.Tensor] = None, rstd: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                        group: int = 0, eps: float = 1e-6, dropout: Optional[Dropout] = None) -> torch.Tensor:
+    """h = residual + dropout(x), output = h * rstd * weight; output float8_e4m3fn: with scales, float32 [..., 1] (group 0) or
+    [..., ceil(N / group)].  sum_out takes h and rstd (float32, one per row) what the backward pass needs beside it."""
+    rc = _call.add_rms_norm_fwd(x, weight, output, residual, sum_out, rstd, scales, group, eps, dropout)
+    if rc:
+        _check(rc)
+    return output
+
+
+def add_rms_norm_bwd_workspace_bytes(n_rows: int, N: int) -> int:
+    return int(lib().tt_add_rms_norm_bwd_workspace_bytes(int(n_rows), int(N)))
+
+
+def tt_add_rms_norm_bwd(grad_output: torch.Tensor, h: torch.Tensor, rstd: torch.Tensor, weight: Optional[torch.Tensor],
+                        grad_x: Optional[torch.Tensor], grad_weight: Optional[torch.Tensor], grad_sum: Optional[torch.Tensor] = None,
+                        grad_residual: Optional[torch.Tensor] = None, dropout: Optional[Dropout] = None, accumulate: bool = False,
+                        workspace: Optional[torch.Tensor] = None) -> None:
+    """Gradients of x, of the residual and of the weight (None: not wanted) from those of the output and, grad_sum, of h.  Without a
+    dropout, and with a residual of x's type, grad_x is the residual's gradient too."""
+    rc = _call.add_rms_norm_bwd(grad_output, h, rstd, weight, grad_x, grad_weight, grad_sum, grad_residual, dropout, accumulate, workspace)
+    if rc:
+        _check(rc)

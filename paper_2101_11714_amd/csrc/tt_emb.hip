@@ -4,12 +4,11 @@
 
 #include "../../include/tt_emb.h"
 
-#include <stdarg.h>
 #include <initializer_list>
 #include <mutex>
-#include <stdio.h>
 #include <string.h>
 
+#include "tt_error.h"
 #include "tt_common.h"
 #include "tt_sort.h"
 #include "tt_select.h"
@@ -39,7 +38,6 @@ static __device__ __align__(256) unsigned char scratch[STATIC_SCRATCH_BYTES];
 
 namespace {
 
-thread_local char g_err[512] = "";
 // Kernel selection of the calling thread (tests only; no other thread's calls change with it):
 // 0: generic kernels, 1: specialised, 2: specialised + grouping pre-pass always + list owners always
 thread_local int g_fast_path = 1;
@@ -119,15 +117,6 @@ int64_t group_min_l(const Params &p, int64_t K, bool kept_t0, bool two_calls)
     return K ? GROUP_MIN_L_CACHE : GROUP_MIN_L;
 }
 
-int fail(int code, const char *fmt, ...)
-{
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(g_err, sizeof(g_err), fmt, ap);
-    va_end(ap);
-    return code;
-}
-
 int check_shape(const tt_shape_t *s, Params *p)
 {
     if (!s) return fail(TT_ERR_NULL, "shape is NULL");
@@ -192,11 +181,6 @@ bool misaligned(std::initializer_list<const void *> ptrs)
     uintptr_t bits = 0;
     for (const void *q : ptrs) bits |= (uintptr_t)q;
     return (bits & 15) != 0;
-}
-
-int hip_fail(hipError_t e, const char *what)
-{
-    return fail(TT_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
 size_t lds_limit()

@@ -77,6 +77,104 @@ struct Args {
         return t->data_ptr();
     }
 
+    // a device tensor seen as rows: its last dimension is dense, the others are one dimension of evenly spaced rows (a row stride
+    // of 0, as expand() makes it, is one)
+    bool rows(int i, tt_rows_t *r, int64_t *n, int64_t *N)
+    {
+        *r = tt_rows_t{nullptr, 0, -1};
+        *n = *N = 0;
+        const at::Tensor *t = ok ? tensor(a[i]) : nullptr;
+        if (!t) return false;
+        if (!t->is_cuda()) return fail("a device tensor is expected");
+        switch (t->scalar_type()) {
+        case at::kFloat: r->type = TT_F32; break;
+        case at::kBFloat16: r->type = TT_BF16; break;
+        case at::kHalf: r->type = TT_F16; break;
+        case at::kFloat8_e4m3fn: r->type = TT_E4M3; break;
+        default: return fail("a tensor of 32- or 16-bit floating values (or float8_e4m3fn) is expected");
+        }
+        const int64_t d = t->dim();
+        if (d < 1) return fail("a tensor of rows is expected");
+        *N = t->size(d - 1);
+        if (*N > 1 && t->stride(d - 1) != 1) return fail("rows must be dense");
+        int64_t n_rows = 1, step = 0, next = 0;              // next: the stride that an outer dimension must have
+        bool any = false;
+        for (int64_t k = d - 2; k >= 0; --k) {
+            const int64_t size = t->size(k);
+            n_rows *= size;
+            if (size <= 1) continue;
+            if (!any) step = t->stride(k);
+            else if (t->stride(k) != next) return fail("rows must be evenly spaced");
+            next = t->stride(k) * size;
+            any = true;
+        }
+        *n = n_rows;
+        r->ld = any ? step : *N;
+        r->data = n_rows && *N ? t->data_ptr() : nullptr;
+        return true;
+    }
+    // the same, of n rows of N columns, or None: null
+    const tt_rows_t *rows_or_null(int i, tt_rows_t *r, int64_t n, int64_t N)
+    {
+        int64_t rn, rN;
+        if (!ok || a[i] == Py_None || !rows(i, r, &rn, &rN)) return nullptr;
+        if (rn != n || rN != N) fail("an array has other sizes than the others");
+        return r;
+    }
+    // tokens: contiguous, of 32 or 64 bits
+    tt_tokens_t tokens(int i)
+    {
+        const at::Tensor *t = ok ? tensor(a[i]) : nullptr;
+        if (!t) return {};
+        const bool wide = t->scalar_type() == at::kLong;
+        if (!t->is_cuda() || !(wide || t->scalar_type() == at::kInt) || !t->is_contiguous()) {
+            fail("a contiguous device tensor of int64 or int32 tokens is expected");
+            return {};
+        }
+        return {t->numel() ? t->data_ptr() : nullptr, t->numel(), wide ? 64 : 32};
+    }
+    // None, or (p, state, site)
+    const tt_dropout_t *dropout(int i, tt_dropout_t *d)
+    {
+        if (!ok || a[i] == Py_None) return nullptr;
+        if (!PyTuple_Check(a[i]) || PyTuple_GET_SIZE(a[i]) != 3) {
+            fail("dropout is (p, state, site)");
+            return nullptr;
+        }
+        int64_t n = 0;
+        d->state = (const int64_t *)dev(PyTuple_GET_ITEM(a[i], 1), at::kLong, &n);
+        if (!ok) return nullptr;
+        if (n < 2) {
+            fail("dropout's state is two 64-bit words");
+            return nullptr;
+        }
+        const double p = PyFloat_AsDouble(PyTuple_GET_ITEM(a[i], 0));
+        const long long site = PyLong_AsLongLong(PyTuple_GET_ITEM(a[i], 2));
+        if (PyErr_Occurred()) {
+            ok = false;
+            return nullptr;
+        }
+        if (site < 0 || site > 0xffffffffll) {
+            fail("dropout's site has 32 bits");
+            return nullptr;
+        }
+        d->p = (float)p;
+        d->site = (uint32_t)site;
+        return d;
+    }
+    // a dense vector of N values of any floating type, or None
+    void *vector_or_null(int i, int64_t N, int32_t *type)
+    {
+        *type = TT_F32;
+        if (!ok || a[i] == Py_None) return nullptr;
+        tt_rows_t r;
+        int64_t n, rN;
+        if (!rows(i, &r, &n, &rN)) return nullptr;
+        if (n != 1 || rN != N) fail("a vector has another size than the rows");
+        *type = r.type;
+        return r.data;
+    }
+
     int64_t integer(int i)
     {
         if (!ok) return 0;
@@ -569,6 +667,160 @@ TT_FUNCTION(freq_export)
     return call([&](void *st) { return tt_freq_export(f, rows, counts, n_out, st); });
 }
 
+// table tokens output scale dropout
+TT_FUNCTION(token_fwd)
+{
+    Args g(args, nargs, 5);
+    if (!g.ok) return nullptr;
+    tt_rows_t table, out;
+    tt_dropout_t d;
+    int64_t num_rows, N, L, M;
+    g.rows(0, &table, &num_rows, &N);
+    const tt_tokens_t tokens = g.tokens(1);
+    g.rows(2, &out, &L, &M);
+    const float scale = g.real(3);
+    const tt_dropout_t *drop = g.dropout(4, &d);
+    if (g.ok && (L != tokens.L || M != N)) g.fail("output has another size");
+    if (!g.ok) return nullptr;
+    return call([&](void *st) { return tt_token_fwd(&table, num_rows, N, &tokens, scale, drop, &out, st); });
+}
+
+// tokens grad_output table scale dropout workspace f(...)
+template <typename F>
+PyObject *token_grad(Args &g, F f)
+{
+    tt_rows_t go, table;
+    tt_dropout_t d;
+    int64_t L, M, num_rows, N;
+    size_t wsb;
+    const tt_tokens_t tokens = g.tokens(0);
+    g.rows(1, &go, &L, &M);
+    g.rows(2, &table, &num_rows, &N);
+    const float scale = g.real(3);
+    const tt_dropout_t *drop = g.dropout(4, &d);
+    void *ws = g.bytes_or_null(5, &wsb);
+    if (g.ok && (L != tokens.L || M != N)) g.fail("grad_output has another size");
+    if (!g.ok) return nullptr;
+    at::DataPtr mem;
+    if (!ws) {
+        wsb = tt_token_bwd_workspace_bytes(L, N);
+        mem = scratch(wsb, stream());
+        if (!mem) wsb = 0;
+        ws = mem.get();
+    }
+    return call([&](void *st) { return f(&tokens, &go, scale, drop, &table, num_rows, N, ws, wsb, st); });
+}
+
+// tokens grad_output grad_table scale dropout workspace accumulate
+TT_FUNCTION(token_bwd)
+{
+    Args g(args, nargs, 7);
+    if (!g.ok) return nullptr;
+    const bool add = g.truth(6);
+    if (!g.ok) return nullptr;
+    return token_grad(g, [&](auto t, auto go, float scale, auto drop, auto table, int64_t rows, int64_t N, void *ws, size_t wsb, void *st) {
+        return tt_token_bwd(t, go, scale, drop, table, rows, N, add ? 1 : 0, ws, wsb, st);
+    });
+}
+
+// tokens grad_output table scale dropout workspace lr
+TT_FUNCTION(token_bwd_sgd)
+{
+    Args g(args, nargs, 7);
+    if (!g.ok) return nullptr;
+    const float lr = g.real(6);
+    if (!g.ok) return nullptr;
+    return token_grad(g, [&](auto t, auto go, float scale, auto drop, auto table, int64_t rows, int64_t N, void *ws, size_t wsb, void *st) {
+        return tt_token_bwd_sgd(t, go, scale, drop, table, rows, N, lr, ws, wsb, st);
+    });
+}
+
+// x output dropout residual
+TT_FUNCTION(dropout_fwd)
+{
+    Args g(args, nargs, 4);
+    if (!g.ok) return nullptr;
+    tt_rows_t x, out, r;
+    tt_dropout_t d;
+    int64_t n, N;
+    g.rows(0, &x, &n, &N);
+    const tt_rows_t *o = g.rows_or_null(1, &out, n, N);
+    const tt_dropout_t *drop = g.dropout(2, &d);
+    const tt_rows_t *res = g.rows_or_null(3, &r, n, N);
+    if (!g.ok) return nullptr;
+    return call([&](void *st) { return tt_dropout_fwd(&x, res, drop, o, n, N, st); });
+}
+
+// grad_output grad_x dropout
+TT_FUNCTION(dropout_bwd)
+{
+    Args g(args, nargs, 3);
+    if (!g.ok) return nullptr;
+    tt_rows_t go, gx;
+    tt_dropout_t d;
+    int64_t n, N;
+    g.rows(0, &go, &n, &N);
+    const tt_rows_t *x = g.rows_or_null(1, &gx, n, N);
+    const tt_dropout_t *drop = g.dropout(2, &d);
+    if (!g.ok) return nullptr;
+    return call([&](void *st) { return tt_dropout_bwd(&go, drop, x, n, N, st); });
+}
+
+// x weight output residual sum rstd scales group eps dropout
+TT_FUNCTION(add_rms_norm_fwd)
+{
+    Args g(args, nargs, 10);
+    if (!g.ok) return nullptr;
+    tt_rows_t x, out, res, sum, sc;
+    tt_dropout_t d;
+    int64_t n, N, nr = 0;
+    int32_t wt;
+    g.rows(0, &x, &n, &N);
+    const void *w = g.vector_or_null(1, N, &wt);
+    const tt_rows_t *o = g.rows_or_null(2, &out, n, N), *r = g.rows_or_null(3, &res, n, N), *s = g.rows_or_null(4, &sum, n, N);
+    float *rstd = g.f32_or_null(5, &nr);
+    const int64_t group = g.integer(7);
+    const tt_rows_t *scales = g.rows_or_null(6, &sc, n, group > 0 ? (N + group - 1) / group : 1);
+    const float eps = g.real(8);
+    const tt_dropout_t *drop = g.dropout(9, &d);
+    if (g.ok && rstd && nr != n) g.fail("rstd has another size");
+    if (g.ok && (group < 0 || group > 128)) g.fail("group is 0, 32, 64 or 128");
+    if (!g.ok) return nullptr;
+    return call([&](void *st) { return tt_add_rms_norm_fwd(&x, r, drop, w, wt, eps, s, o, rstd, scales, (int32_t)group, n, N, st); });
+}
+
+// grad_output h rstd weight grad_x grad_weight grad_sum grad_residual dropout accumulate workspace
+TT_FUNCTION(add_rms_norm_bwd)
+{
+    Args g(args, nargs, 11);
+    if (!g.ok) return nullptr;
+    tt_rows_t go, h, gx, gs, gr;
+    tt_dropout_t d;
+    int64_t n, N, nr = 0;
+    int32_t wt, gwt;
+    size_t wsb;
+    g.rows(0, &go, &n, &N);
+    const tt_rows_t *hp = g.rows_or_null(1, &h, n, N);
+    const float *rstd = g.f32(2, &nr);
+    const void *w = g.vector_or_null(3, N, &wt);
+    const tt_rows_t *x = g.rows_or_null(4, &gx, n, N);
+    void *gw = g.vector_or_null(5, N, &gwt);
+    const tt_rows_t *s = g.rows_or_null(6, &gs, n, N), *r = g.rows_or_null(7, &gr, n, N);
+    const tt_dropout_t *drop = g.dropout(8, &d);
+    const bool add = g.truth(9);
+    void *ws = g.bytes_or_null(10, &wsb);
+    if (g.ok && nr != n) g.fail("rstd has another size");
+    if (!g.ok) return nullptr;
+    at::DataPtr mem;
+    if (!ws && gw) {
+        wsb = tt_add_rms_norm_bwd_workspace_bytes(n, N);
+        mem = scratch(wsb, stream());
+        if (!mem) wsb = 0;
+        ws = mem.get();
+    }
+    return call([&](void *st) { return tt_add_rms_norm_bwd(&go, hp, rstd, w, wt, s, drop, x, r, gw, gwt, add ? 1 : 0, n, N, ws, wsb, st); });
+}
+
 #define TT_METHOD(name, function) {name, (PyCFunction)(void (*)(void))guarded<function>, METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
@@ -587,6 +839,13 @@ PyMethodDef methods[] = {
     TT_METHOD("emb_sgd_update", emb_sgd_update),
     TT_METHOD("freq_update", freq_update),
     TT_METHOD("freq_export", freq_export),
+    TT_METHOD("token_fwd", token_fwd),
+    TT_METHOD("token_bwd", token_bwd),
+    TT_METHOD("token_bwd_sgd", token_bwd_sgd),
+    TT_METHOD("dropout_fwd", dropout_fwd),
+    TT_METHOD("dropout_bwd", dropout_bwd),
+    TT_METHOD("add_rms_norm_fwd", add_rms_norm_fwd),
+    TT_METHOD("add_rms_norm_bwd", add_rms_norm_bwd),
     TT_METHOD("cache_build", cache_fill<tt_cache_build>),
     TT_METHOD("cache_refill", cache_fill<tt_cache_refill>),
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,582 @@
+"""Token embedding, dropout and residual addition + RMS norm against plain implementations in 64 bits (lm_util.py).
+
+Bounds.  A value is rounded once to its type (unit roundoff u) after sums in 32 bits: a product of k factors is off by k 2^-24 of
+itself, a sum of n terms by n 2^-24 of the sum of the terms' magnitudes at most, whatever its order."""
+
+import numpy as np
+import pytest
+import torch
+
+import lm_util as R
+from lm_util import U32, UNIT, TINY
+from paper_2101_11714_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16, F16, E4M3 = torch.float32, torch.bfloat16, torch.float16, torch.float8_e4m3fn
+TYPES = [F32, BF16, F16]
+
+
+def gen(seed):
+    return torch.Generator().manual_seed(seed)
+
+
+def room(rows, N, dtype, lead=0, shift=0):
+    """Rows to write into, with a guard value before, between and behind them."""
+    flat = torch.full((shift + rows * (N + lead) + 8,), 7.0, dtype=torch.float32, device="cuda:0").to(dtype)
+    return torch.as_strided(flat, (rows, N), (N + lead, 1), shift), flat
+
+
+def assert_guard(view, flat):
+    """What lies outside of the rows still has its value."""
+    m = torch.ones_like(flat, dtype=torch.bool)
+    torch.as_strided(m, view.shape, view.stride(), view.storage_offset()).fill_(False)
+    assert bool((flat.float()[m] == 7.0).all())
+
+
+def dropout_of(p, seed=1234567890123456789, step=41, site=5):
+    return None if p is None else B.Dropout(p, torch.tensor([seed, step], dtype=torch.int64, device="cuda:0"), site)
+
+
+def tokens_of(g, L, vocab, kind, dtype=torch.int64):
+    if kind == "uniform":
+        t = torch.randint(0, vocab, (L,), generator=g)
+    elif kind == "hot":                                     # half of the positions have one token
+        t = torch.where(torch.rand(L, generator=g) < 0.5, vocab // 2, torch.randint(0, vocab, (L,), generator=g))
+    elif kind == "one":
+        t = torch.full((L,), vocab - 1)
+    elif kind == "none":
+        t = torch.where(torch.rand(L, generator=g) < 0.5, -1, vocab)
+    else:                                                   # some have none, with every way of saying so
+        t = torch.randint(-3, vocab + 3, (L,), generator=g)
+    return t.to(dtype).to("cuda:0")
+
+
+# ---- token embedding --------------------------------------------------------------------------------------------------
+
+SHAPES = [(1, 10, 1), (3, 7, 2), (5, 100, 7), (64, 50, 8), (65, 50, 9), (257, 1000, 16), (1000, 300, 64), (33, 40, 100), (130, 513, 513),
+          (48, 1000, 1024), (17, 600, 2047), (9, 100, 4096), (4, 30, 8200), (2, 5, 20001)]
+
+
+@pytest.mark.parametrize("L,vocab,N", SHAPES)
+@pytest.mark.parametrize("p", [None, 0.25])
+def test_token_fwd(L, vocab, N, p):
+    g, d = gen(L + N), dropout_of(p)
+    for s, o, ids, lead, shift in [(F32, F32, torch.int64, 0, 0), (BF16, BF16, torch.int32, 3, 1), (F16, F32, torch.int64, 8, 0), (F32, BF16, torch.int32, 1, 2),
+                                   (BF16, F16, torch.int64, 0, 4), (F16, BF16, torch.int64, 5, 3), (BF16, F32, torch.int64, 0, 0), (F32, F16, torch.int64, 2, 0), (F16, F16, torch.int32, 0, 1)]:
+        table = R.rows_of(g, vocab, N, s, lead, shift)
+        tokens = tokens_of(g, L, vocab, "some", ids)
+        out, flat = room(L, N, o, lead, shift)
+        assert B.tt_token_fwd(table, tokens, out, scale=1.75, dropout=d) is out
+        want = R.token_fwd(table, tokens, 1.75, d)
+        R.assert_within(out, want, np.abs(want) * (UNIT[o] + 4 * U32) + TINY[o], (s, o))
+        assert_guard(out, flat)
+
+
+def test_token_fwd_many_rows_and_leading_dimensions():
+    # several rows per thread; tokens and output of three dimensions; a table of one repeated row
+    g = gen(3)
+    for L, vocab, N in [(70_001, 500, 8), (40_000, 300, 16), (9_000, 100, 1000)]:
+        table, tokens = R.rows_of(g, vocab, N, BF16), tokens_of(g, L, vocab, "some")
+        out = room(L, N, BF16)[0]
+        B.tt_token_fwd(table, tokens, out)
+        want = R.token_fwd(table, tokens, 1.0, None)
+        assert np.array_equal(R.f64(out), want)
+    table, tokens = R.rows_of(g, 50, 24, F32), tokens_of(g, 60, 50, "some").view(3, 4, 5)
+    out = torch.empty((3, 4, 5, 24), device="cuda:0")
+    B.tt_token_fwd(table, tokens, out)
+    assert np.array_equal(R.f64(out).reshape(60, 24), R.token_fwd(table, tokens, 1.0, None))
+    one = table[:1].expand(50, 24)
+    B.tt_token_fwd(one, tokens, out)
+    assert np.array_equal(R.f64(out).reshape(60, 24), R.token_fwd(one, tokens, 1.0, None))
+
+
+def test_token_rows_past_32_bits():
+    # element offsets of 2^32 and more in the table, forward and step
+    rows, N = (1 << 26) + 100, 64
+    table = torch.empty((rows, N), dtype=BF16, device="cuda:0")
+    picks = torch.tensor([0, 5, (1 << 25) - 1, 1 << 25, (1 << 26) - 1, 1 << 26, rows - 1, rows, -1, rows - 1], device="cuda:0")
+    used = picks[(picks >= 0) & (picks < rows)]
+    table[used] = torch.randn((used.numel(), N), generator=gen(4)).to(BF16).to("cuda:0")
+    before = table[used].double().cpu()
+    out = torch.empty((picks.numel(), N), dtype=BF16, device="cuda:0")
+    B.tt_token_fwd(table, picks, out)
+    assert torch.equal(out[:7].double().cpu(), before[:7]) and not out[7:9].any() and torch.equal(out[9], out[6])
+    grad = torch.ones((picks.numel(), N), dtype=BF16, device="cuda:0")
+    B.tt_token_bwd_sgd(picks, grad, table, 1.0)
+    times = torch.tensor([1, 1, 1, 1, 1, 1, 2, 2.0])[:, None]
+    want = (before.float() - times).to(BF16)
+    assert torch.equal(table[used].cpu(), want)
+
+
+GRADS = [(1, 1, 1, "uniform"), (1, 9, 5, "none"), (2, 3, 8, "one"), (7, 5, 16, "hot"), (8, 4, 9, "some"), (9, 100, 64, "uniform"), (100, 511, 24, "some"),
+         (255, 512, 100, "hot"), (300, 513, 513, "some"), (1023, 40, 64, "one"), (2048, 1000, 40, "hot"), (2049, 70, 33, "some"), (4097, 3000, 17, "some"),
+         (600, 50, 4100, "hot"), (20_000, 60, 16, "hot"), (20_011, 30_000, 8, "some"), (150_000, 1 << 18, 4, "hot"), (150_001, 700, 3, "some"), (16_400, 3, 20, "one")]
+
+
+def check_grad(L, vocab, N, kind, gt, ot, ids, p, lead, shift, mode):
+    g, d = gen(L + 7 * N), dropout_of(p)
+    tokens = tokens_of(g, L, vocab, kind, ids)
+    grad = R.rows_of(g, L, N, gt, lead, shift, 0.5)
+    want, mag, most = R.token_bwd(tokens, grad, vocab, 1.5, d)
+    out, flat = room(vocab, N, ot, lead, shift)
+    bound = (most + 4) * U32 * mag
+    if mode == "write":
+        got = B.tt_token_bwd(tokens, grad, out, scale=1.5, dropout=d)
+    else:
+        old = R.rows_of(g, vocab, N, ot, lead, shift)
+        out.copy_(old)
+        if mode == "add":
+            got, want = B.tt_token_bwd(tokens, grad, out, scale=1.5, dropout=d, accumulate=True), R.f64(old) + want
+        else:
+            got, want, bound = B.tt_token_bwd_sgd(tokens, grad, out, 0.5, scale=1.5, dropout=d), R.f64(old) - 0.5 * want, 0.5 * bound
+        bound = bound + 2 * U32 * np.abs(R.f64(old))
+        untouched = mag.max(1) == 0
+        assert np.array_equal(R.f64(out)[untouched], R.f64(old)[untouched])
+    assert got is out
+    R.assert_within(out, want, bound + np.abs(want) * (UNIT[ot] + 2 * U32) + TINY[ot], (gt, ot, mode))
+    assert_guard(out, flat)
+
+
+@pytest.mark.parametrize("L,vocab,N,kind", GRADS)
+@pytest.mark.parametrize("mode,gt,ot,ids,p,lead,shift", [("write", F32, F32, torch.int64, None, 0, 0), ("write", BF16, F32, torch.int32, 0.3, 3, 1), ("write", F16, F16, torch.int64, None, 0, 5),
+                                                         ("add", BF16, BF16, torch.int64, None, 8, 0), ("add", F16, F32, torch.int32, 0.1, 1, 0), ("sgd", F32, F32, torch.int64, 0.5, 0, 3),
+                                                         ("sgd", BF16, BF16, torch.int32, None, 2, 2)])
+def test_token_bwd(L, vocab, N, kind, mode, gt, ot, ids, p, lead, shift):
+    check_grad(L, vocab, N, kind, gt, ot, ids, p, lead, shift, mode)
+
+
+@pytest.mark.parametrize("gt", TYPES)
+@pytest.mark.parametrize("ot", TYPES)
+def test_token_bwd_types(gt, ot):
+    check_grad(700, 90, 72, "hot", gt, ot, torch.int64, 0.2, 0, 0, "write")
+
+
+def test_token_bwd_of_nothing():
+    out, flat = room(20, 30, F32, 2, 1)
+    empty = torch.empty(0, dtype=torch.int64, device="cuda:0")
+    B.tt_token_bwd(empty, torch.empty((0, 30), device="cuda:0"), out)
+    assert not out.any()
+    assert_guard(out, flat)
+    old = out.fill_(3.0).clone()
+    B.tt_token_bwd(empty, torch.empty((0, 30), device="cuda:0"), out, accumulate=True)
+    B.tt_token_bwd_sgd(empty, torch.empty((0, 30), device="cuda:0"), out, 1.0)
+    assert torch.equal(out, old)
+    B.tt_token_fwd(old, empty, torch.empty((0, 30), device="cuda:0"))
+
+
+def test_token_bwd_of_a_broadcast_gradient():
+    # every position has the same gradient row (a row stride of 0)
+    tokens = tokens_of(gen(5), 500, 40, "some")
+    row = torch.randn((1, 48), generator=gen(6)).to("cuda:0")
+    out = torch.empty((40, 48), device="cuda:0")
+    B.tt_token_bwd(tokens, row.expand(500, 48), out)
+    want, mag, most = R.token_bwd(tokens, row.expand(500, 48), 40, 1.0, None)
+    R.assert_within(out, want, (most + 4) * U32 * mag)
+
+
+def test_token_gradient_is_the_difference_quotient():
+    # f(table) = <G, token_fwd(table)> is linear: its difference in one entry, over a step of 1, is the gradient there
+    g, d = gen(8), dropout_of(0.3)
+    table, tokens = R.rows_of(g, 30, 20, F32), tokens_of(g, 200, 30, "some")
+    G = R.rows_of(g, 200, 20, F32)
+    grad = torch.empty((30, 20), device="cuda:0")
+    B.tt_token_bwd(tokens, G, grad, scale=2.0, dropout=d)
+
+    def f(t):
+        return float((B.tt_token_fwd(t, tokens, torch.empty((200, 20), device="cuda:0"), scale=2.0, dropout=d).double() * G.double()).sum())
+
+    base = f(table)
+    for v, c in [(0, 0), (7, 19), (29, 3), (15, 8)]:
+        moved = table.clone()
+        moved[v, c] += 1.0
+        step = float(moved[v, c].double() - table[v, c].double())
+        assert abs((f(moved) - base) / step - float(grad[v, c])) < 1e-4     # 32-bit products: 200 of them of size 10 at most, 2^-24 each
+
+
+@pytest.mark.parametrize("L,vocab,N", [(3000, 50, 40), (20_000, 1000, 24), (140_000, 5000, 8)])
+def test_token_bwd_is_the_same_every_time_and_with_any_workspace(L, vocab, N):
+    g = gen(9)
+    tokens, grad = tokens_of(g, L, vocab, "hot"), R.rows_of(g, L, N, F32)
+    outs = []
+    need = B.token_bwd_workspace_bytes(L, N)
+    for ws in (None, torch.full((need,), 255, dtype=torch.uint8, device="cuda:0"), torch.zeros(B.token_bwd_workspace_bytes(2 * L, N), dtype=torch.uint8, device="cuda:0")):
+        outs.append(B.tt_token_bwd(tokens, grad, torch.empty((vocab, N), device="cuda:0"), workspace=ws))
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+# ---- dropout ------------------------------------------------------------------------------------------------------------
+
+DROPS = [(1, 1), (1, 8), (3, 7), (5, 9), (64, 16), (257, 777), (1000, 33), (100, 1024), (7, 8195), (40_000, 24), (9_000, 1000)]
+
+
+@pytest.mark.parametrize("rows,N", DROPS)
+@pytest.mark.parametrize("dtype,p,lead,shift", [(F32, 0.1, 0, 0), (BF16, 0.5, 3, 1), (F16, 0.9, 8, 3)])
+def test_dropout(rows, N, dtype, p, lead, shift):
+    g, d = gen(rows + N), dropout_of(p)
+    x, r = R.rows_of(g, rows, N, dtype, lead, shift), R.rows_of(g, rows, N, dtype, lead, shift)
+    want = R.drop(R.f64(x), d)
+    for residual in (None, r):
+        out, flat = room(rows, N, dtype, lead, shift)
+        B.tt_dropout_fwd(x, out, d, residual=residual)
+        w = want if residual is None else want + R.f64(r)
+        R.assert_within(out, w, np.abs(w) * (UNIT[dtype] + U32) + 2 * U32 * np.abs(want) + TINY[dtype])
+        assert_guard(out, flat)
+    out, flat = room(rows, N, dtype, lead, shift)
+    B.tt_dropout_bwd(x, out, d)
+    R.assert_within(out, want, np.abs(want) * (UNIT[dtype] + 2 * U32) + TINY[dtype])
+    assert_guard(out, flat)
+    inplace = x.clone()
+    B.tt_dropout_bwd(inplace, inplace, d)
+    assert torch.equal(inplace, out)
+
+
+def test_dropout_shares_and_limits():
+    x = torch.ones((1000, 1000), device="cuda:0")
+    for p in (0.1, 0.5, 0.75):
+        out = B.tt_dropout_fwd(x, torch.empty_like(x), dropout_of(p))
+        kept = float((out != 0).double().mean())
+        assert abs(kept - (1 - p)) < 6 * (p * (1 - p) / 1e6) ** 0.5         # six standard deviations
+        assert abs(float(out.max()) * (1 - round(p * 65536) / 65536) - 1) < 1e-6
+    assert torch.equal(B.tt_dropout_fwd(x, torch.empty_like(x), dropout_of(0.0)), x)
+    assert not B.tt_dropout_fwd(x, torch.empty_like(x), dropout_of(1.0)).any()
+    # seeds, steps and sites draw their own elements
+    base = B.tt_dropout_fwd(x, torch.empty_like(x), dropout_of(0.5))
+    for other in (dropout_of(0.5, seed=7), dropout_of(0.5, step=42), dropout_of(0.5, site=6), dropout_of(0.5, seed=1234567890123456789 + (1 << 32))):
+        same = float((B.tt_dropout_fwd(x, torch.empty_like(x), other) == base).double().mean())
+        assert abs(same - 0.5) < 6 * 0.5 / 1e3
+    negative = dropout_of(0.3, seed=-5, step=-1)
+    want = R.drop(np.ones((10, 20)), negative)
+    assert np.array_equal(R.f64(B.tt_dropout_fwd(x[:10, :20], torch.empty((10, 20), device="cuda:0"), negative)) != 0, want != 0)
+
+
+def test_dropped_values_are_zero_whatever_they_were():
+    d = dropout_of(0.5)
+    x = torch.full((64, 100), float("nan"), device="cuda:0")
+    x[:32] = float("inf")
+    out = B.tt_dropout_fwd(x, torch.empty_like(x), d)
+    keep, _ = R.keep_mask(64, 100, 0.5, d.state.cpu().numpy(), d.site)
+    got = out.cpu().numpy()
+    assert (got[~keep] == 0).all() and np.isinf(got[:32][keep[:32]]).all() and np.isnan(got[32:][keep[32:]]).all()
+    table = torch.full((4, 100), float("nan"), device="cuda:0")
+    tokens = torch.tensor([0, 1, -1, 3], device="cuda:0")
+    got = B.tt_token_fwd(table, tokens, torch.empty((4, 100), device="cuda:0"), dropout=d).cpu().numpy()
+    assert (got[~keep[:4]] == 0).all() and (got[2] == 0).all() and np.isnan(got[[0, 1, 3]][keep[[0, 1, 3]]]).all()
+
+
+# ---- norm -----------------------------------------------------------------------------------------------------------------
+
+NORMS = [(1, 1), (2, 3), (1, 8), (5, 9), (70, 16), (3, 100), (1000, 64), (129, 128), (33, 136), (700, 513), (7, 1024), (600, 1000), (40, 2047), (520, 4096),
+         (3, 8192), (600, 8192), (2, 16384), (530, 16400), (5, 20001), (2, 32768)]
+# additions in a row: 32 values a thread, 6 + 16 across its threads; the mean's and root's own roundings; half of it reaches rstd
+ROW = 64
+
+
+def norm_types(i):
+    return [(F32, F32, F32), (BF16, BF16, BF16), (F16, F16, F32), (BF16, F32, BF16), (F16, F32, F16)][i]
+
+
+@pytest.mark.parametrize("rows,N", NORMS)
+@pytest.mark.parametrize("types", range(5))
+def test_norm_fwd(rows, N, types):
+    T, H, W = norm_types(types)
+    g = gen(rows + N)
+    lead, shift = [(0, 0), (3, 1), (8, 0)][(rows + types) % 3]
+    x, r = R.rows_of(g, rows, N, T, lead, shift), R.rows_of(g, rows, N, H, lead, shift, 2.0)
+    w = torch.randn(N, generator=g).to(W).to("cuda:0")
+    for residual, weight, d in [(None, w, None), (r, w, None), (r, None, dropout_of(0.2))]:
+        out, flat = room(rows, N, T, lead, shift)
+        hs, hflat = room(rows, N, H if residual is not None else T, lead, shift)
+        rstd = torch.empty(rows, device="cuda:0")
+        B.tt_add_rms_norm_fwd(x, weight, out, residual=residual, sum_out=hs, rstd=rstd, eps=1e-5, dropout=d)
+        h, rs, y, mag = R.norm_fwd(x, residual, weight, 1e-5, d)
+        R.assert_within(rstd, rs, rs * (ROW + 4 * (mag.max(1) / np.sqrt((h * h).mean(1) + 1e-5))) * U32)
+        R.assert_within(hs, h, np.abs(h) * UNIT[hs.dtype] + 3 * U32 * mag + TINY[hs.dtype])
+        scale = rs[:, None] * (1.0 if weight is None else np.abs(R.f64(weight)))
+        off = (ROW + 8) * U32 * (np.abs(y) * (1 + mag.max(1) * rs)[:, None]) + 4 * U32 * mag * scale
+        R.assert_within(out, y, np.abs(y) * UNIT[T] + off + TINY[T])
+        assert_guard(out, flat)
+        assert_guard(hs, hflat)
+
+
+@pytest.mark.parametrize("rows,N", NORMS)
+@pytest.mark.parametrize("types,group", [(0, 0), (1, 0), (2, 128), (3, 128), (4, 64), (1, 32)])
+def test_norm_fwd_in_8_bits(rows, N, types, group):
+    T, H, W = norm_types(types)
+    g = gen(rows + N + group)
+    lead, shift = [(0, 0), (5, 3), (16, 0)][(rows + types) % 3]
+    x, r = R.rows_of(g, rows, N, T), R.rows_of(g, rows, N, H, 0, 0, 2.0)
+    w = torch.randn(N, generator=g).to(W).to("cuda:0")
+    flat = torch.full((shift + rows * (N + lead) + 8,), 7.0, device="cuda:0").to(E4M3)
+    q = torch.as_strided(flat, (rows, N), (N + lead, 1), shift)
+    groups = -(-N // group) if group else 1
+    scales, sflat = room(rows, groups, F32, 2, 1)
+    B.tt_add_rms_norm_fwd(x, w, q, residual=r, scales=scales, group=group)
+    _, _, y, mag = R.norm_fwd(x, r, w, 1e-6, None)
+    width = group or N
+    want = np.stack([np.abs(y[:, c:c + width]).max(1) / 448 for c in range(0, N, width)], 1)
+    rel = 4 * (ROW + 8) * U32                               # (the sums here do not cancel to less than a quarter of their terms' root mean square)
+    assert (np.abs(R.f64(scales) - want) <= want * rel + 4 * U32 * (mag * np.abs(R.f64(w))).max()).all()
+    s = np.repeat(R.f64(scales), width, 1)[:, :N]
+    got = R.f64(q.float())
+    # half the spacing of e4m3: 2^-4 of the value, 2^-10 below 2^-6; and the value's own error in 32 bits
+    exact = y / np.where(s == 0, 1, s)
+    off = rel * np.abs(exact) + 8 * U32 * mag * np.abs(R.f64(w)) / np.where(s == 0, 1, s)
+    R.assert_within(torch.from_numpy(got), exact, np.maximum(np.abs(exact) * 2.0 ** -4, 2.0 ** -10) * (1 + 1e-5) + off)
+    assert np.abs(got).max(initial=0) <= 448
+    assert_guard(q, flat)
+    assert_guard(scales, sflat)
+
+
+def test_e4m3_rounds_to_nearest_even():
+    # a row whose largest value is 448 has scale 1 up to rounding: with rstd = 1 / 448 * ... every e4m3 value, every midpoint of two
+    # neighbours and values beside it, against torch's conversion of the quotient
+    vals = torch.arange(0, 127, dtype=torch.uint8).view(E4M3).float()
+    mids = (vals[1:] + vals[:-1]) / 2
+    near = torch.cat([vals, mids, mids * (1 + 2 ** -12), mids * (1 - 2 ** -12)])
+    row = torch.cat([near, -near])[None].to("cuda:0")
+    q, scales = torch.empty_like(row, dtype=E4M3), torch.empty((1, 1), device="cuda:0")
+    y = torch.empty_like(row)
+    B.tt_add_rms_norm_fwd(row, None, y)
+    B.tt_add_rms_norm_fwd(row, None, q, scales=scales)
+    exact = y.double() / scales.double()
+    err = (q.double() - exact).abs()
+    lattice = torch.cat([vals, -vals]).double().to("cuda:0")
+    nearest = (exact.reshape(-1, 1) - lattice).abs().min(1).values
+    assert bool((err.reshape(-1) <= nearest + exact.reshape(-1).abs() * 4 * U32).all())
+
+
+def test_norm_of_odd_values():
+    """Rows of zeros, tiny and huge values, infinities and NaN."""
+    N = 300
+    x = torch.randn((8, N), generator=gen(11)).to("cuda:0")
+    x[1] = 0
+    x[2] *= 1e-30
+    x[3] *= 1e15
+    x[4, 7] = float("nan")
+    x[5, 250] = float("inf")
+    x[6, 3] = float("-inf")
+    w = torch.ones(N, device="cuda:0")
+    w[128:] = 0
+    for group in (0, 128):
+        y, q = torch.empty_like(x), torch.empty_like(x, dtype=E4M3)
+        groups = 3 if group else 1
+        scales = torch.empty((8, groups), device="cuda:0")
+        B.tt_add_rms_norm_fwd(x, w, y, eps=0.0)
+        B.tt_add_rms_norm_fwd(x, w, q, scales=scales, group=group, eps=0.0)
+        assert torch.isfinite(y[[0, 3, 7]]).all() and torch.isfinite(q[[0, 3, 7]].float()).all()
+        assert torch.isnan(y[4]).all() and torch.isnan(scales[4]).all() and torch.isnan(q[4].float()).all()
+        for row, col in ((5, 250), (6, 3)):                  # 1 / inf is 0: nothing but the place itself is NaN
+            bad = torch.isnan(y[row])
+            assert bool(bad[col]) and int(bad.sum()) == 1 and not y[row][~bad].any()
+            k = col // 128 if group else 0
+            assert torch.isnan(scales[row]).nonzero().flatten().tolist() == [k]
+            part = slice(128 * k, 128 * k + 128) if group else slice(None)
+            assert torch.isnan(q[row].float()[part]).all()
+            rest = torch.ones(N, dtype=torch.bool, device="cuda:0")
+            rest[part] = False
+            assert not q[row].float()[rest].any()
+        if group:                                            # the weight is 0 from column 128 on
+            assert not scales[[0, 3, 7]][:, 1:].any() and not q[[0, 3, 7]].float()[:, 128:].any()
+    y, q, scales = torch.empty_like(x), torch.empty_like(x, dtype=E4M3), torch.empty((8, 1), device="cuda:0")
+    rstd = torch.empty(8, device="cuda:0")
+    B.tt_add_rms_norm_fwd(x, w, y, rstd=rstd)
+    B.tt_add_rms_norm_fwd(x, w, q, scales=scales)
+    assert not y[1].any() and abs(float(rstd[1]) - 1000) < 1e-3 and float(scales[1]) == 0 and not q[1].float().any()
+    x[2] *= 1e-12                                            # values whose scale is no normal number
+    B.tt_add_rms_norm_fwd(x, w, q, scales=scales)
+    assert float(scales[2]) == 0 and not q[2].float().any()
+
+
+@pytest.mark.parametrize("rows,N", NORMS + [(5000, 40), (3000, 1024), (2100, 16)])
+@pytest.mark.parametrize("types", range(5))
+def test_norm_bwd(rows, N, types):
+    T, H, W = norm_types(types)
+    g = gen(rows + 3 * N)
+    lead, shift = [(0, 0), (3, 1), (8, 0)][(rows + types) % 3]
+    dy, h, ds = R.rows_of(g, rows, N, T, lead, shift), R.rows_of(g, rows, N, H, lead, shift, 2.0), R.rows_of(g, rows, N, H, lead, shift)
+    rstd = (1.0 / (h.double().square().mean(1) + 1e-6).sqrt()).float()
+    w = torch.randn(N, generator=g).to(W).to("cuda:0")
+    for weight, dsum, d in [(w, ds, dropout_of(0.2)), (w, None, None), (None, ds, None)]:
+        gx, fx = room(rows, N, T, lead, shift)
+        gr, fr = room(rows, N, H, lead, shift)
+        gw, fw = room(1, N, W, 0, 1)
+        B.tt_add_rms_norm_bwd(dy, h, rstd, weight, gx, gw[0], grad_sum=dsum, grad_residual=gr, dropout=d)
+        dx, dh, dw, mag, wmag = R.norm_bwd(dy, h, rstd, weight, dsum, d)
+        off = (ROW + 16) * U32 * mag
+        factor = 1.25 if d is not None else 1.0
+        R.assert_within(gx, dx, np.abs(dx) * (UNIT[T] + U32) + factor * off + TINY[T], "dx")
+        R.assert_within(gr, dh, np.abs(dh) * UNIT[H] + off + TINY[H], "dresidual")
+        R.assert_within(gw, dw[None], np.abs(dw) * UNIT[W] + (rows + 4) * U32 * wmag + TINY[W], "dw")
+        for view, flat in ((gx, fx), (gr, fr), (gw, fw)):
+            assert_guard(view, flat)
+    # fewer outputs, and the sums added to what is there: the same values
+    only, old = torch.empty_like(gx), torch.randn(N, generator=g).to("cuda:0")
+    B.tt_add_rms_norm_bwd(dy, h, rstd, None, only, None, grad_sum=ds)
+    assert torch.equal(only, gx)
+    added, alone = old.clone(), torch.empty_like(old)
+    B.tt_add_rms_norm_bwd(dy, h, rstd, None, None, alone, grad_sum=ds)
+    B.tt_add_rms_norm_bwd(dy, h, rstd, None, None, added, grad_sum=ds, accumulate=True)
+    R.assert_within(added, R.f64(old) + R.f64(alone), (64 + 2) * U32 * (np.abs(R.f64(old)) + wmag))
+
+
+def test_norm_gradients_are_difference_quotients():
+    """f = <G, y> + <S, h> in 64 bits from the plain forward; its central differences against the kernels' gradients."""
+    g = gen(21)
+    rows, N, eps, t = 4, 33, 1e-3, 1e-4
+    x, r, w = R.rows_of(g, rows, N, F32), R.rows_of(g, rows, N, F32), torch.randn(N, generator=g).to("cuda:0")
+    G, S, d = R.rows_of(g, rows, N, F32), R.rows_of(g, rows, N, F32), dropout_of(0.3)
+    out, h, rstd = torch.empty((rows, N), device="cuda:0"), torch.empty((rows, N), device="cuda:0"), torch.empty(rows, device="cuda:0")
+    B.tt_add_rms_norm_fwd(x, w, out, residual=r, sum_out=h, rstd=rstd, eps=eps, dropout=d)
+    gx, gr, gw = torch.empty_like(out), torch.empty_like(out), torch.empty_like(w)
+    B.tt_add_rms_norm_bwd(G, h, rstd, w, gx, gw, grad_sum=S, grad_residual=gr, dropout=d)
+
+    def f(x, r, w):
+        h_, _, y, _ = R.norm_fwd(x, r, w, eps, d)
+        return float((R.f64(G) * y).sum() + (R.f64(S) * h_).sum())
+
+    for name, arg, grad in (("x", 0, gx), ("residual", 1, gr), ("weight", 2, gw)):
+        for at in ([(0, 0), (1, 5), (3, 32), (2, 8)] if arg < 2 else [(0,), (7,), (32,)]):
+            two = []
+            for sign in (1, -1):
+                args = [x.double(), r.double(), w.double()]
+                args[arg] = args[arg].clone()
+                args[arg][at] += sign * t
+                two.append(f(*args))
+            # the quotient's own error is of the order of t^2 times a third derivative (1e-8 of values near 1), and 1e-12 / t
+            assert abs((two[0] - two[1]) / (2 * t) - float(grad[at])) < 1e-5, name
+
+
+def test_norm_in_place():
+    g = gen(31)
+    for rows, N in [(9, 100), (700, 4096)]:
+        x, r = R.rows_of(g, rows, N, BF16), R.rows_of(g, rows, N, BF16)
+        w = torch.randn(N, generator=g).to(BF16).to("cuda:0")
+        out, hs, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda:0")
+        B.tt_add_rms_norm_fwd(x, w, out, residual=r, sum_out=hs, rstd=rstd)
+        x2, r2 = x.clone(), r.clone()
+        B.tt_add_rms_norm_fwd(x2, w, x2, residual=r2, sum_out=r2)
+        assert torch.equal(x2, out) and torch.equal(r2, hs)
+        d = dropout_of(0.4)
+        gx, gr = torch.empty_like(x), torch.empty_like(x)
+        B.tt_add_rms_norm_bwd(x, hs, rstd, w, gx, None, grad_sum=r, grad_residual=gr, dropout=d)
+        dy2, ds2 = x.clone(), r.clone()
+        B.tt_add_rms_norm_bwd(dy2, hs, rstd, w, dy2, None, grad_sum=ds2, grad_residual=ds2, dropout=d)
+        assert torch.equal(dy2, gx) and torch.equal(ds2, gr)
+
+
+def test_norm_of_no_rows():
+    e = torch.empty((0, 64), device="cuda:0")
+    w = torch.ones(64, device="cuda:0")
+    B.tt_add_rms_norm_fwd(e, w, e.clone(), residual=e, sum_out=e.clone(), rstd=torch.empty(0, device="cuda:0"))
+    gw = torch.full((64,), 5.0, device="cuda:0")
+    B.tt_add_rms_norm_bwd(e, e, torch.empty(0, device="cuda:0"), w, e.clone(), gw, accumulate=True)
+    assert bool((gw == 5).all())
+    B.tt_add_rms_norm_bwd(e, e, torch.empty(0, device="cuda:0"), w, e.clone(), gw)
+    assert not gw.any()
+
+
+def test_norm_of_a_broadcast_residual():
+    g = gen(41)
+    x, row = R.rows_of(g, 40, 72, F32), R.rows_of(g, 1, 72, F32)
+    out = torch.empty_like(x)
+    B.tt_add_rms_norm_fwd(x, None, out, residual=row.expand(40, 72))
+    same = torch.empty_like(x)
+    B.tt_add_rms_norm_fwd(x, None, same, residual=row.expand(40, 72).contiguous())
+    assert torch.equal(out, same)
+
+
+# ---- streams and graphs -------------------------------------------------------------------------------------------------
+
+
+def block(table, tokens, x, w, state, bufs, ws):
+    """Tokens -> residual stream, a branch added under dropout, norm, and back down to the table's gradient."""
+    emb, h, y, rstd, gx, gr, gw, gt = bufs
+    d0, d1 = B.Dropout(0.1, state, 0), B.Dropout(0.2, state, 1)
+    B.tt_token_fwd(table, tokens, emb, scale=3.0, dropout=d0)
+    B.tt_add_rms_norm_fwd(x, w, y, residual=emb, sum_out=h, rstd=rstd, dropout=d1)
+    B.tt_add_rms_norm_bwd(y, h, rstd, w, gx, gw, grad_sum=emb, grad_residual=gr, dropout=d1, workspace=ws[0])
+    B.tt_token_bwd(tokens, gr, gt, scale=3.0, dropout=d0, workspace=ws[1])
+
+
+def block_buffers(L, vocab, N):
+    e = lambda *s: torch.empty(s, device="cuda:0")  # noqa: E731
+    return [e(L, N), e(L, N), e(L, N), e(L), e(L, N), e(L, N), e(N), e(vocab, N)]
+
+
+def block_inputs(L, vocab, N):
+    g = gen(51)
+    ws = [torch.empty(B.add_rms_norm_bwd_workspace_bytes(L, N), dtype=torch.uint8, device="cuda:0"),
+          torch.empty(B.token_bwd_workspace_bytes(L, N), dtype=torch.uint8, device="cuda:0")]
+    return (R.rows_of(g, vocab, N, F32), tokens_of(g, L, vocab, "hot"), R.rows_of(g, L, N, F32), torch.randn(N, generator=g).to("cuda:0"),
+            torch.tensor([99, 0], dtype=torch.int64, device="cuda:0")), ws
+
+
+@pytest.mark.parametrize("L,vocab,N", [(300, 100, 64), (17_000, 1000, 24)])
+def test_recorded_block_draws_anew_at_every_step(L, vocab, N):
+    inputs, ws = block_inputs(L, vocab, N)
+    state = inputs[-1]
+    bufs = block_buffers(L, vocab, N)
+    block(*inputs, bufs, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        block(*inputs, bufs, ws)
+    seen = []
+    for step in (0, 1, 2, 1):
+        state[1] = step
+        for b in bufs:
+            b.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [b.clone() for b in bufs]
+        eager = block_buffers(L, vocab, N)
+        block(*inputs, eager, [None, None])
+        assert all(torch.equal(a, b) for a, b in zip(got, eager)), step
+        seen.append(got)
+    assert all(torch.equal(a, b) for a, b in zip(seen[1], seen[3]))
+    assert not torch.equal(seen[0][0], seen[1][0])
+
+
+def test_block_on_another_stream():
+    inputs, ws = block_inputs(2000, 300, 256)
+    want, got = block_buffers(2000, 300, 256), block_buffers(2000, 300, 256)
+    block(*inputs, want, ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block(*inputs, got, [None, None])
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+# ---- refusals -------------------------------------------------------------------------------------------------------------
+
+
+def test_binding_refuses_what_does_not_fit():
+    t = lambda *s, dtype=F32: torch.zeros(s, dtype=dtype, device="cuda:0")  # noqa: E731
+    table, tokens, out = t(10, 16), t(5, dtype=torch.int64), t(5, 16)
+    for bad in [lambda: B.tt_token_fwd(table, tokens, t(4, 16)), lambda: B.tt_token_fwd(table, tokens, t(5, 15)), lambda: B.tt_token_fwd(table.cpu(), tokens, out),
+                lambda: B.tt_token_fwd(table, tokens.cpu(), out), lambda: B.tt_token_fwd(table, tokens.float(), out), lambda: B.tt_token_fwd(table, tokens.to(torch.int16), out),
+                lambda: B.tt_token_fwd(table.double(), tokens, out), lambda: B.tt_token_fwd(t(16, 10).t(), tokens, out), lambda: B.tt_token_fwd(table, t(10, dtype=torch.int64)[::2], out),
+                lambda: B.tt_token_fwd(table, tokens, out, dropout=0.1), lambda: B.tt_token_fwd(table, tokens, out, dropout=(0.1, t(2), 0)),
+                lambda: B.tt_token_fwd(table, tokens, out, dropout=(0.1, t(1, dtype=torch.int64), 0)), lambda: B.tt_token_fwd(table, tokens, out, dropout=(0.1, t(2, dtype=torch.int64), -1)),
+                lambda: B.tt_token_bwd(tokens, t(5, 15), table), lambda: B.tt_token_bwd(tokens, t(6, 16), table), lambda: B.tt_token_bwd(tokens, out, table, workspace=torch.zeros(9)),
+                lambda: B.tt_dropout_fwd(out, t(5, 17), dropout_of(0.1)), lambda: B.tt_dropout_fwd(out, out, dropout_of(0.1), residual=t(6, 16)),
+                lambda: B.tt_add_rms_norm_fwd(out, t(15), out), lambda: B.tt_add_rms_norm_fwd(out, t(16), out, rstd=t(6)), lambda: B.tt_add_rms_norm_fwd(out, None, out, residual=t(4, 16)),
+                lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=E4M3), scales=t(5, 2)), lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=E4M3), scales=t(5, 1), group=-1),
+                lambda: B.tt_add_rms_norm_bwd(out, t(5, 17), t(5), None, out, None), lambda: B.tt_add_rms_norm_bwd(out, out, t(4), None, out, None),
+                lambda: B.tt_add_rms_norm_bwd(out, out, t(5), None, out, t(15)), lambda: B.tt_token_fwd(t(3, 4, 8).transpose(0, 1), tokens, t(5, 8))]:
+        with pytest.raises(AssertionError):
+            bad()
+    for code, bad in [(-6, lambda: B.tt_token_fwd(t(10, 16, dtype=E4M3), tokens, out)), (-1, lambda: B.tt_dropout_fwd(out, out, None)), (-3, lambda: B.tt_dropout_fwd(out, out, dropout_of(1.5))),
+                      (-3, lambda: B.tt_dropout_fwd(out, out, dropout_of(float("nan")))), (-6, lambda: B.tt_dropout_fwd(out, t(5, 16, dtype=BF16), dropout_of(0.1))),
+                      (-3, lambda: B.tt_token_bwd(tokens, out, table[:1].expand(10, 16))), (-4, lambda: B.tt_token_bwd(tokens, out, table, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda:0"))),
+                      (-6, lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=BF16))), (-6, lambda: B.tt_add_rms_norm_fwd(out, None, out, residual=t(5, 16, dtype=BF16))),
+                      (-1, lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=E4M3))), (-3, lambda: B.tt_add_rms_norm_fwd(out, None, out, scales=t(5, 1))),
+                      (-6, lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=E4M3), scales=t(5, 1), group=48)), (-3, lambda: B.tt_add_rms_norm_fwd(out, None, out, eps=-1.0)),
+                      (-6, lambda: B.tt_add_rms_norm_fwd(t(1, 32769), None, t(1, 32769))), (-6, lambda: B.tt_add_rms_norm_bwd(out, t(5, 16, dtype=BF16), t(5), None, out, None))]:
+        with pytest.raises(B.TTError) as e:
+            bad()
+        assert e.value.code == code, e.value
+    assert not out.any() and not table.any()
