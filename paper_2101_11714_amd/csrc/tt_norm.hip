@@ -1,0 +1,220 @@
+// C-ABI entry points of the residual addition + RMS norm (declared in include/tt_emb.h): argument checks, workspace layout, kernel
+// selection and launches.  Nothing here allocates device memory or waits for the stream.
+
+#include "../../include/tt_emb.h"
+
+#include "tt_rows_args.h"
+#include "tt_rms_norm.h"
+
+using namespace tt;
+
+namespace {
+
+struct NormShape {
+    int lg, vpt, threads;
+};
+
+// Threads per row (log), vectors per thread, threads per workgroup.
+NormShape norm_shape(int64_t rows, int64_t nv, int least_lg, int most_lg)
+{
+    int lg = lg_ceil(nv);
+    if (rows > 512) {                                        // enough rows: two vectors a thread, a wave's worth of threads at least
+        const int two = lg_ceil(ceil_div(nv, 2));
+        lg = two > 6 ? two : lg < 6 ? lg : 6;
+    }
+    if (lg > most_lg) lg = most_lg;
+    if (lg < least_lg) lg = least_lg;
+    int vpt = 1;
+    while ((int64_t)vpt << lg < nv) vpt <<= 1;
+    return {lg, vpt, lg > 8 ? 1 << lg : WG};
+}
+
+template <typename F>
+void with_vpt(int vpt, F f)
+{
+    if (vpt == 1) f(std::integral_constant<int, 1>{});
+    else if (vpt == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
+}
+
+// (activation, residual stream): the same type, or a stream of 32 bits
+template <typename F>
+void with_types(int32_t type, int32_t stream, F f)
+{
+    with_type(type, [&](auto t) {
+        if (stream == TT_F32) f(t, float{});
+        else f(t, t);
+    });
+}
+
+int check_norm(int64_t rows, int64_t N)
+{
+    int rc = check_sizes(rows, N);
+    if (rc) return rc;
+    if (N > RN_MOST) return fail(TT_ERR_UNSUPPORTED, "more than %d columns", RN_MOST);
+    if (N == 0 && rows > 0) return fail(TT_ERR_BAD_ARG, "rows without columns have no mean square");
+    return TT_OK;
+}
+
+int check_weight(const void *weight, int32_t type)
+{
+    if (!weight) return TT_OK;
+    if (type != TT_F32 && type != TT_BF16 && type != TT_F16) return fail(TT_ERR_UNSUPPORTED, "weight: type %d is not supported", (int)type);
+    return (uintptr_t)weight % element_bytes(type) ? fail(TT_ERR_BAD_ARG, "weight is not aligned to its elements") : TT_OK;
+}
+
+int norm_bwd_groups(const NormShape &s) { return s.threads >> s.lg; }
+
+constexpr int NORM_BWD_THREADS = 512;                       // (1,024 threads have too few registers; they take the longest rows alone)
+constexpr int64_t NORM_BWD_WORKGROUPS = 1024;
+
+int64_t norm_bwd_grid(int64_t rows, const NormShape &s)
+{
+    const int64_t all = ceil_div(rows, norm_bwd_groups(s));
+    return all < NORM_BWD_WORKGROUPS ? all : NORM_BWD_WORKGROUPS;
+}
+
+}  // namespace
+
+extern "C" {
+
+int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_dropout_t *dropout, const void *weight, int32_t weight_type,
+                        float eps, const tt_rows_t *sum, const tt_rows_t *output, float *rstd, const tt_rows_t *scales, int32_t group,
+                        int64_t n_rows, int64_t N, void *stream)
+{
+    NormArgs a{};
+    int rc = check_norm(n_rows, N);
+    if (rc) return rc;
+    if ((rc = check_rows(x, "x", n_rows, N, IN)) || (rc = check_rows(output, "output", n_rows, N, OUT, true)) || (rc = check_weight(weight, weight_type))) return rc;
+    if (residual && (rc = check_rows(residual, "residual", n_rows, N, IN))) return rc;
+    if (sum && (rc = check_rows(sum, "sum", n_rows, N, OUT))) return rc;
+    const int32_t stream_type = residual ? residual->type : sum ? sum->type : x->type;
+    if (stream_type != x->type && stream_type != TT_F32) return fail(TT_ERR_UNSUPPORTED, "the residual has x's type or 32 bits");
+    if (sum && sum->type != stream_type) return fail(TT_ERR_UNSUPPORTED, "sum has the residual's type");
+    const bool bits8 = output->type == TT_E4M3;
+    if (!bits8 && output->type != x->type) return fail(TT_ERR_UNSUPPORTED, "output has x's type or 8 bits");
+    if (!(eps >= 0.f)) return fail(TT_ERR_BAD_ARG, "eps must not be negative");
+    if (bits8) {
+        if (group != 0 && group != 32 && group != 64 && group != 128) return fail(TT_ERR_UNSUPPORTED, "groups of 32, 64 or 128 columns, or 0");
+        if ((rc = check_rows(scales, "scales", n_rows, group ? ceil_div(N, group) : 1, OUT))) return rc;
+        if (scales->type != TT_F32) return fail(TT_ERR_UNSUPPORTED, "scales have 32 bits");
+    } else if (scales || group) {
+        return fail(TT_ERR_BAD_ARG, "scales and groups belong to an output in 8 bits");
+    }
+    if ((uintptr_t)rstd % 4) return fail(TT_ERR_BAD_ARG, "rstd is not aligned");
+    if ((rc = check_dropout(dropout, &a.drop))) return rc;
+    if (n_rows == 0) return TT_OK;
+    a.x = x->data;
+    a.residual = residual ? residual->data : nullptr;
+    a.weight = weight;
+    a.weight_type = weight_type;
+    a.sum = sum ? sum->data : nullptr;
+    a.y = output->data;
+    a.rstd = rstd;
+    a.scales = bits8 ? (float *)scales->data : nullptr;
+    a.ld_x = x->ld;
+    a.ld_res = residual ? residual->ld : 0;
+    a.ld_sum = sum ? sum->ld : 0;
+    a.ld_y = output->ld;
+    a.ld_scales = bits8 ? scales->ld : 0;
+    a.rows = n_rows;
+    a.N = (int)N;
+    a.nv = (int)ceil_div(N, 8);
+    a.group = group;
+    a.eps = eps;
+    const NormShape s = norm_shape(n_rows, a.nv, group ? lg_ceil(group / 8) : 0, 10);
+    if ((rc = check_grid(ceil_div(n_rows, s.threads >> s.lg), s.threads))) return rc;
+    const dim3 grid((unsigned)ceil_div(n_rows, s.threads >> s.lg));
+    with_types(x->type, stream_type, [&](auto t, auto h) {
+        with_vpt(s.vpt, [&](auto vpt) {
+            with_whole(N, [&](auto whole) {
+                with_flag(residual != nullptr, [&](auto res) {
+                    with_flag(bits8, [&](auto y8) {
+                        hipLaunchKernelGGL((norm_fwd_kernel<decltype(t), decltype(h), decltype(y8)::value, decltype(vpt)::value, decltype(whole)::value, decltype(res)::value>), grid,
+                                           dim3(s.threads), 0, (hipStream_t)stream, a, s.lg);
+                    });
+                });
+            });
+        });
+    });
+    return launched("norm launch");
+}
+
+size_t tt_add_rms_norm_bwd_workspace_bytes(int64_t n_rows, int64_t N)
+{
+    if (n_rows <= 0 || N <= 0 || n_rows >= MOST_ROWS || N > RN_MOST) return 0;
+    const int64_t most = n_rows < NORM_BWD_WORKGROUPS ? n_rows : NORM_BWD_WORKGROUPS;
+    return (size_t)most * (size_t)(8 * ceil_div(N, 8)) * sizeof(float);
+}
+
+int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const float *rstd, const void *weight, int32_t weight_type,
+                        const tt_rows_t *grad_sum, const tt_dropout_t *dropout, const tt_rows_t *grad_x, const tt_rows_t *grad_residual,
+                        void *grad_weight, int32_t grad_weight_type, int accumulate, int64_t n_rows, int64_t N,
+                        void *workspace, size_t workspace_bytes, void *stream)
+{
+    NormGradArgs a{};
+    int rc = check_norm(n_rows, N);
+    if (rc) return rc;
+    if ((rc = check_rows(grad_output, "grad_output", n_rows, N, IN)) || (rc = check_rows(h, "h", n_rows, N, IN)) || (rc = check_weight(weight, weight_type))) return rc;
+    if (h->type != grad_output->type && h->type != TT_F32) return fail(TT_ERR_UNSUPPORTED, "h has grad_output's type or 32 bits");
+    if (grad_sum && (rc = check_rows(grad_sum, "grad_sum", n_rows, N, IN))) return rc;
+    if (grad_x && (rc = check_rows(grad_x, "grad_x", n_rows, N, OUT))) return rc;
+    if (grad_residual && (rc = check_rows(grad_residual, "grad_residual", n_rows, N, OUT))) return rc;
+    if ((grad_sum && grad_sum->type != h->type) || (grad_residual && grad_residual->type != h->type))
+        return fail(TT_ERR_UNSUPPORTED, "grad_sum and grad_residual have h's type");
+    if (grad_x && grad_x->type != grad_output->type) return fail(TT_ERR_UNSUPPORTED, "grad_x has grad_output's type");
+    if (grad_weight && (rc = check_weight(grad_weight, grad_weight_type))) return rc;
+    if (n_rows > 0 && !rstd) return fail(TT_ERR_NULL, "rstd is NULL");
+    if ((uintptr_t)rstd % 4) return fail(TT_ERR_BAD_ARG, "rstd is not aligned");
+    if ((rc = check_dropout(dropout, &a.drop))) return rc;
+    if (N == 0 || (n_rows == 0 && (!grad_weight || accumulate))) return TT_OK;
+    if (n_rows > 0 && !grad_weight && !grad_x && !grad_residual) return TT_OK;
+    const size_t need = grad_weight ? tt_add_rms_norm_bwd_workspace_bytes(n_rows, N) : 0;
+    if (need && (!workspace || workspace_bytes < need)) return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+    if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
+    hipStream_t st = (hipStream_t)stream;
+    a.dy = grad_output->data;
+    a.h = h->data;
+    a.weight = weight;
+    a.weight_type = weight_type;
+    a.dsum = grad_sum ? grad_sum->data : nullptr;
+    a.rstd = rstd;
+    a.dx = grad_x ? grad_x->data : nullptr;
+    a.dres = grad_residual ? grad_residual->data : nullptr;
+    a.part = grad_weight ? (float *)workspace : nullptr;
+    a.ld_dy = grad_output->ld;
+    a.ld_h = h->ld;
+    a.ld_dsum = grad_sum ? grad_sum->ld : 0;
+    a.ld_dx = grad_x ? grad_x->ld : 0;
+    a.ld_dres = grad_residual ? grad_residual->ld : 0;
+    a.rows = n_rows;
+    a.N = (int)N;
+    a.nv = (int)ceil_div(N, 8);
+    a.weight_type = weight_type;
+    int64_t grid = 0;
+    if (n_rows > 0) {
+        const NormShape s = norm_shape(n_rows, a.nv, 0, a.nv > 4 * NORM_BWD_THREADS ? 10 : 9);
+        grid = norm_bwd_grid(n_rows, s);
+        const size_t lds = grad_weight ? (size_t)(norm_bwd_groups(s) - 1) * 8 * a.nv * sizeof(float) : 0;
+        with_types(grad_output->type, h->type, [&](auto t, auto ht) {
+            auto launch = [&](auto vpt, auto threads) {
+                with_whole(N, [&](auto whole) {
+                    with_flag(grad_sum != nullptr, [&](auto dsum) {
+                        hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), decltype(ht), decltype(vpt)::value, decltype(threads)::value, decltype(whole)::value, decltype(dsum)::value>),
+                                           dim3((unsigned)grid), dim3(s.threads), lds, st, a, s.lg);
+                    });
+                });
+            };
+            if (s.lg == 10) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 1024>{});
+            else with_vpt(s.vpt, [&](auto vpt) { launch(vpt, std::integral_constant<int, NORM_BWD_THREADS>{}); });
+        });
+    }
+    if (grad_weight)
+        with_type(grad_weight_type, [&](auto w) {
+            hipLaunchKernelGGL(norm_dw_kernel<decltype(w)>, dim3((unsigned)ceil_div(N, 64)), dim3(1024), 0, st, (const float *)workspace, (int)grid, (int)N, a.nv,
+                               (decltype(w) *)grad_weight, accumulate);
+        });
+    return launched("norm gradient launch");
+}
+
+}  // extern "C"

@@ -25,31 +25,47 @@ struct NormArgs {
     DropArgs drop;
 };
 
-// eight weights of any type; ones where there are none
-__device__ __forceinline__ void weights8(const void *w, int type, int v, int n, float (&x)[8])
+// the weights of a thread's vectors, of any type; ones where there are none
+template <bool WHOLE, int VPT, typename W>
+__device__ __forceinline__ void load_weights(const W *p, int g, int t, int nv, int N, float (&w)[VPT][8])
 {
-    if (!w) {
+    Vec8<W> x[VPT];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = 1.f;
+    for (int i = 0; i < VPT; ++i) {
+        const int v = min(i * g + t, nv - 1);
+        x[i] = fetch8<WHOLE>(p + 8 * v, N - 8 * v);
+    }
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) widen8(x[i], w[i]);
+}
+
+template <bool WHOLE, int VPT>
+__device__ __forceinline__ void weights(const void *p, int type, int g, int t, int nv, int N, float (&w)[VPT][8])
+{
+    if (!p) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[i][j] = 1.f;
     } else if (type == TT_F32) {
-        widen8(fetch8((const float *)w + 8 * v, n), x);
+        load_weights<WHOLE>((const float *)p, g, t, nv, N, w);
     } else if (type == TT_BF16) {
-        widen8(fetch8((const bf16_t *)w + 8 * v, n), x);
+        load_weights<WHOLE>((const bf16_t *)p, g, t, nv, N, w);
     } else {
-        widen8(fetch8((const f16_t *)w + 8 * v, n), x);
+        load_weights<WHOLE>((const f16_t *)p, g, t, nv, N, w);
     }
 }
 
-// the larger of two magnitudes, and NaN if either is
-__device__ __forceinline__ float most_or_nan(float a, float b) { return a != a || a > b ? a : b; }
+// Magnitudes as whole numbers: in the order of their values, with NaN above all of them, so that the largest of some is NaN if one is
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7fffffffu; }
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) { return a > b ? a : b; }
 
-// Sum over the 1 << lg threads of a row (up to a wave by lane exchange, then by LDS: one slot per wave, in the waves' order).
-// `slot`: NWAVES floats that no other reduction in flight uses; every thread of the workgroup calls.
-template <typename F>
-__device__ __forceinline__ float row_reduce(float x, int lg, float *slot, F f)
+// f over the 1 << lg threads of a row: up to a wave in registers, then by LDS, one place per wave, in the waves' order.
+// `slot`: a place per wave that no other reduction in flight uses; every thread of the workgroup calls.
+template <typename V, typename F>
+__device__ __forceinline__ V row_reduce(V x, int lg, V *slot, F f)
 {
-    const int in_wave = lg < 6 ? lg : 6;
-    for (int b = 0; b < in_wave; ++b) x = f(x, __shfl_xor(x, 1 << b));
+    x = lanes_reduce(x, lg < 6 ? lg : 6, f);
     if (lg > 6) {
         const int w = threadIdx.x >> 6, per = 1 << (lg - 6), w0 = w & ~(per - 1);
         if ((threadIdx.x & 63) == 0) slot[w] = x;
@@ -60,6 +76,7 @@ __device__ __forceinline__ float row_reduce(float x, int lg, float *slot, F f)
     return x;
 }
 
+template <bool WHOLE>
 __device__ __forceinline__ void put8_e4m3(uint8_t *p, int n, const float (&q)[8])
 {
     struct __attribute__((packed, aligned(1))) Two { uint32_t v[2]; } r;
@@ -69,7 +86,7 @@ __device__ __forceinline__ void put8_e4m3(uint8_t *p, int n, const float (&q)[8]
         w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * k + 2], q[4 * k + 3], w, true);
         r.v[k] = (uint32_t)w;
     }
-    if (n >= 8) {
+    if (WHOLE || n >= 8) {
         *reinterpret_cast<Two *>(p) = r;
     } else {
 #pragma unroll
@@ -78,42 +95,41 @@ __device__ __forceinline__ void put8_e4m3(uint8_t *p, int n, const float (&q)[8]
     }
 }
 
-// T: x and y (Y8: y in 8 bits), H: the residual stream.  1 << lg threads a row, VPT vectors a thread.
-template <typename T, typename H, bool Y8, int VPT, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(const NormArgs a, int lg)
+constexpr int RN_THREADS = 1024, RN_WAVES = RN_THREADS / WAVE;
+
+// T: x and y (Y8: y in 8 bits), H: the residual stream.  1 << lg threads a row, VPT vectors a thread.  No load stands in a branch
+// (it would be waited for there): threads without a row or a vector load the last one.
+template <typename T, typename H, bool Y8, int VPT, bool WHOLE, bool RESIDUAL>
+__global__ __launch_bounds__(RN_THREADS) void norm_fwd_kernel(const NormArgs a, int lg)
 {
-    __shared__ float slots[2][BLOCK / WAVE];
+    __shared__ float sums[RN_WAVES];
+    __shared__ uint32_t mosts[RN_WAVES];
     const int g = 1 << lg, t = threadIdx.x & (g - 1);
-    const int64_t row = (int64_t)blockIdx.x * (BLOCK >> lg) + (threadIdx.x >> lg);
-    const bool in = row < a.rows;
-    float h[VPT][8];
+    const int64_t row_ = (int64_t)blockIdx.x * (blockDim.x >> lg) + (threadIdx.x >> lg);
+    const bool in = row_ < a.rows;
+    const int64_t row = in ? row_ : a.rows - 1;
+    float h[VPT][8], w[VPT][8];
     {
         Vec8<T> x[VPT];
         Vec8<H> res[VPT];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int v = i * g + t, n = a.N - 8 * v;
-            if (in && v < a.nv) {
-                x[i] = fetch8((const T *)a.x + row * a.ld_x + 8 * v, n);
-                if (a.residual) res[i] = fetch8((const H *)a.residual + row * a.ld_res + 8 * v, n);
-            }
+            const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
+            x[i] = fetch8<WHOLE>((const T *)a.x + row_at(row, a.ld_x) + 8 * v, n);
+            if constexpr (RESIDUAL) res[i] = fetch8<WHOLE>((const H *)a.residual + row_at(row, a.ld_res) + 8 * v, n);
         }
         const DropKey key = drop_key(a.drop);
+        weights<WHOLE>(a.weight, a.weight_type, g, t, a.nv, a.N, w);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int v = i * g + t;
-            if (in && v < a.nv) {
-                widen8(x[i], h[i]);
-                if (a.drop.state) drop8(a.drop, drop_mask(a.drop, key, (uint64_t)row * (uint64_t)a.nv + (uint64_t)v), h[i]);
-                if (a.residual) {
-                    float r[8];
-                    widen8(res[i], r);
+            const int v = min(i * g + t, a.nv - 1);
+            widen8(x[i], h[i]);
+            if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, a.drop.factor, h[i]);
+            if constexpr (RESIDUAL) {
+                float r[8];
+                widen8(res[i], r);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) h[i][j] += r[j];
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) h[i][j] = 0.f;
+                for (int j = 0; j < 8; ++j) h[i][j] += r[j];
             }
         }
     }
@@ -121,54 +137,51 @@ __global__ __launch_bounds__(BLOCK) void norm_fwd_kernel(const NormArgs a, int l
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int v = i * g + t;
-        if (a.sum && in && v < a.nv) put8((H *)a.sum + row * a.ld_sum + 8 * v, a.N - 8 * v, h[i]);
+        float part = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) ss = fmaf(h[i][j], h[i][j], ss);
+        for (int j = 0; j < 8; ++j) part = fmaf(h[i][j], h[i][j], part);     // (columns behind the last are 0)
+        if (v < a.nv) {
+            ss += part;
+            if (a.sum && in) put8<WHOLE>((H *)a.sum + row_at(row, a.ld_sum) + 8 * v, a.N - 8 * v, h[i]);
+        }
     }
-    ss = row_reduce(ss, lg, slots[0], [](float p, float q) { return p + q; });
+    ss = row_reduce(ss, lg, sums, [](float p, float q) { return p + q; });
     const float rstd = 1.f / sqrtf(ss / (float)a.N + a.eps);
     if (a.rstd && in && t == 0) a.rstd[row] = rstd;
-    float most = 0.f;
+    uint32_t most[VPT];
+    uint32_t row_most = 0u;
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int v = i * g + t, n = a.N - 8 * v;
-        if (v < a.nv) {
-            float w[8];
-            weights8(a.weight, a.weight_type, v, n, w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) h[i][j] = j < n ? h[i][j] * rstd * w[j] : 0.f;
-        }
+        for (int j = 0; j < 8; ++j) h[i][j] = h[i][j] * rstd * w[i][j];
         if constexpr (Y8) {
-            if (!a.group) {
+            uint32_t m = 0u;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) most = most_or_nan(most, fabsf(h[i][j]));
-            }
+            for (int j = 0; j < 8; ++j) m = larger(m, WHOLE || j < n ? magnitude(h[i][j]) : 0u);
+            most[i] = v < a.nv ? m : 0u;
+            row_most = larger(row_most, most[i]);
         } else {
-            if (in && v < a.nv) put8((T *)a.y + row * a.ld_y + 8 * v, n, h[i]);
+            if (in && v < a.nv) put8<WHOLE>((T *)a.y + row_at(row, a.ld_y) + 8 * v, n, h[i]);
         }
     }
     if constexpr (Y8) {
-        if (!a.group) most = row_reduce(most, lg, slots[1], most_or_nan);
+        int lg_group = 0;                                    // lanes of a group: neighbours, a power of two
+        if (a.group) lg_group = __builtin_ctz(a.group) - 3;
+        else row_most = row_reduce(row_most, lg, mosts, larger);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = i * g + t, n = a.N - 8 * v;
-            float m = most;
-            if (a.group) {                                   // a group's lanes are neighbours: a power of two up to 16 (or all of a shorter row's)
-                m = 0.f;
+            const uint32_t m = a.group ? lanes_reduce(most[i], lg_group, larger) : row_most;
+            const float s = __uint_as_float(m) * (1.f / E4M3_MOST);
+            const bool none = s < 1.17549435e-38f;           // nothing but zeros, or too little for a scale of 32 bits
+            const float inv = none ? 0.f : 1.f / s;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) m = most_or_nan(m, fabsf(h[i][j]));
-                for (int b = 1; b < (a.group >> 3); b <<= 1) m = most_or_nan(m, __shfl_xor(m, b));
-            }
-            const float s = m / E4M3_MOST;
+            for (int j = 0; j < 8; ++j) h[i][j] = none ? 0.f : h[i][j] * inv;
             if (in && v < a.nv) {
-                const bool none = s < 1.17549435e-38f;       // nothing but zeros, or too little for a scale of 32 bits
-                const float inv = none ? 0.f : 1.f / s;
-                float q[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) q[j] = h[i][j] * inv;
-                put8_e4m3((uint8_t *)a.y + row * a.ld_y + 8 * v, n, q);
-                if (a.group ? (8 * v) % a.group == 0 : v == 0)
-                    a.scales[row * a.ld_scales + (a.group ? (8 * v) / a.group : 0)] = none ? 0.f : s;
+                put8_e4m3<WHOLE>((uint8_t *)a.y + row_at(row, a.ld_y) + 8 * v, n, h[i]);
+                if (a.group ? (v & ((1 << lg_group) - 1)) == 0 : v == 0)
+                    a.scales[row_at(row, a.ld_scales) + (a.group ? v >> lg_group : 0)] = none ? 0.f : s;
             }
         }
     }
@@ -185,80 +198,70 @@ struct NormGradArgs {
 };
 
 // Rows go to the groups of threads in turn; a thread's columns are the same for all of them, so the weight's gradient of
-// its rows stays in registers, and each workgroup leaves one row of sums.
-template <typename T, typename H, int VPT, int BLOCK>
-__global__ __launch_bounds__(BLOCK) void norm_bwd_kernel(const NormGradArgs a, int lg)
+// its rows stays in registers, and each workgroup leaves one row of sums.  Loads as in norm_fwd_kernel.
+template <typename T, typename H, int VPT, int THREADS, bool WHOLE, bool DSUM>
+__global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a, int lg)
 {
-    __shared__ float slots[2][BLOCK / WAVE];
+    __shared__ float slots[2][THREADS / WAVE];
     extern __shared__ float lds[];                           // [groups - 1][nv * 8]
-    const int g = 1 << lg, t = threadIdx.x & (g - 1), groups = BLOCK >> lg, gi = threadIdx.x >> lg;
+    const int g = 1 << lg, t = threadIdx.x & (g - 1), groups = blockDim.x >> lg, gi = threadIdx.x >> lg;
     const DropKey key = drop_key(a.drop);
     float w[VPT][8], dw[VPT][8];
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int v = i * g + t;
-        if (v < a.nv) weights8(a.weight, a.weight_type, v, a.N - 8 * v, w[i]);
+    for (int i = 0; i < VPT; ++i)
 #pragma unroll
         for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
-    }
+    weights<WHOLE>(a.weight, a.weight_type, g, t, a.nv, a.N, w);
     const float inv_n = 1.f / (float)a.N;
     int turn = 0;
     for (int64_t r0 = (int64_t)blockIdx.x * groups; r0 < a.rows; r0 += (int64_t)gridDim.x * groups, turn ^= 1) {
-        const int64_t row = r0 + gi;
-        const bool in = row < a.rows;
+        const bool in = r0 + gi < a.rows;
+        const int64_t row = in ? r0 + gi : a.rows - 1;
         Vec8<T> dy[VPT];
         Vec8<H> h[VPT], ds[VPT];
-        float rstd = 0.f;
-        if (in) {
-            rstd = a.rstd[row];
+        const float rstd = a.rstd[row];
 #pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                const int v = i * g + t, n = a.N - 8 * v;
-                if (v < a.nv) {
-                    dy[i] = fetch8((const T *)a.dy + row * a.ld_dy + 8 * v, n);
-                    h[i] = fetch8((const H *)a.h + row * a.ld_h + 8 * v, n);
-                    if (a.dsum) ds[i] = fetch8((const H *)a.dsum + row * a.ld_dsum + 8 * v, n);
-                }
-            }
+        for (int i = 0; i < VPT; ++i) {
+            const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
+            dy[i] = fetch8<WHOLE>((const T *)a.dy + row_at(row, a.ld_dy) + 8 * v, n);
+            h[i] = fetch8<WHOLE>((const H *)a.h + row_at(row, a.ld_h) + 8 * v, n);
+            if constexpr (DSUM) ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, n);
         }
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int v = i * g + t;
-            if (in && v < a.nv) {
-                float p[8], q[8];
-                widen8(dy[i], p);
-                widen8(h[i], q);
+            float p[8], q[8], part = 0.f;
+            widen8(dy[i], p);
+            widen8(h[i], q);
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (8 * v + j < a.N) {
-                        const float m = p[j] * q[j];
-                        dot = fmaf(m, w[i][j], dot);
-                        dw[i][j] = fmaf(m, rstd, dw[i][j]);
-                    }
+            for (int j = 0; j < 8; ++j) {
+                const float m = in ? p[j] * q[j] : 0.f;      // (columns behind the last are 0)
+                part = fmaf(m, w[i][j], part);
+                dw[i][j] = fmaf(m, rstd, dw[i][j]);
             }
+            dot += i * g + t < a.nv ? part : 0.f;
         }
         dot = row_reduce(dot, lg, slots[turn], [](float p, float q) { return p + q; });
         const float c = dot * inv_n * rstd * rstd * rstd;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = i * g + t, n = a.N - 8 * v;
-            if (!in || v >= a.nv) continue;
             float p[8], q[8], d[8];
             widen8(dy[i], p);
             widen8(h[i], q);
 #pragma unroll
             for (int j = 0; j < 8; ++j) d[j] = p[j] * w[i][j] * rstd - q[j] * c;
-            if (a.dsum) {
+            if constexpr (DSUM) {
                 float s[8];
                 widen8(ds[i], s);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[j] += s[j];
             }
-            if (a.dres) put8((H *)a.dres + row * a.ld_dres + 8 * v, n, d);
+            if (!in || v >= a.nv) continue;
+            if (a.dres) put8<WHOLE>((H *)a.dres + row_at(row, a.ld_dres) + 8 * v, n, d);
             if (a.dx) {
-                if (a.drop.state) drop8(a.drop, drop_mask(a.drop, key, (uint64_t)row * (uint64_t)a.nv + (uint64_t)v), d);
-                put8((T *)a.dx + row * a.ld_dx + 8 * v, n, d);
+                if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, a.drop.factor, d);
+                put8<WHOLE>((T *)a.dx + row_at(row, a.ld_dx) + 8 * v, n, d);
             }
         }
     }

@@ -1,0 +1,299 @@
+// C-ABI entry points of token embedding and dropout (declared in include/tt_emb.h): argument checks, workspace layout, kernel
+// selection and launches.  Nothing here allocates device memory or waits for the stream.
+
+#include "../../include/tt_emb.h"
+
+#include "tt_rows_args.h"
+#include "tt_token.h"
+
+using namespace tt;
+
+namespace {
+
+int check_tokens(const tt_tokens_t *t, int64_t *L)
+{
+    if (!t) return fail(TT_ERR_NULL, "tokens is NULL");
+    if (t->bits != 32 && t->bits != 64) return fail(TT_ERR_BAD_ARG, "tokens of 32 or 64 bits are expected");
+    if (t->L < 0) return fail(TT_ERR_BAD_ARG, "negative L");
+    if (t->L >= MOST_ROWS) return fail(TT_ERR_UNSUPPORTED, "2^31 tokens or more");
+    if (t->L > 0 && !t->data) return fail(TT_ERR_NULL, "tokens is NULL");
+    if ((uintptr_t)t->data % (t->bits / 8)) return fail(TT_ERR_BAD_ARG, "tokens are not aligned");
+    *L = t->L;
+    return TT_OK;
+}
+
+int rows_lg(int nv) { return lg_ceil(nv < WG ? nv : WG); }
+
+// rows_kernel: a workgroup covers up to WG vectors of a row
+template <typename S, typename D, int U, bool TOKENS, bool RESIDUAL>
+int launch_rows(const RowsArgs &a, hipStream_t st)
+{
+    const int lg = rows_lg(a.nv), ty = WG >> lg;
+    const int64_t blocks = ceil_div(a.rows, ty * U);
+    const int rc = check_grid(blocks, WG);
+    if (rc) return rc;
+    with_whole(a.N, [&](auto whole) {
+        hipLaunchKernelGGL((rows_kernel<S, D, U, decltype(whole)::value, TOKENS, RESIDUAL>), dim3((unsigned)blocks, (unsigned)ceil_div(a.nv, 1 << lg)), dim3(WG), 0, st, a, lg);
+    });
+    return TT_OK;
+}
+
+constexpr int64_t MOST_COLUMNS = 1 << 20;                    // of the kernels whose second grid dimension runs over the columns
+
+int check_columns(int64_t N)
+{
+    return N > MOST_COLUMNS ? fail(TT_ERR_UNSUPPORTED, "more than 2^20 columns") : TT_OK;
+}
+
+// ---- gradient of a token table ----
+
+constexpr int64_t MOST_GRAD_TOKENS = 1ll << 28;              // (a workgroup per tile of sorted positions)
+
+constexpr int64_t MOST_CLEAR_BLOCKS = 1 << 22;               // (they take turns beyond that)
+
+struct GradWs {
+    uint32_t *k[2], *v[2], *hist, *total;
+    float *part;
+    size_t bytes;
+};
+
+// entries per tile of sorted positions
+int grad_entries(int64_t L) { return L < 16384 ? 8 : TG_ENTRIES; }
+
+GradWs grad_ws(void *ws, int64_t L, int64_t N)
+{
+    GradWs w;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        char *p = ws ? (char *)ws + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return p;
+    };
+    const int64_t sort_tiles = ceil_div(L, TS_TILE);
+    int64_t tiles = ceil_div(L, grad_entries(L));
+    if (L >= 16384 && tiles < 2048) tiles = 2048;            // (what a shorter call needs at most)
+    for (int i = 0; i < 2; ++i) {
+        w.k[i] = (uint32_t *)take((size_t)L * 4);
+        w.v[i] = (uint32_t *)take((size_t)L * 4);
+    }
+    w.hist = (uint32_t *)take((size_t)sort_tiles * TS_BINS * 4);
+    w.total = (uint32_t *)take(TS_BINS * 4);
+    w.part = (float *)take((size_t)tiles * 2 * (size_t)(8 * ceil_div(N, 8)) * 4);
+    w.bytes = at;
+    return w;
+}
+
+hipError_t sort_tokens(const tt_tokens_t *t, int64_t num_rows, const GradWs &w, hipStream_t st, const uint32_t **ks, const uint32_t **vs)
+{
+    SortPass s{};
+    s.tokens = t->data;
+    s.wide = t->bits == 64;
+    s.n = t->L;
+    s.num_rows = num_rows;
+    s.tiles = (int)ceil_div(t->L, TS_TILE);
+    s.hist = w.hist;
+    s.total = w.total;
+    int bits = 1;                                            // num_rows itself is the key of no token
+    while (bits < 32 && (1ll << bits) <= num_rows) ++bits;
+    if (t->L <= TO_MOST) {
+        s.kout = w.k[0];
+        s.vout = w.v[0];
+        *ks = s.kout;
+        *vs = s.vout;
+        const int passes = (bits + 7) / 8;
+        auto one = [&](auto r) {
+            constexpr int R = decltype(r)::value;
+            static OncePerDevice once;
+            const hipError_t e = allow_dynamic_lds(once, (const void *)token_sort_one_kernel<R>, sort_one_lds(R));
+            if (e != hipSuccess) return e;
+            hipLaunchKernelGGL(token_sort_one_kernel<R>, dim3(1), dim3(TO_WG), sort_one_lds(R), st, s, passes);
+            return hipGetLastError();
+        };
+        if (t->L <= TO_WG) return one(std::integral_constant<int, 1>{});
+        if (t->L <= 4 * TO_WG) return one(std::integral_constant<int, 4>{});
+        return one(std::integral_constant<int, 8>{});
+    }
+    int at = 0;
+    for (s.shift = 0; s.shift < bits; s.shift += 9, at ^= 1) {
+        s.kout = w.k[at];
+        s.vout = w.v[at];
+        hipLaunchKernelGGL(token_hist_kernel, dim3(s.tiles), dim3(TS_WG), 0, st, s);
+        if (s.tiles > TS_SCAN_TILES) {
+            hipLaunchKernelGGL(token_scan_kernel, dim3(TS_BINS / WAVE), dim3(TS_WG), 0, st, s);
+            hipLaunchKernelGGL(token_scatter_kernel<true>, dim3(s.tiles), dim3(TS_WG), 0, st, s);
+        } else {
+            hipLaunchKernelGGL(token_scatter_kernel<false>, dim3(s.tiles), dim3(TS_WG), 0, st, s);
+        }
+        s.tokens = nullptr;
+        s.kin = s.kout;
+        s.vin = s.vout;
+    }
+    *ks = s.kin;
+    *vs = s.vin;
+    return hipGetLastError();
+}
+
+// the table's rows become old * row + factor * (sums of the gradient's rows)
+int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropout_t *dropout, const tt_rows_t *table, const char *name,
+               int64_t num_rows, int64_t N, float factor, bool old, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int64_t L;
+    GradArgs a{};
+    int rc = check_tokens(tokens, &L);
+    if (rc) return rc;
+    if (L >= MOST_GRAD_TOKENS) return fail(TT_ERR_UNSUPPORTED, "2^28 tokens or more");
+    if ((rc = check_sizes(num_rows, N)) || (rc = check_columns(N))) return rc;
+    if ((rc = check_rows(table, name, num_rows, N, OUT)) || (rc = check_rows(grad, "grad_output", L, N, IN))) return rc;
+    if ((rc = check_dropout(dropout, &a.drop))) return rc;
+    if (N == 0 || num_rows == 0 || (old && L == 0)) return TT_OK;
+    const size_t need = tt_token_bwd_workspace_bytes(L, N);
+    if (L > 0 && (!workspace || workspace_bytes < need))
+        return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+    if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
+    hipStream_t st = (hipStream_t)stream;
+    const GradWs w = grad_ws(workspace, L, N);
+    a.g = grad->data;
+    a.table = table->data;
+    a.part = w.part;
+    a.ld_g = grad->ld;
+    a.ld_table = table->ld;
+    a.n = L;
+    a.num_rows = num_rows;
+    a.N = (int)N;
+    a.nv = (int)ceil_div(N, 8);
+    a.entries = grad_entries(L);
+    a.tiles = (int)ceil_div(L, a.entries);
+    a.factor = a.drop.state ? factor * a.drop.factor : factor;
+    a.old = old;
+    int lg = lg_ceil(a.nv < WAVE ? a.nv : WAVE);
+    if (lg < TG_LEAST_LG) lg = TG_LEAST_LG;
+    const unsigned chunks = (unsigned)ceil_div(a.nv, 1 << lg);
+    const int64_t tile_blocks = ceil_div(a.tiles, WG >> lg) * chunks;
+    int64_t clear_rows = 65536 / (N * element_bytes(table->type)), clear_blocks = 0;
+    clear_rows = clear_rows < 1 ? 1 : clear_rows > TZ_MOST ? TZ_MOST : clear_rows;
+    if (!old) {
+        clear_blocks = ceil_div(num_rows, clear_rows);
+        if (clear_blocks > MOST_CLEAR_BLOCKS) clear_blocks = MOST_CLEAR_BLOCKS;
+    }
+    if ((rc = check_grid(tile_blocks + clear_blocks, WG))) return rc;
+    if (L > 0) {
+        const hipError_t e = sort_tokens(tokens, num_rows, w, st, &a.ks, &a.vs);
+        if (e != hipSuccess) return hip_fail(e, "token sort");
+    }
+    with_whole(N, [&](auto whole) {
+        with_type(grad->type, [&](auto g) {
+            with_type(table->type, [&](auto o) {
+                hipLaunchKernelGGL((token_grad_kernel<decltype(g), decltype(o), decltype(whole)::value>), dim3((unsigned)(tile_blocks + clear_blocks)), dim3(WG), 0, st,
+                                   a, lg, (int)chunks, tile_blocks, (int)clear_rows);
+            });
+        });
+    });
+    if (a.tiles > 1)
+        with_type(table->type, [&](auto o) { hipLaunchKernelGGL(token_join_kernel<decltype(o)>, dim3(a.tiles, chunks), dim3(WG), 0, st, a, lg); });
+    return launched("token gradient launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_tokens_t *tokens, float scale,
+                 const tt_dropout_t *dropout, const tt_rows_t *output, void *stream)
+{
+    int64_t L;
+    RowsArgs a{};
+    int rc = check_tokens(tokens, &L);
+    if (rc) return rc;
+    if ((rc = check_sizes(num_rows, N)) || (rc = check_columns(N))) return rc;
+    if ((rc = check_rows(table, "table", num_rows, N, IN)) || (rc = check_rows(output, "output", L, N, OUT))) return rc;
+    if ((rc = check_dropout(dropout, &a.drop))) return rc;
+    if (L == 0 || N == 0) return TT_OK;
+    a.src = table->data;
+    a.dst = output->data;
+    a.tokens = tokens->data;
+    a.ld_src = table->ld;
+    a.ld_dst = output->ld;
+    a.rows = L;
+    a.num_rows = num_rows;
+    a.N = (int)N;
+    a.nv = (int)ceil_div(N, 8);
+    a.wide = tokens->bits == 64;
+    a.scale = a.drop.state ? scale * a.drop.factor : scale;
+    if (num_rows == 0) {                                     // no token is one: rows of zeros, for which nothing has to be there to be read
+        a.src = output->data;
+        a.ld_src = 0;
+        a.drop.state = nullptr;
+    }
+    with_type(num_rows ? table->type : output->type, [&](auto s) {
+        with_type(output->type, [&](auto d) {
+            // few tokens: one row per thread, so that more of the device has some
+            if (L * a.nv < (1 << 20)) rc = launch_rows<decltype(s), decltype(d), 1, true, false>(a, (hipStream_t)stream);
+            else rc = launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
+        });
+    });
+    if (rc) return rc;
+    return launched("token lookup launch");
+}
+
+size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t N)
+{
+    if (L <= 0 || N <= 0 || L >= MOST_GRAD_TOKENS || N > MOST_COLUMNS) return 0;
+    return grad_ws(nullptr, L, N).bytes;
+}
+
+int tt_token_bwd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
+                 const tt_rows_t *grad_table, int64_t num_rows, int64_t N, int accumulate,
+                 void *workspace, size_t workspace_bytes, void *stream)
+{
+    return token_grad(tokens, grad_output, dropout, grad_table, "grad_table", num_rows, N, scale, accumulate != 0, workspace, workspace_bytes, stream);
+}
+
+int tt_token_bwd_sgd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
+                     const tt_rows_t *table, int64_t num_rows, int64_t N, float lr,
+                     void *workspace, size_t workspace_bytes, void *stream)
+{
+    return token_grad(tokens, grad_output, dropout, table, "table", num_rows, N, -lr * scale, true, workspace, workspace_bytes, stream);
+}
+
+static int dropout_rows(const tt_rows_t *x, const tt_rows_t *residual, const tt_dropout_t *dropout, const tt_rows_t *out,
+                        const char *in_name, const char *out_name, int64_t rows, int64_t N, void *stream)
+{
+    RowsArgs a{};
+    int rc = check_sizes(rows, N);
+    if (rc) return rc;
+    if ((rc = check_columns(N)) || (rc = check_rows(x, in_name, rows, N, IN)) || (rc = check_rows(out, out_name, rows, N, OUT))) return rc;
+    if (residual && (rc = check_rows(residual, "residual", rows, N, IN))) return rc;
+    if (out->type != x->type || (residual && residual->type != x->type)) return fail(TT_ERR_UNSUPPORTED, "arrays of one type are expected");
+    if (!dropout) return fail(TT_ERR_NULL, "dropout is NULL");
+    if ((rc = check_dropout(dropout, &a.drop))) return rc;
+    if (rows == 0 || N == 0) return TT_OK;
+    a.src = x->data;
+    a.residual = residual ? residual->data : nullptr;
+    a.dst = out->data;
+    a.ld_src = x->ld;
+    a.ld_res = residual ? residual->ld : 0;
+    a.ld_dst = out->ld;
+    a.rows = a.num_rows = rows;
+    a.N = (int)N;
+    a.nv = (int)ceil_div(N, 8);
+    a.scale = a.drop.state ? a.drop.factor : 1.f;
+    with_type(x->type, [&](auto s) {
+        if (residual) rc = launch_rows<decltype(s), decltype(s), 1, false, true>(a, (hipStream_t)stream);
+        else rc = launch_rows<decltype(s), decltype(s), 1, false, false>(a, (hipStream_t)stream);
+    });
+    if (rc) return rc;
+    return launched("dropout launch");
+}
+
+int tt_dropout_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_dropout_t *dropout, const tt_rows_t *output,
+                   int64_t n_rows, int64_t N, void *stream)
+{
+    return dropout_rows(x, residual, dropout, output, "x", "output", n_rows, N, stream);
+}
+
+int tt_dropout_bwd(const tt_rows_t *grad_output, const tt_dropout_t *dropout, const tt_rows_t *grad_x, int64_t n_rows, int64_t N, void *stream)
+{
+    return dropout_rows(grad_output, nullptr, dropout, grad_x, "grad_output", "grad_x", n_rows, N, stream);
+}
+
+}  // extern "C"

@@ -580,3 +580,12 @@ def test_binding_refuses_what_does_not_fit():
             bad()
         assert e.value.code == code, e.value
     assert not out.any() and not table.any()
+
+
+def test_a_table_without_rows_gives_zeros():
+    for N in (5, 64):
+        for s, o in ((F32, BF16), (BF16, F32)):
+            out, flat = room(9, N, o, 1, 1)
+            B.tt_token_fwd(torch.empty((0, N), dtype=s, device="cuda:0"), tokens_of(gen(1), 9, 5, "some"), out, dropout=dropout_of(0.5))
+            assert not out.any()
+            assert_guard(out, flat)
