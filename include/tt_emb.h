@@ -653,9 +653,9 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
  * forward pass).  The positions are sorted by token and every row is written once.  accumulate == 0: all num_rows rows are
  * written, zeros where no token is; else the sums are added to grad_table, whose other rows are not touched.
  * tt_token_bwd_sgd: table -= lr * gradient in place, rows in use only.
- * workspace: tt_token_bwd_workspace_bytes(L, N) bytes, 16-byte aligned (enough for fewer tokens too).  L < 2^28.
+ * workspace: tt_token_bwd_workspace_bytes(L, num_rows, N) bytes, 16-byte aligned (enough for fewer tokens too).  L < 2^28.
  */
-size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t N);
+size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t num_rows, int64_t N);
 int tt_token_bwd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
                  const tt_rows_t *grad_table, int64_t num_rows, int64_t N, int accumulate,
                  void *workspace, size_t workspace_bytes, void *stream);

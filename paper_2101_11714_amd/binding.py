@@ -128,7 +128,7 @@ def lib():
         l.tt_emb_debug_set_fast_path.argtypes = [C.c_int]
         l.tt_token_fwd.argtypes = [vp, i64, i64, vp, f32, vp, vp, vp]
         l.tt_token_bwd_workspace_bytes.restype = C.c_size_t
-        l.tt_token_bwd_workspace_bytes.argtypes = [i64, i64]
+        l.tt_token_bwd_workspace_bytes.argtypes = [i64, i64, i64]
         l.tt_token_bwd.argtypes = [vp, vp, f32, vp, vp, i64, i64, C.c_int, vp, C.c_size_t, vp]
         l.tt_token_bwd_sgd.argtypes = [vp, vp, f32, vp, vp, i64, i64, f32, vp, C.c_size_t, vp]
         l.tt_dropout_fwd.argtypes = [vp, vp, vp, vp, i64, i64, vp]
@@ -648,8 +648,8 @@ def tt_token_fwd(table: torch.Tensor, tokens: torch.Tensor, output: torch.Tensor
     return output
 
 
-def token_bwd_workspace_bytes(L: int, N: int) -> int:
-    return int(lib().tt_token_bwd_workspace_bytes(int(L), int(N)))
+def token_bwd_workspace_bytes(L: int, num_rows: int, N: int) -> int:
+    return int(lib().tt_token_bwd_workspace_bytes(int(L), int(num_rows), int(N)))
 
 
 def tt_token_bwd(tokens: torch.Tensor, grad_output: torch.Tensor, grad_table: torch.Tensor, scale: float = 1.0,

@@ -11,22 +11,40 @@ using namespace tt;
 namespace {
 
 struct NormShape {
-    int lg, vpt, threads;
+    int lg, vpt;
 };
 
-// Threads per row (log), vectors per thread, threads per workgroup.
-NormShape norm_shape(int64_t rows, int64_t nv, int least_lg, int most_lg)
+// Threads per row (log) and vectors per thread.
+NormShape norm_shape(int lg, int64_t nv)
+{
+    int vpt = 1;
+    while ((int64_t)vpt << lg < nv) vpt <<= 1;
+    return {lg, vpt};
+}
+
+// Few rows: as many threads as vectors, so that the call ends soon.  Enough rows: two vectors a thread, a wave's worth of threads
+// at least (rows of 4,096, 16 bits, four vectors: 85 us instead of 81).
+NormShape norm_fwd_shape(int64_t rows, int64_t nv, int least_lg)
 {
     int lg = lg_ceil(nv);
-    if (rows > 512) {                                        // enough rows: two vectors a thread, a wave's worth of threads at least
+    if (rows > 512) {
         const int two = lg_ceil(ceil_div(nv, 2));
         lg = two > 6 ? two : lg < 6 ? lg : 6;
     }
-    if (lg > most_lg) lg = most_lg;
-    if (lg < least_lg) lg = least_lg;
-    int vpt = 1;
-    while ((int64_t)vpt << lg < nv) vpt <<= 1;
-    return {lg, vpt, lg > 8 ? 1 << lg : WG};
+    if (lg > 10) lg = 10;
+    return norm_shape(lg < least_lg ? least_lg : lg, nv);
+}
+
+// The gradients' workgroups have NORM_BWD_THREADS threads (1,024 have too few registers: for the longest rows alone).
+constexpr int NORM_BWD_THREADS = 512;
+constexpr int64_t NORM_BWD_WORKGROUPS = 256;
+
+int norm_bwd_threads(int64_t nv) { return nv > 4 * NORM_BWD_THREADS ? 1024 : NORM_BWD_THREADS; }
+
+NormShape norm_bwd_shape(int64_t nv)
+{
+    const int lg = lg_ceil(nv), most = lg_ceil(norm_bwd_threads(nv));
+    return norm_shape(lg < most ? lg : most, nv);
 }
 
 template <typename F>
@@ -61,17 +79,6 @@ int check_weight(const void *weight, int32_t type)
     if (!weight) return TT_OK;
     if (type != TT_F32 && type != TT_BF16 && type != TT_F16) return fail(TT_ERR_UNSUPPORTED, "weight: type %d is not supported", (int)type);
     return (uintptr_t)weight % element_bytes(type) ? fail(TT_ERR_BAD_ARG, "weight is not aligned to its elements") : TT_OK;
-}
-
-int norm_bwd_groups(const NormShape &s) { return s.threads >> s.lg; }
-
-constexpr int NORM_BWD_THREADS = 512;                       // (1,024 threads have too few registers; they take the longest rows alone)
-constexpr int64_t NORM_BWD_WORKGROUPS = 1024;
-
-int64_t norm_bwd_grid(int64_t rows, const NormShape &s)
-{
-    const int64_t all = ceil_div(rows, norm_bwd_groups(s));
-    return all < NORM_BWD_WORKGROUPS ? all : NORM_BWD_WORKGROUPS;
 }
 
 }  // namespace
@@ -122,16 +129,17 @@ int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_
     a.nv = (int)ceil_div(N, 8);
     a.group = group;
     a.eps = eps;
-    const NormShape s = norm_shape(n_rows, a.nv, group ? lg_ceil(group / 8) : 0, 10);
-    if ((rc = check_grid(ceil_div(n_rows, s.threads >> s.lg), s.threads))) return rc;
-    const dim3 grid((unsigned)ceil_div(n_rows, s.threads >> s.lg));
+    const NormShape s = norm_fwd_shape(n_rows, a.nv, group ? lg_ceil(group / 8) : 0);
+    const int threads = s.lg > 8 ? 1 << s.lg : WG;
+    if ((rc = check_grid(ceil_div(n_rows, threads >> s.lg), threads))) return rc;
+    const dim3 grid((unsigned)ceil_div(n_rows, threads >> s.lg));
     with_types(x->type, stream_type, [&](auto t, auto h) {
         with_vpt(s.vpt, [&](auto vpt) {
             with_whole(N, [&](auto whole) {
                 with_flag(residual != nullptr, [&](auto res) {
                     with_flag(bits8, [&](auto y8) {
                         hipLaunchKernelGGL((norm_fwd_kernel<decltype(t), decltype(h), decltype(y8)::value, decltype(vpt)::value, decltype(whole)::value, decltype(res)::value>), grid,
-                                           dim3(s.threads), 0, (hipStream_t)stream, a, s.lg);
+                                           dim3(threads), 0, (hipStream_t)stream, a, s.lg);
                     });
                 });
             });
@@ -193,19 +201,20 @@ int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const 
     a.weight_type = weight_type;
     int64_t grid = 0;
     if (n_rows > 0) {
-        const NormShape s = norm_shape(n_rows, a.nv, 0, a.nv > 4 * NORM_BWD_THREADS ? 10 : 9);
-        grid = norm_bwd_grid(n_rows, s);
-        const size_t lds = grad_weight ? (size_t)(norm_bwd_groups(s) - 1) * 8 * a.nv * sizeof(float) : 0;
+        const NormShape s = norm_bwd_shape(a.nv);
+        const int threads = norm_bwd_threads(a.nv), groups = threads >> s.lg, parts = s.lg < 6 ? threads / WAVE : groups;
+        grid = ceil_div(n_rows, groups) < NORM_BWD_WORKGROUPS ? ceil_div(n_rows, groups) : NORM_BWD_WORKGROUPS;
+        const size_t lds = grad_weight && parts > 1 ? (size_t)parts * 8 * a.nv * sizeof(float) : 0;
         with_types(grad_output->type, h->type, [&](auto t, auto ht) {
-            auto launch = [&](auto vpt, auto threads) {
+            auto launch = [&](auto vpt, auto most) {
                 with_whole(N, [&](auto whole) {
                     with_flag(grad_sum != nullptr, [&](auto dsum) {
-                        hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), decltype(ht), decltype(vpt)::value, decltype(threads)::value, decltype(whole)::value, decltype(dsum)::value>),
-                                           dim3((unsigned)grid), dim3(s.threads), lds, st, a, s.lg);
+                        hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), decltype(ht), decltype(vpt)::value, decltype(most)::value, decltype(whole)::value, decltype(dsum)::value>),
+                                           dim3((unsigned)grid), dim3(threads), lds, st, a, s.lg);
                     });
                 });
             };
-            if (s.lg == 10) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 1024>{});
+            if (threads == 1024) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 1024>{});
             else with_vpt(s.vpt, [&](auto vpt) { launch(vpt, std::integral_constant<int, NORM_BWD_THREADS>{}); });
         });
     }

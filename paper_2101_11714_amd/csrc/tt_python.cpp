@@ -703,7 +703,7 @@ PyObject *token_grad(Args &g, F f)
     if (!g.ok) return nullptr;
     at::DataPtr mem;
     if (!ws) {
-        wsb = tt_token_bwd_workspace_bytes(L, N);
+        wsb = tt_token_bwd_workspace_bytes(L, num_rows, N);
         mem = scratch(wsb, stream());
         if (!mem) wsb = 0;
         ws = mem.get();

@@ -124,7 +124,9 @@ __global__ __launch_bounds__(RN_THREADS) void norm_fwd_kernel(const NormArgs a, 
         for (int i = 0; i < VPT; ++i) {
             const int v = min(i * g + t, a.nv - 1);
             widen8(x[i], h[i]);
-            if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, a.drop.factor, h[i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[i][j] *= a.drop.factor;
+            if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, h[i]);
             if constexpr (RESIDUAL) {
                 float r[8];
                 widen8(res[i], r);
@@ -203,8 +205,8 @@ template <typename T, typename H, int VPT, int THREADS, bool WHOLE, bool DSUM>
 __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a, int lg)
 {
     __shared__ float slots[2][THREADS / WAVE];
-    extern __shared__ float lds[];                           // [groups - 1][nv * 8]
-    const int g = 1 << lg, t = threadIdx.x & (g - 1), groups = blockDim.x >> lg, gi = threadIdx.x >> lg;
+    extern __shared__ float lds[];                           // [waves, or groups of whole waves][nv * 8], if more than one
+    const int g = 1 << lg, t = threadIdx.x & (g - 1), groups = THREADS >> lg, gi = threadIdx.x >> lg;
     const DropKey key = drop_key(a.drop);
     float w[VPT][8], dw[VPT][8];
 #pragma unroll
@@ -260,38 +262,41 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
             if (!in || v >= a.nv) continue;
             if (a.dres) put8<WHOLE>((H *)a.dres + row_at(row, a.ld_dres) + 8 * v, n, d);
             if (a.dx) {
-                if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, a.drop.factor, d);
+                if (a.drop.state) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[j] *= a.drop.factor;
+                    drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, d);
+                }
                 put8<WHOLE>((T *)a.dx + row_at(row, a.ld_dx) + 8 * v, n, d);
             }
         }
     }
     if (!a.part) return;
-    if (groups > 1) {
-        __syncthreads();
-        if (gi) {
+    // groups of a wave by lane exchange, then waves (or groups of more than one wave) through LDS, in their order
+    for (int b = lg; b < 6; ++b)
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
-                if (i * g + t < a.nv)
+        for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) lds[(gi - 1) * (8 * a.nv) + j * a.nv + i * g + t] = dw[i][j];
+            for (int j = 0; j < 8; ++j) dw[i][j] += __shfl_xor(dw[i][j], 1 << b);
+    const int parts = lg < 6 ? THREADS / WAVE : groups, at = lg < 6 ? threadIdx.x >> 6 : gi, cols = 8 * a.nv;
+    float *out = a.part + (int64_t)blockIdx.x * cols;
+    if (parts > 1) out = lds + at * cols;
+    if (lg >= 6 || (threadIdx.x & 63) < g) {
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) {
+            const int v = i * g + t;
+            if (v < a.nv) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) out[8 * v + j] = dw[i][j];
+            }
         }
-        __syncthreads();
-        if (gi) return;
-        for (int q = 1; q < groups; ++q)
-#pragma unroll
-            for (int i = 0; i < VPT; ++i)
-                if (i * g + t < a.nv)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) dw[i][j] += lds[(q - 1) * (8 * a.nv) + j * a.nv + i * g + t];
     }
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-        const int v = i * g + t;
-        if (v < a.nv) {
-            float *p = a.part + (int64_t)blockIdx.x * (8 * a.nv) + 8 * v;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) p[j] = dw[i][j];
-        }
+    if (parts == 1) return;
+    __syncthreads();
+    for (int c = threadIdx.x; c < cols; c += THREADS) {
+        float s = lds[c];
+        for (int q = 1; q < parts; ++q) s += lds[q * cols + c];
+        a.part[(int64_t)blockIdx.x * cols + c] = s;
     }
 }
 

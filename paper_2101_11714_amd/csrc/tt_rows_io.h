@@ -47,6 +47,17 @@ __device__ __forceinline__ void put8(T *p, int n, const float (&x)[8])
     }
 }
 
+// all zeros unless `keep`, before anything is computed from them (a register holds two 16-bit values)
+template <typename T>
+__device__ __forceinline__ void keep8(bool keep, Vec8<T> &r)
+{
+    struct Words { uint32_t w[2 * sizeof(T)]; };
+    Words x = __builtin_bit_cast(Words, r);
+#pragma unroll
+    for (unsigned j = 0; j < 2 * sizeof(T); ++j) x.w[j] = keep ? x.w[j] : 0u;
+    r = __builtin_bit_cast(Vec8<T>, x);
+}
+
 template <typename T>
 __device__ __forceinline__ void widen8(const Vec8<T> &r, float (&x)[8])
 {
@@ -95,7 +106,7 @@ struct DropArgs {
     const int64_t *state;        // device: seed, step; null: no dropout
     uint32_t site;
     uint32_t most;               // 65536 q - 1: a column is dropped whose draw, as the high half of a word, is at most this
-    float factor;
+    float factor;                // 1 without dropout
 };
 
 struct DropKey {
@@ -114,8 +125,8 @@ __device__ __forceinline__ DropKey drop_key(const DropArgs &d)
     return k;
 }
 
-// Dropout of the columns of one block.  (Chosen, not multiplied: a dropped value is 0 whatever it was.)
-__device__ __forceinline__ void drop8(const DropArgs &d, const DropKey &k, uint64_t block, float factor, float (&x)[8])
+// The columns of one block that are dropped become 0, whatever they were; the factor of the others is the caller's.
+__device__ __forceinline__ void drop8(const DropArgs &d, const DropKey &k, uint64_t block, float (&x)[8])
 {
     uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = d.site, c3 = k.step, k0 = k.k0, k1 = k.k1;
 #pragma unroll
@@ -131,8 +142,8 @@ __device__ __forceinline__ void drop8(const DropArgs &d, const DropKey &k, uint6
     const uint32_t w[4] = {c0, c1, c2, c3};
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[2 * j] = (w[j] << 16) > d.most ? x[2 * j] * factor : 0.f;
-        x[2 * j + 1] = w[j] > d.most ? x[2 * j + 1] * factor : 0.f;
+        x[2 * j] = (w[j] << 16) > d.most ? x[2 * j] : 0.f;
+        x[2 * j + 1] = w[j] > d.most ? x[2 * j + 1] : 0.f;
     }
 }
 

@@ -29,7 +29,7 @@ __device__ __forceinline__ int64_t token_at(const void *tokens, int wide, int64_
 
 // tx threads (a power of two) along a row, WG / tx rows side by side, U rows per thread.  No load stands in a branch: what is loaded
 // there is waited for there, one load after the other; a row or a token that does not exist reads the first one instead.
-// U = 1 for dropout alone (U = 2 and 4 took 10 and 20 % longer: more workgroups hide more than longer ones), 2 for lookups, whose
+// U = 1 for dropout alone (2 and 4 took 10 and 20 % longer: more workgroups hide more than longer ones), more for lookups, whose
 // loads wait for the tokens.
 template <typename S, typename D, int U, bool WHOLE, bool TOKENS, bool RESIDUAL>
 __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
@@ -64,18 +64,12 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
     for (int u = 0; u < U; ++u) {
         const int64_t r = r0 + u * ty;
         if (r >= a.rows) break;
+        if constexpr (TOKENS) keep8(there[u], x[u]);
         float y[8];
         widen8(x[u], y);
-        if (a.drop.state) {
-            drop8(a.drop, key, (uint64_t)row_at(r, a.nv) + (uint64_t)v, a.scale, y);
-        } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] *= a.scale;
-        }
-        if constexpr (TOKENS) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) y[j] = there[u] ? y[j] : 0.f;
-        }
+        for (int j = 0; j < 8; ++j) y[j] *= a.scale;
+        if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(r, a.nv) + (uint64_t)v, y);
         if constexpr (RESIDUAL) {
             float z[8];
             widen8(res[u], z);
@@ -88,10 +82,12 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
 
 // ---- stable sort of (token, position) ------------------------------------------------------------------------------
 
-constexpr int TS_WG = 512, TS_SUB = 4, TS_TILE = TS_WG * TS_SUB;             // keys per workgroup and pass
-constexpr int TS_BINS = 512;                                                // digits of up to 9 bits
+// By digits of up to 10 bits, low ones first, as few passes as that allows.
+constexpr int TS_WG = 1024, TS_SUB = 2, TS_TILE = TS_WG * TS_SUB;           // keys per workgroup and pass
+constexpr int TS_BITS = 10, TS_BINS = 1 << TS_BITS;
 constexpr int TS_WAVES = TS_WG / WAVE;
 constexpr int TS_SCAN_TILES = 64;                                           // more tiles: their counts are scanned by a kernel
+static_assert(TS_BINS == TS_WG, "a thread per bin");
 
 struct SortPass {
     const void *tokens;          // first pass: the keys come from here
@@ -99,10 +95,19 @@ struct SortPass {
     uint32_t *kout, *vout;
     uint32_t *hist;              // [tile][bin] counts; scanned: of the earlier tiles
     uint32_t *total;             // [bin], scanned only
+    uint8_t *named;              // a byte per row, or null: cleared by the first kernel, set by the next one
+    bool blank;                  // (by this kernel)
     int64_t n;
     int64_t num_rows;
-    int wide, shift, tiles;
+    int wide, shift, bits, tiles;
 };
+
+// (16-byte aligned, with room up to a multiple of 16)
+__device__ __forceinline__ void blank_named(const SortPass &s)
+{
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; 16 * i < s.num_rows; i += (int64_t)gridDim.x * blockDim.x)
+        reinterpret_cast<uint4 *>(s.named)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
 
 // no token sorts behind all rows
 __device__ __forceinline__ uint32_t sort_key(const SortPass &s, int64_t i)
@@ -117,18 +122,19 @@ __global__ __launch_bounds__(TS_WG) void token_hist_kernel(const SortPass s)
     __shared__ uint32_t h[TS_BINS];
     const int t = threadIdx.x;
     const int64_t base = (int64_t)blockIdx.x * TS_TILE;
+    if (s.blank) blank_named(s);
     h[t] = 0;
     __syncthreads();
 #pragma unroll
     for (int q = 0; q < TS_SUB; ++q) {
         const int64_t i = base + q * TS_WG + t;
-        if (i < s.n) atomicAdd(&h[(sort_key(s, i) >> s.shift) & (TS_BINS - 1)], 1u);
+        if (i < s.n) atomicAdd(&h[(sort_key(s, i) >> s.shift) & ((1u << s.bits) - 1u)], 1u);
     }
     __syncthreads();
     s.hist[(int64_t)blockIdx.x * TS_BINS + t] = h[t];
 }
 
-// Counts become the counts of the earlier tiles.  64 bins a workgroup, 8 stretches of tiles side by side.
+// Counts become the counts of the earlier tiles.  64 bins a workgroup, a stretch of the tiles per wave.
 __global__ __launch_bounds__(TS_WG) void token_scan_kernel(const SortPass s)
 {
     __shared__ uint32_t sum[TS_WAVES][WAVE];
@@ -153,35 +159,59 @@ __global__ __launch_bounds__(TS_WG) void token_scan_kernel(const SortPass s)
     if (w == 0) s.total[bin] = all;
 }
 
-// Thread t works for bin t: where the bin starts (keys of smaller bins, then the bin's keys of earlier tiles), then the
-// bin's places by (round, wave) of this tile; a key's rank among its wave's equal digits comes from ballots.
-template <bool SCANNED>
-__global__ __launch_bounds__(TS_WG) void token_scatter_kernel(const SortPass s)
+// Among a wave's lanes that are `in`: how many have this lane's digit, in lower lanes (low half) and in all (high half).
+__device__ __forceinline__ uint32_t rank_digit(uint32_t digit, int bits, bool in)
 {
-    __shared__ uint16_t cnt[TS_SUB * TS_WAVES][TS_BINS];
-    __shared__ uint32_t start[TS_BINS], wsum[TS_WAVES];
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-    const int64_t base = (int64_t)blockIdx.x * TS_TILE;
-    uint32_t key[TS_SUB], pos[TS_SUB];
+    const uint64_t there = __ballot(in);
+    uint32_t lo = (uint32_t)there, hi = (uint32_t)(there >> 32);
 #pragma unroll
-    for (int q = 0; q < TS_SUB; ++q) {
-        const int64_t i = base + q * TS_WG + t;
-        key[q] = i < s.n ? sort_key(s, i) : 0u;
-        pos[q] = i < s.n && !s.tokens ? s.vin[i] : (uint32_t)i;
-    }
-    uint32_t all = 0, before = 0;
-    if constexpr (SCANNED) {
-        all = s.total[t];
-        before = s.hist[(int64_t)blockIdx.x * TS_BINS + t];
-    } else {
-#pragma unroll 8
-        for (int b = 0; b < s.tiles; ++b) {
-            const uint32_t c = s.hist[b * TS_BINS + t];
-            all += c;
-            before += b < (int)blockIdx.x ? c : 0u;
+    for (int b = 0; b < TS_BITS; ++b) {
+        if (b < bits) {                                      // uniform
+            const int set = (int)(digit << (31 - b)) >> 31;  // all ones, or none
+            const uint64_t bal = __ballot(set != 0);
+            lo = __builtin_amdgcn_bitop3_b32(lo, (uint32_t)bal, (uint32_t)set, 0x90);    // lo & ~(bal ^ set)
+            hi = __builtin_amdgcn_bitop3_b32(hi, (uint32_t)(bal >> 32), (uint32_t)set, 0x90);
         }
     }
-    for (int g = 0; g < TS_SUB * TS_WAVES; ++g) cnt[g][t] = 0;
+    const uint32_t lower = __builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0u));
+    return lower | (uint32_t)(__popc(lo) + __popc(hi)) << 16;
+}
+
+// The place of a key among its wave's keys of its digit: those that the wave counted before, then the lower lanes'.  `mine`: the
+// wave's own counts in LDS, which it reads and writes in its own order.
+__device__ __forceinline__ uint32_t count_digit(uint16_t *mine, uint32_t digit, uint32_t rank, bool in)
+{
+    const uint32_t before = in ? mine[digit] : 0u;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    if (in && (rank & 0xffffu) == 0) mine[digit] = (uint16_t)(before + (rank >> 16));
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    return before + (rank & 0xffffu);
+}
+
+// Places of the keys of a workgroup of TS_WG threads, R per thread, whose wave w owns R * 64 neighbouring ones, by digit, then by
+// (wave, round, lane): place[r] = start of the key's digit + its place there.  before_me: of thread t, keys of digit t that are not this
+// workgroup's and come first; all_keys: all keys of digit t (0, 0 where there is one workgroup).  cnt: [wave][digit], wsum: [wave].
+template <int R>
+__device__ __forceinline__ void places(const uint32_t (&digit)[R], const bool (&in)[R], int bits, bool one, uint32_t all_keys, uint32_t before_me,
+                                       uint16_t *cnt, uint32_t *start, uint32_t *wsum, uint32_t (&place)[R])
+{
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+    uint16_t *mine = cnt + w * TS_BINS;
+#pragma unroll
+    for (int q = 0; q < TS_BINS / WAVE / 2; ++q) reinterpret_cast<uint32_t *>(mine)[q * WAVE + lane] = 0;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+    for (int r = 0; r < R; ++r) place[r] = rank_digit(digit[r], bits, in[r]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) place[r] = count_digit(mine, digit[r], place[r], in[r]);
+    __syncthreads();
+    uint32_t c[TS_WAVES], own = 0;
+#pragma unroll
+    for (int q = 0; q < TS_WAVES; ++q) {
+        c[q] = cnt[q * TS_BINS + t];
+        own += c[q];
+    }
+    const uint32_t all = one ? own : all_keys;
     uint32_t inc = all;
 #pragma unroll
     for (int d = 1; d < WAVE; d <<= 1) {
@@ -189,118 +219,96 @@ __global__ __launch_bounds__(TS_WG) void token_scatter_kernel(const SortPass s)
         if (lane >= d) inc += o;
     }
     if (lane == WAVE - 1) wsum[w] = inc;
+    uint32_t run = 0;
+#pragma unroll
+    for (int q = 0; q < TS_WAVES; ++q) {
+        cnt[q * TS_BINS + t] = (uint16_t)run;
+        run += c[q];
+    }
     __syncthreads();
-    uint32_t first = inc - all + before;
+    uint32_t first = inc - all + before_me;
     for (int q = 0; q < w; ++q) first += wsum[q];
-    int rank[TS_SUB];
-#pragma unroll
-    for (int q = 0; q < TS_SUB; ++q) {
-        const bool in = base + q * TS_WG + t < s.n;
-        const uint32_t dg = (key[q] >> s.shift) & (TS_BINS - 1);
-        uint64_t same = __ballot(in);
-#pragma unroll
-        for (int b = 0; b < 9; ++b) {
-            const bool bit = (dg >> b) & 1u;
-            const uint64_t bal = __ballot(bit);
-            same &= bit ? bal : ~bal;
-        }
-        rank[q] = __popcll(same & lanemask_lt());
-        if (in && rank[q] == 0) cnt[q * TS_WAVES + w][dg] = (uint16_t)__popcll(same);
-    }
-    __syncthreads();
-    {
-        uint32_t run = 0;
-        for (int g = 0; g < TS_SUB * TS_WAVES; ++g) {
-            const uint32_t c = cnt[g][t];
-            cnt[g][t] = (uint16_t)run;
-            run += c;
-        }
-        start[t] = first;
-    }
+    start[t] = first;
     __syncthreads();
 #pragma unroll
+    for (int r = 0; r < R; ++r) place[r] += start[digit[r]] + mine[digit[r]];
+}
+
+template <bool SCANNED>
+__global__ __launch_bounds__(TS_WG) void token_scatter_kernel(const SortPass s)
+{
+    __shared__ uint32_t start[TS_BINS], wsum[TS_WAVES];
+    __shared__ __align__(16) uint16_t cnt[TS_WAVES * TS_BINS];
+    const int t = threadIdx.x;
+    const int64_t base = (int64_t)blockIdx.x * TS_TILE + (t >> 6) * (TS_SUB * WAVE) + (t & 63);
+    uint32_t key[TS_SUB], pos[TS_SUB], digit[TS_SUB], place[TS_SUB];
+    bool in[TS_SUB];
+#pragma unroll
     for (int q = 0; q < TS_SUB; ++q) {
-        if (base + q * TS_WG + t >= s.n) continue;
-        const uint32_t dg = (key[q] >> s.shift) & (TS_BINS - 1);
-        const uint32_t to = start[dg] + cnt[q * TS_WAVES + w][dg] + (uint32_t)rank[q];
-        s.kout[to] = key[q];
-        s.vout[to] = pos[q];
+        const int64_t i = base + q * WAVE;
+        in[q] = i < s.n;
+        key[q] = in[q] ? sort_key(s, i) : 0u;
+        pos[q] = in[q] && !s.tokens ? s.vin[i] : (uint32_t)i;
+        digit[q] = (key[q] >> s.shift) & ((1u << s.bits) - 1u);
+        if (s.named && in[q] && key[q] < (uint32_t)s.num_rows) s.named[key[q]] = 1;
+    }
+    uint32_t all = 0, before = 0;
+    if constexpr (SCANNED) {
+        all = s.total[t];
+        before = s.hist[(int64_t)blockIdx.x * TS_BINS + t];
+    } else {
+        for (int b0 = 0; b0 < s.tiles; b0 += 16) {
+            uint32_t c[16];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) c[q] = s.hist[min(b0 + q, s.tiles - 1) * TS_BINS + t];
+#pragma unroll
+            for (int q = 0; q < 16; ++q) {
+                all += b0 + q < s.tiles ? c[q] : 0u;
+                before += b0 + q < (int)blockIdx.x ? c[q] : 0u;
+            }
+        }
+    }
+    places<TS_SUB>(digit, in, s.bits, false, all, before, cnt, start, wsum, place);
+#pragma unroll
+    for (int q = 0; q < TS_SUB; ++q) {
+        if (!in[q]) continue;
+        s.kout[place[q]] = key[q];
+        s.vout[place[q]] = pos[q];
     }
 }
 
-// Up to 8,192 tokens: the whole sort in one workgroup, in LDS.  A wave owns R * 64 neighbouring entries and ranks 64 of them at a
-// time among the wave's earlier ones with the same digit; the counts by (digit, wave) become starting places.  One launch instead
-// of two per digit.  Not beyond: one workgroup took 48 us for 16,384 tokens of 1,000,000 rows, the launches per digit 32.
-constexpr int TO_WG = 1024, TO_WAVES = TO_WG / WAVE, TO_BINS = 256, TO_MOST = 8 * TO_WG;
+// Few tokens: the whole sort in one workgroup, in LDS.  One launch instead of two per digit.
+constexpr int TO_MOST = 8 * TS_WG;
 
-static inline size_t sort_one_lds(int R) { return (size_t)R * TO_WG * 6 + (size_t)TO_WAVES * TO_BINS * 4 + 32; }
+static inline size_t sort_one_lds(int R) { return (size_t)R * TS_WG * 6 + (size_t)TS_WAVES * TS_BINS * 2 + TS_BINS * 4 + TS_WAVES * 4; }
 
 template <int R>
-__global__ __launch_bounds__(TO_WG) void token_sort_one_kernel(const SortPass s, int passes)
+__global__ __launch_bounds__(TS_WG) void token_sort_one_kernel(const SortPass s, int passes)
 {
     extern __shared__ uint32_t lds_u32[];
-    uint32_t *keys = lds_u32, *cnt = keys + R * TO_WG;       // cnt[wave][digit]
-    uint32_t *wsum = cnt + TO_WAVES * TO_BINS;
-    uint16_t *poss = (uint16_t *)(wsum + 8);
-    const int t = threadIdx.x, lane = t & 63, w = t >> 6, n = (int)s.n;
-    uint32_t key[R], pos[R];                                 // pos: and, in the high half, the rank
+    uint32_t *keys = lds_u32, *start = keys + R * TS_WG, *wsum = start + TS_BINS;
+    uint16_t *cnt = (uint16_t *)(wsum + TS_WAVES), *poss = cnt + TS_WAVES * TS_BINS;
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, n = (int)s.n;
+    if (s.blank) blank_named(s);                             // (before the marks behind the next barrier)
+    uint32_t key[R], pos[R], digit[R], place[R];
+    bool in[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int i = (w * R + r) * WAVE + lane;
-        key[r] = i < n ? sort_key(s, i) : 0xffffffffu;       // places without a token sort behind all
+        in[r] = i < n;                                       // (the places behind stay where they are)
+        key[r] = in[r] ? sort_key(s, i) : 0u;
         pos[r] = (uint32_t)i;
     }
-    for (int pass = 0, shift = 0; pass < passes; ++pass, shift += 8) {
-        uint32_t *mine = cnt + w * TO_BINS;
+    for (int pass = 0; pass < passes; ++pass) {
 #pragma unroll
-        for (int q = 0; q < TO_BINS / WAVE; ++q) mine[q * WAVE + lane] = 0;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const uint32_t dg = (key[r] >> shift) & (TO_BINS - 1);
-            uint64_t same = ~0ull;
-#pragma unroll
-            for (int b = 0; b < 8; ++b) {
-                const bool bit = (dg >> b) & 1u;
-                const uint64_t bal = __ballot(bit);
-                same &= bit ? bal : ~bal;
-            }
-            const int rank = __popcll(same & lanemask_lt());
-            const uint32_t before = mine[dg];                // (a wave's LDS accesses are done in their order)
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            if (rank == 0) mine[dg] = before + (uint32_t)__popcll(same);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            pos[r] |= (before + (uint32_t)rank) << 16;
-        }
-        __syncthreads();
-        if (t < TO_BINS) {
-            uint32_t c[TO_WAVES], all = 0;
-#pragma unroll
-            for (int q = 0; q < TO_WAVES; ++q) {
-                c[q] = cnt[q * TO_BINS + t];
-                all += c[q];
-            }
-            uint32_t inc = all;
-#pragma unroll
-            for (int d = 1; d < WAVE; d <<= 1) {
-                const uint32_t o = __shfl_up(inc, d);
-                if (lane >= d) inc += o;
-            }
-            if (lane == WAVE - 1) wsum[w] = inc;
-            uint32_t run = inc - all;
-#pragma unroll
-            for (int q = 0; q < TO_WAVES; ++q) {
-                cnt[q * TO_BINS + t] = run;
-                run += c[q];
-            }
-        }
-        __syncthreads();
+        for (int r = 0; r < R; ++r) digit[r] = (key[r] >> (pass * s.bits)) & ((1u << s.bits) - 1u);
+        places<R>(digit, in, s.bits, true, 0u, 0u, cnt, start, wsum, place);
+        __syncthreads();                                     // (cnt and start have been read)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
-            const uint32_t dg = (key[r] >> shift) & (TO_BINS - 1);
-            uint32_t to = mine[dg] + (pos[r] >> 16);
-            for (uint32_t q = 0; q < dg >> 6; ++q) to += wsum[q];
-            keys[to] = key[r];
-            poss[to] = (uint16_t)pos[r];
+            if (!in[r]) continue;
+            keys[place[r]] = key[r];
+            poss[place[r]] = (uint16_t)pos[r];
         }
         __syncthreads();
 #pragma unroll
@@ -309,22 +317,21 @@ __global__ __launch_bounds__(TO_WG) void token_sort_one_kernel(const SortPass s,
             key[r] = keys[i];
             pos[r] = poss[i];
         }
-        // (the next pass writes cnt, which nobody reads any more, and keys only behind its barriers)
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
+        if (!in[r]) continue;
         const int i = (w * R + r) * WAVE + lane;
-        if (i < n) {
-            s.kout[i] = key[r];
-            s.vout[i] = pos[r];
-        }
+        s.kout[i] = key[r];
+        s.vout[i] = pos[r];
+        if (s.named && key[r] < (uint32_t)s.num_rows) s.named[key[r]] = 1;
     }
 }
 
 // ---- gradient -------------------------------------------------------------------------------------------------------
 
-constexpr int TG_LEAST_LG = 2, TG_ENTRIES = 32;              // lanes per tile (log), entries per tile: least and most
-constexpr int TG_MOST = (WG >> TG_LEAST_LG) * TG_ENTRIES;
+constexpr int TG_LEAST_LG = 2;                               // lanes per tile (log), at least
+constexpr int TG_MOST = 2048;                                // entries of a workgroup, at most
 
 // new row = old * table row (not read where old is 0) + sum * factor
 struct GradArgs {
@@ -356,62 +363,46 @@ __device__ __forceinline__ void apply_row(const GradArgs &a, int64_t row, int v,
     put8<WHOLE>(p, n, y);
 }
 
-// The first place of the sorted tokens whose token is at least `row`, found by a wave 64 places at a time.
-__device__ __forceinline__ int64_t first_at_least(const uint32_t *ks, int64_t n, uint32_t row)
-{
-    int64_t lo = 0, len = n;                                 // the answer is in [lo, lo + len]
-    const int lane = threadIdx.x & 63;
-    while (len > 0) {
-        const int64_t step = (len + WAVE - 1) / WAVE;
-        const int64_t i = lo + (int64_t)lane * step;         // the last place of the lane's stretch decides
-        const int64_t last = i + step - 1 < lo + len - 1 ? i + step - 1 : lo + len - 1;
-        const bool below = i < lo + len && ks[last] < row;
-        const int k = __popcll(__ballot(below));             // whole stretches below `row`
-        const int64_t at = lo + k * step;
-        if (at >= lo + len) return lo + len;
-        len = step < lo + len - at ? step : lo + len - at;
-        lo = at;
-        if (len == 1) return lo;                             // its one place is not below
-        len -= 1;                                            // the last place of the stretch is known not to be
-    }
-    return lo;
-}
+// Rows that no token names are zero.  A byte per row says which are named (bytes, since any number of tokens can set one without an
+// atomic).  A workgroup clears TZ_SWEEPS neighbouring parts of WG * 32 bytes, and is done.  The stores' order decides: clearing
+// 2 GB in the order of the addresses, 16 bytes a thread and nothing else, runs at 6.85 TB/s; with a byte to be looked at first, parts
+// per workgroup 1 / 2 / 4 / 8: 5.3 / 5.6 / 6.4 / 5.5 TB/s.
+constexpr int TZ_SWEEPS = 4;
 
-constexpr int TZ_MOST = 1024;                                // rows of a clearing workgroup, at most
+__global__ __launch_bounds__(WG) void token_blank_kernel(const SortPass s) { blank_named(s); }
 
-// Rows that no token names are zero.  A workgroup takes `rows` neighbouring ones, marks those that occur among the sorted tokens
-// in LDS and clears the others, 16 bytes a thread; 64 KB or so, so that the workgroups at work sweep through memory together.
+struct ClearArgs {
+    const uint8_t *named;        // null: no row is
+    uint32_t parts, chunks;      // parts of WG * 32 bytes; of a row (or rows side by side in one part)
+    int lg;                      // threads along a row (log)
+};
+
 template <typename O>
-__device__ __forceinline__ void clear_absent(const GradArgs &a, int64_t block, int rows, uint32_t *marks, int64_t *range)
+__device__ __forceinline__ void clear_rows(const ClearArgs &k, O *table, int64_t ld, uint32_t num_rows, int N, uint32_t block, uint32_t blocks)
 {
-    constexpr int E = 16 / sizeof(O);
+    constexpr int E = 32 / sizeof(O);
     struct __attribute__((packed, aligned(sizeof(O)))) Piece { O v[E]; };
-    const int64_t v0 = block * rows, v1 = v0 + rows < a.num_rows ? v0 + rows : a.num_rows;
-    const int t = threadIdx.x, w = t >> 6;
-    if (t < TZ_MOST / 32) marks[t] = 0;
-    if (w < 2) {
-        const int64_t at = first_at_least(a.ks, a.n, (uint32_t)(w ? v1 : v0));
-        if ((t & 63) == 0) range[w] = at;
-    }
-    __syncthreads();
-    for (int64_t i = range[0] + t; i < range[1]; i += WG) {
-        const uint32_t r = a.ks[i] - (uint32_t)v0;
-        if (!((marks[r >> 5] >> (r & 31)) & 1u)) atomicOr(&marks[r >> 5], 1u << (r & 31));
-    }
-    __syncthreads();
-    const int pieces = (a.N + E - 1) / E;
-    int lg = 0;
-    while (lg < 8 && (1 << lg) < pieces) ++lg;
-    const Piece zero{};
-    for (int r = t >> lg; r < (int)(v1 - v0); r += WG >> lg) {
-        if ((marks[r >> 5] >> (r & 31)) & 1u) continue;
-        O *p = (O *)a.table + (v0 + r) * a.ld_table;
-        for (int c = t & ((1 << lg) - 1); c < pieces; c += 1 << lg) {
-            const int n = a.N - E * c;
+    for (uint32_t b = block; (uint64_t)b * TZ_SWEEPS < k.parts; b += blocks) {           // (once, but for the largest tables)
+        uint32_t row[TZ_SWEEPS];
+        int c[TZ_SWEEPS];
+        bool absent[TZ_SWEEPS];
+#pragma unroll
+        for (int q = 0; q < TZ_SWEEPS; ++q) {
+            const uint32_t part = b * TZ_SWEEPS + q, g = part / k.chunks;
+            row[q] = g * (WG >> k.lg) + (threadIdx.x >> k.lg);
+            c[q] = E * ((int)(part - g * k.chunks) * (1 << k.lg) + (threadIdx.x & ((1 << k.lg) - 1)));
+            absent[q] = part < k.parts && row[q] < num_rows && c[q] < N;
+            if (k.named) absent[q] = absent[q] && !k.named[absent[q] ? row[q] : 0];
+        }
+#pragma unroll
+        for (int q = 0; q < TZ_SWEEPS; ++q) {
+            if (!absent[q]) continue;
+            O *p = table + row_at(row[q], ld) + c[q];
+            const int n = N - c[q];
             if (n >= E) {
-                *reinterpret_cast<Piece *>(p + E * c) = zero;
+                *reinterpret_cast<Piece *>(p) = Piece{};
             } else {
-                for (int j = 0; j < n; ++j) p[E * c + j] = (O)0.f;
+                for (int j = 0; j < n; ++j) p[j] = (O)0.f;
             }
         }
     }
@@ -419,19 +410,15 @@ __device__ __forceinline__ void clear_absent(const GradArgs &a, int64_t block, i
 
 // A tile of sorted entries for tx lanes, each with a vector of columns.  A run of equal tokens that lies inside the tile is
 // applied here; the part of a run that goes on in the next tile is left in part[tile][1], the part of one that began in an
-// earlier tile in part[tile][0].  The workgroups behind the tiles' clear the rows that no token names.
+// earlier tile in part[tile][0].  The workgroups behind the tiles' clear the rows that no token names, in the same launch: few sums
+// do not fill the device.
 template <typename G, typename O, bool WHOLE>
-__global__ __launch_bounds__(WG) void token_grad_kernel(const GradArgs a, int lg_tx, int chunks, int64_t tile_blocks, int clear_rows)
+__global__ __launch_bounds__(WG) void token_grad_kernel(const GradArgs a, int lg_tx, int chunks, uint32_t sum_blocks, const ClearArgs k)
 {
     constexpr int NB = 8;
-    __shared__ uint32_t marks[TZ_MOST / 32];
-    __shared__ int64_t range[2];
     __shared__ uint32_t keys[TG_MOST + 2], poss[TG_MOST + 2];
-    if ((int64_t)blockIdx.x >= tile_blocks) {
-        for (int64_t b = (int64_t)blockIdx.x - tile_blocks; b * clear_rows < a.num_rows; b += (int64_t)gridDim.x - tile_blocks) {
-            clear_absent<O>(a, b, clear_rows, marks, range);
-            __syncthreads();
-        }
+    if (blockIdx.x >= sum_blocks) {
+        clear_rows<O>(k, (O *)a.table, a.ld_table, (uint32_t)a.num_rows, a.N, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
         return;
     }
     const int tx = 1 << lg_tx, in_wg = WG >> lg_tx;
@@ -485,7 +472,7 @@ __global__ __launch_bounds__(WG) void token_grad_kernel(const GradArgs a, int lg
             }
             float y[8];
             widen8(x[q], y);
-            if (a.drop.state) drop8(a.drop, dk, (uint64_t)row_at(tp[e0 + q], a.nv) + (uint64_t)v, 1.f, y);   // (a.factor has the dropout's)
+            if (a.drop.state) drop8(a.drop, dk, (uint64_t)row_at(tp[e0 + q], a.nv) + (uint64_t)v, y);   // (a.factor has the dropout's)
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] += y[j];
         }
@@ -519,11 +506,15 @@ __global__ __launch_bounds__(WG) void token_join_kernel(const GradArgs a, int lg
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j] = p[j];
         }
-#pragma unroll 4
-        for (int u = tile + 1 + gi; u < lo; u += groups) {
-            const float *p = a.part + (int64_t)u * 2 * (8 * a.nv) + 8 * v;
+        constexpr int NB = 8;
+        for (int u0 = tile + 1 + gi; u0 < lo; u0 += NB * groups) {
+            Vec8<float> x[NB];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) sum[j] += p[j];
+            for (int q = 0; q < NB; ++q) x[q] = fetch8<true>(a.part + (int64_t)min(u0 + q * groups, lo - 1) * 2 * (8 * a.nv) + 8 * v, 8);
+#pragma unroll
+            for (int q = 0; q < NB; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += u0 + q * groups < lo ? x[q].v[j] : 0.f;
         }
     }
 #pragma unroll

@@ -49,18 +49,21 @@ int check_columns(int64_t N)
 
 constexpr int64_t MOST_GRAD_TOKENS = 1ll << 28;              // (a workgroup per tile of sorted positions)
 
-constexpr int64_t MOST_CLEAR_BLOCKS = 1 << 22;               // (they take turns beyond that)
+constexpr int64_t MOST_CLEAR = 1 << 23;                      // workgroups (they take turns beyond that)
 
 struct GradWs {
     uint32_t *k[2], *v[2], *hist, *total;
+    uint8_t *named;
     float *part;
     size_t bytes;
 };
 
-// entries per tile of sorted positions
-int grad_entries(int64_t L) { return L < 16384 ? 8 : TG_ENTRIES; }
+// Entries per tile of sorted positions: 8 where there is little work, so that more of the device has some; 64 else, for fewer sums
+// of runs that cross tiles.
+constexpr int64_t GRAD_SHORT = 1 << 22;                      // vectors of the gradient
+int grad_entries(int64_t L, int64_t nv) { return L * nv < GRAD_SHORT ? 8 : nv >= WAVE ? 64 : 16; }
 
-GradWs grad_ws(void *ws, int64_t L, int64_t N)
+GradWs grad_ws(void *ws, int64_t L, int64_t num_rows, int64_t N)
 {
     GradWs w;
     size_t at = 0;
@@ -70,20 +73,26 @@ GradWs grad_ws(void *ws, int64_t L, int64_t N)
         return p;
     };
     const int64_t sort_tiles = ceil_div(L, TS_TILE);
-    int64_t tiles = ceil_div(L, grad_entries(L));
-    if (L >= 16384 && tiles < 2048) tiles = 2048;            // (what a shorter call needs at most)
+    const int64_t nv = ceil_div(N, 8);
+    int64_t tiles = ceil_div(L, grad_entries(L, nv));
+    const int64_t shorter = ceil_div(ceil_div(GRAD_SHORT, nv), 8);           // what a call below the limit needs at most
+    if (L * nv >= GRAD_SHORT && tiles < shorter) tiles = shorter;
     for (int i = 0; i < 2; ++i) {
         w.k[i] = (uint32_t *)take((size_t)L * 4);
         w.v[i] = (uint32_t *)take((size_t)L * 4);
     }
     w.hist = (uint32_t *)take((size_t)sort_tiles * TS_BINS * 4);
     w.total = (uint32_t *)take(TS_BINS * 4);
-    w.part = (float *)take((size_t)tiles * 2 * (size_t)(8 * ceil_div(N, 8)) * 4);
+    w.named = (uint8_t *)take((size_t)num_rows);
+    w.part = (float *)take((size_t)tiles * 2 * (size_t)(8 * nv) * 4);
     w.bytes = at;
     return w;
 }
 
-hipError_t sort_tokens(const tt_tokens_t *t, int64_t num_rows, const GradWs &w, hipStream_t st, const uint32_t **ks, const uint32_t **vs)
+// rows up to which the first kernel of the sort, of one workgroup or of a few, clears their bytes itself
+constexpr int64_t BLANK_ONE = 1 << 18, BLANK_FEW = 1 << 20;
+
+hipError_t sort_tokens(const tt_tokens_t *t, int64_t num_rows, const GradWs &w, bool named, hipStream_t st, const uint32_t **ks, const uint32_t **vs)
 {
     SortPass s{};
     s.tokens = t->data;
@@ -95,29 +104,37 @@ hipError_t sort_tokens(const tt_tokens_t *t, int64_t num_rows, const GradWs &w, 
     s.total = w.total;
     int bits = 1;                                            // num_rows itself is the key of no token
     while (bits < 32 && (1ll << bits) <= num_rows) ++bits;
-    if (t->L <= TO_MOST) {
+    const int passes = (bits + TS_BITS - 1) / TS_BITS;
+    s.bits = (bits + passes - 1) / passes;
+    const bool one = t->L <= TO_MOST;
+    if (named) {
+        s.named = w.named;
+        s.blank = num_rows <= (one ? BLANK_ONE : BLANK_FEW);
+        if (!s.blank) hipLaunchKernelGGL(token_blank_kernel, dim3(1024), dim3(WG), 0, st, s);
+    }
+    if (one) {
         s.kout = w.k[0];
         s.vout = w.v[0];
         *ks = s.kout;
         *vs = s.vout;
-        const int passes = (bits + 7) / 8;
-        auto one = [&](auto r) {
+        auto launch = [&](auto r) {
             constexpr int R = decltype(r)::value;
             static OncePerDevice once;
             const hipError_t e = allow_dynamic_lds(once, (const void *)token_sort_one_kernel<R>, sort_one_lds(R));
             if (e != hipSuccess) return e;
-            hipLaunchKernelGGL(token_sort_one_kernel<R>, dim3(1), dim3(TO_WG), sort_one_lds(R), st, s, passes);
+            hipLaunchKernelGGL(token_sort_one_kernel<R>, dim3(1), dim3(TS_WG), sort_one_lds(R), st, s, passes);
             return hipGetLastError();
         };
-        if (t->L <= TO_WG) return one(std::integral_constant<int, 1>{});
-        if (t->L <= 4 * TO_WG) return one(std::integral_constant<int, 4>{});
-        return one(std::integral_constant<int, 8>{});
+        if (t->L <= TS_WG) return launch(std::integral_constant<int, 1>{});
+        if (t->L <= 4 * TS_WG) return launch(std::integral_constant<int, 4>{});
+        return launch(std::integral_constant<int, 8>{});
     }
     int at = 0;
-    for (s.shift = 0; s.shift < bits; s.shift += 9, at ^= 1) {
+    for (s.shift = 0; s.shift < bits; s.shift += s.bits, at ^= 1) {
         s.kout = w.k[at];
         s.vout = w.v[at];
         hipLaunchKernelGGL(token_hist_kernel, dim3(s.tiles), dim3(TS_WG), 0, st, s);
+        s.blank = false;
         if (s.tiles > TS_SCAN_TILES) {
             hipLaunchKernelGGL(token_scan_kernel, dim3(TS_BINS / WAVE), dim3(TS_WG), 0, st, s);
             hipLaunchKernelGGL(token_scatter_kernel<true>, dim3(s.tiles), dim3(TS_WG), 0, st, s);
@@ -125,6 +142,7 @@ hipError_t sort_tokens(const tt_tokens_t *t, int64_t num_rows, const GradWs &w, 
             hipLaunchKernelGGL(token_scatter_kernel<false>, dim3(s.tiles), dim3(TS_WG), 0, st, s);
         }
         s.tokens = nullptr;
+        s.named = nullptr;
         s.kin = s.kout;
         s.vin = s.vout;
     }
@@ -146,12 +164,12 @@ int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropou
     if ((rc = check_rows(table, name, num_rows, N, OUT)) || (rc = check_rows(grad, "grad_output", L, N, IN))) return rc;
     if ((rc = check_dropout(dropout, &a.drop))) return rc;
     if (N == 0 || num_rows == 0 || (old && L == 0)) return TT_OK;
-    const size_t need = tt_token_bwd_workspace_bytes(L, N);
+    const size_t need = tt_token_bwd_workspace_bytes(L, num_rows, N);
     if (L > 0 && (!workspace || workspace_bytes < need))
         return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
     if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
     hipStream_t st = (hipStream_t)stream;
-    const GradWs w = grad_ws(workspace, L, N);
+    const GradWs w = grad_ws(workspace, L, num_rows, N);
     a.g = grad->data;
     a.table = table->data;
     a.part = w.part;
@@ -161,35 +179,42 @@ int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropou
     a.num_rows = num_rows;
     a.N = (int)N;
     a.nv = (int)ceil_div(N, 8);
-    a.entries = grad_entries(L);
+    a.entries = grad_entries(L, a.nv);
     a.tiles = (int)ceil_div(L, a.entries);
-    a.factor = a.drop.state ? factor * a.drop.factor : factor;
+    a.factor = factor * a.drop.factor;
     a.old = old;
-    int lg = lg_ceil(a.nv < WAVE ? a.nv : WAVE);
+    // the lanes of a tile: up to the whole workgroup, so that a row of the gradient is read in long pieces; to join few, for many groups
+    int lg = lg_ceil(a.nv < WG ? a.nv : WG), lg_join = lg < 6 ? lg : 6;
     if (lg < TG_LEAST_LG) lg = TG_LEAST_LG;
-    const unsigned chunks = (unsigned)ceil_div(a.nv, 1 << lg);
-    const int64_t tile_blocks = ceil_div(a.tiles, WG >> lg) * chunks;
-    int64_t clear_rows = 65536 / (N * element_bytes(table->type)), clear_blocks = 0;
-    clear_rows = clear_rows < 1 ? 1 : clear_rows > TZ_MOST ? TZ_MOST : clear_rows;
+    const unsigned chunks = (unsigned)ceil_div(a.nv, 1 << lg), join_chunks = (unsigned)ceil_div(a.nv, 1 << lg_join);
+    const int64_t sum_blocks = ceil_div(a.tiles, WG >> lg) * chunks;
+    ClearArgs k{};
+    int64_t clear_blocks = 0;
     if (!old) {
-        clear_blocks = ceil_div(num_rows, clear_rows);
-        if (clear_blocks > MOST_CLEAR_BLOCKS) clear_blocks = MOST_CLEAR_BLOCKS;
+        const int64_t pieces = ceil_div(N * element_bytes(table->type), 32);
+        k.named = L > 0 ? w.named : nullptr;
+        k.lg = lg_ceil(pieces < WG ? pieces : WG);
+        const int64_t along = ceil_div(pieces, 1 << k.lg), parts = ceil_div(num_rows, WG >> k.lg) * along;
+        if (parts >= (1ll << 32)) return fail(TT_ERR_UNSUPPORTED, "a table of more than 2^45 bytes");
+        k.chunks = (uint32_t)along;
+        k.parts = (uint32_t)parts;
+        clear_blocks = ceil_div(parts, TZ_SWEEPS) < MOST_CLEAR ? ceil_div(parts, TZ_SWEEPS) : MOST_CLEAR;
     }
-    if ((rc = check_grid(tile_blocks + clear_blocks, WG))) return rc;
+    if ((rc = check_grid(sum_blocks + clear_blocks, WG))) return rc;
     if (L > 0) {
-        const hipError_t e = sort_tokens(tokens, num_rows, w, st, &a.ks, &a.vs);
+        const hipError_t e = sort_tokens(tokens, num_rows, w, !old, st, &a.ks, &a.vs);
         if (e != hipSuccess) return hip_fail(e, "token sort");
     }
     with_whole(N, [&](auto whole) {
         with_type(grad->type, [&](auto g) {
             with_type(table->type, [&](auto o) {
-                hipLaunchKernelGGL((token_grad_kernel<decltype(g), decltype(o), decltype(whole)::value>), dim3((unsigned)(tile_blocks + clear_blocks)), dim3(WG), 0, st,
-                                   a, lg, (int)chunks, tile_blocks, (int)clear_rows);
+                hipLaunchKernelGGL((token_grad_kernel<decltype(g), decltype(o), decltype(whole)::value>), dim3((unsigned)(sum_blocks + clear_blocks)), dim3(WG), 0, st, a, lg,
+                                   (int)chunks, (uint32_t)sum_blocks, k);
             });
         });
     });
     if (a.tiles > 1)
-        with_type(table->type, [&](auto o) { hipLaunchKernelGGL(token_join_kernel<decltype(o)>, dim3(a.tiles, chunks), dim3(WG), 0, st, a, lg); });
+        with_type(table->type, [&](auto o) { hipLaunchKernelGGL(token_join_kernel<decltype(o)>, dim3(a.tiles, join_chunks), dim3(WG), 0, st, a, lg_join); });
     return launched("token gradient launch");
 }
 
@@ -218,7 +243,7 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     a.N = (int)N;
     a.nv = (int)ceil_div(N, 8);
     a.wide = tokens->bits == 64;
-    a.scale = a.drop.state ? scale * a.drop.factor : scale;
+    a.scale = scale * a.drop.factor;
     if (num_rows == 0) {                                     // no token is one: rows of zeros, for which nothing has to be there to be read
         a.src = output->data;
         a.ld_src = 0;
@@ -226,19 +251,21 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     }
     with_type(num_rows ? table->type : output->type, [&](auto s) {
         with_type(output->type, [&](auto d) {
-            // few tokens: one row per thread, so that more of the device has some
+            // few tokens: one row per thread, so that more of the device has some; else two, or, where the generator's products take the
+            // time, four (32,768 tokens of 4,096 columns in 16 bits, 1 / 2 / 4 rows: 96 / 76 / 78 us, with dropout 109 / 85 / 80)
             if (L * a.nv < (1 << 20)) rc = launch_rows<decltype(s), decltype(d), 1, true, false>(a, (hipStream_t)stream);
-            else rc = launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
+            else if (!a.drop.state) rc = launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
+            else rc = launch_rows<decltype(s), decltype(d), 4, true, false>(a, (hipStream_t)stream);
         });
     });
     if (rc) return rc;
     return launched("token lookup launch");
 }
 
-size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t N)
+size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t num_rows, int64_t N)
 {
-    if (L <= 0 || N <= 0 || L >= MOST_GRAD_TOKENS || N > MOST_COLUMNS) return 0;
-    return grad_ws(nullptr, L, N).bytes;
+    if (L <= 0 || num_rows <= 0 || num_rows >= MOST_ROWS || N <= 0 || L >= MOST_GRAD_TOKENS || N > MOST_COLUMNS) return 0;
+    return grad_ws(nullptr, L, num_rows, N).bytes;
 }
 
 int tt_token_bwd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
@@ -276,7 +303,7 @@ static int dropout_rows(const tt_rows_t *x, const tt_rows_t *residual, const tt_
     a.rows = a.num_rows = rows;
     a.N = (int)N;
     a.nv = (int)ceil_div(N, 8);
-    a.scale = a.drop.state ? a.drop.factor : 1.f;
+    a.scale = a.drop.factor;
     with_type(x->type, [&](auto s) {
         if (residual) rc = launch_rows<decltype(s), decltype(s), 1, false, true>(a, (hipStream_t)stream);
         else rc = launch_rows<decltype(s), decltype(s), 1, false, false>(a, (hipStream_t)stream);

@@ -199,8 +199,8 @@ def test_token_bwd_is_the_same_every_time_and_with_any_workspace(L, vocab, N):
     g = gen(9)
     tokens, grad = tokens_of(g, L, vocab, "hot"), R.rows_of(g, L, N, F32)
     outs = []
-    need = B.token_bwd_workspace_bytes(L, N)
-    for ws in (None, torch.full((need,), 255, dtype=torch.uint8, device="cuda:0"), torch.zeros(B.token_bwd_workspace_bytes(2 * L, N), dtype=torch.uint8, device="cuda:0")):
+    need = B.token_bwd_workspace_bytes(L, vocab, N)
+    for ws in (None, torch.full((need,), 255, dtype=torch.uint8, device="cuda:0"), torch.zeros(B.token_bwd_workspace_bytes(2 * L, vocab, N), dtype=torch.uint8, device="cuda:0")):
         outs.append(B.tt_token_bwd(tokens, grad, torch.empty((vocab, N), device="cuda:0"), workspace=ws))
     assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
 
@@ -507,7 +507,7 @@ def block_buffers(L, vocab, N):
 def block_inputs(L, vocab, N):
     g = gen(51)
     ws = [torch.empty(B.add_rms_norm_bwd_workspace_bytes(L, N), dtype=torch.uint8, device="cuda:0"),
-          torch.empty(B.token_bwd_workspace_bytes(L, N), dtype=torch.uint8, device="cuda:0")]
+          torch.empty(B.token_bwd_workspace_bytes(L, vocab, N), dtype=torch.uint8, device="cuda:0")]
     return (R.rows_of(g, vocab, N, F32), tokens_of(g, L, vocab, "hot"), R.rows_of(g, L, N, F32), torch.randn(N, generator=g).to("cuda:0"),
             torch.tensor([99, 0], dtype=torch.int64, device="cuda:0")), ws
 
@@ -589,3 +589,17 @@ def test_a_table_without_rows_gives_zeros():
             B.tt_token_fwd(torch.empty((0, N), dtype=s, device="cuda:0"), tokens_of(gen(1), 9, 5, "some"), out, dropout=dropout_of(0.5))
             assert not out.any()
             assert_guard(out, flat)
+
+
+@pytest.mark.parametrize("L", [5, 9000])
+def test_token_bwd_of_a_table_of_many_rows(L):
+    # more rows than the sort's first kernel blanks the bits of (2^22), few and many tokens
+    vocab, N = (1 << 22) + 77, 3
+    g = gen(61)
+    tokens, grad = tokens_of(g, L, vocab, "some"), R.rows_of(g, L, N, F32)
+    tokens[:3] = torch.tensor([0, vocab - 1, vocab - 33])
+    out, flat = room(vocab, N, F32, 1, 0)
+    B.tt_token_bwd(tokens, grad, out)
+    want, mag, most = R.token_bwd(tokens, grad, vocab, 1.0, None)
+    R.assert_within(out, want, (most + 4) * U32 * mag)
+    assert_guard(out, flat)

@@ -44,7 +44,7 @@ def test_token_calls_check_their_arguments():
         assert len(l.tt_last_error()) > 0
     assert l.tt_token_fwd(*good(tokens=toks(data=None, L=0))) == 0
     assert l.tt_token_fwd(*good(N=0)) == 0
-    need = l.tt_token_bwd_workspace_bytes(5, 16)
+    need = l.tt_token_bwd_workspace_bytes(5, 10, 16)
     assert need > 0
     for f, tail in ((l.tt_token_bwd, (0,)), (l.tt_token_bwd_sgd, (0.1,))):
         args = lambda **k: (k.get("tokens", toks()), k.get("grad", rows()), 1.0, k.get("drop"), k.get("table", rows()), k.get("num_rows", 10), k.get("N", 16), *tail,  # noqa: E731
@@ -92,11 +92,12 @@ def test_workspaces_are_enough_for_shorter_calls():
     l = B.lib()
     lengths = [1, 2, 2047, 2048, 2049, 16_383, 16_384, 16_385, 65_536, 131_072, 131_073, 1_000_000, 2**28 - 1]
     for N in (1, 7, 64, 4096):
-        sizes = [l.tt_token_bwd_workspace_bytes(L, N) for L in lengths]
+        sizes = [l.tt_token_bwd_workspace_bytes(L, 1000, N) for L in lengths]
         assert sizes[0] > 0 and sizes == sorted(sizes), (N, sizes)
         sizes = [l.tt_add_rms_norm_bwd_workspace_bytes(L, N) for L in lengths]
         assert sizes[0] > 0 and sizes == sorted(sizes), (N, sizes)
-    assert l.tt_token_bwd_workspace_bytes(2**28, 8) == 0 and l.tt_token_bwd_workspace_bytes(0, 8) == 0 and l.tt_token_bwd_workspace_bytes(8, 2**20 + 1) == 0
+    assert l.tt_token_bwd_workspace_bytes(2**28, 10, 8) == 0 and l.tt_token_bwd_workspace_bytes(0, 10, 8) == 0 and l.tt_token_bwd_workspace_bytes(8, 10, 2**20 + 1) == 0
+    assert l.tt_token_bwd_workspace_bytes(8, 2**31, 8) == 0 and l.tt_token_bwd_workspace_bytes(8, 0, 8) == 0
     assert l.tt_add_rms_norm_bwd_workspace_bytes(8, 32769) == 0
 
 
