@@ -372,38 +372,37 @@ constexpr int TZ_SWEEPS = 4;
 __global__ __launch_bounds__(WG) void token_blank_kernel(const SortPass s) { blank_named(s); }
 
 struct ClearArgs {
-    const uint8_t *named;        // null: no row is
+    const uint8_t *named;
     uint32_t parts, chunks;      // parts of WG * 32 bytes; of a row (or rows side by side in one part)
     int lg;                      // threads along a row (log)
 };
 
-template <typename O>
-__device__ __forceinline__ void clear_rows(const ClearArgs &k, O *table, int64_t ld, uint32_t num_rows, int N, uint32_t block, uint32_t blocks)
+// TZ_SWEEPS parts of the table, the rows but those that named(row) names
+template <typename O, typename F>
+__device__ __forceinline__ void clear_rows(const ClearArgs &k, O *table, int64_t ld, uint32_t num_rows, int N, uint32_t b, F named)
 {
     constexpr int E = 32 / sizeof(O);
     struct __attribute__((packed, aligned(sizeof(O)))) Piece { O v[E]; };
-    for (uint32_t b = block; (uint64_t)b * TZ_SWEEPS < k.parts; b += blocks) {           // (once, but for the largest tables)
-        uint32_t row[TZ_SWEEPS];
-        int c[TZ_SWEEPS];
-        bool absent[TZ_SWEEPS];
+    uint32_t row[TZ_SWEEPS];
+    int c[TZ_SWEEPS];
+    bool absent[TZ_SWEEPS];
 #pragma unroll
-        for (int q = 0; q < TZ_SWEEPS; ++q) {
-            const uint32_t part = b * TZ_SWEEPS + q, g = part / k.chunks;
-            row[q] = g * (WG >> k.lg) + (threadIdx.x >> k.lg);
-            c[q] = E * ((int)(part - g * k.chunks) * (1 << k.lg) + (threadIdx.x & ((1 << k.lg) - 1)));
-            absent[q] = part < k.parts && row[q] < num_rows && c[q] < N;
-            if (k.named) absent[q] = absent[q] && !k.named[absent[q] ? row[q] : 0];
-        }
+    for (int q = 0; q < TZ_SWEEPS; ++q) {
+        const uint32_t part = b * TZ_SWEEPS + q, g = part / k.chunks;
+        row[q] = g * (WG >> k.lg) + (threadIdx.x >> k.lg);
+        c[q] = E * ((int)(part - g * k.chunks) * (1 << k.lg) + (threadIdx.x & ((1 << k.lg) - 1)));
+        absent[q] = part < k.parts && row[q] < num_rows && c[q] < N;
+        absent[q] = absent[q] && !named(absent[q] ? row[q] : 0u);
+    }
 #pragma unroll
-        for (int q = 0; q < TZ_SWEEPS; ++q) {
-            if (!absent[q]) continue;
-            O *p = table + row_at(row[q], ld) + c[q];
-            const int n = N - c[q];
-            if (n >= E) {
-                *reinterpret_cast<Piece *>(p) = Piece{};
-            } else {
-                for (int j = 0; j < n; ++j) p[j] = (O)0.f;
-            }
+    for (int q = 0; q < TZ_SWEEPS; ++q) {
+        if (!absent[q]) continue;
+        O *p = table + row_at(row[q], ld) + c[q];
+        const int n = N - c[q];
+        if (n >= E) {
+            *reinterpret_cast<Piece *>(p) = Piece{};
+        } else {
+            for (int j = 0; j < n; ++j) p[j] = (O)0.f;
         }
     }
 }
@@ -418,7 +417,8 @@ __global__ __launch_bounds__(WG) void token_grad_kernel(const GradArgs a, int lg
     constexpr int NB = 8;
     __shared__ uint32_t keys[TG_MOST + 2], poss[TG_MOST + 2];
     if (blockIdx.x >= sum_blocks) {
-        clear_rows<O>(k, (O *)a.table, a.ld_table, (uint32_t)a.num_rows, a.N, blockIdx.x - sum_blocks, gridDim.x - sum_blocks);
+        for (uint32_t b = blockIdx.x - sum_blocks; (uint64_t)b * TZ_SWEEPS < k.parts; b += gridDim.x - sum_blocks)     // (once, but for the largest tables)
+            clear_rows(k, (O *)a.table, a.ld_table, (uint32_t)a.num_rows, a.N, b, [&](uint32_t row) { return k.named[row] != 0; });
         return;
     }
     const int tx = 1 << lg_tx, in_wg = WG >> lg_tx;
@@ -525,6 +525,102 @@ __global__ __launch_bounds__(WG) void token_join_kernel(const GradArgs a, int lg
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum[j] += lds[j * WG + q * tx + threadIdx.x];
     apply_row<O, false>(a, key, v, sum);
+}
+
+// Few tokens (or none): no sort.  A workgroup takes a position and up to WG vectors of columns; it ends if the position's token has
+// an earlier one, else it lists the token's positions, which groups of 1 << lg_tx lanes add up side by side; the groups' sums are
+// added in their order.  The workgroups behind clear the rows that no token names, after a look at all tokens.
+constexpr int TF_MOST = 1024, TF_ROUNDS = TF_MOST / WG;
+
+template <typename G, typename O, bool WHOLE>
+__global__ __launch_bounds__(WG) void token_few_kernel(const GradArgs a, const void *tokens, int wide, int lg_tx, int chunks, uint32_t sum_blocks, const ClearArgs k)
+{
+    constexpr int NB = 8;
+    __shared__ uint32_t list[TF_MOST], marks[TZ_SWEEPS * WG / 32];
+    __shared__ uint64_t equal[TF_MOST / WAVE];
+    __shared__ float lds[WG * 8];
+    const int t = threadIdx.x, lane = t & 63, w = t >> 6, total = (int)a.n;
+    const uint32_t none = (uint32_t)a.num_rows;
+    uint32_t key[TF_ROUNDS];
+#pragma unroll
+    for (int q = 0; q < TF_ROUNDS; ++q) {
+        const int i = q * WG + t;
+        const int64_t x = i < total ? token_at(tokens, wide, i) : -1;
+        key[q] = x >= 0 && x < a.num_rows ? (uint32_t)x : none;
+    }
+    if (blockIdx.x >= sum_blocks) {
+        for (uint32_t b = blockIdx.x - sum_blocks; (uint64_t)b * TZ_SWEEPS < k.parts; b += gridDim.x - sum_blocks) {
+            const uint32_t first = b * TZ_SWEEPS / k.chunks * (WG >> k.lg), rows = (TZ_SWEEPS - 1 + k.chunks) / k.chunks * (WG >> k.lg) + (WG >> k.lg);
+            for (int i = t; i < TZ_SWEEPS * WG / 32; i += WG) marks[i] = 0;
+            __syncthreads();
+#pragma unroll
+            for (int q = 0; q < TF_ROUNDS; ++q) {
+                const uint32_t r = key[q] - first;
+                if (key[q] != none && r < rows && r < TZ_SWEEPS * WG) atomicOr(&marks[r >> 5], 1u << (r & 31));
+            }
+            __syncthreads();
+            clear_rows(k, (O *)a.table, a.ld_table, (uint32_t)a.num_rows, a.N, b, [&](uint32_t row) { return (marks[(row - first) >> 5] >> ((row - first) & 31)) & 1u; });
+            __syncthreads();
+        }
+        return;
+    }
+    const int p = (int)(blockIdx.x / (unsigned)chunks);
+    const int64_t mine_ = token_at(tokens, wide, p);
+    if (mine_ < 0 || mine_ >= a.num_rows) return;
+    const uint32_t mine = (uint32_t)mine_;
+    uint64_t bal[TF_ROUNDS];
+#pragma unroll
+    for (int q = 0; q < TF_ROUNDS; ++q) {
+        bal[q] = __ballot(key[q] == mine);
+        if (lane == 0) equal[q * NWAVE + w] = bal[q];
+    }
+    __syncthreads();
+    int cnt = 0;
+    bool earlier = false;
+    int before[TF_ROUNDS];                                   // positions of the token in earlier words than this wave's
+    for (int x = 0; x < TF_MOST / WAVE; ++x) {
+        const uint64_t m = equal[x];
+#pragma unroll
+        for (int q = 0; q < TF_ROUNDS; ++q)
+            if (x == q * NWAVE + w) before[q] = cnt;
+        cnt += __popcll(m);
+        earlier |= x < p / WAVE ? m != 0 : x == p / WAVE && (m & ((1ull << (p & 63)) - 1ull)) != 0;
+    }
+    if (earlier) return;
+#pragma unroll
+    for (int q = 0; q < TF_ROUNDS; ++q)
+        if (key[q] == mine) list[before[q] + __popcll(bal[q] & lanemask_lt())] = (uint32_t)(q * WG + t);
+    __syncthreads();
+    const int tx = 1 << lg_tx, groups = WG >> lg_tx, gi = t >> lg_tx, v = (int)(blockIdx.x % (unsigned)chunks) * tx + (t & (tx - 1));
+    const int vc = min(v, a.nv - 1), n = a.N - 8 * vc;
+    const DropKey dk = drop_key(a.drop);
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int e0 = gi; e0 < cnt; e0 += NB * groups) {
+        Vec8<G> x[NB];
+#pragma unroll
+        for (int q = 0; q < NB; ++q) x[q] = fetch8<WHOLE>((const G *)a.g + row_at(list[min(e0 + q * groups, cnt - 1)], a.ld_g) + 8 * vc, n);
+#pragma unroll
+        for (int q = 0; q < NB; ++q) {
+            const int e = e0 + q * groups;
+            if (e >= cnt) break;
+            float y[8];
+            widen8(x[q], y);
+            if (a.drop.state) drop8(a.drop, dk, (uint64_t)row_at(list[e], a.nv) + (uint64_t)vc, y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) sum[j] += y[j];
+        }
+    }
+    if (groups > 1 && cnt > 1) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) lds[j * WG + t] = sum[j];
+        __syncthreads();
+        const int with = min(groups, cnt);
+        if (gi == 0)
+            for (int q = 1; q < with; ++q)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum[j] += lds[j * WG + q * tx + t];
+    }
+    if (gi == 0 && v < a.nv) apply_row<O, WHOLE>(a, mine, v, sum);
 }
 
 }  // namespace tt
