@@ -33,10 +33,13 @@ __device__ __forceinline__ void load_weights(const W *p, int g, int t, int nv, i
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int v = min(i * g + t, nv - 1);
-        x[i] = fetch8<WHOLE>(p + 8 * v, N - 8 * v);
+        x[i] = fetch8<WHOLE>(p + 8 * v, N - 8 * v, N);
     }
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) widen8(x[i], w[i]);
+    for (int i = 0; i < VPT; ++i) {
+        settle8<WHOLE>(x[i], N - 8 * min(i * g + t, nv - 1), N);
+        widen8(x[i], w[i]);
+    }
 }
 
 template <bool WHOLE, int VPT>
@@ -115,20 +118,22 @@ __global__ __launch_bounds__(RN_THREADS) void norm_fwd_kernel(const NormArgs a, 
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
-            x[i] = fetch8<WHOLE>((const T *)a.x + row_at(row, a.ld_x) + 8 * v, n);
-            if constexpr (RESIDUAL) res[i] = fetch8<WHOLE>((const H *)a.residual + row_at(row, a.ld_res) + 8 * v, n);
+            x[i] = fetch8<WHOLE>((const T *)a.x + row_at(row, a.ld_x) + 8 * v, n, a.N);
+            if constexpr (RESIDUAL) res[i] = fetch8<WHOLE>((const H *)a.residual + row_at(row, a.ld_res) + 8 * v, n, a.N);
         }
         const DropKey key = drop_key(a.drop);
         weights<WHOLE>(a.weight, a.weight_type, g, t, a.nv, a.N, w);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = min(i * g + t, a.nv - 1);
+            settle8<WHOLE>(x[i], a.N - 8 * v, a.N);
             widen8(x[i], h[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] *= a.drop.factor;
             if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, h[i]);
             if constexpr (RESIDUAL) {
                 float r[8];
+                settle8<WHOLE>(res[i], a.N - 8 * v, a.N);
                 widen8(res[i], r);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[i][j] += r[j];
@@ -225,14 +230,17 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
-            dy[i] = fetch8<WHOLE>((const T *)a.dy + row_at(row, a.ld_dy) + 8 * v, n);
-            h[i] = fetch8<WHOLE>((const H *)a.h + row_at(row, a.ld_h) + 8 * v, n);
-            if constexpr (DSUM) ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, n);
+            dy[i] = fetch8<WHOLE>((const T *)a.dy + row_at(row, a.ld_dy) + 8 * v, n, a.N);
+            h[i] = fetch8<WHOLE>((const H *)a.h + row_at(row, a.ld_h) + 8 * v, n, a.N);
+            if constexpr (DSUM) ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, n, a.N);
         }
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
+            const int n = a.N - 8 * min(i * g + t, a.nv - 1);
             float p[8], q[8], part = 0.f;
+            settle8<WHOLE>(dy[i], n, a.N);
+            settle8<WHOLE>(h[i], n, a.N);
             widen8(dy[i], p);
             widen8(h[i], q);
 #pragma unroll
@@ -255,6 +263,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
             for (int j = 0; j < 8; ++j) d[j] = p[j] * w[i][j] * rstd - q[j] * c;
             if constexpr (DSUM) {
                 float s[8];
+                settle8<WHOLE>(ds[i], a.N - 8 * min(v, a.nv - 1), a.N);
                 widen8(ds[i], s);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[j] += s[j];

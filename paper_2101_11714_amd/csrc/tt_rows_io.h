@@ -9,24 +9,72 @@ namespace tt {
 typedef __bf16 bf16_t;
 typedef _Float16 f16_t;
 
-// Eight neighbouring columns of a row, as they lie in memory.  Rows may start on any multiple of the element's size (odd
-// dimensions and strides): the type's alignment is the element's, and the device loads and stores 16 bytes from any address.
+// Eight neighbouring columns of a row, as they lie in memory, as 32-bit words (not as values: the compiler would join stores of single
+// values at a row's end with the whole vectors' and split those).  Rows may start on any multiple of the element's size (odd
+// dimensions and strides): the device loads and stores 16 bytes from any address.
 template <typename T>
-struct __attribute__((packed, aligned(sizeof(T)))) Vec8 {
-    T v[8];
+struct Vec8 {
+    static constexpr int W = 2 * sizeof(T), PER = 4 / sizeof(T);             // words, values of a word
+    typedef uint32_t Words __attribute__((ext_vector_type(W)));
+    typedef Words Anywhere __attribute__((aligned(sizeof(T))));
+    Words w;
 };
 
-// n: how many of the eight columns exist (8 or more: all).  WHOLE: all of them do, whatever n is; the kernels that move the most
-// exist for rows of whole vectors and for others, since the test in front of every load keeps loads from being issued together.
+// The columns of a vector of which n exist (8 or more: all) in rows of N.  No branch stands around a load, since what is loaded under
+// a condition is waited for there: where fewer than eight are left the row's last eight are loaded, and settle8 moves the right
+// ones into place when they are needed (rows of less than eight columns: one by one, the last one again for those behind it).
+// WHOLE: N is a multiple of 8, and all of this away.
 template <bool WHOLE = false, typename T>
-__device__ __forceinline__ Vec8<T> fetch8(const T *p, int n)
+__device__ __forceinline__ Vec8<T> fetch8(const T *p, int n, int N)
 {
     Vec8<T> r;
-    if (WHOLE || n >= 8) {
-        r = *reinterpret_cast<const Vec8<T> *>(p);
+    if (WHOLE || N >= 8) {
+        r.w = *reinterpret_cast<const typename Vec8<T>::Anywhere *>(p - (WHOLE || n >= 8 ? 0 : 8 - n));
+    } else {
+        struct Values { T v[8]; } x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x.v[j] = p[min(j, n - 1)];
+        r.w = __builtin_bit_cast(typename Vec8<T>::Words, x);
+    }
+    return r;
+}
+
+// zeros behind the last column
+template <bool WHOLE = false, typename T>
+__device__ __forceinline__ void settle8(Vec8<T> &r, int n, int N)
+{
+    if (WHOLE || n >= 8) return;
+    constexpr int W = Vec8<T>::W, PER = Vec8<T>::PER;
+    if (N >= 8) {                                            // down by 8 - n places (the same for all rows)
+        const int d = 8 - n;
+#pragma unroll
+        for (int by = 4; by >= 1; by >>= 1) {
+            const bool move = d & by;
+#pragma unroll
+            for (int k = 0; k < W; ++k) {
+                uint32_t x;
+                if (by >= PER) x = k + by / PER < W ? r.w[k + by / PER < W ? k + by / PER : 0] : 0u;
+                else x = r.w[k] >> 16 | (k + 1 < W ? r.w[k + 1 < W ? k + 1 : 0] << 16 : 0u);
+                r.w[k] = move ? x : r.w[k];
+            }
+        }
     } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.v[j] = j < n ? p[j] : (T)0.f;
+        for (int j = 0; j < 8; ++j)
+            if (j >= n) r.w[j / PER] &= PER == 1 ? 0u : j & 1 ? 0x0000ffffu : 0xffff0000u;
+    }
+}
+
+template <typename T>
+__device__ __forceinline__ Vec8<T> narrow8(const float (&x)[8])
+{
+    typedef float Two __attribute__((ext_vector_type(2)));
+    typedef T Narrow __attribute__((ext_vector_type(2)));
+    Vec8<T> r;
+#pragma unroll
+    for (int k = 0; k < Vec8<T>::W; ++k) {
+        if constexpr (sizeof(T) == 4) r.w[k] = __float_as_uint(x[k]);
+        else r.w[k] = __builtin_bit_cast(uint32_t, __builtin_convertvector((Two{x[2 * k], x[2 * k + 1]}), Narrow));
     }
     return r;
 }
@@ -35,34 +83,33 @@ __device__ __forceinline__ Vec8<T> fetch8(const T *p, int n)
 template <bool WHOLE = false, typename T>
 __device__ __forceinline__ void put8(T *p, int n, const float (&x)[8])
 {
-    Vec8<T> r;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) r.v[j] = (T)x[j];
+    const Vec8<T> r = narrow8<T>(x);
     if (WHOLE || n >= 8) {
-        *reinterpret_cast<Vec8<T> *>(p) = r;
+        *reinterpret_cast<typename Vec8<T>::Anywhere *>(p) = r.w;
     } else {
+        struct Values { T v[8]; };
+        const Values y = __builtin_bit_cast(Values, r.w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (j < n) p[j] = r.v[j];
+        for (int j = 0; j < 7; ++j)
+            if (j < n) p[j] = y.v[j];
     }
 }
 
-// all zeros unless `keep`, before anything is computed from them (a register holds two 16-bit values)
+// all zeros unless `keep`, before anything is computed from them
 template <typename T>
 __device__ __forceinline__ void keep8(bool keep, Vec8<T> &r)
 {
-    struct Words { uint32_t w[2 * sizeof(T)]; };
-    Words x = __builtin_bit_cast(Words, r);
 #pragma unroll
-    for (unsigned j = 0; j < 2 * sizeof(T); ++j) x.w[j] = keep ? x.w[j] : 0u;
-    r = __builtin_bit_cast(Vec8<T>, x);
+    for (int k = 0; k < Vec8<T>::W; ++k) r.w[k] = keep ? r.w[k] : 0u;
 }
 
 template <typename T>
 __device__ __forceinline__ void widen8(const Vec8<T> &r, float (&x)[8])
 {
+    struct Values { T v[8]; };
+    const Values y = __builtin_bit_cast(Values, r.w);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = (float)r.v[j];
+    for (int j = 0; j < 8; ++j) x[j] = (float)y.v[j];
 }
 
 // element offset of row r; a row's number and a row stride have 31 bits each

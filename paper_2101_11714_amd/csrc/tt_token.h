@@ -57,8 +57,8 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const int64_t r = r0 + u * ty;
-        x[u] = fetch8<WHOLE>((const S *)a.src + row_at(from[u], a.ld_src) + 8 * v, n);
-        if constexpr (RESIDUAL) res[u] = fetch8<WHOLE>((const S *)a.residual + row_at(r < a.rows ? r : 0, a.ld_res) + 8 * v, n);
+        x[u] = fetch8<WHOLE>((const S *)a.src + row_at(from[u], a.ld_src) + 8 * v, n, a.N);
+        if constexpr (RESIDUAL) res[u] = fetch8<WHOLE>((const S *)a.residual + row_at(r < a.rows ? r : 0, a.ld_res) + 8 * v, n, a.N);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -66,12 +66,14 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
         if (r >= a.rows) break;
         if constexpr (TOKENS) keep8(there[u], x[u]);
         float y[8];
+        settle8<WHOLE>(x[u], n, a.N);
         widen8(x[u], y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] *= a.scale;
         if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(r, a.nv) + (uint64_t)v, y);
         if constexpr (RESIDUAL) {
             float z[8];
+            settle8<WHOLE>(res[u], n, a.N);
             widen8(res[u], z);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += z[j];
@@ -353,7 +355,9 @@ __device__ __forceinline__ void apply_row(const GradArgs &a, int64_t row, int v,
     const int n = a.N - 8 * v;
     float y[8];
     if (a.old) {
-        widen8(fetch8<WHOLE>(p, n), y);
+        Vec8<O> x = fetch8<WHOLE>(p, n, a.N);
+        settle8<WHOLE>(x, n, a.N);
+        widen8(x, y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] = fmaf(sum[j], a.factor, y[j]);
     } else {
@@ -458,7 +462,7 @@ __global__ __launch_bounds__(WG) void token_grad_kernel(const GradArgs a, int lg
     for (int e0 = 0; e0 < cnt; e0 += NB) {
         Vec8<G> x[NB];
 #pragma unroll
-        for (int q = 0; q < NB; ++q) x[q] = fetch8<WHOLE>((const G *)a.g + row_at(tp[min(e0 + q, cnt - 1)], a.ld_g) + 8 * v, n);
+        for (int q = 0; q < NB; ++q) x[q] = fetch8<WHOLE>((const G *)a.g + row_at(tp[min(e0 + q, cnt - 1)], a.ld_g) + 8 * v, n, a.N);
 #pragma unroll
         for (int q = 0; q < NB; ++q) {
             if (e0 + q >= cnt) break;
@@ -471,6 +475,7 @@ __global__ __launch_bounds__(WG) void token_grad_kernel(const GradArgs a, int lg
                 for (int j = 0; j < 8; ++j) sum[j] = 0.f;
             }
             float y[8];
+            settle8<WHOLE>(x[q], n, a.N);
             widen8(x[q], y);
             if (a.drop.state) drop8(a.drop, dk, (uint64_t)row_at(tp[e0 + q], a.nv) + (uint64_t)v, y);   // (a.factor has the dropout's)
 #pragma unroll
@@ -510,11 +515,11 @@ __global__ __launch_bounds__(WG) void token_join_kernel(const GradArgs a, int lg
         for (int u0 = tile + 1 + gi; u0 < lo; u0 += NB * groups) {
             Vec8<float> x[NB];
 #pragma unroll
-            for (int q = 0; q < NB; ++q) x[q] = fetch8<true>(a.part + (int64_t)min(u0 + q * groups, lo - 1) * 2 * (8 * a.nv) + 8 * v, 8);
+            for (int q = 0; q < NB; ++q) x[q] = fetch8<true>(a.part + (int64_t)min(u0 + q * groups, lo - 1) * 2 * (8 * a.nv) + 8 * v, 8, 8);
 #pragma unroll
             for (int q = 0; q < NB; ++q)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sum[j] += u0 + q * groups < lo ? x[q].v[j] : 0.f;
+                for (int j = 0; j < 8; ++j) sum[j] += u0 + q * groups < lo ? __uint_as_float(x[q].w[j]) : 0.f;
         }
     }
 #pragma unroll
@@ -598,12 +603,13 @@ __global__ __launch_bounds__(WG) void token_few_kernel(const GradArgs a, const v
     for (int e0 = gi; e0 < cnt; e0 += NB * groups) {
         Vec8<G> x[NB];
 #pragma unroll
-        for (int q = 0; q < NB; ++q) x[q] = fetch8<WHOLE>((const G *)a.g + row_at(list[min(e0 + q * groups, cnt - 1)], a.ld_g) + 8 * vc, n);
+        for (int q = 0; q < NB; ++q) x[q] = fetch8<WHOLE>((const G *)a.g + row_at(list[min(e0 + q * groups, cnt - 1)], a.ld_g) + 8 * vc, n, a.N);
 #pragma unroll
         for (int q = 0; q < NB; ++q) {
             const int e = e0 + q * groups;
             if (e >= cnt) break;
             float y[8];
+            settle8<WHOLE>(x[q], n, a.N);
             widen8(x[q], y);
             if (a.drop.state) drop8(a.drop, dk, (uint64_t)row_at(list[e], a.nv) + (uint64_t)vc, y);
 #pragma unroll
