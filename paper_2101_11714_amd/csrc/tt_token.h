@@ -18,6 +18,7 @@ struct RowsArgs {
     const void *tokens;          // null: row r of the source
     int64_t ld_src, ld_res, ld_dst, rows, num_rows;
     int N, nv, wide;             // columns, vectors per row, tokens of 64 bits
+    double nv_d, inv_nv, half_nv;            // nv, 1 / nv, 0.5 / nv
     float scale;                 // with the dropout's factor
     DropArgs drop;
 };
@@ -27,25 +28,31 @@ __device__ __forceinline__ int64_t token_at(const void *tokens, int wide, int64_
     return wide ? ((const int64_t *)tokens)[i] : (int64_t)((const int32_t *)tokens)[i];
 }
 
-// tx threads (a power of two) along a row, WG / tx rows side by side, U rows per thread.  No load stands in a branch: what is loaded
-// there is waited for there, one load after the other; a row or a token that does not exist reads the first one instead.
+// A thread per vector, in the order of the rows, U of them per thread, WG apart; a vector's number is parted into row and place in
+// 64-bit floating point (exact below 2^51; one division of whole numbers would take longer than all the rest).  No load stands in a
+// branch: what is loaded there is waited for there, one load after the other; a row or a token that does not exist reads the first
+// one instead.
 // U = 1 for dropout alone (2 and 4 took 10 and 20 % longer: more workgroups hide more than longer ones), more for lookups, whose
 // loads wait for the tokens.
 template <typename S, typename D, int U, bool WHOLE, bool TOKENS, bool RESIDUAL>
-__global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
+__global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
 {
-    const int tx = 1 << lg_tx, ty = WG >> lg_tx;
-    const int v = blockIdx.y * tx + (threadIdx.x & (tx - 1));
-    if (v >= a.nv) return;
-    const int64_t r0 = (int64_t)blockIdx.x * (ty * U) + (threadIdx.x >> lg_tx);
-    const int n = a.N - 8 * v;
+    int64_t row[U];
+    int v[U], n[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const double i = (double)blockIdx.x * (double)(U * WG) + (double)(u * WG + (int)threadIdx.x);
+        const double r = floor(fma(i, a.inv_nv, a.half_nv));
+        row[u] = (int64_t)(uint32_t)r;                       // (behind the last row: cut off where it is looked at)
+        v[u] = (int)fma(-r, a.nv_d, i);
+        n[u] = a.N - 8 * v[u];
+    }
     const DropKey key = drop_key(a.drop);
     int64_t from[U];
     bool there[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t r = r0 + u * ty;
-        from[u] = r < a.rows ? r : 0;
+        from[u] = row[u] < a.rows ? row[u] : 0;
         there[u] = true;
         if constexpr (TOKENS) {
             const int64_t t = token_at(a.tokens, a.wide, from[u]);
@@ -56,29 +63,27 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a, int lg_tx)
     Vec8<S> x[U], res[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t r = r0 + u * ty;
-        x[u] = fetch8<WHOLE>((const S *)a.src + row_at(from[u], a.ld_src) + 8 * v, n, a.N);
-        if constexpr (RESIDUAL) res[u] = fetch8<WHOLE>((const S *)a.residual + row_at(r < a.rows ? r : 0, a.ld_res) + 8 * v, n, a.N);
+        x[u] = fetch8<WHOLE>((const S *)a.src + row_at(from[u], a.ld_src) + 8 * v[u], n[u], a.N);
+        if constexpr (RESIDUAL) res[u] = fetch8<WHOLE>((const S *)a.residual + row_at(row[u] < a.rows ? row[u] : 0, a.ld_res) + 8 * v[u], n[u], a.N);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int64_t r = r0 + u * ty;
-        if (r >= a.rows) break;
+        if (row[u] >= a.rows) break;
         if constexpr (TOKENS) keep8(there[u], x[u]);
         float y[8];
-        settle8<WHOLE>(x[u], n, a.N);
+        settle8<WHOLE>(x[u], n[u], a.N);
         widen8(x[u], y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] *= a.scale;
-        if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(r, a.nv) + (uint64_t)v, y);
+        if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row[u], a.nv) + (uint64_t)v[u], y);
         if constexpr (RESIDUAL) {
             float z[8];
-            settle8<WHOLE>(res[u], n, a.N);
+            settle8<WHOLE>(res[u], n[u], a.N);
             widen8(res[u], z);
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += z[j];
         }
-        put8<WHOLE>((D *)a.dst + row_at(r, a.ld_dst) + 8 * v, n, y);
+        put8<WHOLE>((D *)a.dst + row_at(row[u], a.ld_dst) + 8 * v[u], n[u], y);
     }
 }
 

@@ -22,18 +22,17 @@ int check_tokens(const tt_tokens_t *t, int64_t *L)
     return TT_OK;
 }
 
-int rows_lg(int nv) { return lg_ceil(nv < WG ? nv : WG); }
-
-// rows_kernel: a workgroup covers up to WG vectors of a row
 template <typename S, typename D, int U, bool TOKENS, bool RESIDUAL>
-int launch_rows(const RowsArgs &a, hipStream_t st)
+int launch_rows(RowsArgs &a, hipStream_t st)
 {
-    const int lg = rows_lg(a.nv), ty = WG >> lg;
-    const int64_t blocks = ceil_div(a.rows, ty * U);
+    const int64_t blocks = ceil_div(a.rows * a.nv, WG * U);
     const int rc = check_grid(blocks, WG);
     if (rc) return rc;
+    a.nv_d = (double)a.nv;
+    a.inv_nv = 1.0 / a.nv_d;
+    a.half_nv = 0.5 * a.inv_nv;
     with_whole(a.N, [&](auto whole) {
-        hipLaunchKernelGGL((rows_kernel<S, D, U, decltype(whole)::value, TOKENS, RESIDUAL>), dim3((unsigned)blocks, (unsigned)ceil_div(a.nv, 1 << lg)), dim3(WG), 0, st, a, lg);
+        hipLaunchKernelGGL((rows_kernel<S, D, U, decltype(whole)::value, TOKENS, RESIDUAL>), dim3((unsigned)blocks), dim3(WG), 0, st, a);
     });
     return TT_OK;
 }
@@ -58,10 +57,11 @@ struct GradWs {
     size_t bytes;
 };
 
-// Entries per tile of sorted positions: 8 where there is little work, so that more of the device has some; 64 else, for fewer sums
-// of runs that cross tiles.
-constexpr int64_t GRAD_SHORT = 1 << 22;                      // vectors of the gradient
-int grad_entries(int64_t L, int64_t nv) { return L * nv < GRAD_SHORT ? 8 : nv >= WAVE ? 64 : 16; }
+// Entries per tile of sorted positions: as many as leave 4,096 waves some work, and at least 8 and at most 64 (then fewer sums of
+// runs cross tiles).  16-bit gradients, 8 / 16 / 32 / 64 entries: 16,384 tokens of 1,024 columns 65 / 64 / 66 / 79 us, 32,768 of 4,096
+// columns 525 / 500 / 488 / 482.
+constexpr int64_t GRAD_SHORT = 1 << 22;                      // vectors of the gradient up to which it is 8
+int grad_entries(int64_t L, int64_t nv) { return L * nv < GRAD_SHORT ? 8 : L * nv < 2 * GRAD_SHORT ? 16 : L * nv < 4 * GRAD_SHORT ? 32 : 64; }
 
 // The path without a sort, whose workgroups each look at all tokens: up to 4,096 of them.  16-bit gradients of 1,024 columns added to a
 // table, sort / without: 30 tokens 14.4 / 5.1 us, 500 16 / 5.5, 1,000 17.2 / 8.1 (all of one token 17 / 26); of 4,096 columns,
@@ -188,11 +188,9 @@ int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropou
     a.tiles = (int)ceil_div(L, a.entries);
     a.factor = factor * a.drop.factor;
     a.old = old;
-    // the lanes of a tile: up to the whole workgroup, so that a row of the gradient is read in long pieces; to join few, for many groups
     const bool few = few_tokens(L, a.nv);
-    int lg = lg_ceil(a.nv < WG ? a.nv : WG), lg_join = lg < 6 ? lg : 6;
-    if (few) lg = lg_join;
-    else if (lg < TG_LEAST_LG) lg = TG_LEAST_LG;
+    int lg = lg_ceil(a.nv < WAVE ? a.nv : WAVE), lg_join = lg;
+    if (!few && lg < TG_LEAST_LG) lg = TG_LEAST_LG;
     const unsigned chunks = (unsigned)ceil_div(a.nv, 1 << lg), join_chunks = (unsigned)ceil_div(a.nv, 1 << lg_join);
     const int64_t sum_blocks = (few ? L : ceil_div(a.tiles, WG >> lg)) * chunks;
     ClearArgs k{};
