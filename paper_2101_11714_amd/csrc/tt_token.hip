@@ -61,7 +61,13 @@ struct GradWs {
 // runs cross tiles).  16-bit gradients, 8 / 16 / 32 / 64 entries: 16,384 tokens of 1,024 columns 65 / 64 / 66 / 79 us, 32,768 of 4,096
 // columns 525 / 500 / 488 / 482.
 constexpr int64_t GRAD_SHORT = 1 << 22;                      // vectors of the gradient up to which it is 8
-int grad_entries(int64_t L, int64_t nv) { return L * nv < GRAD_SHORT ? 8 : L * nv < 2 * GRAD_SHORT ? 16 : L * nv < 4 * GRAD_SHORT ? 32 : 64; }
+int grad_entries(int64_t L, int64_t nv)
+{
+    if (L * nv < GRAD_SHORT) return 8;
+    if (L * nv < 2 * GRAD_SHORT) return 16;
+    return L * nv < 4 * GRAD_SHORT || nv <= 1 << TG_LEAST_LG ? 32 : 64;      // (the shortest rows: as many as a workgroup's LDS holds)
+}
+static_assert((WG >> TG_LEAST_LG) * 32 <= TG_MOST && (WG >> (TG_LEAST_LG + 1)) * 64 <= TG_MOST, "a workgroup's entries fit its LDS");
 
 // The path without a sort, whose workgroups each look at all tokens: up to 4,096 of them.  16-bit gradients of 1,024 columns added to a
 // table, sort / without: 30 tokens 14.4 / 5.1 us, 500 16 / 5.5, 1,000 17.2 / 8.1 (all of one token 17 / 26); of 4,096 columns,

@@ -603,3 +603,60 @@ def test_token_bwd_of_a_table_of_many_rows(L):
     want, mag, most = R.token_bwd(tokens, grad, vocab, 1.0, None)
     R.assert_within(out, want, (most + 4) * U32 * mag)
     assert_guard(out, flat)
+
+
+def run_lengths(E):
+    """Runs of sorted tokens that begin and end at every place of a tile of E entries, of up to four tiles."""
+    lengths = []
+    for pad in (0, 1, E // 2, E - 1):
+        for n in (1, E - 1, E, E + 1, 2 * E - 1, 2 * E, 2 * E + 1, 3 * E - 1, 3 * E, 4 * E + 3):
+            lengths += [n, (pad - sum(lengths) - n) % E or E]    # then a run up to the next start at place `pad`
+    return lengths
+
+
+@pytest.mark.parametrize("N,E", [(72, 8), (20, 8), (3, 8), (8 * 2600, 16), (4096 * 8, 32), (8 * 2600, 64)])
+@pytest.mark.parametrize("p", [None, 0.3])
+def test_token_bwd_of_runs_of_every_kind(N, E, p):
+    lengths = run_lengths(E) * (2 if E == 8 else 1)          # (more tokens than the call without a sort takes)
+    tokens = torch.repeat_interleave(torch.arange(len(lengths)), torch.tensor(lengths))
+    tokens = torch.cat([tokens, torch.full((13,), -1)])
+    g = gen(71)
+    L = tokens.numel()
+    if L * N > 3e7:                                          # (tiles of 16 and 32 entries take wide rows; a column in 4,096 is looked at)
+        tokens = tokens[torch.randperm(L, generator=g)].to("cuda:0")
+        grad = torch.randn((L, N), generator=torch.Generator(device="cuda:0").manual_seed(3), device="cuda:0")
+        out = torch.empty((len(lengths), N), device="cuda:0")
+        d = dropout_of(p)
+        B.tt_token_bwd(tokens, grad, out, dropout=d)
+        live = tokens >= 0
+        if d is not None:
+            grad = B.tt_dropout_bwd(grad, grad, d)
+        want = torch.zeros((len(lengths), N), dtype=torch.float64, device="cuda:0").index_add_(0, tokens[live], grad[live].double())
+        mag = torch.zeros((len(lengths), N), dtype=torch.float64, device="cuda:0").index_add_(0, tokens[live], grad[live].abs().double())
+        assert bool(((out.double() - want).abs() <= (max(lengths) + 6) * U32 * mag).all())
+        return
+    tokens = tokens[torch.randperm(L, generator=g)].to("cuda:0")
+    grad, d = R.rows_of(g, L, N, F32), dropout_of(p)
+    out, flat = room(len(lengths) + 3, N, F32, 1, 1)
+    B.tt_token_bwd(tokens, grad, out, dropout=d)
+    want, mag, most = R.token_bwd(tokens, grad, len(lengths) + 3, 1.0, d)
+    R.assert_within(out, want, (most + 4) * U32 * mag)
+    assert_guard(out, flat)
+
+
+@pytest.mark.parametrize("L,N", [((1 << 24) + 5, 3), ((1 << 22) + 3, 32), ((1 << 21) + 1, 64)])
+def test_token_bwd_of_very_many_tokens(L, N):
+    # the longest tiles with the fewest lanes per tile, scanned counts of the sort's tiles
+    vocab = 5000
+    dg = torch.Generator(device="cuda:0").manual_seed(5)
+    tokens = torch.randint(-1, vocab, (L,), generator=dg, device="cuda:0")
+    tokens[::3] = 77
+    grad = torch.randn((L, N), generator=dg, device="cuda:0").to(BF16)
+    out = torch.empty((vocab, N), device="cuda:0")
+    B.tt_token_bwd(tokens, grad, out)
+    live = tokens >= 0
+    want = torch.zeros((vocab, N), dtype=torch.float64, device="cuda:0").index_add_(0, tokens[live], grad[live].double())
+    mag = torch.zeros((vocab, N), dtype=torch.float64, device="cuda:0").index_add_(0, tokens[live], grad[live].abs().double())
+    # terms of a sum: those of a tile one after the other, then the tiles' sums, of which a lane adds at most a quarter
+    terms = 64 + (int((tokens == 77).sum()) // 32 + 8) / 4 + 8
+    assert bool(((out.double() - want).abs() <= terms * U32 * mag).all())
