@@ -35,15 +35,14 @@ NormShape norm_fwd_shape(int64_t rows, int64_t nv, int least_lg)
     return norm_shape(lg < least_lg ? least_lg : lg, nv);
 }
 
-// The gradients' workgroups have NORM_BWD_THREADS threads (1,024 have too few registers: for the longest rows alone).
-constexpr int NORM_BWD_THREADS = 512;
 constexpr int64_t NORM_BWD_WORKGROUPS = 256;
-
-int norm_bwd_threads(int64_t nv) { return nv > 4 * NORM_BWD_THREADS ? 1024 : NORM_BWD_THREADS; }
+// Rows that give so many workgroups work are left to one, whose sums are the weight's gradient: one launch instead of two (two rows of
+// 4,096 columns 7.9 -> 6.0 us, three 8.5 -> 6.9, 128 of 64 7.9 -> 5.4; not three of 16,000: 13.8 -> 15.5).
+constexpr int64_t NORM_BWD_ALONE = 3;
 
 NormShape norm_bwd_shape(int64_t nv)
 {
-    const int lg = lg_ceil(nv), most = lg_ceil(norm_bwd_threads(nv));
+    const int lg = lg_ceil(nv), most = lg_ceil(RN_BWD_THREADS);
     return norm_shape(lg < most ? lg : most, nv);
 }
 
@@ -189,7 +188,8 @@ int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const 
     a.rstd = rstd;
     a.dx = grad_x ? grad_x->data : nullptr;
     a.dres = grad_residual ? grad_residual->data : nullptr;
-    a.part = grad_weight ? (float *)workspace : nullptr;
+    a.dw_type = grad_weight_type;
+    a.add = accumulate != 0;
     a.ld_dy = grad_output->ld;
     a.ld_h = h->ld;
     a.ld_dsum = grad_sum ? grad_sum->ld : 0;
@@ -202,23 +202,26 @@ int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const 
     int64_t grid = 0;
     if (n_rows > 0) {
         const NormShape s = norm_bwd_shape(a.nv);
-        const int threads = norm_bwd_threads(a.nv), groups = threads >> s.lg, parts = s.lg < 6 ? threads / WAVE : groups;
+        const int threads = RN_BWD_THREADS, groups = threads >> s.lg, parts = s.lg < 6 ? threads / WAVE : groups;
         grid = ceil_div(n_rows, groups) < NORM_BWD_WORKGROUPS ? ceil_div(n_rows, groups) : NORM_BWD_WORKGROUPS;
+        if (grid <= NORM_BWD_ALONE && s.vpt <= 2) grid = 1;
+        if (grid > 1) a.part = grad_weight ? (float *)workspace : nullptr;
+        else a.dw = grad_weight;
         const size_t lds = grad_weight && parts > 1 ? (size_t)parts * 8 * a.nv * sizeof(float) : 0;
         with_types(grad_output->type, h->type, [&](auto t, auto ht) {
-            auto launch = [&](auto vpt, auto most) {
+            auto launch = [&](auto vpt) {
                 with_whole(N, [&](auto whole) {
                     with_flag(grad_sum != nullptr, [&](auto dsum) {
-                        hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), decltype(ht), decltype(vpt)::value, decltype(most)::value, decltype(whole)::value, decltype(dsum)::value>),
+                        hipLaunchKernelGGL((norm_bwd_kernel<decltype(t), decltype(ht), decltype(vpt)::value, decltype(whole)::value, decltype(dsum)::value>),
                                            dim3((unsigned)grid), dim3(threads), lds, st, a, s.lg);
                     });
                 });
             };
-            if (threads == 1024) launch(std::integral_constant<int, 4>{}, std::integral_constant<int, 1024>{});
-            else with_vpt(s.vpt, [&](auto vpt) { launch(vpt, std::integral_constant<int, NORM_BWD_THREADS>{}); });
+            if (s.vpt > 4) launch(std::integral_constant<int, 8>{});
+            else with_vpt(s.vpt, launch);
         });
     }
-    if (grad_weight)
+    if (grad_weight && !a.dw)
         with_type(grad_weight_type, [&](auto w) {
             hipLaunchKernelGGL(norm_dw_kernel<decltype(w)>, dim3((unsigned)ceil_div(N, 64)), dim3(1024), 0, st, (const float *)workspace, (int)grid, (int)N, a.nv,
                                (decltype(w) *)grad_weight, accumulate);

@@ -198,18 +198,31 @@ struct NormGradArgs {
     const void *dy, *h, *weight, *dsum;                      // dsum: of h's type, or null
     const float *rstd;
     void *dx, *dres;                                         // either may be null
-    float *part;                                             // [workgroup][nv * 8], or null: no gradient of the weight
+    float *part;                                             // [workgroup][nv * 8], or null: no gradient of the weight, or
+    void *dw;                                                // here, from the only workgroup
+    int dw_type, add;
     int64_t ld_dy, ld_h, ld_dsum, ld_dx, ld_dres, rows;
     int N, nv, weight_type;
     DropArgs drop;
 };
 
-// Rows go to the groups of threads in turn; a thread's columns are the same for all of them, so the weight's gradient of
-// its rows stays in registers, and each workgroup leaves one row of sums.  Loads as in norm_fwd_kernel.
-template <typename T, typename H, int VPT, int THREADS, bool WHOLE, bool DSUM>
-__global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a, int lg)
+template <typename W>
+__device__ __forceinline__ void put_weight(W *p, float x, int add)
 {
-    __shared__ float slots[2][THREADS / WAVE];
+    *p = (W)(add ? (float)*p + x : x);
+}
+
+// Rows go to the groups of threads in turn; a thread's columns are the same for all of them, so the weight's gradient of
+// its rows stays in registers, and each workgroup leaves one row of sums.  Loads as in norm_fwd_kernel.  AGAIN: the longest rows do not
+// fit the registers beside it: they are read a second time, mostly from the L2.
+constexpr int RN_BWD_THREADS = 512;                          // (1,024 have too few registers)
+
+template <typename T, typename H, int VPT, bool WHOLE, bool DSUM>
+__global__ __launch_bounds__(RN_BWD_THREADS) void norm_bwd_kernel(const NormGradArgs a, int lg)
+{
+    __shared__ float slots[2][RN_BWD_THREADS / WAVE];
+    constexpr int THREADS = RN_BWD_THREADS;
+    constexpr bool AGAIN = VPT > 4;
     extern __shared__ float lds[];                           // [waves, or groups of whole waves][nv * 8], if more than one
     const int g = 1 << lg, t = threadIdx.x & (g - 1), groups = THREADS >> lg, gi = threadIdx.x >> lg;
     const DropKey key = drop_key(a.drop);
@@ -227,20 +240,33 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
         Vec8<T> dy[VPT];
         Vec8<H> h[VPT], ds[VPT];
         const float rstd = a.rstd[row];
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
+        auto load = [&](int i) {
             const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
             dy[i] = fetch8<WHOLE>((const T *)a.dy + row_at(row, a.ld_dy) + 8 * v, n, a.N);
             h[i] = fetch8<WHOLE>((const H *)a.h + row_at(row, a.ld_h) + 8 * v, n, a.N);
-            if constexpr (DSUM) ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, n, a.N);
+        };
+        auto load_sum = [&](int i) {
+            const int v = min(i * g + t, a.nv - 1);
+            if constexpr (DSUM) ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, a.N - 8 * v, a.N);
+        };
+        auto settle = [&](int i) {
+            const int n = a.N - 8 * min(i * g + t, a.nv - 1);
+            settle8<WHOLE>(dy[i], n, a.N);
+            settle8<WHOLE>(h[i], n, a.N);
+        };
+        if constexpr (!AGAIN) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                load(i);
+                load_sum(i);
+            }
         }
         float dot = 0.f;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
-            const int n = a.N - 8 * min(i * g + t, a.nv - 1);
+            if constexpr (AGAIN) load(i);
+            settle(i);
             float p[8], q[8], part = 0.f;
-            settle8<WHOLE>(dy[i], n, a.N);
-            settle8<WHOLE>(h[i], n, a.N);
             widen8(dy[i], p);
             widen8(h[i], q);
 #pragma unroll
@@ -256,6 +282,11 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = i * g + t, n = a.N - 8 * v;
+            if constexpr (AGAIN) {
+                load(i);
+                load_sum(i);
+                settle(i);
+            }
             float p[8], q[8], d[8];
             widen8(dy[i], p);
             widen8(h[i], q);
@@ -280,7 +311,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
             }
         }
     }
-    if (!a.part) return;
+    if (!a.part && !a.dw) return;
     // groups of a wave by lane exchange, then waves (or groups of more than one wave) through LDS, in their order
     for (int b = lg; b < 6; ++b)
 #pragma unroll
@@ -288,15 +319,24 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
 #pragma unroll
             for (int j = 0; j < 8; ++j) dw[i][j] += __shfl_xor(dw[i][j], 1 << b);
     const int parts = lg < 6 ? THREADS / WAVE : groups, at = lg < 6 ? threadIdx.x >> 6 : gi, cols = 8 * a.nv;
-    float *out = a.part + (int64_t)blockIdx.x * cols;
-    if (parts > 1) out = lds + at * cols;
+    auto leave = [&](int c, float x) {
+        if (a.part) a.part[(int64_t)blockIdx.x * cols + c] = x;
+        else if (c < a.N) {
+            if (a.dw_type == TT_F32) put_weight((float *)a.dw + c, x, a.add);
+            else if (a.dw_type == TT_BF16) put_weight((bf16_t *)a.dw + c, x, a.add);
+            else put_weight((f16_t *)a.dw + c, x, a.add);
+        }
+    };
     if (lg >= 6 || (threadIdx.x & 63) < g) {
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = i * g + t;
             if (v < a.nv) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) out[8 * v + j] = dw[i][j];
+                for (int j = 0; j < 8; ++j) {
+                    if (parts > 1) lds[at * cols + 8 * v + j] = dw[i][j];
+                    else leave(8 * v + j, dw[i][j]);
+                }
             }
         }
     }
@@ -305,7 +345,7 @@ __global__ __launch_bounds__(THREADS) void norm_bwd_kernel(const NormGradArgs a,
     for (int c = threadIdx.x; c < cols; c += THREADS) {
         float s = lds[c];
         for (int q = 1; q < parts; ++q) s += lds[q * cols + c];
-        a.part[(int64_t)blockIdx.x * cols + c] = s;
+        leave(c, s);
     }
 }
 

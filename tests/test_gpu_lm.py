@@ -665,3 +665,17 @@ def test_token_bwd_of_very_many_tokens(L, N):
     # terms of a sum: those of a tile one after the other, then the tiles' sums, of which a lane adds at most a quarter
     terms = 64 + (int((tokens == 77).sum()) // 32 + 8) / 4 + 8
     assert bool(((out.double() - want).abs() <= terms * U32 * mag).all())
+
+
+def test_example_learns_and_serves():
+    from paper_2101_11714_amd import token_block
+    block, first, last = token_block.train(steps=120)
+    assert last < 0.5 * first, (first, last)
+    # served rows are the plain forward pass of the block's own parameters
+    tokens = torch.tensor([3], device="cuda:0")
+    pairs = block.pairs(tokens)
+    out, scales = block.serve(tokens, pairs)
+    branch = B.tt_emb_fwd(block.shape, block.cores, pairs, None, 1, torch.empty((1, block.N), device="cuda:0"))
+    _, _, y, _ = R.norm_fwd(branch, block.table[3:4] * block.scale, block.weight, 1e-6, None)
+    got = R.f64(out.float()) * R.f64(scales)
+    assert np.abs(got - y).max() <= np.abs(y).max() * 2.0 ** -4
