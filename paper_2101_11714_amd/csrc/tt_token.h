@@ -3,7 +3,9 @@
 // Forward: out[t] = m_t . (scale table[token_t]); a token outside [0, num_rows) is none and gets a row of zeros.
 // Backward: G[v] = scale sum_{t: token_t = v} m_t . g[t], in 32 bits, in the order of t within a tile of sorted positions
 // and tile after tile, so that the result is the same in every run; nothing is added with atomics.
-// Both are bound by HBM; the gather reads whole rows, the gradient is one pass over g and one over the rows it writes.
+// Both are bound by HBM where there is work; the gather reads whole rows, the gradient is one pass over g and one over the rows it
+// writes.  32,768 tokens of 4,096 columns in 16 bits: lookup with dropout 79 us (4.6 TB/s of distinct rows and output; without 76), gradient
+// of 131,072 rows in 32 bits 482 us (5.0 TB/s), of which sorting takes 25 and joining 13.
 #pragma once
 
 #include "tt_rows_io.h"
@@ -284,7 +286,8 @@ __global__ __launch_bounds__(TS_WG) void token_scatter_kernel(const SortPass s)
     }
 }
 
-// Few tokens: the whole sort in one workgroup, in LDS.  One launch instead of two per digit.
+// Few tokens: the whole sort in one workgroup, in LDS.  One launch instead of two per digit: 13 us for 4,093 tokens of 50,001 rows, where
+// four launches take 24; 37 us for 16,384 (an earlier form), where they take 22.
 constexpr int TO_MOST = 8 * TS_WG;
 
 static inline size_t sort_one_lds(int R) { return (size_t)R * TS_WG * 6 + (size_t)TS_WAVES * TS_BINS * 2 + TS_BINS * 4 + TS_WAVES * 4; }
