@@ -653,7 +653,8 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
  * forward pass).  The positions are sorted by token and every row is written once.  accumulate == 0: all num_rows rows are
  * written, zeros where no token is; else the sums are added to grad_table, whose other rows are not touched.
  * tt_token_bwd_sgd: table -= lr * gradient in place, rows in use only.
- * workspace: tt_token_bwd_workspace_bytes(L, num_rows, N) bytes, 16-byte aligned (enough for fewer tokens too).  L < 2^28.
+ * workspace: tt_token_bwd_workspace_bytes(L, num_rows, N) bytes, 16-byte aligned (enough for fewer tokens too; 0 for few: none is
+ * needed).  L < 2^28.
  */
 size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t num_rows, int64_t N);
 int tt_token_bwd(const tt_tokens_t *tokens, const tt_rows_t *grad_output, float scale, const tt_dropout_t *dropout,
@@ -689,7 +690,8 @@ int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_
  * grad_sum: the gradient that reaches h through the residual stream, NULL for none.  grad_x, grad_residual, grad_weight: any of
  * them may be NULL.  Types: grad_output and grad_x one, any of 32 or 16 bits; h, grad_sum and grad_residual one, that or 32 bits;
  * weight and grad_weight any.  accumulate != 0 adds to grad_weight.  grad_x may be grad_output, grad_residual may be grad_sum.
- * workspace: tt_add_rms_norm_bwd_workspace_bytes(n_rows, N) bytes, 16-byte aligned, if grad_weight is asked for.
+ * workspace: tt_add_rms_norm_bwd_workspace_bytes(n_rows, N) bytes, 16-byte aligned, if grad_weight is asked for (0 for few rows; enough
+ * for fewer rows too).
  */
 size_t tt_add_rms_norm_bwd_workspace_bytes(int64_t n_rows, int64_t N);
 int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const float *rstd, const void *weight, int32_t weight_type,

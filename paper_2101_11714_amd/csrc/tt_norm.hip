@@ -46,6 +46,14 @@ NormShape norm_bwd_shape(int64_t nv)
     return norm_shape(lg < most ? lg : most, nv);
 }
 
+int64_t norm_bwd_grid(int64_t rows, int64_t nv)
+{
+    const NormShape s = norm_bwd_shape(nv);
+    const int64_t all = ceil_div(rows, RN_BWD_THREADS >> s.lg);
+    if (all <= NORM_BWD_ALONE && s.vpt <= 2) return 1;
+    return all < NORM_BWD_WORKGROUPS ? all : NORM_BWD_WORKGROUPS;
+}
+
 template <typename F>
 void with_vpt(int vpt, F f)
 {
@@ -150,8 +158,8 @@ int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_
 size_t tt_add_rms_norm_bwd_workspace_bytes(int64_t n_rows, int64_t N)
 {
     if (n_rows <= 0 || N <= 0 || n_rows >= MOST_ROWS || N > RN_MOST) return 0;
-    const int64_t most = n_rows < NORM_BWD_WORKGROUPS ? n_rows : NORM_BWD_WORKGROUPS;
-    return (size_t)most * (size_t)(8 * ceil_div(N, 8)) * sizeof(float);
+    const int64_t nv = ceil_div(N, 8), grid = norm_bwd_grid(n_rows, nv);
+    return grid > 1 ? (size_t)grid * (size_t)(8 * nv) * sizeof(float) : 0;
 }
 
 int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const float *rstd, const void *weight, int32_t weight_type,
@@ -203,8 +211,7 @@ int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const 
     if (n_rows > 0) {
         const NormShape s = norm_bwd_shape(a.nv);
         const int threads = RN_BWD_THREADS, groups = threads >> s.lg, parts = s.lg < 6 ? threads / WAVE : groups;
-        grid = ceil_div(n_rows, groups) < NORM_BWD_WORKGROUPS ? ceil_div(n_rows, groups) : NORM_BWD_WORKGROUPS;
-        if (grid <= NORM_BWD_ALONE && s.vpt <= 2) grid = 1;
+        grid = norm_bwd_grid(n_rows, a.nv);
         if (grid > 1) a.part = grad_weight ? (float *)workspace : nullptr;
         else a.dw = grad_weight;
         const size_t lds = grad_weight && parts > 1 ? (size_t)parts * 8 * a.nv * sizeof(float) : 0;

@@ -79,13 +79,14 @@ __device__ __forceinline__ Vec8<T> narrow8(const float (&x)[8])
     return r;
 }
 
-// one rounding, to the nearest even
+// one rounding, to the nearest even.  past: past the caches (the same for all threads)
 template <bool WHOLE = false, typename T>
-__device__ __forceinline__ void put8(T *p, int n, const float (&x)[8])
+__device__ __forceinline__ void put8(T *p, int n, const float (&x)[8], bool past = false)
 {
     const Vec8<T> r = narrow8<T>(x);
     if (WHOLE || n >= 8) {
-        *reinterpret_cast<typename Vec8<T>::Anywhere *>(p) = r.w;
+        if (past) __builtin_nontemporal_store(r.w, reinterpret_cast<typename Vec8<T>::Anywhere *>(p));
+        else *reinterpret_cast<typename Vec8<T>::Anywhere *>(p) = r.w;
     } else {
         struct Values { T v[8]; };
         const Values y = __builtin_bit_cast(Values, r.w);
@@ -172,8 +173,12 @@ __device__ __forceinline__ DropKey drop_key(const DropArgs &d)
     return k;
 }
 
-// The columns of one block that are dropped become 0, whatever they were; the factor of the others is the caller's.
-__device__ __forceinline__ void drop8(const DropArgs &d, const DropKey &k, uint64_t block, float (&x)[8])
+struct DropWords {
+    uint32_t w[4];
+};
+
+// the words of one block
+__device__ __forceinline__ DropWords drop_words(const DropArgs &d, const DropKey &k, uint64_t block)
 {
     uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = d.site, c3 = k.step, k0 = k.k0, k1 = k.k1;
 #pragma unroll
@@ -186,12 +191,19 @@ __device__ __forceinline__ void drop8(const DropArgs &d, const DropKey &k, uint6
         k0 += 0x9E3779B9u;
         k1 += 0xBB67AE85u;
     }
-    const uint32_t w[4] = {c0, c1, c2, c3};
+    return {{c0, c1, c2, c3}};
+}
+
+// The columns of the words' block that are dropped become 0, whatever they were; the factor of the others is the caller's.
+__device__ __forceinline__ void drop8(const DropArgs &d, const DropWords &words, float (&x)[8])
+{
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        x[2 * j] = (w[j] << 16) > d.most ? x[2 * j] : 0.f;
-        x[2 * j + 1] = w[j] > d.most ? x[2 * j + 1] : 0.f;
+        x[2 * j] = (words.w[j] << 16) > d.most ? x[2 * j] : 0.f;
+        x[2 * j + 1] = words.w[j] > d.most ? x[2 * j + 1] : 0.f;
     }
 }
+
+__device__ __forceinline__ void drop8(const DropArgs &d, const DropKey &k, uint64_t block, float (&x)[8]) { drop8(d, drop_words(d, k, block), x); }
 
 }  // namespace tt

@@ -20,6 +20,7 @@ struct RowsArgs {
     const void *tokens;          // null: row r of the source
     int64_t ld_src, ld_res, ld_dst, rows, num_rows;
     int N, nv, wide;             // columns, vectors per row, tokens of 64 bits
+    bool past;                   // the output goes past the caches, which hold rows of the table
     double nv_d, inv_nv, half_nv;            // nv, 1 / nv, 0.5 / nv
     float scale;                 // with the dropout's factor
     DropArgs drop;
@@ -68,6 +69,11 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
         x[u] = fetch8<WHOLE>((const S *)a.src + row_at(from[u], a.ld_src) + 8 * v[u], n[u], a.N);
         if constexpr (RESIDUAL) res[u] = fetch8<WHOLE>((const S *)a.residual + row_at(row[u] < a.rows ? row[u] : 0, a.ld_res) + 8 * v[u], n[u], a.N);
     }
+    DropWords words[U];                                      // (while the vectors are on their way)
+    if (a.drop.state) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) words[u] = drop_words(a.drop, key, (uint64_t)row_at(row[u], a.nv) + (uint64_t)v[u]);
+    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         if (row[u] >= a.rows) break;
@@ -77,7 +83,7 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
         widen8(x[u], y);
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[j] *= a.scale;
-        if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row[u], a.nv) + (uint64_t)v[u], y);
+        if (a.drop.state) drop8(a.drop, words[u], y);
         if constexpr (RESIDUAL) {
             float z[8];
             settle8<WHOLE>(res[u], n[u], a.N);
@@ -85,7 +91,7 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += z[j];
         }
-        put8<WHOLE>((D *)a.dst + row_at(row[u], a.ld_dst) + 8 * v[u], n[u], y);
+        put8<WHOLE>((D *)a.dst + row_at(row[u], a.ld_dst) + 8 * v[u], n[u], y, TOKENS && a.past);
     }
 }
 

@@ -176,7 +176,7 @@ int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropou
     if ((rc = check_dropout(dropout, &a.drop))) return rc;
     if (N == 0 || num_rows == 0 || (old && L == 0)) return TT_OK;
     const size_t need = tt_token_bwd_workspace_bytes(L, num_rows, N);
-    if (L > 0 && (!workspace || workspace_bytes < need))
+    if (need && (!workspace || workspace_bytes < need))
         return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
     if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
     hipStream_t st = (hipStream_t)stream;
@@ -261,6 +261,9 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     a.nv = (int)ceil_div(N, 8);
     a.wide = tokens->bits == 64;
     a.scale = scale * a.drop.factor;
+    // an output that the memory-side cache does not hold for whoever reads it next leaves that to the table's rows (32,768 tokens of
+    // 4,096 columns in 16 bits 75 -> 72 us; 8,192 of 2,048 10.0 -> 9.3, but whoever reads those 32 MB then would find them in no cache)
+    a.past = L * N * element_bytes(output->type) >= 256ll << 20;
     if (num_rows == 0) {                                     // no token is one: rows of zeros, for which nothing has to be there to be read
         a.src = output->data;
         a.ld_src = 0;
@@ -268,11 +271,10 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     }
     with_type(num_rows ? table->type : output->type, [&](auto s) {
         with_type(output->type, [&](auto d) {
-            // few tokens: one row per thread, so that more of the device has some; else two, or, where the generator's products take the
-            // time, four (32,768 tokens of 4,096 columns in 16 bits, 1 / 2 / 4 rows: 96 / 76 / 78 us, with dropout 109 / 85 / 80)
+            // few tokens: one vector per thread, so that more of the device has some; else two (32,768 tokens of 4,096 columns in 16 bits
+            // under dropout, 1 / 2 / 4 vectors: 97 / 75 / 77 us)
             if (L * a.nv < (1 << 20)) rc = launch_rows<decltype(s), decltype(d), 1, true, false>(a, (hipStream_t)stream);
-            else if (!a.drop.state) rc = launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
-            else rc = launch_rows<decltype(s), decltype(d), 4, true, false>(a, (hipStream_t)stream);
+            else rc = launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
         });
     });
     if (rc) return rc;
@@ -281,7 +283,7 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
 
 size_t tt_token_bwd_workspace_bytes(int64_t L, int64_t num_rows, int64_t N)
 {
-    if (L <= 0 || num_rows <= 0 || num_rows >= MOST_ROWS || N <= 0 || L >= MOST_GRAD_TOKENS || N > MOST_COLUMNS) return 0;
+    if (L <= 0 || few_tokens(L, ceil_div(N, 8)) || num_rows <= 0 || num_rows >= MOST_ROWS || N <= 0 || L >= MOST_GRAD_TOKENS || N > MOST_COLUMNS) return 0;
     return grad_ws(nullptr, L, num_rows, N).bytes;
 }
 

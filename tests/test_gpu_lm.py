@@ -571,7 +571,7 @@ def test_binding_refuses_what_does_not_fit():
             bad()
     for code, bad in [(-6, lambda: B.tt_token_fwd(t(10, 16, dtype=E4M3), tokens, out)), (-1, lambda: B.tt_dropout_fwd(out, out, None)), (-3, lambda: B.tt_dropout_fwd(out, out, dropout_of(1.5))),
                       (-3, lambda: B.tt_dropout_fwd(out, out, dropout_of(float("nan")))), (-6, lambda: B.tt_dropout_fwd(out, t(5, 16, dtype=BF16), dropout_of(0.1))),
-                      (-3, lambda: B.tt_token_bwd(tokens, out, table[:1].expand(10, 16))), (-4, lambda: B.tt_token_bwd(tokens, out, table, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda:0"))),
+                      (-3, lambda: B.tt_token_bwd(tokens, out, table[:1].expand(10, 16))), (-4, lambda: B.tt_token_bwd(t(2000, dtype=torch.int64), t(2000, 16), table, workspace=torch.zeros(64, dtype=torch.uint8, device="cuda:0"))),
                       (-6, lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=BF16))), (-6, lambda: B.tt_add_rms_norm_fwd(out, None, out, residual=t(5, 16, dtype=BF16))),
                       (-1, lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=E4M3))), (-3, lambda: B.tt_add_rms_norm_fwd(out, None, out, scales=t(5, 1))),
                       (-6, lambda: B.tt_add_rms_norm_fwd(out, None, t(5, 16, dtype=E4M3), scales=t(5, 1), group=48)), (-3, lambda: B.tt_add_rms_norm_fwd(out, None, out, eps=-1.0)),

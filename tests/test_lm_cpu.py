@@ -44,10 +44,11 @@ def test_token_calls_check_their_arguments():
         assert len(l.tt_last_error()) > 0
     assert l.tt_token_fwd(*good(tokens=toks(data=None, L=0))) == 0
     assert l.tt_token_fwd(*good(N=0)) == 0
-    need = l.tt_token_bwd_workspace_bytes(5, 10, 16)
+    assert l.tt_token_bwd_workspace_bytes(5, 10, 16) == 0      # few tokens need none
+    need = l.tt_token_bwd_workspace_bytes(2000, 10, 16)
     assert need > 0
     for f, tail in ((l.tt_token_bwd, (0,)), (l.tt_token_bwd_sgd, (0.1,))):
-        args = lambda **k: (k.get("tokens", toks()), k.get("grad", rows()), 1.0, k.get("drop"), k.get("table", rows()), k.get("num_rows", 10), k.get("N", 16), *tail,  # noqa: E731
+        args = lambda **k: (k.get("tokens", toks(L=2000)), k.get("grad", rows()), 1.0, k.get("drop"), k.get("table", rows()), k.get("num_rows", 10), k.get("N", 16), *tail,  # noqa: E731
                             k.get("ws", 256), k.get("bytes", need), None)
         for code, k in [(-1, dict(tokens=None)), (-6, dict(tokens=toks(L=2**28))), (-1, dict(grad=None)), (-6, dict(grad=rows(type=E4M3))), (-3, dict(table=rows(ld=0))), (-1, dict(table=None)),
                         (-3, dict(num_rows=-1)), (-6, dict(N=2**20 + 1, table=rows(ld=2**21))), (-4, dict(ws=None)), (-4, dict(bytes=need - 1)), (-3, dict(ws=8)), (-1, dict(drop=drop(state=None)))]:
@@ -78,9 +79,10 @@ def test_norm_calls_check_their_arguments():
                     (-1, dict(drop=drop(state=None))), (-6, dict(N=16000, out=rows(ld=16000), rows=2**30))]:
         assert l.tt_add_rms_norm_fwd(*fwd(**k)) == code, k
     assert l.tt_add_rms_norm_fwd(*fwd(rows=0)) == 0
-    need = l.tt_add_rms_norm_bwd_workspace_bytes(5, 16)
+    assert l.tt_add_rms_norm_bwd_workspace_bytes(5, 16) == 0      # few rows need none
+    need = l.tt_add_rms_norm_bwd_workspace_bytes(5000, 16)
     bwd = lambda **k: (k.get("dy", rows()), k.get("h", rows()), k.get("rstd", 64), k.get("w"), k.get("wt", F32), k.get("ds"), k.get("drop"), k.get("dx", rows()), k.get("dr"),  # noqa: E731
-                       k.get("dw", 64), k.get("dwt", F32), 0, k.get("rows", 5), k.get("N", 16), k.get("ws", 256), k.get("bytes", need), None)
+                       k.get("dw", 64), k.get("dwt", F32), 0, k.get("rows", 5000), k.get("N", 16), k.get("ws", 256), k.get("bytes", need), None)
     for code, k in [(-1, dict(dy=None)), (-1, dict(h=None)), (-1, dict(rstd=None)), (-6, dict(h=rows(type=BF16))), (-6, dict(ds=rows(type=BF16))), (-6, dict(dr=rows(type=F16))), (-6, dict(dx=rows(type=F16))),
                     (-6, dict(dw=64, dwt=E4M3)), (-4, dict(ws=None)), (-4, dict(bytes=need - 4)), (-3, dict(ws=24)), (-3, dict(rstd=65)), (-6, dict(N=32769, dx=rows(ld=40000))), (-1, dict(drop=drop(state=None)))]:
         assert l.tt_add_rms_norm_bwd(*bwd(**k)) == code, k
@@ -93,9 +95,9 @@ def test_workspaces_are_enough_for_shorter_calls():
     lengths = [1, 2, 2047, 2048, 2049, 16_383, 16_384, 16_385, 65_536, 131_072, 131_073, 1_000_000, 2**28 - 1]
     for N in (1, 7, 64, 4096):
         sizes = [l.tt_token_bwd_workspace_bytes(L, 1000, N) for L in lengths]
-        assert sizes[0] > 0 and sizes == sorted(sizes), (N, sizes)
+        assert sizes[0] == 0 and sizes[-1] > 0 and sizes == sorted(sizes), (N, sizes)
         sizes = [l.tt_add_rms_norm_bwd_workspace_bytes(L, N) for L in lengths]
-        assert sizes[0] > 0 and sizes == sorted(sizes), (N, sizes)
+        assert sizes[0] == 0 and sizes[-1] > 0 and sizes == sorted(sizes), (N, sizes)
     assert l.tt_token_bwd_workspace_bytes(2**28, 10, 8) == 0 and l.tt_token_bwd_workspace_bytes(0, 10, 8) == 0 and l.tt_token_bwd_workspace_bytes(8, 10, 2**20 + 1) == 0
     assert l.tt_token_bwd_workspace_bytes(8, 2**31, 8) == 0 and l.tt_token_bwd_workspace_bytes(8, 0, 8) == 0
     assert l.tt_add_rms_norm_bwd_workspace_bytes(8, 32769) == 0
