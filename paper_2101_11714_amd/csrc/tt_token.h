@@ -4,8 +4,8 @@
 // Backward: G[v] = scale sum_{t: token_t = v} m_t . g[t], in 32 bits, in the order of t within a tile of sorted positions
 // and tile after tile, so that the result is the same in every run; nothing is added with atomics.
 // Both are bound by HBM where there is work; the gather reads whole rows, the gradient is one pass over g and one over the rows it
-// writes.  32,768 tokens of 4,096 columns in 16 bits: lookup with dropout 79 us (4.6 TB/s of distinct rows and output; without 76), gradient
-// of 131,072 rows in 32 bits 482 us (5.0 TB/s), of which sorting takes 25 and joining 13.
+// writes.  32,768 tokens of 4,096 columns in 16 bits: lookup with dropout 74 us (4.9 TB/s of distinct rows and output), gradient of
+// 131,072 rows in 32 bits 478 us (5.0 TB/s), of which sorting takes 25 and joining 13.
 #pragma once
 
 #include "tt_rows_io.h"
@@ -319,7 +319,6 @@ __global__ __launch_bounds__(TS_WG) void token_sort_one_kernel(const SortPass s,
 #pragma unroll
         for (int r = 0; r < R; ++r) digit[r] = (key[r] >> (pass * s.bits)) & ((1u << s.bits) - 1u);
         places<R>(digit, in, s.bits, true, 0u, 0u, cnt, start, wsum, place);
-        __syncthreads();                                     // (cnt and start have been read)
 #pragma unroll
         for (int r = 0; r < R; ++r) {
             if (!in[r]) continue;
