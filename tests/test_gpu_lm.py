@@ -512,7 +512,7 @@ def block_inputs(L, vocab, N):
             torch.tensor([99, 0], dtype=torch.int64, device="cuda:0")), ws
 
 
-@pytest.mark.parametrize("L,vocab,N", [(300, 100, 64), (17_000, 1000, 24)])
+@pytest.mark.parametrize("L,vocab,N", [(300, 100, 64), (3000, 500, 32), (17_000, 1000, 24)])
 def test_recorded_block_draws_anew_at_every_step(L, vocab, N):
     inputs, ws = block_inputs(L, vocab, N)
     state = inputs[-1]
