@@ -27,6 +27,12 @@ struct NormArgs {
     DropArgs drop;
 };
 
+// N for fetch8 and settle8.  Rows that take two vectors of one thread have more than 8 columns: said here, so that the code for
+// narrower ones is left out (with it odd widths spilled: gradients of 4,096 rows of 12,001 columns 356 -> 167 us, of 20,001
+// 2,280 -> 609; forward, of 16,383, 133 -> 117)
+template <int VPT>
+__device__ __forceinline__ int row_columns(int N) { return VPT > 1 ? max(N, 8) : N; }
+
 // the weights of a thread's vectors, of any type; ones where there are none
 template <bool WHOLE, int VPT, typename W>
 __device__ __forceinline__ void load_weights(const W *p, int g, int t, int nv, int N, float (&w)[VPT][8])
@@ -35,11 +41,11 @@ __device__ __forceinline__ void load_weights(const W *p, int g, int t, int nv, i
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         const int v = min(i * g + t, nv - 1);
-        x[i] = fetch8<WHOLE>(p + 8 * v, N - 8 * v, N);
+        x[i] = fetch8<WHOLE>(p + 8 * v, N - 8 * v, row_columns<VPT>(N));
     }
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        settle8<WHOLE>(x[i], N - 8 * min(i * g + t, nv - 1), N);
+        settle8<WHOLE>(x[i], N - 8 * min(i * g + t, nv - 1), row_columns<VPT>(N));
         widen8(x[i], w[i]);
     }
 }
@@ -120,22 +126,22 @@ __global__ __launch_bounds__(RN_THREADS) void norm_fwd_kernel(const NormArgs a, 
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
-            x[i] = fetch8<WHOLE>((const T *)a.x + row_at(row, a.ld_x) + 8 * v, n, a.N);
-            if constexpr (RESIDUAL) res[i] = fetch8<WHOLE>((const H *)a.residual + row_at(row, a.ld_res) + 8 * v, n, a.N);
+            x[i] = fetch8<WHOLE>((const T *)a.x + row_at(row, a.ld_x) + 8 * v, n, row_columns<VPT>(a.N));
+            if constexpr (RESIDUAL) res[i] = fetch8<WHOLE>((const H *)a.residual + row_at(row, a.ld_res) + 8 * v, n, row_columns<VPT>(a.N));
         }
         const DropKey key = drop_key(a.drop);
         weights<WHOLE>(a.weight, a.weight_type, g, t, a.nv, a.N, w);
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             const int v = min(i * g + t, a.nv - 1);
-            settle8<WHOLE>(x[i], a.N - 8 * v, a.N);
+            settle8<WHOLE>(x[i], a.N - 8 * v, row_columns<VPT>(a.N));
             widen8(x[i], h[i]);
 #pragma unroll
             for (int j = 0; j < 8; ++j) h[i][j] *= a.drop.factor;
             if (a.drop.state) drop8(a.drop, key, (uint64_t)row_at(row, a.nv) + (uint64_t)v, h[i]);
             if constexpr (RESIDUAL) {
                 float r[8];
-                settle8<WHOLE>(res[i], a.N - 8 * v, a.N);
+                settle8<WHOLE>(res[i], a.N - 8 * v, row_columns<VPT>(a.N));
                 widen8(res[i], r);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) h[i][j] += r[j];
@@ -243,12 +249,12 @@ __global__ __launch_bounds__(RN_BWD_THREADS) void norm_bwd_kernel(const NormGrad
     };
     auto load = [&](Row &x, int64_t row, int i) {
         const int v = min(i * g + t, a.nv - 1), n = a.N - 8 * v;
-        x.dy[i] = fetch8<WHOLE>((const T *)a.dy + row_at(row, a.ld_dy) + 8 * v, n, a.N);
-        x.h[i] = fetch8<WHOLE>((const H *)a.h + row_at(row, a.ld_h) + 8 * v, n, a.N);
+        x.dy[i] = fetch8<WHOLE>((const T *)a.dy + row_at(row, a.ld_dy) + 8 * v, n, row_columns<VPT>(a.N));
+        x.h[i] = fetch8<WHOLE>((const H *)a.h + row_at(row, a.ld_h) + 8 * v, n, row_columns<VPT>(a.N));
     };
     auto load_sum = [&](Row &x, int64_t row, int i) {
         const int v = min(i * g + t, a.nv - 1);
-        if constexpr (DSUM) x.ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, a.N - 8 * v, a.N);
+        if constexpr (DSUM) x.ds[i] = fetch8<WHOLE>((const H *)a.dsum + row_at(row, a.ld_dsum) + 8 * v, a.N - 8 * v, row_columns<VPT>(a.N));
     };
     auto load_row = [&](Row &x, int64_t r) {
         const int64_t row = r < a.rows ? r : a.rows - 1;
@@ -278,8 +284,8 @@ __global__ __launch_bounds__(RN_BWD_THREADS) void norm_bwd_kernel(const NormGrad
         const float rstd = x.rstd;
         auto settle = [&](int i) {
             const int n = a.N - 8 * min(i * g + t, a.nv - 1);
-            settle8<WHOLE>(x.dy[i], n, a.N);
-            settle8<WHOLE>(x.h[i], n, a.N);
+            settle8<WHOLE>(x.dy[i], n, row_columns<VPT>(a.N));
+            settle8<WHOLE>(x.h[i], n, row_columns<VPT>(a.N));
         };
         float dot = 0.f;
 #pragma unroll
@@ -314,7 +320,7 @@ __global__ __launch_bounds__(RN_BWD_THREADS) void norm_bwd_kernel(const NormGrad
             for (int j = 0; j < 8; ++j) d[j] = p[j] * w[i][j] * rstd - q[j] * c;
             if constexpr (DSUM) {
                 float s[8];
-                settle8<WHOLE>(x.ds[i], a.N - 8 * min(v, a.nv - 1), a.N);
+                settle8<WHOLE>(x.ds[i], a.N - 8 * min(v, a.nv - 1), row_columns<VPT>(a.N));
                 widen8(x.ds[i], s);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[j] += s[j];
