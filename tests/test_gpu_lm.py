@@ -267,7 +267,7 @@ def test_dropped_values_are_zero_whatever_they_were():
 # ---- norm -----------------------------------------------------------------------------------------------------------------
 
 NORMS = [(1, 1), (2, 3), (1, 8), (5, 9), (70, 16), (3, 100), (1000, 64), (129, 128), (33, 136), (700, 513), (7, 1024), (600, 1000), (40, 2047), (520, 4096),
-         (3, 8192), (600, 8192), (2, 16384), (530, 16400), (5, 20001), (2, 32768)]
+         (3, 8192), (600, 8192), (2, 16384), (530, 16400), (5, 20001), (2, 32768), (530, 12001), (300, 16393)]
 # additions in a row: 32 values a thread, 6 + 16 across its threads; the mean's and root's own roundings; half of it reaches rstd
 ROW = 64
 
