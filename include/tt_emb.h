@@ -675,9 +675,9 @@ int tt_dropout_bwd(const tt_rows_t *grad_output, const tt_dropout_t *dropout, co
  * h = residual + dropout(x);  rstd = 1 / sqrt(mean of h^2 over the row + eps);  y = h * rstd * weight.
  * residual, dropout, weight: NULL for none.  sum: h, stored (NULL: not).  rstd: fp32 [n_rows] or NULL; it and y come from the
  * unrounded h.  Types: x any of 32 or 16 bits; residual and sum x's or 32 bits; weight any, N values; output x's, or TT_E4M3.
- * TT_E4M3: output = y / s rounded to the nearest even, s = max |y| / 448 over the row (group == 0) or over each group of
- * 32, 64 or 128 columns; scales: fp32 rows of 1 or ceil(N / group) values.  A scale below 2^-126 is stored as 0, with values 0.
- * NaN in y makes its scale and all values under that scale NaN.  scales == NULL and group == 0 for other types.
+ * TT_E4M3: output = y / s rounded to the nearest even, s = max |y| / 448 (both quotients as 32-bit division gives them) over the row
+ * (group == 0) or over each group of 32, 64 or 128 columns; scales: fp32 rows of 1 or ceil(N / group) values.  A scale below
+ * 2^-126 is stored as 0, with values 0.  NaN in y makes its scale and all values under that scale NaN.  scales == NULL and group == 0 for other types.
  * output may be x, and sum may be residual.
  */
 int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_dropout_t *dropout, const void *weight, int32_t weight_type,

@@ -1,0 +1,72 @@
+"""Edges of the operators at a language model's way in: exact quotients and ties in 8 bits, values that are not finite, arrays at the
+limits of a launch, and each rule's branches on both of its sides.  Plain implementations and bounds as in test_gpu_lm.py."""
+
+import numpy as np
+import pytest
+import torch
+
+import lm_util as R
+from lm_util import U32
+from paper_2101_11714_amd import binding as B
+from test_gpu_lm import BF16, E4M3, F16, F32, assert_guard, dropout_of, gen, room, tokens_of
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- 8 bits -------------------------------------------------------------------------------------------------------------
+
+
+def in_8_bits(y, group):
+    """(values, scales) of rows y of 32 bits: scales max |y| / 448, values y / scale to the nearest even e4m3, both quotients rounded
+    to 32 bits, on the host."""
+    y = y.cpu()
+    rows, N = y.shape
+    width = group or N
+    parts = [y[:, c:c + width] for c in range(0, N, width)]
+    scales = torch.stack([p.abs().amax(1) / torch.tensor(448.0) for p in parts], 1)
+    q = torch.cat([(p / s[:, None]).to(E4M3) for p, s in zip(parts, scales.unbind(1))], 1)
+    return q, scales
+
+
+def assert_same_8_bits(x, w, group, eps):
+    rows, N = x.shape
+    y = torch.empty_like(x)
+    q, scales = torch.empty_like(x, dtype=E4M3), torch.empty((rows, -(-N // group) if group else 1), device="cuda:0")
+    B.tt_add_rms_norm_fwd(x, w, y, eps=eps)
+    B.tt_add_rms_norm_fwd(x, w, q, scales=scales, group=group, eps=eps)
+    want_q, want_s = in_8_bits(y, group)
+    assert np.array_equal(scales.cpu().numpy(), want_s.numpy(), equal_nan=True)
+    q, number = q.cpu(), ~torch.isnan(want_q.float())
+    assert torch.equal(~torch.isnan(q.float()), number)
+    assert torch.equal(q.view(torch.uint8)[number], want_q.view(torch.uint8)[number])     # (zeros with their signs)
+
+
+@pytest.mark.parametrize("group", [0, 32, 128])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -60, 2.0 ** -75])
+def test_ties_in_8_bits_go_to_the_even_value(group, size):
+    # With eps = 2^100 the mean square vanishes: y = 2^-50 x exactly.  Row c holds (times `size`) whole multiples of c, 448 c the largest in each group:
+    # its scale is 2^-50 c and its quotients are the multiples, among them every value of e4m3 and every midpoint of two neighbours.
+    vals = torch.arange(0, 127, dtype=torch.uint8).view(E4M3).float()
+    points = torch.cat([vals, (vals[1:] + vals[:-1]) / 2])
+    points = torch.cat([points, -points, torch.zeros(-2 * points.numel() % 31)]).view(-1, 31)
+    row = torch.cat([torch.full((points.shape[0], 1), 448.0), points], 1).reshape(-1)      # (448 leads every 32 columns)
+    c = torch.arange(1, 4097, 2).float()
+    x = (c[:, None] * row * size).to("cuda:0")
+    assert_same_8_bits(x, None, group, 2.0 ** 100)
+
+
+@pytest.mark.parametrize("rows,N", [(300, 512), (37, 1001), (5, 8192), (1000, 40)])
+@pytest.mark.parametrize("group", [0, 64])
+def test_quotients_in_8_bits_are_rounded_once(rows, N, group):
+    g = gen(rows + N)
+    assert_same_8_bits(R.rows_of(g, rows, N, F32), torch.randn(N, generator=g).to("cuda:0"), group, 1e-6)
+
+
+def test_quotients_in_8_bits_by_scales_that_are_not_finite():
+    # y is infinite in a column of rows 0 and 1, NaN in all of row 2
+    x = torch.randn((4, 128), generator=gen(3)).to("cuda:0")
+    w = torch.ones(128, device="cuda:0")
+    w[5], x[:, 5] = 3e38, 1e3
+    x[0, 5], x[1, 5], x[2, 9] = 2.0 ** 60, -2.0 ** 60, float("nan")
+    for group in (0, 32):
+        assert_same_8_bits(x, w, group, 2.0 ** 100)
