@@ -604,8 +604,8 @@ int tt_emb_debug_set_fast_path(int mode);
  * They work on arrays of rows in 32- and 16-bit types.  Every sum, mean square and gradient is held in 32 bits; a value is
  * rounded once, when it is stored.  Arrays need no more alignment than their elements; rows may be parts of wider ones (odd
  * strides included), and an array that is only read may repeat one row (ld = 0).  Unless a comment says otherwise no output
- * overlaps another array.  Sizes: less than 2^31 rows, up to 2^20 columns (32,768 in the norms), row strides up to 2^31 elements;
- * element offsets have 64 bits.
+ * overlaps another array.  Sizes: less than 2^31 rows, up to 2^20 columns (32,768 in the norms), less than 2^40 elements (rows times
+ * columns), row strides up to 2^31 elements; element offsets have 64 bits.
  * The results are bit-identical from run to run.  n_rows == 0 or L == 0 is valid.
  */
 enum {

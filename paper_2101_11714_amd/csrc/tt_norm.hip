@@ -138,8 +138,7 @@ int tt_add_rms_norm_fwd(const tt_rows_t *x, const tt_rows_t *residual, const tt_
     a.eps = eps;
     const NormShape s = norm_fwd_shape(n_rows, a.nv, group ? lg_ceil(group / 8) : 0);
     const int threads = s.lg > 8 ? 1 << s.lg : WG;
-    if ((rc = check_grid(ceil_div(n_rows, threads >> s.lg), threads))) return rc;
-    const dim3 grid((unsigned)ceil_div(n_rows, threads >> s.lg));
+    const dim3 grid = grid_of(ceil_div(n_rows, threads >> s.lg), threads);
     with_types(x->type, stream_type, [&](auto t, auto h) {
         with_vpt(s.vpt, [&](auto vpt) {
             with_whole(N, [&](auto whole) {

@@ -137,7 +137,7 @@ __global__ __launch_bounds__(RN_THREADS) void norm_fwd_kernel(const NormArgs a, 
     __shared__ float sums[RN_WAVES];
     __shared__ uint32_t mosts[RN_WAVES];
     const int g = 1 << lg, t = threadIdx.x & (g - 1);
-    const int64_t row_ = (int64_t)blockIdx.x * (blockDim.x >> lg) + (threadIdx.x >> lg);
+    const int64_t row_ = workgroup() * (blockDim.x >> lg) + (threadIdx.x >> lg);
     const bool in = row_ < a.rows;
     const int64_t row = in ? row_ : a.rows - 1;
     float h[VPT][8], w[VPT][8];

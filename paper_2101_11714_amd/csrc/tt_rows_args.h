@@ -8,7 +8,8 @@
 
 namespace tt {
 
-constexpr int64_t MOST_ROWS = 1ll << 31;                     // rows and columns stay below (elements may be 2^62)
+constexpr int64_t MOST_ROWS = 1ll << 31;                     // rows and columns stay below
+constexpr int64_t MOST_ELEMENTS = 1ll << 40;                 // so do rows times columns: what every launch here takes, and no card holds
 
 inline int element_bytes(int32_t type) { return type == TT_F32 ? 4 : type == TT_E4M3 ? 1 : 2; }
 
@@ -65,6 +66,7 @@ inline int check_sizes(int64_t rows, int64_t N)
 {
     if (rows < 0 || N < 0) return fail(TT_ERR_BAD_ARG, "negative size");
     if (rows >= MOST_ROWS || N >= MOST_ROWS) return fail(TT_ERR_UNSUPPORTED, "2^31 rows or columns, or more");
+    if (rows * N >= MOST_ELEMENTS) return fail(TT_ERR_UNSUPPORTED, "2^40 elements or more");
     return TT_OK;
 }
 
@@ -87,10 +89,12 @@ inline int launched(const char *what)
     return e == hipSuccess ? TT_OK : hip_fail(e, what);
 }
 
-// what a launch takes: less than 2^32 threads along x
-inline int check_grid(int64_t workgroups, int threads)
+// A grid for kernels that take their number from workgroup().  A launch takes less than 2^32 threads along x; where there are more, y goes on
+// (with MOST_ELEMENTS to about 2^10), and the last row's surplus workgroups find nothing to do.
+inline dim3 grid_of(int64_t workgroups, int threads)
 {
-    return workgroups * threads < (1ll << 32) ? TT_OK : fail(TT_ERR_UNSUPPORTED, "more rows than one launch takes");
+    if (workgroups * threads < (1ll << 32)) return dim3((unsigned)workgroups);
+    return dim3(1u << GRID_LG, (unsigned)ceil_div(workgroups, 1ll << GRID_LG));
 }
 
 }  // namespace tt

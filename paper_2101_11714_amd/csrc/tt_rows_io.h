@@ -116,6 +116,10 @@ __device__ __forceinline__ void widen8(const Vec8<T> &r, float (&x)[8])
 // element offset of row r; a row's number and a row stride have 31 bits each
 __device__ __forceinline__ int64_t row_at(int64_t r, int64_t ld) { return (int64_t)((uint64_t)(uint32_t)r * (uint64_t)(uint32_t)ld); }
 
+// the number of a workgroup in a grid that may go on along y, which then has 1 << GRID_LG of them along x
+constexpr int GRID_LG = 21;
+__device__ __forceinline__ int64_t workgroup() { return ((int64_t)blockIdx.y << GRID_LG) + blockIdx.x; }
+
 // ---- sums over lanes ----------------------------------------------------------------------------------------------
 
 template <int CTRL>

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
     int v[U], n[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const double i = (double)blockIdx.x * (double)(U * WG) + (double)(u * WG + (int)threadIdx.x);
+        const double i = (double)workgroup() * (double)(U * WG) + (double)(u * WG + (int)threadIdx.x);
         const double r = floor(fma(i, a.inv_nv, a.half_nv));
         row[u] = (int64_t)(uint32_t)r;                       // (behind the last row: cut off where it is looked at)
         v[u] = (int)fma(-r, a.nv_d, i);

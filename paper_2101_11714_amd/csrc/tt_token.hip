@@ -23,18 +23,15 @@ int check_tokens(const tt_tokens_t *t, int64_t *L)
 }
 
 template <typename S, typename D, int U, bool TOKENS, bool RESIDUAL>
-int launch_rows(RowsArgs &a, hipStream_t st)
+void launch_rows(RowsArgs &a, hipStream_t st)
 {
-    const int64_t blocks = ceil_div(a.rows * a.nv, WG * U);
-    const int rc = check_grid(blocks, WG);
-    if (rc) return rc;
+    const dim3 grid = grid_of(ceil_div(a.rows * a.nv, WG * U), WG);
     a.nv_d = (double)a.nv;
     a.inv_nv = 1.0 / a.nv_d;
     a.half_nv = 0.5 * a.inv_nv;
     with_whole(a.N, [&](auto whole) {
-        hipLaunchKernelGGL((rows_kernel<S, D, U, decltype(whole)::value, TOKENS, RESIDUAL>), dim3((unsigned)blocks), dim3(WG), 0, st, a);
+        hipLaunchKernelGGL((rows_kernel<S, D, U, decltype(whole)::value, TOKENS, RESIDUAL>), grid, dim3(WG), 0, st, a);
     });
-    return TT_OK;
 }
 
 constexpr int64_t MOST_COLUMNS = 1 << 20;                    // of the kernels whose second grid dimension runs over the columns
@@ -48,7 +45,9 @@ int check_columns(int64_t N)
 
 constexpr int64_t MOST_GRAD_TOKENS = 1ll << 28;              // (a workgroup per tile of sorted positions)
 
-constexpr int64_t MOST_CLEAR = 1 << 23;                      // workgroups (they take turns beyond that)
+// Workgroups that clear (they take turns beyond that).  With less than MOST_ELEMENTS there are less than 2^32 parts to be cleared, and less
+// than 2^23 + 2^21 workgroups that add, so that all of them fit a launch along x.
+constexpr int64_t MOST_CLEAR = 1 << 22;
 
 struct GradWs {
     uint32_t *k[2], *v[2], *hist, *total;
@@ -171,7 +170,7 @@ int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropou
     int rc = check_tokens(tokens, &L);
     if (rc) return rc;
     if (L >= MOST_GRAD_TOKENS) return fail(TT_ERR_UNSUPPORTED, "2^28 tokens or more");
-    if ((rc = check_sizes(num_rows, N)) || (rc = check_columns(N))) return rc;
+    if ((rc = check_sizes(num_rows, N)) || (rc = check_sizes(L, N)) || (rc = check_columns(N))) return rc;
     if ((rc = check_rows(table, name, num_rows, N, OUT)) || (rc = check_rows(grad, "grad_output", L, N, IN))) return rc;
     if ((rc = check_dropout(dropout, &a.drop))) return rc;
     if (N == 0 || num_rows == 0 || (old && L == 0)) return TT_OK;
@@ -206,12 +205,10 @@ int token_grad(const tt_tokens_t *tokens, const tt_rows_t *grad, const tt_dropou
         k.named = w.named;
         k.lg = lg_ceil(pieces < WG ? pieces : WG);
         const int64_t along = ceil_div(pieces, 1 << k.lg), parts = ceil_div(num_rows, WG >> k.lg) * along;
-        if (parts >= (1ll << 32)) return fail(TT_ERR_UNSUPPORTED, "a table of more than 2^45 bytes");
         k.chunks = (uint32_t)along;
         k.parts = (uint32_t)parts;
         clear_blocks = ceil_div(parts, TZ_SWEEPS) < MOST_CLEAR ? ceil_div(parts, TZ_SWEEPS) : MOST_CLEAR;
     }
-    if ((rc = check_grid(sum_blocks + clear_blocks, WG))) return rc;
     if (!few) {
         const hipError_t e = sort_tokens(tokens, num_rows, w, !old, st, &a.ks, &a.vs);
         if (e != hipSuccess) return hip_fail(e, "token sort");
@@ -246,7 +243,7 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     RowsArgs a{};
     int rc = check_tokens(tokens, &L);
     if (rc) return rc;
-    if ((rc = check_sizes(num_rows, N)) || (rc = check_columns(N))) return rc;
+    if ((rc = check_sizes(num_rows, N)) || (rc = check_sizes(L, N)) || (rc = check_columns(N))) return rc;
     if ((rc = check_rows(table, "table", num_rows, N, IN)) || (rc = check_rows(output, "output", L, N, OUT))) return rc;
     if ((rc = check_dropout(dropout, &a.drop))) return rc;
     if (L == 0 || N == 0) return TT_OK;
@@ -273,11 +270,10 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
         with_type(output->type, [&](auto d) {
             // few tokens: one vector per thread, so that more of the device has some; else two (32,768 tokens of 4,096 columns in 16 bits
             // under dropout, 1 / 2 / 4 vectors: 97 / 75 / 77 us)
-            if (L * a.nv < (1 << 20)) rc = launch_rows<decltype(s), decltype(d), 1, true, false>(a, (hipStream_t)stream);
-            else rc = launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
+            if (L * a.nv < (1 << 20)) launch_rows<decltype(s), decltype(d), 1, true, false>(a, (hipStream_t)stream);
+            else launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
         });
     });
-    if (rc) return rc;
     return launched("token lookup launch");
 }
 
@@ -324,10 +320,9 @@ static int dropout_rows(const tt_rows_t *x, const tt_rows_t *residual, const tt_
     a.nv = (int)ceil_div(N, 8);
     a.scale = a.drop.factor;
     with_type(x->type, [&](auto s) {
-        if (residual) rc = launch_rows<decltype(s), decltype(s), 1, false, true>(a, (hipStream_t)stream);
-        else rc = launch_rows<decltype(s), decltype(s), 1, false, false>(a, (hipStream_t)stream);
+        if (residual) launch_rows<decltype(s), decltype(s), 1, false, true>(a, (hipStream_t)stream);
+        else launch_rows<decltype(s), decltype(s), 1, false, false>(a, (hipStream_t)stream);
     });
-    if (rc) return rc;
     return launched("dropout launch");
 }
 

@@ -70,3 +70,67 @@ def test_quotients_in_8_bits_by_scales_that_are_not_finite():
     x[0, 5], x[1, 5], x[2, 9] = 2.0 ** 60, -2.0 ** 60, float("nan")
     for group in (0, 32):
         assert_same_8_bits(x, w, group, 2.0 ** 100)
+
+
+# ---- more rows than a launch takes along one dimension --------------------------------------------------------------------
+
+
+def need(gib):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gib << 30:
+        pytest.skip("%d GiB of free memory are needed" % gib)
+
+
+def pieces(rows, n=1 << 26):
+    return [slice(r, min(r + n, rows)) for r in range(0, rows, n)]
+
+
+def test_dropout_of_2_to_the_32_vectors():
+    # rows of three vectors of eight columns, in place; ones become 0 or 2
+    need(60)
+    rows, N = (1 << 32) // 3 + 1000, 17
+    x = torch.ones((rows, N), dtype=BF16, device="cuda:0")
+    d = dropout_of(0.5)
+    B.tt_dropout_fwd(x, x, d)
+    kept = 0
+    for p in pieces(rows):
+        zero, two = x[p] == 0, x[p] == 2
+        assert bool((zero ^ two).all())
+        kept += int(two.sum())
+    assert abs(kept / (rows * N) - 0.5) < 6 * 0.5 / (rows * N) ** 0.5
+    seed, step = (int(v) for v in d.state.cpu())
+    for first in (0, (1 << 30) + 5, (1 << 32) // 3 - 50, rows - 100):   # (every vector is a block of the generator)
+        words = R.philox_blocks(3 * first, 300, d.site, step, seed)
+        draws = np.stack([words & 0xFFFF, words >> 16], 2).reshape(100, 24)[:, :N]
+        assert np.array_equal(x[first:first + 100].float().cpu().numpy(), 2.0 * (draws >= 32768))
+
+
+def test_lookup_of_2_to_the_33_vectors():
+    need(140)
+    rows, N, vocab = (1 << 33) // 5 + 1000, 33, 1021
+    tokens = (torch.arange(rows, dtype=torch.int32, device="cuda:0") % 1024).sub_(2)         # (-1, 1021 and their like are none)
+    table = R.rows_of(gen(5), vocab, N, BF16)
+    out = torch.empty((rows, N), dtype=BF16, device="cuda:0")
+    B.tt_token_fwd(table, tokens, out)
+    padded = torch.cat([torch.zeros((2, N), dtype=BF16, device="cuda:0"), table, torch.zeros((1, N), dtype=BF16, device="cuda:0")])
+    whole = padded.repeat(1 << 14, 1)
+    for p in pieces(rows, whole.shape[0]):
+        assert torch.equal(out[p], whole[:out[p].shape[0]])
+
+
+@pytest.mark.parametrize("bits8", [False, True])
+def test_norm_of_2_to_the_32_threads(bits8):
+    # four threads a row; all rows are one and the same
+    need(70)
+    rows, N = (1 << 30) + 1000, 17
+    row, w = R.rows_of(gen(6), 1, N, BF16), torch.randn(N, generator=gen(7)).to("cuda:0")
+    first = torch.empty((1, N), dtype=E4M3 if bits8 else BF16, device="cuda:0")
+    one = torch.empty((1, 1), device="cuda:0") if bits8 else None
+    B.tt_add_rms_norm_fwd(row, w, first, scales=one)
+    out = torch.zeros((rows, N), dtype=first.dtype, device="cuda:0")
+    scales = torch.zeros((rows, 1), device="cuda:0") if bits8 else None
+    B.tt_add_rms_norm_fwd(row.expand(rows, N), w, out, scales=scales)
+    as_bits = torch.uint8 if bits8 else torch.int16
+    for p in pieces(rows):
+        assert bool((out[p].view(as_bits) == first.view(as_bits)).all())
+        assert scales is None or bool((scales[p] == one).all())
