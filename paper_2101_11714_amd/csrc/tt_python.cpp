@@ -783,7 +783,7 @@ TT_FUNCTION(add_rms_norm_fwd)
     const tt_rows_t *scales = g.rows_or_null(6, &sc, n, group > 0 ? (N + group - 1) / group : 1);
     const float eps = g.real(8);
     const tt_dropout_t *drop = g.dropout(9, &d);
-    if (g.ok && rstd && nr != n) g.fail("rstd has another size");
+    if (g.ok && args[5] != Py_None && nr != n) g.fail("rstd has another size");
     if (g.ok && (group < 0 || group > 128)) g.fail("group is 0, 32, 64 or 128");
     if (!g.ok) return nullptr;
     return call([&](void *st) { return tt_add_rms_norm_fwd(&x, r, drop, w, wt, eps, s, o, rstd, scales, (int32_t)group, n, N, st); });

@@ -134,3 +134,13 @@ def test_norm_of_2_to_the_32_threads(bits8):
     for p in pieces(rows):
         assert bool((out[p].view(as_bits) == first.view(as_bits)).all())
         assert scales is None or bool((scales[p] == one).all())
+
+
+# ---- refusals and values that are not finite -------------------------------------------------------------------------------
+
+
+def test_norm_refuses_an_empty_array_for_its_roots():
+    x = torch.ones((5, 16), device="cuda:0")
+    with pytest.raises(AssertionError):
+        B.tt_add_rms_norm_fwd(x, None, torch.empty_like(x), rstd=torch.empty(0, device="cuda:0"))
+    B.tt_add_rms_norm_fwd(x[:0], None, x[:0].clone(), rstd=torch.empty(0, device="cuda:0"))
