@@ -78,11 +78,12 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
     for (int u = 0; u < U; ++u) {
         if (row[u] >= a.rows) break;
         if constexpr (TOKENS) keep8(there[u], x[u]);
+        const float scale = !TOKENS || there[u] ? a.scale : 0.f;     // (zeros by any scale)
         float y[8];
         settle8<WHOLE>(x[u], n[u], a.N);
         widen8(x[u], y);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) y[j] *= a.scale;
+        for (int j = 0; j < 8; ++j) y[j] *= scale;
         if (a.drop.state) drop8(a.drop, words[u], y);
         if constexpr (RESIDUAL) {
             float z[8];

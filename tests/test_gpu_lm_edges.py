@@ -144,3 +144,16 @@ def test_norm_refuses_an_empty_array_for_its_roots():
     with pytest.raises(AssertionError):
         B.tt_add_rms_norm_fwd(x, None, torch.empty_like(x), rstd=torch.empty(0, device="cuda:0"))
     B.tt_add_rms_norm_fwd(x[:0], None, x[:0].clone(), rstd=torch.empty(0, device="cuda:0"))
+
+
+@pytest.mark.parametrize("L", [6, 140_000])
+@pytest.mark.parametrize("scale", [float("inf"), float("nan"), -float("inf")])
+def test_rows_of_no_token_are_zero_under_any_scale(L, scale):
+    table = torch.ones((9, 64), device="cuda:0")
+    tokens = tokens_of(gen(8), L, 9, "some")
+    none = (tokens < 0) | (tokens >= 9)
+    for t in (table, table[:0]):
+        out = torch.full((L, 64), 7.0, device="cuda:0")
+        B.tt_token_fwd(t, tokens, out, scale=scale)
+        zero = none if t.shape[0] else torch.ones_like(none)
+        assert bool((out[zero] == 0).all()) and not torch.isfinite(out[~zero]).any()
