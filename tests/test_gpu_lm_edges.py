@@ -8,7 +8,7 @@ import torch
 import lm_util as R
 from lm_util import U32
 from paper_2101_11714_amd import binding as B
-from test_gpu_lm import BF16, E4M3, F16, F32, assert_guard, dropout_of, gen, room, tokens_of
+from test_gpu_lm import BF16, E4M3, F16, F32, assert_guard, check_grad, dropout_of, gen, room, tokens_of
 
 pytestmark = pytest.mark.gpu
 
@@ -157,3 +157,87 @@ def test_rows_of_no_token_are_zero_under_any_scale(L, scale):
         B.tt_token_fwd(t, tokens, out, scale=scale)
         zero = none if t.shape[0] else torch.ones_like(none)
         assert bool((out[zero] == 0).all()) and not torch.isfinite(out[~zero]).any()
+
+
+# ---- both sides of each rule ---------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("L", [1025, 3000, 8192, 8193])
+@pytest.mark.parametrize("vocab", [1 << 18, (1 << 18) + 1, (1 << 18) + 77, (1 << 20) + 5])
+def test_token_bwd_of_rows_whose_marks_another_kernel_clears(L, vocab):
+    # the sort of one workgroup (up to 8,192 tokens) clears the bytes of 2^18 rows itself, that of several 2^20
+    N, g = 3, gen(L + vocab)
+    tokens, grad = tokens_of(g, L, vocab, "some"), R.rows_of(g, L, N, F32)
+    tokens[:3] = torch.tensor([0, vocab - 1, vocab - 17])
+    dirty = torch.full((B.token_bwd_workspace_bytes(L, vocab, N),), 255, dtype=torch.uint8, device="cuda:0")
+    out, flat = room(vocab, N, F32, 1, 0)
+    B.tt_token_bwd(tokens, grad, out, workspace=dirty)
+    want, mag, most = R.token_bwd(tokens, grad, vocab, 1.0, None)
+    R.assert_within(out, want, (most + 4) * U32 * mag)
+    assert_guard(out, flat)
+
+
+@pytest.mark.parametrize("L", [5, 60])
+@pytest.mark.parametrize("N", [2048, 2056, 4100, 8200])
+@pytest.mark.parametrize("kind", ["some", "one", "none"])
+def test_token_bwd_without_a_sort_into_rows_of_several_pieces(L, N, kind):
+    check_grad(L, 300, N, kind, F32, F32, torch.int64, 0.2, 1, 1, "write")
+    check_grad(L, 300, N, kind, BF16, F16, torch.int32, None, 0, 0, "write")
+
+
+@pytest.mark.parametrize("L,N,s,o", [(9_000, 1001, F16, BF16), (9_001, 1001, BF16, F32), (35_000, 1024, F32, BF16), (70_001, 1001, BF16, F32), (66_000, 1024, F16, F32),
+                                     (140_000, 1003, F32, F16), (132_000, 1024, BF16, BF16)])
+def test_large_lookups(L, N, s, o):
+    # two vectors a thread, and outputs on either side of 256 MiB, against lookups of few rows and dropout on its own
+    g = gen(L + N)
+    table, tokens = R.rows_of(g, 500, N, s, 3, 1), tokens_of(g, L, 500, "some")
+    out, flat = room(L, N, o, 3, 1)
+    B.tt_token_fwd(table, tokens, out, scale=1.5)
+    assert_guard(out, flat)
+    wide = torch.empty((L, N), device="cuda:0")
+    for p in pieces(L, 1000):
+        few = torch.empty((out[p].shape[0], N), dtype=o, device="cuda:0")
+        assert torch.equal(B.tt_token_fwd(table, tokens[p], few, scale=1.5), out[p])
+        B.tt_token_fwd(table, tokens[p], wide[p])
+    d = dropout_of(0.25)
+    B.tt_token_fwd(table, tokens, out, dropout=d)
+    assert torch.equal(out, B.tt_dropout_fwd(wide, wide, d).to(o))
+    assert_guard(out, flat)
+
+
+@pytest.mark.parametrize("N", [777, 12001, 16400, 20001, 32768])
+@pytest.mark.parametrize("T,H", [(BF16, BF16), (F16, F32), (F32, F32)])
+def test_norm_gradients_in_place(N, T, H):
+    g, rows = gen(N), 530
+    dy, h, ds = R.rows_of(g, rows, N, T, 1, 1), R.rows_of(g, rows, N, H, 0, 0, 2.0), R.rows_of(g, rows, N, H, 3, 0)
+    rstd, w, d = (h.double().square().mean(1) + 1e-6).rsqrt().float(), torch.randn(N, generator=g).to("cuda:0"), dropout_of(0.4)
+    gx, gr, gw, same = torch.empty_like(dy), torch.empty_like(ds), torch.empty(N, device="cuda:0"), torch.empty(N, device="cuda:0")
+    B.tt_add_rms_norm_bwd(dy, h, rstd, w, gx, gw, grad_sum=ds, grad_residual=gr, dropout=d)
+    B.tt_add_rms_norm_bwd(dy, h, rstd, w, dy, same, grad_sum=ds, grad_residual=ds, dropout=d)
+    assert torch.equal(dy, gx) and torch.equal(ds, gr) and torch.equal(same, gw)
+
+
+@pytest.mark.parametrize("N", [777, 12001, 16400, 20001, 32768])
+def test_norms_in_place(N):
+    g, rows = gen(N), 530
+    x, r, w = R.rows_of(g, rows, N, F16, 1, 1), R.rows_of(g, rows, N, F32, 3, 0), torch.randn(N, generator=g).to("cuda:0")
+    out, hs = torch.empty_like(x), torch.empty_like(r)
+    B.tt_add_rms_norm_fwd(x, w, out, residual=r, sum_out=hs)
+    B.tt_add_rms_norm_fwd(x, w, x, residual=r, sum_out=r)
+    assert torch.equal(x, out) and torch.equal(r, hs)
+
+
+@pytest.mark.parametrize("E,N", [(16, 39_000), (32, 22_000), (64, 10_800)])
+def test_token_bwd_of_runs_from_every_place_of_a_tile(E, N):
+    # one run after the other of a length that is prime to E: their starts pass through every place of a tile of E sorted positions
+    lengths = [E + 1] * E + [2 * E + 1] * E + [3] * E + [1] * E
+    vocab, L = len(lengths), sum(lengths)
+    vectors = L * -(-N // 8)
+    assert {16: 1 << 22, 32: 1 << 23, 64: 1 << 24}[E] <= vectors < {16: 1 << 23, 32: 1 << 24, 64: 1 << 60}[E]     # (what the rule takes tiles of E for)
+    tokens = torch.repeat_interleave(torch.arange(vocab), torch.tensor(lengths))[torch.randperm(L, generator=gen(E))].to("cuda:0")
+    grad = torch.randn((L, N), generator=torch.Generator(device="cuda:0").manual_seed(3), device="cuda:0")
+    out = torch.empty((vocab, N), device="cuda:0")
+    B.tt_token_bwd(tokens, grad, out)
+    zeros = lambda: torch.zeros((vocab, N), dtype=torch.float64, device="cuda:0")  # noqa: E731
+    want, mag = zeros().index_add_(0, tokens, grad.double()), zeros().index_add_(0, tokens, grad.abs().double())
+    assert bool(((out.double() - want).abs() <= (max(lengths) + 6) * U32 * mag).all())
