@@ -79,14 +79,13 @@ __device__ __forceinline__ Vec8<T> narrow8(const float (&x)[8])
     return r;
 }
 
-// one rounding, to the nearest even.  past: past the caches (the same for all threads)
+// one rounding, to the nearest even
 template <bool WHOLE = false, typename T>
-__device__ __forceinline__ void put8(T *p, int n, const float (&x)[8], bool past = false)
+__device__ __forceinline__ void put8(T *p, int n, const float (&x)[8])
 {
     const Vec8<T> r = narrow8<T>(x);
     if (WHOLE || n >= 8) {
-        if (past) __builtin_nontemporal_store(r.w, reinterpret_cast<typename Vec8<T>::Anywhere *>(p));
-        else *reinterpret_cast<typename Vec8<T>::Anywhere *>(p) = r.w;
+        *reinterpret_cast<typename Vec8<T>::Anywhere *>(p) = r.w;
     } else {
         struct Values { T v[8]; };
         const Values y = __builtin_bit_cast(Values, r.w);

@@ -20,7 +20,6 @@ struct RowsArgs {
     const void *tokens;          // null: row r of the source
     int64_t ld_src, ld_res, ld_dst, rows, num_rows;
     int N, nv, wide;             // columns, vectors per row, tokens of 64 bits
-    bool past;                   // the output goes past the caches, which hold rows of the table
     double nv_d, inv_nv, half_nv;            // nv, 1 / nv, 0.5 / nv
     float scale;                 // with the dropout's factor
     DropArgs drop;
@@ -92,7 +91,7 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) y[j] += z[j];
         }
-        put8<WHOLE>((D *)a.dst + row_at(row[u], a.ld_dst) + 8 * v[u], n[u], y, TOKENS && a.past);
+        put8<WHOLE>((D *)a.dst + row_at(row[u], a.ld_dst) + 8 * v[u], n[u], y);
     }
 }
 

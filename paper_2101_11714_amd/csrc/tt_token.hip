@@ -258,9 +258,6 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     a.nv = (int)ceil_div(N, 8);
     a.wide = tokens->bits == 64;
     a.scale = scale * a.drop.factor;
-    // an output that the memory-side cache does not hold for whoever reads it next leaves that to the table's rows (32,768 tokens of
-    // 4,096 columns in 16 bits 75 -> 72 us; 8,192 of 2,048 10.0 -> 9.3, but whoever reads those 32 MB then would find them in no cache)
-    a.past = L * N * element_bytes(output->type) >= 256ll << 20;
     if (num_rows == 0) {                                     // no token is one: rows of zeros, for which nothing has to be there to be read
         a.src = output->data;
         a.ld_src = 0;

@@ -188,7 +188,7 @@ def test_token_bwd_without_a_sort_into_rows_of_several_pieces(L, N, kind):
 @pytest.mark.parametrize("L,N,s,o", [(9_000, 1001, F16, BF16), (9_001, 1001, BF16, F32), (35_000, 1024, F32, BF16), (70_001, 1001, BF16, F32), (66_000, 1024, F16, F32),
                                      (140_000, 1003, F32, F16), (132_000, 1024, BF16, BF16)])
 def test_large_lookups(L, N, s, o):
-    # two vectors a thread, and outputs on either side of 256 MiB, against lookups of few rows and dropout on its own
+    # two vectors a thread, between types, odd widths, dropout: against lookups of few rows and dropout on its own
     g = gen(L + N)
     table, tokens = R.rows_of(g, 500, N, s, 3, 1), tokens_of(g, L, 500, "some")
     out, flat = room(L, N, o, 3, 1)
