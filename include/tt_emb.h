@@ -645,7 +645,8 @@ typedef struct tt_dropout_t {
     float p;
 } tt_dropout_t;
 
-/* output[t][:] = dropout(scale * table[token t][:]); dropout == NULL: none.  The table's and the output's types are free. */
+/* output[t][:] = dropout(scale * table[token t][:]); dropout == NULL: none.  The table's and the output's types are free.  Here and in the
+ * gradients scale, lr and the dropout's factor are multiplied with each other first, in 32 bits. */
 int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_tokens_t *tokens, float scale,
                  const tt_dropout_t *dropout, const tt_rows_t *output, void *stream);
 

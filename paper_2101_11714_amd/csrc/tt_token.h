@@ -1,8 +1,9 @@
 // Token embedding: rows of a table by token, scaled, with dropout or without; and the table's gradient by sorted tokens.
 //
 // Forward: out[t] = m_t . (scale table[token_t]); a token outside [0, num_rows) is none and gets a row of zeros.
-// Backward: G[v] = scale sum_{t: token_t = v} m_t . g[t], in 32 bits, in the order of t within a tile of sorted positions
-// and tile after tile, so that the result is the same in every run; nothing is added with atomics.
+// Backward: G[v] = scale sum_{t: token_t = v} m_t . g[t], in 32 bits: in the order of t within a tile of sorted positions, the tiles' sums by
+// groups of lanes that take every so many-th of them each, the groups' sums in their order (few tokens: the positions by such groups).  The order
+// depends on the tokens alone, so that the result is the same in every run; nothing is added with atomics.
 // Both are bound by HBM where there is work; the gather reads whole rows, the gradient is one pass over g and one over the rows it
 // writes.  32,768 tokens of 4,096 columns in 16 bits: lookup with dropout 74 us (4.9 TB/s of distinct rows and output), gradient of
 // 131,072 rows in 32 bits 478 us (5.0 TB/s), of which sorting takes 25 and joining 13.
@@ -97,7 +98,8 @@ __global__ __launch_bounds__(WG) void rows_kernel(const RowsArgs a)
 
 // ---- stable sort of (token, position) ------------------------------------------------------------------------------
 
-// By digits of up to 10 bits, low ones first, as few passes as that allows.
+// By digits of up to 10 bits, low ones first, as few passes as that allows.  Counts of the tiles added up by each workgroup itself / scanned by
+// a kernel, gradient of 64 columns: 16 tiles 37 / 39 us, 32 46 / 48, 64 61 / 61, 128 91 / 85, 256 128 / 113.
 constexpr int TS_WG = 1024, TS_SUB = 2, TS_TILE = TS_WG * TS_SUB;           // keys per workgroup and pass
 constexpr int TS_BITS = 10, TS_BINS = 1 << TS_BITS;
 constexpr int TS_WAVES = TS_WG / WAVE;

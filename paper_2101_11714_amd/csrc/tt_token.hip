@@ -57,8 +57,9 @@ struct GradWs {
 };
 
 // Entries per tile of sorted positions: as many as leave 4,096 waves some work, and at least 8 and at most 64 (then fewer sums of
-// runs cross tiles).  16-bit gradients, 8 / 16 / 32 / 64 entries: 16,384 tokens of 1,024 columns 65 / 64 / 66 / 79 us, 32,768 of 4,096
-// columns 525 / 500 / 488 / 482.
+// runs cross tiles).  16-bit gradients added to a 16-bit table, 8 / 16 / 32 / 64 entries: 2^21 vectors (16,384 tokens of 1,024 columns) 46 / 45 / 51 / 66 us,
+// 2^22 (32,768 of 1,024) 61 / 54 / 56 / 69, 2^23 (65,536 of 1,024) 109 / 93 / 88 / 99, 2^24 (32,768 of 4,096) 175 / 151 / 139 / 141, 2^25 (65,536 of
+// 4,096) 317 / 268 / 245 / 232.
 constexpr int64_t GRAD_SHORT = 1 << 22;                      // vectors of the gradient up to which it is 8
 int grad_entries(int64_t L, int64_t nv)
 {
@@ -69,8 +70,8 @@ int grad_entries(int64_t L, int64_t nv)
 static_assert((WG >> TG_LEAST_LG) * 32 <= TG_MOST && (WG >> (TG_LEAST_LG + 1)) * 64 <= TG_MOST, "a workgroup's entries fit its LDS");
 
 // The path without a sort, whose workgroups each look at all tokens: up to 4,096 of them.  16-bit gradients of 1,024 columns added to a
-// table, sort / without: 30 tokens 14.4 / 5.1 us, 500 16 / 5.5, 1,000 17.2 / 8.1 (all of one token 17 / 26); of 4,096 columns,
-// 1,000 tokens (8,000 workgroups) 24 / 25.5.
+// table, sort / without: 30 tokens 13.6 / 4.2 us, 500 15.7 / 5.5, 1,000 16.5 / 8.1 (all of one token 17 / 27); of 4,096 columns,
+// 500 tokens (4,000 workgroups) 16.2 / 13.7, 1,000 19.5 / 25.3.
 bool few_tokens(int64_t L, int64_t nv) { return L <= TF_MOST && L * ceil_div(nv, WAVE) <= 4096; }
 
 GradWs grad_ws(void *ws, int64_t L, int64_t num_rows, int64_t N)
@@ -99,7 +100,9 @@ GradWs grad_ws(void *ws, int64_t L, int64_t num_rows, int64_t N)
     return w;
 }
 
-// rows up to which the first kernel of the sort, of one workgroup or of a few, clears their bytes itself
+// Rows up to which the first kernel of the sort, of one workgroup or of a few, clears their bytes itself.  By another kernel / itself, 16
+// columns: 4,000 tokens (one workgroup), 2^17 rows 29.1 / 28.2 us, 2^18 30.4 / 30.5, 2^19 32.0 / 33.7; 16,384 tokens, 2^19 rows 46.9 / 45.3, 2^20 58.9 / 58.0,
+// 2^22 78.1 / 79.2.
 constexpr int64_t BLANK_ONE = 1 << 18, BLANK_FEW = 1 << 20;
 
 hipError_t sort_tokens(const tt_tokens_t *t, int64_t num_rows, const GradWs &w, bool named, hipStream_t st, const uint32_t **ks, const uint32_t **vs)
@@ -266,7 +269,7 @@ int tt_token_fwd(const tt_rows_t *table, int64_t num_rows, int64_t N, const tt_t
     with_type(num_rows ? table->type : output->type, [&](auto s) {
         with_type(output->type, [&](auto d) {
             // few tokens: one vector per thread, so that more of the device has some; else two (32,768 tokens of 4,096 columns in 16 bits
-            // under dropout, 1 / 2 / 4 vectors: 97 / 75 / 77 us)
+            // under dropout, 1 / 2 / 4 vectors: 97 / 75 / 77 us; 1 / 2, 2^20 vectors 5.7 / 5.9, under dropout 6.5 / 6.2, 2^21 9.9 / 9.9 and 10.4 / 9.9)
             if (L * a.nv < (1 << 20)) launch_rows<decltype(s), decltype(d), 1, true, false>(a, (hipStream_t)stream);
             else launch_rows<decltype(s), decltype(d), 2, true, false>(a, (hipStream_t)stream);
         });
