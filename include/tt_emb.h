@@ -701,6 +701,124 @@ int tt_add_rms_norm_bwd(const tt_rows_t *grad_output, const tt_rows_t *h, const 
                         void *grad_weight, int32_t grad_weight_type, int accumulate, int64_t n_rows, int64_t N,
                         void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * ---- The products of a language model and what is done to their rows: matrix product with its epilogue, norm and rotation of
+ * queries and keys, log probabilities of tokens ----
+ *
+ * Rows, types and limits as above.
+ */
+enum {
+    TT_ACT_NONE = 0,
+    TT_ACT_RELU = 1,
+    TT_ACT_GELU = 2,         /* z (1 + erf(z / sqrt 2)) / 2                                       */
+    TT_ACT_GELU_TANH = 3,    /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2                 */
+    TT_ACT_SILU = 4          /* z / (1 + exp(-z))                                                 */
+};
+
+/*
+ * z = x weight^T + bias,  output = act(z) + residual:  x [n_rows][K], weight [N][K] (a token table as the way out among them), output,
+ * residual and pre [n_rows][N].
+ * bias: N values of any type, NULL for none.  residual: NULL for none.  pre: z, stored for the gradient (NULL: not).
+ * Types: weight and pre x's; output x's or 32 bits; residual the output's.  output may be residual, at the same stride.
+ * workspace: tt_linear_fwd_workspace_bytes(n_rows, K, N, x's type) bytes, 16-byte aligned (0: none is needed; enough for fewer rows too).
+ * K and N up to 2^24.  K == 0 is valid: z = bias.
+ */
+size_t tt_linear_fwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type);
+int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias, int32_t bias_type, int32_t activation,
+                  const tt_rows_t *residual, const tt_rows_t *pre, const tt_rows_t *output, int64_t n_rows, int64_t K, int64_t N,
+                  void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients, from x, the weight and the stored z (pre; not read where there is no activation):
+ *   dz = grad_output * act'(z),  grad_x = dz weight,  grad_weight = dz^T x,  grad_bias = sum over the rows of dz.
+ * The residual's gradient is grad_output itself.  grad_x, grad_weight, grad_bias: any of them may be NULL, and weight or x with what
+ * needs it.  Types: x, weight, pre and grad_x grad_output's; grad_weight that or 32 bits; grad_bias any.  dz is rounded to that type
+ * before the products where there is an activation (not before its sums over the rows).  accumulate != 0 adds to grad_weight and grad_bias.
+ * No output may overlap another array.
+ * workspace: tt_linear_bwd_workspace_bytes(n_rows, K, N, type, activation) bytes, 16-byte aligned (enough for fewer rows and fewer gradients too).
+ */
+size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation);
+int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_rows_t *weight, const tt_rows_t *pre, int32_t activation,
+                  const tt_rows_t *grad_x, const tt_rows_t *grad_weight, void *grad_bias, int32_t grad_bias_type, int accumulate,
+                  int64_t n_rows, int64_t K, int64_t N, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Heads of an array: head h of row r begins at data + r * ld + h * ld_head elements.  The struct is host memory, data is device memory. */
+typedef struct tt_heads_t {
+    void *data;
+    int64_t ld, ld_head;
+    int32_t heads;
+    int32_t type;
+} tt_heads_t;
+
+/*
+ * Rotation by position: of a head's D columns the first 2 * pairs are turned, pair i of row r by the angle positions[a][r] * freqs[i]
+ * (radians), where a is the axis of the pair: the first sections[0] pairs belong to axis 0, the next sections[1] to axis 1, and so on
+ * (one axis: text; time, height, width: images and video); the sections' sum is `pairs`, and a section may be 0.  Pair i is columns i and
+ * pairs + i, or 2 i and 2 i + 1 (neighbours != 0).  A pair (u, v) becomes (u cos - v sin, v cos + u sin).
+ * positions: axes x n_rows whole numbers of 32 or 64 bits (signed, any value up to 2^52 in size), row stride ld_positions between axes.
+ * freqs: fp32 [pairs].  Angles are held in 64 bits.  Host struct, device data.
+ */
+typedef struct tt_rotation_t {
+    const void *positions;
+    int64_t ld_positions;
+    const float *freqs;
+    int32_t bits;
+    int32_t axes;            /* 1 to 4 */
+    int32_t sections[4];
+    int32_t pairs;
+    int32_t neighbours;
+} tt_rotation_t;
+
+/*
+ * Norm of every head and rotation, of queries and keys in one call (k == NULL: of q alone):
+ *   u = x * w / sqrt(mean of x^2 over the head + eps) (norm == 0: u = x),  output = u turned by its row's position (rotation == NULL: u).
+ * weights: D values of any type, NULL for ones.  All arrays of heads have one type; heads may lie apart (parts of a product's wider
+ * rows).  An output may be its input.  D up to 512.
+ */
+int tt_qk_norm_rotate_fwd(const tt_heads_t *q, const tt_heads_t *k, const tt_rotation_t *rotation, int norm, float eps,
+                          const void *q_weight, int32_t q_weight_type, const void *k_weight, int32_t k_weight_type,
+                          const tt_heads_t *q_output, const tt_heads_t *k_output, int64_t n_rows, int64_t D, void *stream);
+
+/*
+ * Gradients from the inputs q and k (not read where norm == 0; NULL then will do) and the outputs' gradients.  With g the gradient turned back and
+ * r = 1 / sqrt(mean x^2 + eps):
+ *   grad_x = r (g w - x r^2 mean(g w x)),   grad_weight = sum over rows and heads of g x r   (norm == 0: grad_x = g).
+ * grad_q and grad_k may be the outputs' gradients.  grad_q_weight, grad_k_weight: D values of any type, NULL: not wanted; accumulate != 0 adds to them.
+ * workspace: tt_qk_norm_rotate_bwd_workspace_bytes(n_rows, heads of q, heads of k, D) bytes, 16-byte aligned, if a weight's gradient is asked for
+ * (enough for fewer rows and heads too).
+ */
+size_t tt_qk_norm_rotate_bwd_workspace_bytes(int64_t n_rows, int64_t q_heads, int64_t k_heads, int64_t D);
+int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *grad_k_output, const tt_heads_t *q, const tt_heads_t *k,
+                          const tt_rotation_t *rotation, int norm, float eps,
+                          const void *q_weight, int32_t q_weight_type, const void *k_weight, int32_t k_weight_type,
+                          const tt_heads_t *grad_q, const tt_heads_t *grad_k, void *grad_q_weight, int32_t grad_q_weight_type,
+                          void *grad_k_weight, int32_t grad_k_weight_type, int accumulate, int64_t n_rows, int64_t D,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Log probabilities of tokens under z = scale * logits (0 < scale <= 1e30), logits [n_rows][V] of 32 or 16 bits:
+ *   lse[r] = log(sum over the row of exp(z)),  logprob[r] = z[r][token r] - lse[r],  entropy[r] = lse[r] - sum of exp(z - lse) z.
+ * A logit of -inf has no probability and adds nothing.  A row of nothing else: lse and logprob -inf, entropy 0.  A row with a NaN or +inf: NaN in
+ * all three.  A token outside [0, V) is no token: its logprob is 0.  tokens->L == n_rows.
+ * lse, logprob, entropy: fp32 [n_rows]; any of them may be NULL, and tokens if logprob is.
+ * k > 0: the k likeliest columns, equal ones by their number (NaN before all others), ids [n_rows][k] of 32 or 64 bits and their log probabilities
+ * fp32 [n_rows][k] (NULL: not wanted); columns of logit -inf are no alternatives, and places for which there is none get -1 and -inf.
+ * k <= 64.
+ * workspace: tt_token_logprob_fwd_workspace_bytes(n_rows, V, k) bytes, 16-byte aligned (enough for fewer rows too).
+ */
+size_t tt_token_logprob_fwd_workspace_bytes(int64_t n_rows, int64_t V, int32_t k);
+int tt_token_logprob_fwd(const tt_rows_t *logits, const tt_tokens_t *tokens, float scale, float *logprob, float *lse, float *entropy,
+                         int32_t k, void *top_ids, int32_t top_ids_bits, float *top_logprobs, int64_t n_rows, int64_t V,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * grad_logits = scale (g (1[column = token] - p) - ge p (log p + entropy)),  p = exp(z - lse), with g = grad_logprob[r] (0 for a row without a token;
+ * NULL: 0) and ge = grad_entropy[r] (NULL: 0; else entropy is needed).  Columns of logit -inf, and rows whose lse is -inf, have no gradient (0).
+ * grad_logits: the logits' type; it may be logits.
+ */
+int tt_token_logprob_bwd(const tt_rows_t *logits, const tt_tokens_t *tokens, float scale, const float *lse, const float *entropy,
+                         const float *grad_logprob, const float *grad_entropy, const tt_rows_t *grad_logits, int64_t n_rows, int64_t V, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -14,7 +14,7 @@ from __future__ import annotations
 import ctypes as C
 import importlib.util
 import os
-from typing import List, NamedTuple, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence, Union
 
 import torch
 
@@ -35,7 +35,10 @@ EXPORTS = ("tt_last_error", "tt_cache_table_capacity", "tt_emb_workspace_bytes",
            "tt_emb_fwd", "tt_emb_bwd", "tt_emb_bwd_sgd", "tt_emb_sgd_update", "tt_cache_build", "tt_cache_lookup",
            "tt_emb_debug_decode", "tt_emb_debug_decode_as", "tt_emb_debug_dedup", "tt_emb_debug_set_fast_path",
            "tt_token_fwd", "tt_token_bwd_workspace_bytes", "tt_token_bwd", "tt_token_bwd_sgd", "tt_dropout_fwd", "tt_dropout_bwd",
-           "tt_add_rms_norm_fwd", "tt_add_rms_norm_bwd_workspace_bytes", "tt_add_rms_norm_bwd")
+           "tt_add_rms_norm_fwd", "tt_add_rms_norm_bwd_workspace_bytes", "tt_add_rms_norm_bwd",
+           "tt_linear_fwd_workspace_bytes", "tt_linear_fwd", "tt_linear_bwd_workspace_bytes", "tt_linear_bwd",
+           "tt_qk_norm_rotate_fwd", "tt_qk_norm_rotate_bwd_workspace_bytes", "tt_qk_norm_rotate_bwd",
+           "tt_token_logprob_fwd_workspace_bytes", "tt_token_logprob_fwd", "tt_token_logprob_bwd")
 
 
 class TTShape(C.Structure):
@@ -137,6 +140,19 @@ def lib():
         l.tt_add_rms_norm_bwd_workspace_bytes.restype = C.c_size_t
         l.tt_add_rms_norm_bwd_workspace_bytes.argtypes = [i64, i64]
         l.tt_add_rms_norm_bwd.argtypes = [vp, vp, vp, vp, C.c_int32, vp, vp, vp, vp, vp, C.c_int32, C.c_int, i64, i64, vp, C.c_size_t, vp]
+        i32, size = C.c_int32, C.c_size_t
+        for name in ("tt_linear_fwd", "tt_linear_bwd", "tt_qk_norm_rotate_bwd", "tt_token_logprob_fwd"):
+            getattr(l, name + "_workspace_bytes").restype = size
+        l.tt_linear_fwd_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        l.tt_linear_fwd.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, i64, i64, i64, vp, size, vp]
+        l.tt_linear_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        l.tt_linear_bwd.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, C.c_int, i64, i64, i64, vp, size, vp]
+        l.tt_qk_norm_rotate_fwd.argtypes = [vp, vp, vp, C.c_int, f32, vp, i32, vp, i32, vp, vp, i64, i64, vp]
+        l.tt_qk_norm_rotate_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64]
+        l.tt_qk_norm_rotate_bwd.argtypes = [vp, vp, vp, vp, vp, C.c_int, f32, vp, i32, vp, i32, vp, vp, vp, i32, vp, i32, C.c_int, i64, i64, vp, size, vp]
+        l.tt_token_logprob_fwd_workspace_bytes.argtypes = [i64, i64, i32]
+        l.tt_token_logprob_fwd.argtypes = [vp, vp, f32, vp, vp, vp, i32, vp, i32, vp, i64, i64, vp, size, vp]
+        l.tt_token_logprob_bwd.argtypes = [vp, vp, f32, vp, vp, vp, vp, vp, i64, i64, vp]
         _lib = l
     return _lib
 
@@ -709,3 +725,114 @@ def tt_add_rms_norm_bwd(grad_output: torch.Tensor, h: torch.Tensor, rstd: torch.
     rc = _call.add_rms_norm_bwd(grad_output, h, rstd, weight, grad_x, grad_weight, grad_sum, grad_residual, dropout, accumulate, workspace)
     if rc:
         _check(rc)
+
+
+# ---- the products of a language model and what is done to their rows ------------------------------------------------------
+# Arrays as above, all on the current device.
+
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
+ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH, "silu": ACT_SILU}
+
+
+class TTHeads(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("ld", C.c_int64), ("ld_head", C.c_int64), ("heads", C.c_int32), ("type", C.c_int32)]
+
+
+class TTRotation(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("ld_positions", C.c_int64), ("freqs", C.c_void_p), ("bits", C.c_int32), ("axes", C.c_int32),
+                ("sections", C.c_int32 * 4), ("pairs", C.c_int32), ("neighbours", C.c_int32)]
+
+
+class Rotation(NamedTuple):
+    """Pair i of a head's columns is turned by positions * freqs[i] radians.  positions: int64 or int32, [axes, rows] ([rows] will do for one
+    axis); freqs: float32, one per pair; sections: how many pairs belong to each axis, in their order; neighbours: pairs of
+    neighbouring columns instead of one column of each half.  A plain tuple will do as well."""
+    positions: torch.Tensor
+    freqs: torch.Tensor
+    sections: Sequence[int]
+    neighbours: bool = False
+
+
+_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+
+
+def _activation(a: Union[str, int]) -> int:
+    if isinstance(a, str):
+        if a not in ACTIVATIONS:
+            raise ValueError("activation %r: one of %s is expected" % (a, ", ".join(ACTIVATIONS)))
+        return ACTIVATIONS[a]
+    return int(a)
+
+
+def linear_fwd_workspace_bytes(n_rows: int, K: int, N: int, dtype: torch.dtype) -> int:
+    return int(lib().tt_linear_fwd_workspace_bytes(int(n_rows), int(K), int(N), _TYPES[dtype]))
+
+
+def tt_linear_fwd(x: torch.Tensor, weight: torch.Tensor, output: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Union[str, int] = ACT_NONE,
+                  residual: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """output = activation(x @ weight.T + bias) + residual; x [..., K], weight [N, K].  activation: "none", "relu", "gelu", "gelu_tanh", "silu".
+    pre takes what the activation is applied to, which the backward pass needs.  output may be residual."""
+    rc = _call.linear_fwd(x, weight, output, bias, _activation(activation), residual, pre, workspace)
+    if rc:
+        _check(rc)
+    return output
+
+
+def linear_bwd_workspace_bytes(n_rows: int, K: int, N: int, dtype: torch.dtype, activation: Union[str, int] = ACT_NONE) -> int:
+    return int(lib().tt_linear_bwd_workspace_bytes(int(n_rows), int(K), int(N), _TYPES[dtype], _activation(activation)))
+
+
+def tt_linear_bwd(grad_output: torch.Tensor, x: Optional[torch.Tensor], weight: Optional[torch.Tensor], grad_x: Optional[torch.Tensor], grad_weight: Optional[torch.Tensor],
+                  grad_bias: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, activation: Union[str, int] = ACT_NONE, accumulate: bool = False,
+                  workspace: Optional[torch.Tensor] = None) -> None:
+    """Gradients of x, of the weight and of the bias (None: not wanted, nor then x for grad_weight and weight for grad_x); the residual's is
+    grad_output.  accumulate adds to grad_weight and grad_bias."""
+    rc = _call.linear_bwd(grad_output, x, weight, pre, _activation(activation), grad_x, grad_weight, grad_bias, accumulate, workspace)
+    if rc:
+        _check(rc)
+
+
+def tt_qk_norm_rotate_fwd(q: torch.Tensor, k: Optional[torch.Tensor], q_output: torch.Tensor, k_output: Optional[torch.Tensor], rotation: Optional[Rotation] = None,
+                          norm: bool = True, q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6) -> None:
+    """Every head's RMS norm (norm=False: none), then its rotation (None: none); q [..., heads, D], k [..., its heads, D] or None, parts
+    of a product's wider rows among them.  An output may be its input."""
+    rc = _call.qk_norm_rotate_fwd(q, k, q_output, k_output, rotation, norm, q_weight, k_weight, eps)
+    if rc:
+        _check(rc)
+
+
+def qk_norm_rotate_bwd_workspace_bytes(n_rows: int, q_heads: int, k_heads: int, D: int) -> int:
+    return int(lib().tt_qk_norm_rotate_bwd_workspace_bytes(int(n_rows), int(q_heads), int(k_heads), int(D)))
+
+
+def tt_qk_norm_rotate_bwd(grad_q_output: torch.Tensor, grad_k_output: Optional[torch.Tensor], q: Optional[torch.Tensor], k: Optional[torch.Tensor], grad_q: torch.Tensor,
+                          grad_k: Optional[torch.Tensor], rotation: Optional[Rotation] = None, norm: bool = True, q_weight: Optional[torch.Tensor] = None,
+                          k_weight: Optional[torch.Tensor] = None, grad_q_weight: Optional[torch.Tensor] = None, grad_k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                          accumulate: bool = False, workspace: Optional[torch.Tensor] = None) -> None:
+    """Gradients from the forward pass's inputs q and k (None will do without a norm).  grad_q may be grad_q_output, grad_k grad_k_output;
+    accumulate adds to the weights' gradients."""
+    rc = _call.qk_norm_rotate_bwd(grad_q_output, grad_k_output, q, k, grad_q, grad_k, rotation, norm, q_weight, k_weight, grad_q_weight, grad_k_weight, eps, accumulate, workspace)
+    if rc:
+        _check(rc)
+
+
+def token_logprob_fwd_workspace_bytes(n_rows: int, V: int, k: int = 0) -> int:
+    return int(lib().tt_token_logprob_fwd_workspace_bytes(int(n_rows), int(V), int(k)))
+
+
+def tt_token_logprob_fwd(logits: torch.Tensor, tokens: Optional[torch.Tensor], logprob: Optional[torch.Tensor], lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                         top_ids: Optional[torch.Tensor] = None, top_logprobs: Optional[torch.Tensor] = None, scale: float = 1.0, workspace: Optional[torch.Tensor] = None) -> None:
+    """Of scale * logits: each row's log probability of its token (0 for a token outside of the columns), the logarithm of the sum of
+    exponentials and the entropy (float32, one per row), and the likeliest columns with their log probabilities, [..., k] (int64 or int32; float32)."""
+    rc = _call.token_logprob_fwd(logits, tokens, logprob, lse, entropy, top_ids, top_logprobs, scale, workspace)
+    if rc:
+        _check(rc)
+
+
+def tt_token_logprob_bwd(logits: torch.Tensor, tokens: Optional[torch.Tensor], lse: torch.Tensor, grad_logprob: Optional[torch.Tensor], grad_logits: torch.Tensor,
+                         entropy: Optional[torch.Tensor] = None, grad_entropy: Optional[torch.Tensor] = None, scale: float = 1.0) -> torch.Tensor:
+    """The logits' gradient from those of the log probabilities and of the entropy (which then is needed).  grad_logits may be logits."""
+    rc = _call.token_logprob_bwd(logits, tokens, lse, entropy, grad_logprob, grad_entropy, grad_logits, scale)
+    if rc:
+        _check(rc)
+    return grad_logits

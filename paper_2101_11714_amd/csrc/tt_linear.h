@@ -1,0 +1,76 @@
+// What the gradients of a product with an activation need beside the products: the gradient in front of the activation, and the
+// bias's, whose columns' sums are left per band of rows.
+#pragma once
+
+#include "tt_product.h"
+
+namespace tt {
+
+struct SlopeArgs {
+    const void *dy, *pre;        // pre null: no activation
+    void *dz;                    // null: not wanted (no activation)
+    float *part;                 // [bands][8 nv] sums of columns, null: not wanted
+    int64_t ld_dy, ld_pre, ld_dz;
+    int64_t rows, band;          // rows of a band
+    int N, nv, act;
+};
+
+// 32 vectors of eight columns x 8 rows per workgroup at a time, down a band of rows.
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+{
+    __shared__ float sums[8][32][8];
+    const int v = blockIdx.x * 32 + (threadIdx.x & 31), lane_row = threadIdx.x >> 5;
+    const int n = a.N - 8 * v;
+    const int64_t first = (int64_t)blockIdx.y * a.band, last = first + a.band < a.rows ? first + a.band : a.rows;
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (v < a.nv) {
+#pragma unroll 4
+        for (int64_t r = first + lane_row; r < last; r += 8) {
+            float d[8];
+            Vec8<T> x = fetch8<WHOLE>((const T *)a.dy + row_at(r, a.ld_dy) + 8 * v, n, a.N);
+            if (a.pre) {
+                float z[8];
+                Vec8<T> y = fetch8<WHOLE>((const T *)a.pre + row_at(r, a.ld_pre) + 8 * v, n, a.N);
+                settle8<WHOLE>(x, n, a.N);
+                settle8<WHOLE>(y, n, a.N);
+                widen8(x, d);
+                widen8(y, z);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], a.act);
+                if (a.dz) put8<true>((T *)a.dz + row_at(r, a.ld_dz) + 8 * v, 8, d);      // (its rows are whole vectors)
+            } else {
+                settle8<WHOLE>(x, n, a.N);
+                widen8(x, d);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s[j] += d[j];
+        }
+    }
+    if (!a.part) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sums[lane_row][threadIdx.x & 31][j] = s[j];
+    __syncthreads();
+    const int c = threadIdx.x, at = blockIdx.x * 256 + c;
+    if (at >= 8 * a.nv) return;
+    float y = 0.f;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) y += sums[q][c >> 3][c & 7];
+    a.part[(int64_t)blockIdx.y * 8 * a.nv + at] = y;
+}
+
+// the bands' sums added in their order
+template <typename W>
+__global__ __launch_bounds__(256) void bias_sum_kernel(const float *part, int bands, int N, int cols, W *db, int add)
+{
+    __shared__ float sums[4][64];
+    const int c = threadIdx.x & 63, q = threadIdx.x >> 6, at = blockIdx.x * 64 + c;
+    float s = 0.f;
+    if (at < N)
+        for (int b = q; b < bands; b += 4) s += part[(int64_t)b * cols + at];
+    sums[q][c] = s;
+    __syncthreads();
+    if (q == 0 && at < N) db[at] = (W)((add ? (float)db[at] : 0.f) + ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])));
+}
+
+}  // namespace tt

@@ -1,0 +1,331 @@
+// Log probabilities of tokens under rows of logits, with entropy and the likeliest alternatives, and the gradient.
+//
+// One pass over a row holds the largest logit m so far, S = sum of exp(z - m) and T = sum of exp(z - m) (z - m) in 32 bits, and multiplies the two
+// sums when m grows; lse = m + log S, entropy = log S - T / S, both without a difference of large numbers.  Few rows are cut into
+// pieces, a workgroup each, which a second launch joins.
+// The k likeliest: the k-th largest of the threads' largest logits is no larger than the k-th largest of all, so that a second look at the
+// piece, by then in the caches, leaves little more than k to be ranked.  Logits are ordered by a 64-bit key, value first and column
+// after it, so that no two are equal.
+#pragma once
+
+#include "tt_rows_io.h"
+
+namespace tt {
+
+constexpr int LP_UNROLL = 4;                                 // vectors of eight logits a thread loads at a time
+constexpr int LP_LIST = 1024;                                // candidates that a workgroup can rank
+constexpr int LP_MOST_K = 64;
+constexpr float LP_LEAST = -3.402823466e38f, LOG2E = 1.4426950408889634f;
+
+struct LogprobArgs {
+    const void *logits;
+    int64_t ld;
+    const void *tokens;          // null: none
+    int tokens64;
+    float scale;
+    float *logprob, *lse, *entropy;
+    int k, ids64;
+    void *ids;
+    float *top;
+    int64_t rows;
+    int V, nv;                   // vectors of eight of a row
+    int pieces, piece;           // of a row, vectors of one
+    float *sums;                 // [rows][pieces][4]: m, S, T of pieces
+    uint64_t *keys;              // [rows][pieces][k]
+};
+
+struct Sums {
+    float m, s, t;
+};
+
+// the sums about the larger of two maxima; -0 and 0 for what has none
+__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c)
+{
+    const float m = fmaxf(a.m, b.m);
+    auto part = [&](const Sums &x, float &s, float &t) {
+        const float d = fmaxf(x.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
+        s += x.s * f;
+        t += f == 0.f ? 0.f : f * (x.t + d * x.s);
+    };
+    Sums r{m, 0.f, 0.f};
+    part(a, r.s, r.t);
+    part(b, r.s, r.t);
+    return r;
+}
+
+__device__ __forceinline__ uint32_t order_of(float x)
+{
+    const uint32_t u = __float_as_uint(x + 0.f);             // (-0 is 0)
+    if (x != x) return 0xffffffffu;
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(uint32_t order) { return order == 0xffffffffu ? __uint_as_float(0x7fc00000u) : __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
+
+// 0: no alternative
+__device__ __forceinline__ uint64_t key_of(float x, uint32_t column)
+{
+    return x == -INFINITY ? 0ull : (uint64_t)order_of(x) << 32 | (uint32_t)~column;
+}
+
+// how many of n keys are larger
+__device__ __forceinline__ int rank_of(const uint64_t *keys, int n, uint64_t key)
+{
+    int r = 0;
+#pragma unroll 8
+    for (int i = 0; i < n; ++i) r += keys[i] > key;
+    return r;
+}
+
+__device__ __forceinline__ int64_t token_at(const LogprobArgs &a, int64_t row) { return a.tokens64 ? ((const int64_t *)a.tokens)[row] : ((const int32_t *)a.tokens)[row]; }
+
+// What a row's sums say.  Log probabilities are taken from the largest logit and not from lse, which has lost log S in rows of the lowest
+// values of a type.
+template <typename T>
+__device__ __forceinline__ void leave_row(const LogprobArgs &a, int64_t row, const Sums &r, float log_s)
+{
+    const bool none = r.s == 0.f;
+    if (a.lse) a.lse[row] = none ? -INFINITY : r.m * a.scale + log_s;
+    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - a.scale * (r.t / r.s);
+    if (a.logprob) {
+        const int64_t token = token_at(a, row);
+        float y = 0.f;
+        if (token >= 0 && token < a.V) {
+            const float z = (float)((const T *)a.logits)[row * a.ld + token];
+            y = none ? -INFINITY : a.scale * (z - r.m) - log_s;
+        }
+        a.logprob[row] = y;
+    }
+}
+
+__device__ __forceinline__ void leave_top(const LogprobArgs &a, int64_t row, int place, uint64_t key, float m, float log_s)
+{
+    const int64_t at = row * a.k + place, column = key ? (int64_t)(uint32_t)~(uint32_t)key : -1;
+    if (a.ids64) ((int64_t *)a.ids)[at] = column;
+    else ((int32_t *)a.ids)[at] = (int32_t)column;
+    if (a.top) a.top[at] = key ? a.scale * (value_of((uint32_t)(key >> 32)) - m) - log_s : -INFINITY;
+}
+
+// the vectors [from, to) of a row, U at a time per thread: f(vector's number, its eight logits), -inf where there is no column
+template <typename T, bool WHOLE, typename F>
+__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
+{
+    for (int v0 = from + threadIdx.x; v0 < to; v0 += WG * LP_UNROLL) {
+        Vec8<T> r[LP_UNROLL];
+#pragma unroll
+        for (int i = 0; i < LP_UNROLL; ++i) {
+            const int v = v0 + i * WG < to ? v0 + i * WG : v0;
+            r[i] = fetch8<WHOLE>(line + 8 * (int64_t)v, V - 8 * v, V);
+        }
+#pragma unroll
+        for (int i = 0; i < LP_UNROLL; ++i) {
+            const int v = v0 + i * WG;
+            if (v >= to) break;
+            float x[8];
+            settle8<WHOLE>(r[i], V - 8 * v, V);
+            widen8(r[i], x);
+            if (!WHOLE)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) x[j] = 8 * v + j < V ? x[j] : -INFINITY;
+            f(v, x);
+        }
+    }
+}
+
+// The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  `best`: the thread's largest.
+template <typename T, bool WHOLE>
+__device__ void largest_keys(const T *line, int from, int to, int V, int k, uint64_t best, uint64_t *list, int *count, uint64_t *least, uint64_t *out)
+{
+    list[threadIdx.x] = best;
+    if (threadIdx.x == 0) {
+        *count = 0;
+        *least = 1;
+    }
+    __syncthreads();
+    if (best && rank_of(list, WG, best) == k - 1) *least = best;
+    __syncthreads();
+    int n;
+    for (;;) {
+        const uint64_t bound = *least;
+        each_vector<T, WHOLE>(line, from, to, V, [&](int v, float (&x)[8]) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const uint64_t key = key_of(x[j], 8 * v + j);
+                if (key >= bound) {
+                    const int at = atomicAdd(count, 1);
+                    if (at < LP_LIST) list[at] = key;
+                }
+            }
+        });
+        __syncthreads();
+        n = *count;
+        if (n <= LP_LIST) break;
+        // more than the list takes: the k-th largest of those that it took is a closer bound
+        uint64_t closer = 0;
+        for (int i = threadIdx.x; i < LP_LIST; i += WG)
+            if (rank_of(list, LP_LIST, list[i]) == k - 1) closer = list[i];
+        __syncthreads();
+        if (closer) *least = closer;
+        if (threadIdx.x == 0) *count = 0;
+        __syncthreads();
+    }
+    for (int i = threadIdx.x; i < n; i += WG) {
+        const uint64_t key = list[i];
+        const int r = rank_of(list, n, key);
+        if (r < k) out[r] = key;
+    }
+    for (int i = n + threadIdx.x; i < k; i += WG) out[i] = 0;
+}
+
+template <typename T, bool TOP, bool WHOLE>
+__global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
+{
+    __shared__ Sums waves[NWAVE];
+    __shared__ __attribute__((aligned(16))) uint64_t list[TOP ? LP_LIST : 1];
+    __shared__ uint64_t found[TOP ? LP_MOST_K : 1], least;
+    __shared__ int count;
+    const int64_t id = workgroup(), row = id / a.pieces;
+    if (row >= a.rows) return;
+    const int piece = (int)(id - row * a.pieces), from = piece * a.piece, to = min(from + a.piece, a.nv);
+    const T *line = (const T *)a.logits + row * a.ld;
+    const float c = a.scale * LOG2E;
+    Sums r{LP_LEAST, 0.f, 0.f};
+    float best = -INFINITY;
+    uint32_t column = 0, order = 0;
+    each_vector<T, WHOLE>(line, from, to, a.V, [&](int v, float (&x)[8]) {
+        float m = r.m;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
+        if (m > r.m) {
+            const float d = fmaxf(r.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
+            r.t = f == 0.f ? 0.f : f * (r.t + d * r.s);
+            r.s *= f;
+            r.m = m;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * c);
+            r.s += e;
+            r.t += e * fmaxf(d, LP_LEAST);
+            if (TOP) {
+                const uint32_t o = order_of(x[j]);
+                if (o > order && x[j] != -INFINITY) {
+                    order = o;
+                    best = x[j];
+                    column = 8 * v + j;
+                }
+            }
+        }
+    });
+    const uint64_t key = TOP ? key_of(best, column) : 0;
+    // lanes, then waves
+#pragma unroll
+    for (int b = 1; b < WAVE; b <<= 1) {
+        const Sums o{__shfl_xor(r.m, b), __shfl_xor(r.s, b), __shfl_xor(r.t, b)};
+        r = joined(r, o, c);
+    }
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = r;
+    __syncthreads();
+    r = joined(joined(waves[0], waves[1], c), joined(waves[2], waves[3], c), c);
+    if (TOP) largest_keys<T, WHOLE>(line, from, to, a.V, a.k, key, list, &count, &least, found);
+    if (a.pieces > 1) {
+        if (threadIdx.x == 0) {
+            float *p = a.sums + id * 4;
+            p[0] = r.m;
+            p[1] = r.s;
+            p[2] = r.t;
+        }
+        if (TOP) {
+            __syncthreads();
+            for (int i = threadIdx.x; i < a.k; i += WG) a.keys[id * a.k + i] = found[i];
+        }
+        return;
+    }
+    const float log_s = logf(r.s);
+    if (threadIdx.x == 0) leave_row<T>(a, row, r, log_s);
+    if (TOP) {
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.k; i += WG) leave_top(a, row, i, found[i], r.m, log_s);
+    }
+}
+
+// a row's pieces joined, in their order: a workgroup of one wave per row without alternatives, of four with them
+template <typename T, bool TOP>
+__global__ __launch_bounds__(WG) void logprob_join_kernel(LogprobArgs a)
+{
+    __shared__ __attribute__((aligned(16))) uint64_t list[TOP ? LP_LIST : 1];
+    __shared__ float row_m, row_log_s;
+    const int64_t row = workgroup();
+    if (row >= a.rows) return;
+    const float c = a.scale * LOG2E;
+    if (threadIdx.x < WAVE) {
+        Sums r{LP_LEAST, 0.f, 0.f};
+        for (int p = threadIdx.x; p < a.pieces; p += WAVE) {
+            const float *s = a.sums + (row * a.pieces + p) * 4;
+            r = joined(r, Sums{s[0], s[1], s[2]}, c);
+        }
+#pragma unroll
+        for (int b = 1; b < WAVE; b <<= 1) {
+            const Sums o{__shfl_xor(r.m, b), __shfl_xor(r.s, b), __shfl_xor(r.t, b)};
+            r = joined(r, o, c);
+        }
+        if (threadIdx.x == 0) {
+            row_m = r.m;
+            row_log_s = logf(r.s);
+            leave_row<T>(a, row, r, row_log_s);
+        }
+    }
+    if (!TOP) return;
+    const int n = a.pieces * a.k;                            // (at most LP_LIST)
+    for (int i = threadIdx.x; i < n; i += WG) list[i] = a.keys[row * n + i];
+    __syncthreads();
+    int there = 0;
+    for (int i = threadIdx.x; i < n; i += WG) {
+        const uint64_t key = list[i];
+        if (!key) continue;
+        const int r = rank_of(list, n, key);
+        if (r < a.k) leave_top(a, row, r, key, row_m, row_log_s);
+    }
+    // places that no key takes
+    for (int i = threadIdx.x; i < a.k; i += WG) {
+        there = 0;
+        for (int j = 0; j < n; ++j) there += list[j] != 0;
+        if (i >= there) leave_top(a, row, i, 0, row_m, row_log_s);
+    }
+}
+
+struct LogprobGradArgs {
+    const void *logits, *tokens;
+    void *out;
+    int64_t ld, ld_out;
+    const float *lse, *entropy, *g, *ge;
+    int64_t rows;
+    int tokens64, V, nv, pieces, piece;
+    float scale;
+};
+
+template <typename T, bool WHOLE>
+__global__ __launch_bounds__(WG) void logprob_bwd_kernel(LogprobGradArgs a)
+{
+    const int64_t id = workgroup(), row = id / a.pieces;
+    if (row >= a.rows) return;
+    const int from = (int)(id - row * a.pieces) * a.piece, to = min(from + a.piece, a.nv);
+    const T *line = (const T *)a.logits + row * a.ld;
+    T *out = (T *)a.out + row * a.ld_out;
+    int64_t token = -1;
+    if (a.tokens && a.g) token = a.tokens64 ? ((const int64_t *)a.tokens)[row] : ((const int32_t *)a.tokens)[row];
+    if (token < 0 || token >= a.V) token = -1;
+    const float g = token >= 0 ? a.g[row] : 0.f, ge = a.ge ? a.ge[row] : 0.f, h = a.ge ? a.entropy[row] : 0.f, lse = a.lse[row];
+    const bool none = lse == -INFINITY;
+    each_vector<T, WHOLE>(line, from, to, a.V, [&](int v, float (&x)[8]) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float l = fmaf(x[j], a.scale, -lse), p = __builtin_amdgcn_exp2f(l * LOG2E);
+            float d = -p * (g + (ge != 0.f ? ge * (l + h) : 0.f));
+            if (8 * v + j == token) d += g;
+            x[j] = none || x[j] == -INFINITY ? 0.f : d * a.scale;
+        }
+        put8<WHOLE>(out + 8 * (int64_t)v, a.V - 8 * v, x);
+    });
+}
+
+}  // namespace tt

@@ -1,0 +1,355 @@
+// Matrix products on the matrix cores, C[m][n] = sum over k of A(m, k) B(n, k), in 32-bit sums, for operands of 32 or 16 bits whose
+// rows are dense in k (x, a weight) or in m or n (the gradients' operands), with an epilogue on the sums.
+#pragma once
+
+#include "tt_rows_io.h"
+
+namespace tt {
+
+typedef float mfma_acc_t __attribute__((ext_vector_type(4)));
+
+// ---- what is done with the sums -----------------------------------------------------------------------------------------
+
+enum { ACT_NONE = 0, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU, ACT_COUNT };
+
+constexpr float GELU_TANH_SCALE = 0.7978845608028654f, GELU_TANH_CUBE = 0.044715f;      // sqrt(2 / pi)
+
+// Where an exponential passes 2^127 its reciprocal is 0, as it should be.  (1 + tanh(u)) / 2 is the logistic function of 2 u.
+__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + expf(-z)); }
+
+__device__ __forceinline__ float act_of(float z, int act)
+{
+    switch (act) {
+    case ACT_RELU: return z > 0.f || z != z ? z : 0.f;
+    case ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
+    case ACT_GELU_TANH: return z * logistic(2.f * GELU_TANH_SCALE * (z + GELU_TANH_CUBE * z * z * z));
+    case ACT_SILU: return z * logistic(z);
+    default: return z;
+    }
+}
+
+// the activation's slope
+__device__ __forceinline__ float act_slope(float z, int act)
+{
+    switch (act) {
+    case ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
+    case ACT_GELU: return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * expf(-0.5f * z * z) * 0.3989422804014327f;
+    case ACT_GELU_TANH: {
+        const float p = logistic(2.f * GELU_TANH_SCALE * (z + GELU_TANH_CUBE * z * z * z));
+        return p + 2.f * GELU_TANH_SCALE * z * p * (1.f - p) * (1.f + 3.f * GELU_TANH_CUBE * z * z);
+    }
+    case ACT_SILU: {
+        const float p = logistic(z);
+        return p * (1.f + z * (1.f - p));
+    }
+    default: return 1.f;
+    }
+}
+
+// y = act(sum + bias) + add, and the value before the activation.  add may be the output itself.
+struct EpilogueArgs {
+    const void *bias;            // null: none
+    int bias_type;               // TT_F32, ...
+    int act;
+    const void *add;             // of the output's type; null: none
+    void *pre;                   // of the operands' type; null: not kept
+    void *out;
+    int64_t ld_add, ld_pre, ld_out;
+};
+
+__device__ __forceinline__ void load_bias(const EpilogueArgs &e, int64_t n, int have, float (&b)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        b[j] = 0.f;
+        if (!e.bias || j >= have) continue;
+        b[j] = e.bias_type == TT_F32 ? ((const float *)e.bias)[n + j] : e.bias_type == TT_BF16 ? (float)((const bf16_t *)e.bias)[n + j] : (float)((const f16_t *)e.bias)[n + j];
+    }
+}
+
+// Eight neighbouring sums of row m from column n on, of which `have` exist (at least one).  T: the operands' type, O: the output's.
+template <typename T, typename O>
+__device__ __forceinline__ void finish8(const EpilogueArgs &e, int64_t m, int64_t n, int have, const float (&b)[8], float (&v)[8])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += b[j];
+    if (e.pre) put8((T *)e.pre + m * e.ld_pre + n, have, v);
+    if (e.act != ACT_NONE)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = act_of(v[j], e.act);
+    if (e.add) {
+        const O *p = (const O *)e.add + m * e.ld_add + n;
+        if (have >= 8) {
+            float r[8];
+            widen8(fetch8<true>(p, 8, 8), r);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += r[j];
+        } else {
+#pragma unroll
+            for (int j = 0; j < 7; ++j)
+                if (j < have) v[j] += (float)p[j];
+        }
+    }
+    put8((O *)e.out + m * e.ld_out + n, have, v);
+}
+
+// ---- tiles of operands in LDS -------------------------------------------------------------------------------------------
+//
+// A step takes 128 bytes of k: PB_K<T> values.  A matrix instruction 16 x 16 takes of each operand 16 bytes of k per lane from one
+// of 16 rows (8 values of 16 bits: one instruction of k = 32; 4 of 32 bits: four of k = 4 whose k are not neighbours, the same
+// ones in both operands), so that a step is two "halves" of 64 bytes.
+//   dense in k:   the tile is [rows][128 bytes], read by 16 bytes per lane;
+//   strided in k: it is [PB_K][rows], as it lies in memory; 16-bit values are read transposed by the LDS (4 rows of k x 16
+//                 columns to 16 lanes), 32-bit values one by one.
+// In both, 16-byte chunks are permuted along a row by an exclusive or with bits of its number, so that the lanes that read at
+// the same time find different banks.
+// The second operand's blocks of 16 rows are interleaved (JOIN): of 64 rows block b has those with (row / 4) % 4 == b.  It is the
+// instruction's first operand, whose rows go to a lane's four registers in fours, so that over four blocks a lane has
+// 16 neighbouring columns of one row of C.
+
+template <typename T>
+constexpr int PB_K = 128 / (int)sizeof(T);
+
+constexpr int BLOCK = 16;
+
+template <typename T, bool KDENSE, bool JOIN, int ROWS>
+struct OperandTile {
+    static constexpr int CH = 16 / sizeof(T);                // values of a chunk
+    static constexpr int LINE = KDENSE ? 8 : ROWS / CH;      // chunks of a line
+    static constexpr int LINES = KDENSE ? ROWS : PB_K<T>;
+    static constexpr int CHUNKS = LINE * LINES, BYTES = CHUNKS * 16;
+    static_assert((LINE & (LINE - 1)) == 0, "a permutation of the line's chunks");
+
+    static __device__ __forceinline__ int swizzle(int line)
+    {
+        int x;
+        if (KDENSE) x = JOIN ? (line & 3) | (line >> 2 & 4) : line & 7;
+        else if (sizeof(T) == 4) x = JOIN ? line >> 2 & 3 : (line >> 2 & 3) << 2;
+        else x = JOIN ? (line & 1) | (line & 2) << 2 : (line & 3) << 1;
+        return x & (LINE - 1);
+    }
+    // byte offset of a chunk
+    static __device__ __forceinline__ int at(int line, int chunk) { return (line * LINE + (chunk ^ swizzle(line))) * 16; }
+
+    // this lane's 16 bytes of block b of the wave's rows from `row0` on, half h of the step
+    static __device__ __forceinline__ uint4 fragment(const char *lds, int row0, int b, int h, int lane)
+    {
+        const int r = lane & 15, q = lane >> 4;
+        if constexpr (KDENSE) {
+            const int row = row0 + (JOIN ? 64 * (b >> 2) + 16 * (r >> 2) + 4 * (b & 3) + (r & 3) : 16 * b + r);
+            return *reinterpret_cast<const uint4 *>(lds + at(row, 4 * h + q));
+        } else if constexpr (sizeof(T) == 2) {
+            typedef short Four __attribute__((ext_vector_type(4)));
+            typedef __attribute__((address_space(3))) Four *Shared;
+            const int col = row0 + (JOIN ? 64 * (b >> 2) + 16 * (r & 3) + 4 * (b & 3) : 16 * b + 4 * (r & 3));
+            const int k = 32 * h + 8 * q + (r >> 2);
+            struct { Four lo, hi; } x;
+            x.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared)(lds + at(k, col >> 3) + (col & 4) * 2));
+            x.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared)(lds + at(k + 4, col >> 3) + (col & 4) * 2));
+            return __builtin_bit_cast(uint4, x);
+        } else {
+            const int col = row0 + (JOIN ? 64 * (b >> 2) + 16 * (r >> 2) + 4 * (b & 3) + (r & 3) : 16 * b + r);
+            uint4 x;
+            uint32_t *w = reinterpret_cast<uint32_t *>(&x);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = *reinterpret_cast<const uint32_t *>(lds + at(16 * h + 4 * q + j, col >> 2) + (col & 3) * 4);
+            return x;
+        }
+    }
+};
+
+// acc += (16 rows of B) x (16 rows of A): lane l has row l & 15 of A and rows 4 (l >> 4) .. + 3 of the block of B
+template <typename T>
+__device__ __forceinline__ void block_product(const uint4 &b, const uint4 &a, mfma_acc_t &acc)
+{
+    if constexpr (sizeof(T) == 4) {
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.x), __uint_as_float(a.x), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.y), __uint_as_float(a.y), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.z), __uint_as_float(a.z), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(b.w), __uint_as_float(a.w), acc, 0, 0, 0);
+    } else {
+        typedef T Eight __attribute__((ext_vector_type(8)));
+        const Eight x = __builtin_bit_cast(Eight, b), y = __builtin_bit_cast(Eight, a);
+        if constexpr (__is_same(T, bf16_t)) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, acc, 0, 0, 0);
+        else acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, acc, 0, 0, 0);
+    }
+}
+
+// ---- loads that bear any alignment and any edge ---------------------------------------------------------------------------
+
+template <typename T>
+struct Chunk {
+    static constexpr int W = 16 / sizeof(T) * sizeof(T) / 4;                 // words
+    typedef uint32_t Words __attribute__((ext_vector_type(W)));
+    typedef Words Anywhere __attribute__((aligned(sizeof(T))));
+};
+
+// 16 bytes of a line of N values from value c on; zeros behind the line's end.  The last 16 bytes of the line are loaded where
+// fewer are left, and moved into place; lines of less than 16 bytes value by value.
+template <typename T>
+__device__ __forceinline__ uint4 fetch_chunk(const T *line, int64_t c, int64_t N)
+{
+    constexpr int CH = 16 / sizeof(T);
+    typedef typename Chunk<T>::Words Words;
+    Words w = {0u, 0u, 0u, 0u};
+    if (N >= CH) {
+        const int64_t last = N - CH, from = c < last ? c : last;
+        w = *reinterpret_cast<const typename Chunk<T>::Anywhere *>(line + from);
+        const int64_t d = c - from;
+        if (d > 0) {
+            if (d >= CH) return uint4{0u, 0u, 0u, 0u};
+            unsigned __int128 all = __builtin_bit_cast(unsigned __int128, w);
+            all >>= 8 * (int)sizeof(T) * (int)d;
+            w = __builtin_bit_cast(Words, all);
+        }
+    } else if (c == 0) {
+        struct { T v[CH]; } x;
+#pragma unroll
+        for (int j = 0; j < CH; ++j) x.v[j] = j < N ? line[j] : (T)0.f;
+        w = __builtin_bit_cast(Words, x);
+    }
+    return __builtin_bit_cast(uint4, w);
+}
+
+struct ProductArgs {
+    const void *a, *b;
+    int64_t lda, ldb;            // between rows of a tile that is dense in k, between values of k otherwise
+    int64_t M, N, K;
+    int tiles_m, tiles_n;
+    int64_t k_part;              // values of k of one part (a multiple of the step's)
+    float *part;                 // sums of parts, [parts][M][ld_part]; null: one part, whose sums go through the epilogue
+    int64_t ld_part;
+};
+
+// tile number -> place: eight rows of tiles at a time, so that the tiles that run together share operands
+__device__ __forceinline__ void tile_place(int tile, int tiles_m, int tiles_n, int &tm, int &tn)
+{
+    constexpr int BAND = 8;
+    const int band = tile / (BAND * tiles_n), rest = tile - band * BAND * tiles_n, rows = min(BAND, tiles_m - band * BAND);
+    tn = rest / rows;
+    tm = band * BAND + rest - tn * rows;
+}
+
+// A wave's sums on their way out: parts' sums as they are, others through the epilogue.
+template <typename T, typename O, int BM, int BN>
+__device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueArgs &e, int64_t m0, int64_t n0, int lane, mfma_acc_t (&acc)[BM][BN])
+{
+#pragma unroll
+    for (int j4 = 0; j4 < BN; j4 += 4) {
+        const int64_t n = n0 + 16 * j4 + 16 * (lane >> 4);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int64_t left = p.N - (n + 8 * half);
+            if (left <= 0) continue;
+            const int have = left < 8 ? (int)left : 8;
+            float bias[8];
+            if (!p.part) load_bias(e, n + 8 * half, have, bias);
+#pragma unroll
+            for (int i = 0; i < BM; ++i) {
+                const int64_t m = m0 + 16 * i + (lane & 15);
+                if (m >= p.M) continue;
+                float v[8];
+#pragma unroll
+                for (int c = 0; c < 8; ++c) v[c] = acc[i][j4 + 2 * half + (c >> 2)][c & 3];
+                if (p.part) put8(p.part + ((int64_t)blockIdx.z * p.M + m) * p.ld_part + n + 8 * half, 8, v);
+                else finish8<T, O>(e, m, n + 8 * half, have, bias, v);
+            }
+        }
+    }
+}
+
+// The parts' sums added in their order, and the epilogue: eight columns per thread.
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, EpilogueArgs e, int parts)
+{
+    const int64_t nv = p.ld_part / 8, at = workgroup() * 256 + threadIdx.x, m = at / nv, n = 8 * (at - m * nv);
+    if (m >= p.M) return;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bias[8];
+    const int have = p.N - n < 8 ? (int)(p.N - n) : 8;
+    load_bias(e, n, have, bias);
+    for (int s = 0; s < parts; ++s) {
+        float x[8];
+        widen8(fetch8<true>(p.part + ((int64_t)s * p.M + m) * p.ld_part + n, 8, 8), x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += x[j];
+    }
+    finish8<T, O>(e, m, n, have, bias, v);
+}
+
+// A tile of TM x TN per workgroup of 2 x 2 waves, operands through registers into LDS, so that every alignment and edge is right.
+template <typename T, typename O, bool AK, bool BK, int TM, int TN>
+__global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArgs e)
+{
+    typedef OperandTile<T, AK, false, TM> TA;
+    typedef OperandTile<T, BK, true, TN> TB;
+    constexpr int KB = PB_K<T>, BM = TM / 2 / BLOCK, BN = TN / 2 / BLOCK, PA = TA::CHUNKS / 256, PB = TB::CHUNKS / 256;
+    static_assert(BN % 4 == 0, "a lane's columns are neighbours over four blocks");
+    __shared__ __attribute__((aligned(16))) char lds[TA::BYTES + TB::BYTES];
+    if (workgroup() >= (int64_t)p.tiles_m * p.tiles_n) return;
+    int tm, tn;
+    tile_place((int)workgroup(), p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN, k0 = (int64_t)blockIdx.z * p.k_part;
+    const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = (wave >> 1) * (TM / 2), wn = (wave & 1) * (TN / 2);
+
+    uint4 ra[PA], rb[PB];
+    auto fetch = [&](int64_t k) {
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const int s = i * 256 + threadIdx.x, line = s / TA::LINE, chunk = s % TA::LINE;
+            if (AK) {
+                const int64_t row = m0 + line < p.M ? m0 + line : p.M - 1;
+                ra[i] = fetch_chunk((const T *)p.a + row * p.lda, k + chunk * TA::CH, k_end);
+            } else {
+                ra[i] = k + line < k_end ? fetch_chunk((const T *)p.a + (k + line) * p.lda, m0 + chunk * TA::CH, p.M) : uint4{0u, 0u, 0u, 0u};
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const int s = i * 256 + threadIdx.x, line = s / TB::LINE, chunk = s % TB::LINE;
+            if (BK) {
+                const int64_t row = n0 + line < p.N ? n0 + line : p.N - 1;
+                rb[i] = fetch_chunk((const T *)p.b + row * p.ldb, k + chunk * TB::CH, k_end);
+            } else {
+                rb[i] = k + line < k_end ? fetch_chunk((const T *)p.b + (k + line) * p.ldb, n0 + chunk * TB::CH, p.N) : uint4{0u, 0u, 0u, 0u};
+            }
+        }
+    };
+
+    mfma_acc_t acc[BM][BN];
+#pragma unroll
+    for (int i = 0; i < BM; ++i)
+#pragma unroll
+        for (int j = 0; j < BN; ++j) acc[i][j] = mfma_acc_t{0.f, 0.f, 0.f, 0.f};
+    if (k0 < k_end) fetch(k0);
+    for (int64_t k = k0; k < k_end; k += KB) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const int s = i * 256 + threadIdx.x;
+            *reinterpret_cast<uint4 *>(lds + TA::at(s / TA::LINE, s % TA::LINE)) = ra[i];
+        }
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            const int s = i * 256 + threadIdx.x;
+            *reinterpret_cast<uint4 *>(lds + TA::BYTES + TB::at(s / TB::LINE, s % TB::LINE)) = rb[i];
+        }
+        __syncthreads();
+        if (k + KB < k_end) fetch(k + KB);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint4 fa[BM], fb[BN];
+#pragma unroll
+            for (int i = 0; i < BM; ++i) fa[i] = TA::fragment(lds, wm, i, h, lane);
+#pragma unroll
+            for (int j = 0; j < BN; ++j) fb[j] = TB::fragment(lds + TA::BYTES, wn, j, h, lane);
+#pragma unroll
+            for (int i = 0; i < BM; ++i)
+#pragma unroll
+                for (int j = 0; j < BN; ++j) block_product<T>(fb[j], fa[i], acc[i][j]);
+        }
+    }
+    leave_tile<T, O, BM, BN>(p, e, m0 + wm, n0 + wn, lane, acc);
+}
+
+}  // namespace tt

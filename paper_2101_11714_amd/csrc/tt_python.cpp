@@ -175,6 +175,102 @@ struct Args {
         return r.data;
     }
 
+    // The arrays of a call live where it is enqueued: a tensor on another device than the current one is refused.
+    void here(int i)
+    {
+        if (!ok || a[i] == Py_None || !THPVariable_Check(a[i])) return;
+        const at::Tensor &t = THPVariable_Unpack(a[i]);
+        if (t.is_cuda() && t.get_device() != c10::hip::current_device()) fail("a tensor is on another device than the current one");
+    }
+    // a tensor [..., H, D], its last dimension dense: n rows of H heads of D columns
+    const tt_heads_t *heads(int i, tt_heads_t *h, int64_t *n, int64_t *D)
+    {
+        if (!ok || a[i] == Py_None) return nullptr;
+        const at::Tensor *t = tensor(a[i]);
+        if (!t) return nullptr;
+        *h = tt_heads_t{nullptr, 0, 0, 0, -1};
+        if (!t->is_cuda()) return fail("a device tensor is expected"), nullptr;
+        switch (t->scalar_type()) {
+        case at::kFloat: h->type = TT_F32; break;
+        case at::kBFloat16: h->type = TT_BF16; break;
+        case at::kHalf: h->type = TT_F16; break;
+        default: return fail("a tensor of 32- or 16-bit floating values is expected"), nullptr;
+        }
+        const int64_t d = t->dim();
+        if (d < 2) return fail("a tensor of heads, [..., heads, columns], is expected"), nullptr;
+        const int64_t H = t->size(d - 2), cols = t->size(d - 1);
+        if (H > INT32_MAX) return fail("too many heads"), nullptr;
+        if (cols > 1 && t->stride(d - 1) != 1) return fail("heads must be dense"), nullptr;
+        int64_t rows = 1, step = 0, next = 0;
+        bool any = false;
+        for (int64_t k = d - 3; k >= 0; --k) {
+            const int64_t size = t->size(k);
+            rows *= size;
+            if (size <= 1) continue;
+            if (!any) step = t->stride(k);
+            else if (t->stride(k) != next) return fail("rows must be evenly spaced"), nullptr;
+            next = t->stride(k) * size;
+            any = true;
+        }
+        if (*n >= 0 && (rows != *n || cols != *D)) return fail("an array has other sizes than the others"), nullptr;
+        *n = rows;
+        *D = cols;
+        h->heads = (int32_t)H;
+        h->ld = any ? step : H * cols;
+        h->ld_head = H > 1 ? t->stride(d - 2) : cols;
+        h->data = rows && H && cols ? t->data_ptr() : nullptr;
+        return h;
+    }
+    // None, or (positions, freqs, sections, neighbours)
+    const tt_rotation_t *rotation(int i, tt_rotation_t *r, int64_t n)
+    {
+        if (!ok || a[i] == Py_None) return nullptr;
+        if (!PyTuple_Check(a[i]) || PyTuple_GET_SIZE(a[i]) != 4) return fail("rotation is (positions, freqs, sections, neighbours)"), nullptr;
+        *r = tt_rotation_t{};
+        const at::Tensor *p = tensor(PyTuple_GET_ITEM(a[i], 0)), *f = tensor(PyTuple_GET_ITEM(a[i], 1));
+        if (!ok) return nullptr;
+        const bool wide = p->scalar_type() == at::kLong;
+        if (!p->is_cuda() || !(wide || p->scalar_type() == at::kInt) || p->dim() < 1) return fail("positions are a device tensor of int64 or int32"), nullptr;
+        if (!f->is_cuda() || f->scalar_type() != at::kFloat || !f->is_contiguous()) return fail("freqs is a contiguous device tensor of float32"), nullptr;
+        if (p->get_device() != c10::hip::current_device() || f->get_device() != c10::hip::current_device()) return fail("a tensor is on another device than the current one"), nullptr;
+        // [axes, rows...] or, of one axis, [rows...]; the rows in their order, dense
+        PyObject *seq = PySequence_Fast(PyTuple_GET_ITEM(a[i], 2), "sections are whole numbers");
+        if (!seq) {
+            ok = false;
+            return nullptr;
+        }
+        const Py_ssize_t axes = PySequence_Fast_GET_SIZE(seq);
+        if (axes < 1 || axes > 4) fail("rotation has one to four sections");
+        for (Py_ssize_t k = 0; ok && k < axes; ++k) {
+            const long long v = PyLong_AsLongLong(PySequence_Fast_GET_ITEM(seq, k));
+            if (v == -1 && PyErr_Occurred()) ok = false;
+            else if (v < 0 || v > INT32_MAX) fail("a section is out of range");
+            else r->sections[k] = (int32_t)v;
+        }
+        Py_DECREF(seq);
+        const int neighbours = ok ? PyObject_IsTrue(PyTuple_GET_ITEM(a[i], 3)) : 0;
+        if (neighbours < 0) ok = false;
+        if (!ok) return nullptr;
+        r->axes = (int32_t)axes;
+        r->neighbours = neighbours;
+        if (f->numel() > INT32_MAX) return fail("too many frequencies"), nullptr;
+        r->pairs = (int32_t)f->numel();
+        r->bits = wide ? 64 : 32;
+        if (p->numel() != axes * n) return fail("positions are [axes, rows]"), nullptr;
+        if (axes > 1 && p->size(0) != axes) return fail("positions are [axes, rows]"), nullptr;
+        if (p->numel() && (axes > 1 || p->size(0) == 1) && p->dim() > 1) {
+            if (!p->select(0, 0).is_contiguous()) return fail("the rows' positions must be dense"), nullptr;
+            r->ld_positions = axes > 1 ? p->stride(0) : 0;
+        } else if (!p->is_contiguous()) {
+            return fail("the rows' positions must be dense"), nullptr;
+        } else {
+            r->ld_positions = axes > 1 ? n : 0;
+        }
+        r->positions = p->numel() ? p->data_ptr() : nullptr;
+        r->freqs = r->pairs ? (const float *)f->data_ptr() : nullptr;
+        return r;
+    }
+
     int64_t integer(int i)
     {
         if (!ok) return 0;
@@ -821,6 +917,173 @@ TT_FUNCTION(add_rms_norm_bwd)
     return call([&](void *st) { return tt_add_rms_norm_bwd(&go, hp, rstd, w, wt, s, drop, x, r, gw, gwt, add ? 1 : 0, n, N, ws, wsb, st); });
 }
 
+// the workspace that is given, or scratch memory
+struct Room {
+    at::DataPtr mem;
+    void *data;
+    size_t bytes;
+
+    Room(void *ws, size_t given, size_t need) : data(ws), bytes(given)
+    {
+        if (ws) return;
+        mem = scratch(need, stream());
+        bytes = mem ? need : 0;
+        data = mem.get();
+    }
+};
+
+// x weight output bias activation residual pre workspace
+TT_FUNCTION(linear_fwd)
+{
+    Args g(args, nargs, 8);
+    if (!g.ok) return nullptr;
+    tt_rows_t x, w, out, res, pre;
+    int64_t n, K, N, Kw;
+    int32_t bt;
+    size_t wsb;
+    g.rows(0, &x, &n, &K);
+    g.rows(1, &w, &N, &Kw);
+    if (g.ok && Kw != K) g.fail("weight has another number of columns than x");
+    const tt_rows_t *o = g.rows_or_null(2, &out, n, N), *r = g.rows_or_null(5, &res, n, N), *p = g.rows_or_null(6, &pre, n, N);
+    const void *b = g.vector_or_null(3, N, &bt);
+    const int64_t act = g.integer(4);
+    void *ws = g.bytes_or_null(7, &wsb);
+    for (int i : {0, 1, 2, 3, 5, 6}) g.here(i);
+    if (!g.ok) return nullptr;
+    const Room room(ws, wsb, tt_linear_fwd_workspace_bytes(n, K, N, x.type));
+    return call([&](void *st) { return tt_linear_fwd(&x, &w, b, bt, (int32_t)act, r, p, o, n, K, N, room.data, room.bytes, st); });
+}
+
+// grad_output x weight pre activation grad_x grad_weight grad_bias accumulate workspace
+TT_FUNCTION(linear_bwd)
+{
+    Args g(args, nargs, 10);
+    if (!g.ok) return nullptr;
+    tt_rows_t go, xs, ws_, pre, gxs, gws;
+    int64_t n, N, K = -1;
+    int32_t bt;
+    size_t wsb;
+    g.rows(0, &go, &n, &N);
+    // K is the columns of whichever array of rows is there
+    auto matrix = [&](int i, tt_rows_t *r, int64_t rows) -> const tt_rows_t * {
+        int64_t m, cols;
+        if (!g.ok || args[i] == Py_None || !g.rows(i, r, &m, &cols)) return nullptr;
+        if (m != rows || (K >= 0 && cols != K)) g.fail("an array has other sizes than the others");
+        K = cols;
+        return r;
+    };
+    const tt_rows_t *x = matrix(1, &xs, n), *w = matrix(2, &ws_, N), *gx = matrix(5, &gxs, n), *gw = matrix(6, &gws, N);
+    const tt_rows_t *p = g.rows_or_null(3, &pre, n, N);
+    const int64_t act = g.integer(4);
+    void *gb = g.vector_or_null(7, N, &bt);
+    const bool add = g.truth(8);
+    void *ws = g.bytes_or_null(9, &wsb);
+    for (int i : {0, 1, 2, 3, 5, 6, 7}) g.here(i);
+    if (!g.ok) return nullptr;
+    if (K < 0) K = 0;
+    const Room room(ws, wsb, tt_linear_bwd_workspace_bytes(n, K, N, go.type, (int32_t)act));
+    return call([&](void *st) { return tt_linear_bwd(&go, x, w, p, (int32_t)act, gx, gw, gb, bt, add ? 1 : 0, n, K, N, room.data, room.bytes, st); });
+}
+
+// q k q_output k_output rotation norm q_weight k_weight eps
+TT_FUNCTION(qk_norm_rotate_fwd)
+{
+    Args g(args, nargs, 9);
+    if (!g.ok) return nullptr;
+    tt_heads_t q, k, qo, ko;
+    tt_rotation_t rot;
+    int64_t n = -1, D = -1;
+    int32_t qt, kt;
+    const tt_heads_t *pq = g.heads(0, &q, &n, &D), *pk = g.heads(1, &k, &n, &D), *pqo = g.heads(2, &qo, &n, &D), *pko = g.heads(3, &ko, &n, &D);
+    const tt_rotation_t *r = g.rotation(4, &rot, n);
+    const bool norm = g.truth(5);
+    const void *qw = g.vector_or_null(6, D, &qt), *kw = g.vector_or_null(7, D, &kt);
+    const float eps = g.real(8);
+    for (int i : {0, 1, 2, 3, 6, 7}) g.here(i);
+    if (!g.ok) return nullptr;
+    return call([&](void *st) { return tt_qk_norm_rotate_fwd(pq, pk, r, norm ? 1 : 0, eps, qw, qt, kw, kt, pqo, pko, n, D, st); });
+}
+
+// grad_q_output grad_k_output q k grad_q grad_k rotation norm q_weight k_weight grad_q_weight grad_k_weight eps accumulate workspace
+TT_FUNCTION(qk_norm_rotate_bwd)
+{
+    Args g(args, nargs, 15);
+    if (!g.ok) return nullptr;
+    tt_heads_t gqo, gko, q, k, gq, gk;
+    tt_rotation_t rot;
+    int64_t n = -1, D = -1;
+    int32_t qt, kt, gqt, gkt;
+    size_t wsb;
+    const tt_heads_t *pgqo = g.heads(0, &gqo, &n, &D), *pgko = g.heads(1, &gko, &n, &D), *pq = g.heads(2, &q, &n, &D), *pk = g.heads(3, &k, &n, &D), *pgq = g.heads(4, &gq, &n, &D),
+                     *pgk = g.heads(5, &gk, &n, &D);
+    const tt_rotation_t *r = g.rotation(6, &rot, n);
+    const bool norm = g.truth(7);
+    const void *qw = g.vector_or_null(8, D, &qt), *kw = g.vector_or_null(9, D, &kt);
+    void *gqw = g.vector_or_null(10, D, &gqt), *gkw = g.vector_or_null(11, D, &gkt);
+    const float eps = g.real(12);
+    const bool add = g.truth(13);
+    void *ws = g.bytes_or_null(14, &wsb);
+    for (int i : {0, 1, 2, 3, 4, 5, 8, 9, 10, 11}) g.here(i);
+    if (!g.ok) return nullptr;
+    const Room room(ws, wsb, gqw || gkw ? tt_qk_norm_rotate_bwd_workspace_bytes(n, pgqo ? gqo.heads : 0, pgko ? gko.heads : 0, D) : 0);
+    return call([&](void *st) {
+        return tt_qk_norm_rotate_bwd(pgqo, pgko, pq, pk, r, norm ? 1 : 0, eps, qw, qt, kw, kt, pgq, pgk, gqw, gqt, gkw, gkt, add ? 1 : 0, n, D, room.data, room.bytes, st);
+    });
+}
+
+// logits tokens logprob lse entropy top_ids top_logprobs scale workspace
+TT_FUNCTION(token_logprob_fwd)
+{
+    Args g(args, nargs, 9);
+    if (!g.ok) return nullptr;
+    tt_rows_t logits;
+    int64_t n, V, nl = 0, ns = 0, ne = 0, ni = 0, nt = 0, k = 0;
+    size_t wsb;
+    g.rows(0, &logits, &n, &V);
+    tt_tokens_t t{};
+    if (args[1] != Py_None) t = g.tokens(1);
+    float *logprob = g.f32_or_null(2, &nl), *lse = g.f32_or_null(3, &ns), *entropy = g.f32_or_null(4, &ne);
+    tt_tokens_t ids{};
+    if (args[5] != Py_None) {
+        ids = g.tokens(5);
+        if (g.ok) {
+            const at::Tensor &x = THPVariable_Unpack(args[5]);
+            k = x.dim() ? x.size(x.dim() - 1) : 0;
+            ni = ids.L;
+        }
+    }
+    float *top = g.f32_or_null(6, &nt);
+    const float scale = g.real(7);
+    void *ws = g.bytes_or_null(8, &wsb);
+    for (int i = 0; i < 7; ++i) g.here(i);
+    if (g.ok && ((args[2] != Py_None && nl != n) || (args[3] != Py_None && ns != n) || (args[4] != Py_None && ne != n))) g.fail("logprob, lse and entropy have one value per row");
+    if (g.ok && (k > 64 || ni != n * k || (args[6] != Py_None && nt != ni))) g.fail("top_ids and top_logprobs are [rows, k], k up to 64");
+    if (!g.ok) return nullptr;
+    const Room room(ws, wsb, tt_token_logprob_fwd_workspace_bytes(n, V, (int32_t)k));
+    return call([&](void *st) {
+        return tt_token_logprob_fwd(&logits, args[1] != Py_None ? &t : nullptr, scale, logprob, lse, entropy, (int32_t)k, const_cast<void *>(ids.data), ids.bits, top, n, V, room.data, room.bytes, st);
+    });
+}
+
+// logits tokens lse entropy grad_logprob grad_entropy grad_logits scale
+TT_FUNCTION(token_logprob_bwd)
+{
+    Args g(args, nargs, 8);
+    if (!g.ok) return nullptr;
+    tt_rows_t logits, out;
+    int64_t n, V, nl = 0, ne = 0, ng = 0, nh = 0;
+    g.rows(0, &logits, &n, &V);
+    tt_tokens_t t{};
+    if (args[1] != Py_None) t = g.tokens(1);
+    const float *lse = g.f32(2, &nl), *entropy = g.f32_or_null(3, &ne), *gl = g.f32_or_null(4, &ng), *ge = g.f32_or_null(5, &nh);
+    const tt_rows_t *o = g.rows_or_null(6, &out, n, V);
+    const float scale = g.real(7);
+    for (int i = 0; i < 7; ++i) g.here(i);
+    if (g.ok && (nl != n || (args[3] != Py_None && ne != n) || (args[4] != Py_None && ng != n) || (args[5] != Py_None && nh != n))) g.fail("lse, entropy and their gradients have one value per row");
+    if (!g.ok) return nullptr;
+    return call([&](void *st) { return tt_token_logprob_bwd(&logits, args[1] != Py_None ? &t : nullptr, scale, lse, entropy, gl, ge, o, n, V, st); });
+}
+
 #define TT_METHOD(name, function) {name, (PyCFunction)(void (*)(void))guarded<function>, METH_FASTCALL, nullptr}
 
 PyMethodDef methods[] = {
@@ -846,6 +1109,12 @@ PyMethodDef methods[] = {
     TT_METHOD("dropout_bwd", dropout_bwd),
     TT_METHOD("add_rms_norm_fwd", add_rms_norm_fwd),
     TT_METHOD("add_rms_norm_bwd", add_rms_norm_bwd),
+    TT_METHOD("linear_fwd", linear_fwd),
+    TT_METHOD("linear_bwd", linear_bwd),
+    TT_METHOD("qk_norm_rotate_fwd", qk_norm_rotate_fwd),
+    TT_METHOD("qk_norm_rotate_bwd", qk_norm_rotate_bwd),
+    TT_METHOD("token_logprob_fwd", token_logprob_fwd),
+    TT_METHOD("token_logprob_bwd", token_logprob_bwd),
     TT_METHOD("cache_build", cache_fill<tt_cache_build>),
     TT_METHOD("cache_refill", cache_fill<tt_cache_refill>),
     {nullptr, nullptr, 0, nullptr}};

@@ -1,0 +1,188 @@
+"""Host side of the matrix product, of the norm and rotation of queries and keys and of the log probabilities: refusals of the C ABI
+before anything touches a device, sizes of workspaces, and pins of the plain implementations that the kernels are tested against."""
+
+import ctypes as C
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import products_util as P
+from paper_2101_11714_amd import binding as B
+
+F32, BF16, F16, E4M3 = 0, 1, 2, 3
+
+
+def rows(data=64, ld=16, type=F32):
+    return C.byref(B.TTRows(data, ld, type))
+
+
+def heads(data=64, ld=64, ld_head=16, n=4, type=F32):
+    return C.byref(B.TTHeads(data, ld, ld_head, n, type))
+
+
+def toks(data=64, L=5, bits=64):
+    return C.byref(B.TTTokens(data, L, bits))
+
+
+def rot(positions=64, ld=0, freqs=64, bits=64, axes=1, sections=(8,), pairs=8, neighbours=0):
+    return C.byref(B.TTRotation(positions, ld, freqs, bits, axes, (C.c_int32 * 4)(*sections), pairs, neighbours))
+
+
+def test_struct_layouts_match_the_header():
+    assert C.sizeof(B.TTHeads) == 32 and B.TTHeads.ld_head.offset == 16 and B.TTHeads.heads.offset == 24 and B.TTHeads.type.offset == 28
+    assert C.sizeof(B.TTRotation) == 56 and B.TTRotation.freqs.offset == 16 and B.TTRotation.bits.offset == 24 and B.TTRotation.sections.offset == 32
+    assert B.TTRotation.pairs.offset == 48 and B.TTRotation.neighbours.offset == 52
+
+
+# (no call here may reach a launch: each is refused, or has nothing to do)
+def test_linear_calls_check_their_arguments():
+    l = B.lib()
+    fwd = lambda **k: (k.get("x", rows()), k.get("w", rows()), k.get("b"), k.get("bt", F32), k.get("act", 0), k.get("res"), k.get("pre"), k.get("out", rows()), k.get("rows", 5),  # noqa: E731
+                       k.get("K", 16), k.get("N", 16), k.get("ws"), k.get("bytes", 0), None)
+    for code, k in [(-1, dict(x=None)), (-1, dict(w=None)), (-1, dict(out=None)), (-1, dict(x=rows(data=None))), (-6, dict(x=rows(type=E4M3))), (-6, dict(w=rows(type=BF16))),
+                    (-6, dict(out=rows(type=BF16))), (-6, dict(x=rows(type=BF16), w=rows(type=BF16), out=rows(type=F16))), (-6, dict(res=rows(type=BF16))),
+                    (-6, dict(x=rows(type=F16), w=rows(type=F16), out=rows(), res=rows(type=F16))), (-6, dict(x=rows(type=F16), w=rows(type=F16), pre=rows())), (-3, dict(act=5)), (-3, dict(act=-1)),
+                    (-6, dict(b=64, bt=E4M3)), (-3, dict(b=66)), (-3, dict(out=rows(ld=15))), (-3, dict(pre=rows(ld=15))), (-3, dict(rows=-1)), (-3, dict(K=-1)), (-3, dict(N=-1)),
+                    (-6, dict(K=2**24 + 1)), (-6, dict(N=2**24 + 1, out=rows(ld=2**25))), (-6, dict(rows=2**31)), (-3, dict(x=rows(data=66))), (-6, dict(x=rows(ld=2**31 + 1))),
+                    (-4, dict(K=4096, ws=None)), (-4, dict(K=4096, ws=256, bytes=16)), (-3, dict(ws=8))]:
+        assert l.tt_linear_fwd(*fwd(**k)) == code, k
+        assert len(l.tt_last_error()) > 0
+    assert l.tt_linear_fwd(*fwd(rows=0)) == 0
+    assert l.tt_linear_fwd(*fwd(N=0)) == 0
+    need = l.tt_linear_bwd_workspace_bytes(5, 16, 16, F32, 1)
+    assert need > 0
+    bwd = lambda **k: (k.get("dy", rows()), k.get("x", rows()), k.get("w", rows()), k.get("pre", rows()), k.get("act", 1), k.get("dx", rows()), k.get("dw", rows()), k.get("db", 64),  # noqa: E731
+                       k.get("dbt", F32), k.get("add", 0), k.get("rows", 5), k.get("K", 16), k.get("N", 16), k.get("ws", 256), k.get("bytes", need), None)
+    for code, k in [(-1, dict(dy=None)), (-1, dict(x=None)), (-1, dict(w=None)), (-1, dict(pre=None)), (-3, dict(act=9)), (-6, dict(pre=rows(type=BF16))), (-6, dict(w=rows(type=BF16))),
+                    (-6, dict(x=rows(type=F16))), (-6, dict(dx=rows(type=F16))), (-6, dict(dw=rows(type=BF16))), (-6, dict(dbt=E4M3)), (-3, dict(db=65)), (-4, dict(ws=None)), (-4, dict(bytes=need - 256)),
+                    (-3, dict(ws=24)), (-3, dict(dx=rows(ld=15))), (-3, dict(dw=rows(ld=0))), (-6, dict(K=2**24 + 1))]:
+        assert l.tt_linear_bwd(*bwd(**k)) == code, k
+    assert l.tt_linear_bwd(*bwd(dx=None, dw=None, db=None)) == 0
+    assert l.tt_linear_bwd(*bwd(rows=0, add=1, db=None)) == 0
+
+
+def test_linear_workspaces_are_enough_for_fewer_rows():
+    l = B.lib()
+    counts = [1, 2, 31, 32, 33, 127, 128, 129, 255, 256, 257, 1000, 1024, 4096, 16384, 20_000]
+    for K, N in [(16, 16), (4096, 4096), (777, 1283), (8192, 64), (64, 8192), (50_000, 10), (1024, 131072)]:
+        for type in (F32, BF16):
+            for f in (lambda n: l.tt_linear_fwd_workspace_bytes(n, K, N, type), lambda n: l.tt_linear_bwd_workspace_bytes(n, K, N, type, 1)):
+                sizes = [f(n) for n in counts]
+                assert sizes == sorted(sizes), (K, N, type, sizes)
+    assert l.tt_linear_fwd_workspace_bytes(5, 16, 2**25, F32) == 0 and l.tt_linear_fwd_workspace_bytes(5, 16, 16, 7) == 0
+
+
+def test_rotation_calls_check_their_arguments():
+    l = B.lib()
+    fwd = lambda **k: (k.get("q", heads()), k.get("k", heads()), k.get("rot", rot()), k.get("norm", 1), k.get("eps", 1e-6), k.get("qw"), k.get("qt", F32), k.get("kw"), k.get("kt", F32),  # noqa: E731
+                       k.get("qo", heads()), k.get("ko", heads()), k.get("rows", 5), k.get("D", 16), None)
+    bad = [(-1, dict(q=None)), (-1, dict(qo=None)), (-1, dict(k=None)), (-1, dict(ko=None)), (-6, dict(q=heads(type=E4M3))), (-6, dict(k=heads(type=BF16))), (-6, dict(qo=heads(type=F16))),
+           (-2, dict(qo=heads(n=5))), (-2, dict(ko=heads(n=3))), (-3, dict(qo=heads(ld_head=15))), (-3, dict(qo=heads(ld=63))), (-3, dict(q=heads(data=66))), (-3, dict(q=heads(ld=-1))),
+           (-6, dict(q=heads(ld=2**31 + 1))), (-1, dict(q=heads(data=None))), (-3, dict(rows=-1)), (-3, dict(D=-1)), (-6, dict(D=513)), (-6, dict(rows=2**31)), (-3, dict(eps=-1.0)),
+           (-3, dict(eps=float("nan"))), (-3, dict(norm=0, qw=64)), (-6, dict(qw=64, qt=E4M3)), (-3, dict(kw=66)), (-3, dict(rot=rot(axes=0))), (-3, dict(rot=rot(axes=5))), (-3, dict(rot=rot(bits=16))),
+           (-3, dict(rot=rot(pairs=9, sections=(9,)))), (-3, dict(rot=rot(sections=(7,)))), (-3, dict(rot=rot(axes=2, sections=(9, -1)))), (-3, dict(rot=rot(pairs=-1, sections=(0,)))),
+           (-1, dict(rot=rot(positions=None))), (-1, dict(rot=rot(freqs=None))), (-3, dict(rot=rot(positions=68))), (-3, dict(rot=rot(freqs=66))), (-3, dict(rot=rot(ld=-1)))]
+    for code, k in bad:
+        assert l.tt_qk_norm_rotate_fwd(*fwd(**k)) == code, k
+        assert len(l.tt_last_error()) > 0
+    for k in (dict(rows=0), dict(D=0, rot=None), dict(q=heads(n=0), qo=heads(n=0), k=None, ko=None)):
+        assert l.tt_qk_norm_rotate_fwd(*fwd(**k)) == 0, k
+    need = l.tt_qk_norm_rotate_bwd_workspace_bytes(5, 4, 4, 16)
+    assert need > 0
+    bwd = lambda **k: (k.get("gqo", heads()), k.get("gko", heads()), k.get("q", heads()), k.get("k", heads()), k.get("rot", rot()), k.get("norm", 1), k.get("eps", 1e-6), k.get("qw"), k.get("qt", F32),  # noqa: E731
+                       k.get("kw"), k.get("kt", F32), k.get("gq", heads()), k.get("gk", heads()), k.get("gqw", 64), k.get("gqt", F32), k.get("gkw", 64), k.get("gkt", F32), 0, k.get("rows", 5), k.get("D", 16),
+                       k.get("ws", 256), k.get("bytes", need), None)
+    for code, k in [(-1, dict(gqo=None)), (-1, dict(gko=None)), (-1, dict(q=None)), (-1, dict(k=None)), (-1, dict(gq=None)), (-2, dict(gq=heads(n=3))), (-2, dict(k=heads(n=3))), (-6, dict(gq=heads(type=BF16))),
+                    (-6, dict(q=heads(type=BF16))), (-3, dict(norm=0)), (-3, dict(gko=None, gk=None)), (-6, dict(gqt=E4M3)), (-3, dict(gkw=66)), (-4, dict(ws=None)), (-4, dict(bytes=need - 4)), (-3, dict(ws=24)),
+                    (-3, dict(rot=rot(sections=(7,)))), (-6, dict(D=513))]:
+        assert l.tt_qk_norm_rotate_bwd(*bwd(**k)) == code, k
+    assert l.tt_qk_norm_rotate_bwd(*bwd(rows=0, gqw=None, gkw=None)) == 0
+    sizes = [l.tt_qk_norm_rotate_bwd_workspace_bytes(n, 4, 2, 128) for n in (1, 2, 100, 1023, 1024, 1025, 100_000)]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+
+
+def test_logprob_calls_check_their_arguments():
+    l = B.lib()
+    fwd = lambda **k: (k.get("x", rows()), k.get("t", toks()), k.get("scale", 1.0), k.get("lp", 64), k.get("lse", 64), k.get("h", 64), k.get("k", 0), k.get("ids"), k.get("bits", 64), k.get("top"),  # noqa: E731
+                       k.get("rows", 5), k.get("V", 16), k.get("ws"), k.get("bytes", 0), None)
+    for code, k in [(-1, dict(x=None)), (-1, dict(t=None)), (-1, dict(x=rows(data=None))), (-6, dict(x=rows(type=E4M3))), (-2, dict(t=toks(L=4))), (-3, dict(t=toks(bits=16))), (-1, dict(t=toks(data=None))),
+                    (-3, dict(t=toks(data=68))), (-3, dict(scale=0.0)), (-3, dict(scale=-1.0)), (-3, dict(scale=float("nan"))), (-3, dict(scale=float("inf"))), (-3, dict(lp=66)), (-3, dict(lse=66)), (-3, dict(h=66)),
+                    (-6, dict(k=65, ids=64)), (-6, dict(k=-1)), (-1, dict(k=3)), (-3, dict(k=3, ids=64, bits=16)), (-3, dict(k=3, ids=68)), (-3, dict(k=3, ids=64, top=66)), (-3, dict(rows=-1)), (-3, dict(V=0)),
+                    (-6, dict(V=2**30 + 1)), (-4, dict(V=100_000)), (-4, dict(V=100_000, ws=256, bytes=16)), (-3, dict(ws=8))]:
+        assert l.tt_token_logprob_fwd(*fwd(**k)) == code, k
+        assert len(l.tt_last_error()) > 0
+    assert l.tt_token_logprob_fwd(*fwd(rows=0, t=toks(L=0))) == 0
+    bwd = lambda **k: (k.get("x", rows()), k.get("t", toks()), k.get("scale", 1.0), k.get("lse", 64), k.get("h", 64), k.get("g", 64), k.get("gh", 64), k.get("out", rows()), k.get("rows", 5), k.get("V", 16), None)  # noqa: E731
+    for code, k in [(-1, dict(x=None)), (-1, dict(out=None)), (-1, dict(t=None)), (-1, dict(lse=None)), (-1, dict(h=None)), (-6, dict(out=rows(type=BF16))), (-3, dict(out=rows(ld=15))), (-2, dict(t=toks(L=6))),
+                    (-3, dict(scale=0.0)), (-3, dict(lse=66)), (-3, dict(g=66)), (-3, dict(gh=66)), (-3, dict(V=0)), (-3, dict(rows=-1))]:
+        assert l.tt_token_logprob_bwd(*bwd(**k)) == code, k
+    assert l.tt_token_logprob_bwd(*bwd(rows=0, t=toks(L=0))) == 0
+    for V in (100, 50257, 131072):
+        for k in (0, 20, 64):
+            sizes = [l.tt_token_logprob_fwd_workspace_bytes(n, V, k) for n in (1, 2, 3, 24, 511, 512, 513, 10_000)]
+            assert sizes == sorted(sizes), sizes
+
+
+def test_activation_names():
+    with pytest.raises(ValueError):
+        B._activation("tanh")
+    assert [B._activation(n) for n in P.ACTS] == [0, 1, 2, 3, 4]
+
+
+# ---- the plain implementations -------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("kind", P.ACTS)
+def test_plain_product_is_autograd_s(kind):
+    g = torch.Generator().manual_seed(1)
+    x, w, b = (torch.randn(s, generator=g, dtype=torch.float64, requires_grad=True) for s in ((6, 9), (5, 9), (5,)))
+    dy = torch.randn((6, 5), generator=g, dtype=torch.float64)
+    F = torch.nn.functional
+    z = F.linear(x, w, b)
+    y = {"none": lambda v: v, "relu": F.relu, "gelu": F.gelu, "gelu_tanh": lambda v: F.gelu(v, approximate="tanh"), "silu": F.silu}[kind](z)
+    y.backward(dy)
+    assert np.allclose(P.linear_fwd(x, w, b, kind, None)[0], y.detach())
+    dx, dw, db, _, _, _ = P.linear_bwd(dy, x, w, z, kind)
+    assert np.allclose(dx, x.grad) and np.allclose(dw, w.grad) and np.allclose(db, b.grad)
+
+
+@pytest.mark.parametrize("neighbours", [False, True])
+def test_plain_rotation_is_a_turn_and_its_gradient_autograd_s(neighbours):
+    g = torch.Generator().manual_seed(2)
+    x, w = (torch.randn(s, generator=g, dtype=torch.float64, requires_grad=True) for s in ((4, 3, 12), (12,)))
+    dy = torch.randn((4, 3, 12), generator=g, dtype=torch.float64)
+    positions = torch.tensor([[0, 1, 5, -2], [7, 7, 0, 1]])
+    freqs = torch.tensor([1.0, 0.5, 0.25, 0.125])
+    r = (positions, freqs, (1, 3), neighbours)
+    a = torch.stack([positions[0] * 1.0, positions[1] * 0.5, positions[1] * 0.25, positions[1] * 0.125], 1).double()[:, None]
+    u = x * (x.square().mean(2, keepdim=True) + 1e-3).rsqrt() * w
+    first, second = (u[..., 0:8:2], u[..., 1:8:2]) if neighbours else (u[..., 0:4], u[..., 4:8])
+    z = torch.complex(first, second) * torch.polar(torch.ones_like(a), a)
+    y = torch.stack([z.real, z.imag], 3).flatten(2) if neighbours else torch.cat([z.real, z.imag], 2)
+    y = torch.cat([y, u[..., 8:]], 2)
+    y.backward(dy)
+    assert np.allclose(P.rotate_fwd(x, w, r, True, 1e-3)[0], y.detach())
+    dx, dw, _, _ = P.rotate_bwd(dy, x, w, r, True, 1e-3)
+    assert np.allclose(dx, x.grad) and np.allclose(dw, w.grad)
+
+
+def test_plain_log_probabilities_are_autograd_s():
+    g = torch.Generator().manual_seed(3)
+    x = torch.randn((5, 11), generator=g, dtype=torch.float64, requires_grad=True)
+    tokens = torch.tensor([3, 0, -1, 10, 11])
+    gl, ge = (torch.randn(5, generator=g, dtype=torch.float64) for _ in range(2))
+    log_p = torch.log_softmax(1.5 * x, 1)
+    there = (tokens >= 0) & (tokens < 11)
+    lp = torch.where(there, log_p.gather(1, tokens.clamp(0, 10)[:, None])[:, 0], 0.0)
+    h = -(log_p.exp() * log_p).sum(1)
+    (lp * gl + h * ge).sum().backward()
+    got, lse, ent, ids, top = P.logprob_fwd(x, tokens, 1.5, 4)
+    assert np.allclose(got, lp.detach()) and np.allclose(ent, h.detach()) and np.allclose(lse, torch.logsumexp(1.5 * x, 1).detach())
+    want = torch.topk(log_p, 4, dim=1)
+    assert np.array_equal(ids, want.indices.numpy()) and np.allclose(top, want.values.detach())
+    assert np.allclose(P.logprob_bwd(x, tokens, 1.5, torch.from_numpy(lse), torch.from_numpy(ent), gl, ge)[0], x.grad)
+    none = torch.full((1, 4), -math.inf, dtype=torch.float64)
+    got = P.logprob_fwd(none, torch.tensor([1]), 1.0, 2)
+    assert got[0][0] == -math.inf and got[1][0] == -math.inf and got[2][0] == 0 and (got[3] == -1).all()
