@@ -103,16 +103,15 @@ __device__ __forceinline__ void finish8(const EpilogueArgs &e, int64_t m, int64_
 //                 columns to 16 lanes), 32-bit values one by one.
 // In both, 16-byte chunks are permuted along a row by an exclusive or with bits of its number, so that the lanes that read at
 // the same time find different banks.
-// The second operand's blocks of 16 rows are interleaved (JOIN): of 64 rows block b has those with (row / 4) % 4 == b.  It is the
-// instruction's first operand, whose rows go to a lane's four registers in fours, so that over four blocks a lane has
-// 16 neighbouring columns of one row of C.
+// The second operand is the instruction's first, whose rows go to a lane's four registers in fours: a lane has four neighbouring
+// columns of one row of C.
 
 template <typename T>
 constexpr int PB_K = 128 / (int)sizeof(T);
 
 constexpr int BLOCK = 16;
 
-template <typename T, bool KDENSE, bool JOIN, int ROWS>
+template <typename T, bool KDENSE, int ROWS>
 struct OperandTile {
     static constexpr int CH = 16 / sizeof(T);                // values of a chunk
     static constexpr int LINE = KDENSE ? 8 : ROWS / CH;      // chunks of a line
@@ -122,11 +121,8 @@ struct OperandTile {
 
     static __device__ __forceinline__ int swizzle(int line)
     {
-        int x;
-        if (KDENSE) x = JOIN ? (line & 3) | (line >> 2 & 4) : line & 7;
-        else if (sizeof(T) == 4) x = JOIN ? line >> 2 & 3 : (line >> 2 & 3) << 2;
-        else x = JOIN ? (line & 1) | (line & 2) << 2 : (line & 3) << 1;
-        return x & (LINE - 1);
+        const int x = KDENSE ? line : sizeof(T) == 4 ? (line >> 2) << 2 : line << 1;
+        return x & (KDENSE ? 7 : sizeof(T) == 4 ? 12 : 6) & (LINE - 1);
     }
     // byte offset of a chunk
     static __device__ __forceinline__ int at(int line, int chunk) { return (line * LINE + (chunk ^ swizzle(line))) * 16; }
@@ -134,21 +130,19 @@ struct OperandTile {
     // this lane's 16 bytes of block b of the wave's rows from `row0` on, half h of the step
     static __device__ __forceinline__ uint4 fragment(const char *lds, int row0, int b, int h, int lane)
     {
-        const int r = lane & 15, q = lane >> 4;
+        const int r = lane & 15, q = lane >> 4, first = row0 + 16 * b;
         if constexpr (KDENSE) {
-            const int row = row0 + (JOIN ? 64 * (b >> 2) + 16 * (r >> 2) + 4 * (b & 3) + (r & 3) : 16 * b + r);
-            return *reinterpret_cast<const uint4 *>(lds + at(row, 4 * h + q));
+            return *reinterpret_cast<const uint4 *>(lds + at(first + r, 4 * h + q));
         } else if constexpr (sizeof(T) == 2) {
             typedef short Four __attribute__((ext_vector_type(4)));
             typedef __attribute__((address_space(3))) Four *Shared;
-            const int col = row0 + (JOIN ? 64 * (b >> 2) + 16 * (r & 3) + 4 * (b & 3) : 16 * b + 4 * (r & 3));
-            const int k = 32 * h + 8 * q + (r >> 2);
+            const int col = first + 4 * (r & 3), k = 32 * h + 8 * q + (r >> 2);
             struct { Four lo, hi; } x;
             x.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared)(lds + at(k, col >> 3) + (col & 4) * 2));
             x.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Shared)(lds + at(k + 4, col >> 3) + (col & 4) * 2));
             return __builtin_bit_cast(uint4, x);
         } else {
-            const int col = row0 + (JOIN ? 64 * (b >> 2) + 16 * (r >> 2) + 4 * (b & 3) + (r & 3) : 16 * b + r);
+            const int col = first + r;
             uint4 x;
             uint32_t *w = reinterpret_cast<uint32_t *>(&x);
 #pragma unroll
@@ -230,30 +224,44 @@ __device__ __forceinline__ void tile_place(int tile, int tiles_m, int tiles_n, i
     tm = band * BAND + rest - tn * rows;
 }
 
-// A wave's sums on their way out: parts' sums as they are, others through the epilogue.
-template <typename T, typename O, int BM, int BN>
-__device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueArgs &e, int64_t m0, int64_t n0, int lane, mfma_acc_t (&acc)[BM][BN])
+// The workgroups of one XCD, which have every eighth number, take neighbouring tiles, whose operands its L2 then holds.
+__device__ __forceinline__ int xcd_tile(int id, int tiles)
 {
+    const int each = tiles / 8, more = tiles % 8, xcd = id % 8, nth = id / 8;
+    return xcd * each + min(xcd, more) + nth;
+}
+
+// A wave's sums on their way out, 16 * BM rows of 64: SOME blocks of 16 rows at a time through LDS of the wave's own (4 KB a block), from where a
+// lane takes eight neighbouring columns, eight lanes a row's 64, through the epilogue, or as they are where they are a part's.
+constexpr int LEAVE_BLOCK = BLOCK * 64 * 4;
+
+template <typename T, typename O, int BM, int SOME>
+__device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueArgs &e, int64_t m0, int64_t n0, int lane, char *lds, mfma_acc_t (&acc)[BM][4])
+{
+    const int c = lane & 7;
+    const int64_t n = n0 + 8 * c;
+    const int have = p.N - n < 8 ? (int)(p.N - n) : 8;
+    float bias[8];
+    if (!p.part) load_bias(e, n, have, bias);
 #pragma unroll
-    for (int j4 = 0; j4 < BN; j4 += 4) {
-        const int64_t n = n0 + 16 * j4 + 16 * (lane >> 4);
+    for (int i0 = 0; i0 < BM; i0 += SOME) {
 #pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            const int64_t left = p.N - (n + 8 * half);
-            if (left <= 0) continue;
-            const int have = left < 8 ? (int)left : 8;
-            float bias[8];
-            if (!p.part) load_bias(e, n + 8 * half, have, bias);
+        for (int i = 0; i < SOME; ++i)
 #pragma unroll
-            for (int i = 0; i < BM; ++i) {
-                const int64_t m = m0 + 16 * i + (lane & 15);
-                if (m >= p.M) continue;
-                float v[8];
-#pragma unroll
-                for (int c = 0; c < 8; ++c) v[c] = acc[i][j4 + 2 * half + (c >> 2)][c & 3];
-                if (p.part) put8(p.part + ((int64_t)blockIdx.z * p.M + m) * p.ld_part + n + 8 * half, 8, v);
-                else finish8<T, O>(e, m, n + 8 * half, have, bias, v);
+            for (int j = 0; j < 4; ++j) {
+                const int row = lane & 15, chunk = (4 * j + (lane >> 4)) ^ row;
+                *reinterpret_cast<mfma_acc_t *>(lds + i * LEAVE_BLOCK + row * 256 + chunk * 16) = acc[i0 + i][j];
             }
+#pragma unroll 1
+        for (int r = lane >> 3; r < 16 * SOME; r += 8) {
+            const int row = r & 15;
+            float v[8];
+            *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(lds + r * 256 + ((2 * c) ^ row) * 16);
+            *reinterpret_cast<float4 *>(v + 4) = *reinterpret_cast<const float4 *>(lds + r * 256 + ((2 * c + 1) ^ row) * 16);
+            const int64_t m = m0 + 16 * i0 + r;
+            if (m >= p.M || have <= 0) continue;
+            if (p.part) put8<true>(p.part + ((int64_t)blockIdx.z * p.M + m) * p.ld_part + n, 8, v);
+            else finish8<T, O>(e, m, n, have, bias, v);
         }
     }
 }
@@ -280,10 +288,12 @@ __global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, Epilogue
 template <typename T, typename O, bool AK, bool BK, int TM, int TN>
 __global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArgs e)
 {
-    typedef OperandTile<T, AK, false, TM> TA;
-    typedef OperandTile<T, BK, true, TN> TB;
+    typedef OperandTile<T, AK, TM> TA;
+    typedef OperandTile<T, BK, TN> TB;
     constexpr int KB = PB_K<T>, BM = TM / 2 / BLOCK, BN = TN / 2 / BLOCK, PA = TA::CHUNKS / 256, PB = TB::CHUNKS / 256;
-    static_assert(BN % 4 == 0, "a lane's columns are neighbours over four blocks");
+    static_assert(BN == 4, "what a wave leaves is 64 columns wide");
+    constexpr int SOME = BM < 2 ? 1 : 2;
+    static_assert(4 * SOME * LEAVE_BLOCK <= TA::BYTES + TB::BYTES, "room for the sums");
     __shared__ __attribute__((aligned(16))) char lds[TA::BYTES + TB::BYTES];
     if (workgroup() >= (int64_t)p.tiles_m * p.tiles_n) return;
     int tm, tn;
@@ -349,7 +359,8 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArg
                 for (int j = 0; j < BN; ++j) block_product<T>(fb[j], fa[i], acc[i][j]);
         }
     }
-    leave_tile<T, O, BM, BN>(p, e, m0 + wm, n0 + wn, lane, acc);
+    __syncthreads();
+    leave_tile<T, O, BM, SOME>(p, e, m0 + wm, n0 + wn, lane, lds + wave * SOME * LEAVE_BLOCK, acc);
 }
 
 }  // namespace tt

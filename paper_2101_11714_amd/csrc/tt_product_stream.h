@@ -1,0 +1,158 @@
+// Products of 16-bit operands that are whole 16-byte chunks: operands straight from memory into LDS, two steps' worth.
+#pragma once
+
+#include "tt_product.h"
+
+namespace tt {
+
+constexpr uint32_t PS_RECORDS = 0x7ffffff0u, PS_NOWHERE = 0x80000000u;       // a buffer's bytes; an offset behind them: zeros are loaded
+constexpr int64_t PS_MOST_STRIDE = 1 << 22;                  // of rows, so that offsets in a tile stay below PS_RECORDS
+
+template <bool WIDE>
+struct StreamShape {
+    static constexpr int TILE = WIDE ? 256 : 128, THREADS = WIDE ? 512 : 256, WAVES = THREADS / WAVE;
+    static constexpr int BM = TILE / 2 / BLOCK;              // a wave's blocks along m; along n they are four
+    static constexpr int STAGE = 2 * TILE * 128, LDS = 2 * STAGE;
+};
+
+// What a wave loads of an operand's tile: PIECES times 64 chunks, one per lane, which go to 1 KB of LDS in the lanes' order.
+template <typename T, bool KDENSE, bool WIDE>
+struct Stream {
+    typedef StreamShape<WIDE> S;
+    typedef OperandTile<T, KDENSE, S::TILE> Tile;
+    static constexpr int PIECES = Tile::CHUNKS / S::THREADS, CH = Tile::CH;
+    const char *base;            // of the step's values
+    int64_t step;                // bytes to the next one's
+    uint32_t at[PIECES];         // the lane's offsets
+    int k[PIECES];               // where in the step their values of k begin
+    int wave;
+
+    __device__ __forceinline__ Stream(const void *data, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int w, int lane) : wave(w)
+    {
+        base = (const char *)data + (KDENSE ? row0 * ld + k0 : k0 * ld + row0) * (int64_t)sizeof(T);
+        step = (KDENSE ? (int64_t)PB_K<T> : PB_K<T> * ld) * (int64_t)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int s = (i * S::WAVES + wave) * WAVE + lane, line = s / Tile::LINE, chunk = (s % Tile::LINE) ^ Tile::swizzle(line);
+            if (KDENSE) {
+                const int64_t left = rows - row0 - 1;
+                at[i] = (uint32_t)((line < left ? line : (int)left) * ld + chunk * CH) * (uint32_t)sizeof(T);
+                k[i] = chunk * CH;
+            } else {
+                at[i] = row0 + chunk * CH < rows ? (uint32_t)(line * ld + chunk * CH) * (uint32_t)sizeof(T) : PS_NOWHERE;
+                k[i] = line;
+            }
+        }
+    }
+    // `left`: values of k from the step's first on.  In assembly, since the compiler takes every read of LDS for one of what is still on its way and waits
+    // for it; nothing but LDS and M0 is written, which nothing else here uses, and the waits are landed()'s.
+    __device__ __forceinline__ void load(char *lds, int64_t left)
+    {
+        typedef uint32_t Words __attribute__((ext_vector_type(4)));
+        const uint64_t from = (uint64_t)base;
+        const Words r = {(uint32_t)from, (uint32_t)(from >> 32), PS_RECORDS, 0x00020000u};
+        const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint32_t o = left >= PB_K<T> || k[i] < left ? at[i] : PS_NOWHERE;
+            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * S::WAVES * 1024), "v"(o), "s"(r) : "memory");
+        }
+        base += step;
+    }
+    static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+};
+
+// WIDE: tiles of 256 x 256 by eight waves of 128 x 64 in two groups of four, one of each group on every SIMD.  A step is two halves, each first
+// read from LDS into registers and then multiplied; the second group is one phase behind, so that a SIMD's matrix core works for one
+// wave while the other one reads.  A barrier ends every phase.
+// Else: tiles of 128 x 128 by four waves of 64 x 64, two workgroups on a compute unit, which find their turns by themselves.
+template <typename T, typename O, bool AK, bool BK, bool WIDE>
+__global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_kernel(ProductArgs p, EpilogueArgs e)
+{
+    typedef StreamShape<WIDE> S;
+    typedef Stream<T, AK, WIDE> SA;
+    typedef Stream<T, BK, WIDE> SB;
+    constexpr int KB = PB_K<T>, BM = S::BM, BN = 4;
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, id = workgroup();
+    if (id >= tiles) return;
+    int tm, tn;
+    tile_place(xcd_tile((int)id, (int)tiles), p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * S::TILE, n0 = (int64_t)tn * S::TILE, k0 = (int64_t)blockIdx.z * p.k_part;
+    const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> (WIDE ? 2 : 1);
+    const int wm = group * (S::TILE / 2), wn = (wave & (WIDE ? 3 : 1)) * 64;
+    SA a(p.a, p.lda, m0, p.M, k0, wave, lane);
+    SB b(p.b, p.ldb, n0, p.N, k0, wave, lane);
+
+    mfma_acc_t acc[BM][BN];
+#pragma unroll
+    for (int i = 0; i < BM; ++i)
+#pragma unroll
+        for (int j = 0; j < BN; ++j) acc[i][j] = mfma_acc_t{0.f, 0.f, 0.f, 0.f};
+    uint4 fa[BM], fb[BN];
+    auto read = [&](const char *stage, int h) {
+#pragma unroll
+        for (int j = 0; j < BN; ++j) fb[j] = SB::Tile::fragment(stage + SA::Tile::BYTES, wn, j, h, lane);
+#pragma unroll
+        for (int i = 0; i < BM; ++i) fa[i] = SA::Tile::fragment(stage, wm, i, h, lane);
+    };
+    auto multiply = [&] {
+        __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+        for (int i = 0; i < BM; ++i)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) block_product<T>(fb[j], fa[i], acc[i][j]);
+        __builtin_amdgcn_s_setprio(0);
+    };
+    auto phase = [] {
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    if (k0 < k_end) {
+        a.load(lds, k_end - k0);
+        b.load(lds + SA::Tile::BYTES, k_end - k0);
+        SA::landed();
+    }
+    phase();
+    int stage = 0;
+    if (WIDE && group) phase();
+    for (int64_t k = k0; k < k_end; k += KB, stage ^= 1) {
+        const char *now = lds + stage * S::STAGE;
+        char *next = lds + (stage ^ 1) * S::STAGE;
+        const bool more = k + KB < k_end;
+        if (WIDE) {
+            read(now, 0);
+            if (more) {
+                a.load(next, k_end - k - KB);
+                b.load(next + SA::Tile::BYTES, k_end - k - KB);
+            }
+            phase();
+            multiply();
+            phase();
+            read(now, 1);
+            if (group) SA::landed();
+            phase();
+            multiply();
+            if (!group) SA::landed();
+            phase();
+        } else {
+            if (more) {
+                a.load(next, k_end - k - KB);
+                b.load(next + SA::Tile::BYTES, k_end - k - KB);
+            }
+            read(now, 0);
+            multiply();
+            read(now, 1);
+            multiply();
+            SA::landed();
+            phase();
+        }
+    }
+    if (WIDE && !group) phase();
+    leave_tile<T, O, BM, 4>(p, e, m0 + wm, n0 + wn, lane, lds + wave * 4 * LEAVE_BLOCK, acc);
+}
+
+}  // namespace tt

@@ -44,7 +44,7 @@ def vector(g, n, dtype, mean=0.0):
 
 # rows, K, N: one of everything, edges of tiles and of steps, few rows over a long sum, wide and narrow
 PRODUCTS = [(1, 1, 1), (1, 7, 3), (2, 8, 8), (5, 33, 17), (16, 64, 64), (17, 65, 129), (31, 128, 100), (32, 256, 256), (33, 31, 8), (64, 64, 128), (100, 200, 300), (127, 96, 127), (128, 128, 128),
-            (129, 129, 129), (257, 72, 40), (256, 512, 384), (3, 4096, 40), (1, 5000, 130), (300, 1000, 16), (40, 8, 1000), (513, 640, 257), (1025, 40, 520)]
+            (129, 129, 129), (257, 72, 40), (256, 512, 384), (3, 4096, 40), (1, 5000, 130), (300, 1000, 16), (40, 8, 1000), (513, 640, 257), (1025, 40, 520), (65, 96, 72), (200, 1096, 328), (3000, 264, 1400), (2056, 72, 3592)]
 
 
 def output_bound(y, z, mag, n, u, tiny):
@@ -519,9 +519,9 @@ def test_a_captured_run_replays_on_new_inputs():
 
 
 def test_a_recorded_call_without_its_workspace_is_refused():
-    x, w = torch.zeros((4, 4096), device="cuda:0"), torch.zeros((64, 4096), device="cuda:0")
-    out = torch.empty((4, 64), device="cuda:0")
-    assert B.linear_fwd_workspace_bytes(4, 4096, 64, F32) > 0
+    x, w = torch.zeros((100, 4096), device="cuda:0"), torch.zeros((64, 4096), device="cuda:0")
+    out = torch.empty((100, 64), device="cuda:0")
+    assert B.linear_fwd_workspace_bytes(100, 4096, 64, F32) > 0
     graph = torch.cuda.CUDAGraph()
     with pytest.raises(B.TTError) as e:
         with torch.cuda.graph(graph):

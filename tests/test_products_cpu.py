@@ -46,7 +46,7 @@ def test_linear_calls_check_their_arguments():
                     (-6, dict(x=rows(type=F16), w=rows(type=F16), out=rows(), res=rows(type=F16))), (-6, dict(x=rows(type=F16), w=rows(type=F16), pre=rows())), (-3, dict(act=5)), (-3, dict(act=-1)),
                     (-6, dict(b=64, bt=E4M3)), (-3, dict(b=66)), (-3, dict(out=rows(ld=15))), (-3, dict(pre=rows(ld=15))), (-3, dict(rows=-1)), (-3, dict(K=-1)), (-3, dict(N=-1)),
                     (-6, dict(K=2**24 + 1)), (-6, dict(N=2**24 + 1, out=rows(ld=2**25))), (-6, dict(rows=2**31)), (-3, dict(x=rows(data=66))), (-6, dict(x=rows(ld=2**31 + 1))),
-                    (-4, dict(K=4096, ws=None)), (-4, dict(K=4096, ws=256, bytes=16)), (-3, dict(ws=8))]:
+                    (-4, dict(rows=100, K=4096, ws=None)), (-4, dict(rows=100, K=4096, ws=256, bytes=16)), (-3, dict(ws=8))]:
         assert l.tt_linear_fwd(*fwd(**k)) == code, k
         assert len(l.tt_last_error()) > 0
     assert l.tt_linear_fwd(*fwd(rows=0)) == 0
