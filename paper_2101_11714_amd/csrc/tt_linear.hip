@@ -5,118 +5,14 @@
 
 #include "tt_rows_args.h"
 #include "tt_linear.h"
-#include "tt_product_few.h"
-#include "tt_product_stream.h"
+#include "tt_product_launch.h"
 
 using namespace tt;
 
 namespace {
 
+
 constexpr int64_t MOST_COLUMNS = 1ll << 24;                  // of x, weight and output
-
-// How a product is computed.
-enum Way { FEW, TILES, STREAM, STREAM_WIDE };
-
-struct Plan {
-    Way way;
-    int64_t tiles_m, tiles_n;
-    int parts;
-    int64_t k_part;
-};
-
-constexpr int64_t MOST_TILES = 512;                          // workgroups that parts are made for
-
-// Parts of k, of four steps at least, where the tiles alone are too few for the device.
-int64_t parts_of(int64_t tiles, int64_t steps)
-{
-    int64_t parts = tiles < 256 ? MOST_TILES / (tiles > 0 ? tiles : 1) : 1;
-    if (parts > steps / 4) parts = steps / 4;
-    return parts < 1 ? 1 : parts;
-}
-
-Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense, bool whole)
-{
-    Plan p{};
-    const int64_t step = 128 / element_bytes(type);
-    p.parts = 1;
-    p.k_part = K;
-    if (dense && M <= PF_MOST) {
-        p.way = FEW;
-        return p;
-    }
-    p.way = !whole || type == TT_F32 ? TILES : ceil_div(M, 256) * ceil_div(N, 256) >= 128 ? STREAM_WIDE : STREAM;
-    const int64_t tile = p.way == STREAM_WIDE ? 256 : 128, steps = ceil_div(K, step);
-    p.tiles_m = ceil_div(M, p.way == TILES && M <= 32 ? 32 : tile);
-    p.tiles_n = ceil_div(N, tile);
-    const int64_t parts = parts_of(p.tiles_m * p.tiles_n, steps);
-    p.k_part = ceil_div(steps, parts) * step;
-    p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
-    return p;
-}
-
-// What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but a part is
-// no larger than its tiles.
-size_t parts_bytes(int64_t M, int64_t N, int64_t K, int32_t type)
-{
-    if (M <= 0 || N <= 0) return 0;
-    const int64_t most = ceil_div(K, 128 / element_bytes(type)) / 4, wide = ceil_div(N, 256);
-    if (wide >= 256 || most < 2) return 0;
-    const int64_t rows = M * (most < MOST_TILES ? most : MOST_TILES), tiled = MOST_TILES * 256 / wide;
-    return (size_t)(rows < tiled ? rows : tiled) * (size_t)(8 * ceil_div(N, 8)) * sizeof(float);
-}
-
-bool whole_chunks(const void *p, int64_t ld, int64_t columns, int32_t type)
-{
-    return type != TT_F32 && columns % 8 == 0 && ld % 8 == 0 && (uintptr_t)p % 16 == 0 && ld <= PS_MOST_STRIDE;
-}
-
-// C = A B^T; AK, BK: the operands' rows are dense in k
-template <typename T, typename O, bool AK, bool BK>
-int product(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st)
-{
-    if (M == 0 || N == 0) return TT_OK;
-    const int32_t type = sizeof(T) == 4 ? TT_F32 : TT_BF16;
-    const bool whole = whole_chunks(a, lda, AK ? K : M, type) && whole_chunks(b, ldb, BK ? K : N, type);
-    const Plan p = plan_of(M, N, K, type, AK && BK, whole);
-    ProductArgs q{a, b, lda, ldb, M, N, K, (int)p.tiles_m, (int)p.tiles_n, p.k_part, p.parts > 1 ? (float *)workspace : nullptr, 8 * ceil_div(N, 8)};
-    if (p.way == FEW) {
-        if constexpr (AK && BK) {
-            const dim3 grid = grid_of(ceil_div(N, BLOCK), PF_WAVES * WAVE);
-            const bool chunks = whole || (type == TT_F32 && K % 4 == 0 && lda % 4 == 0 && ldb % 4 == 0 && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0);
-            with_flag(chunks && K > 0, [&](auto w) {
-                auto launch = [&](auto mb) { hipLaunchKernelGGL((product_few_kernel<T, O, decltype(mb)::value, decltype(w)::value>), grid, dim3(PF_WAVES * WAVE), 0, st, q, e); };
-                if (M <= 16) launch(std::integral_constant<int, 1>{});
-                else if (M <= 32) launch(std::integral_constant<int, 2>{});
-                else launch(std::integral_constant<int, 4>{});
-            });
-        }
-        return launched("product launch");
-    }
-    if (p.way == TILES) {
-        dim3 grid = grid_of(p.tiles_m * p.tiles_n, WG);
-        grid.z = (unsigned)p.parts;
-        if (M <= 32) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 32, 128>), grid, dim3(WG), 0, st, q, e);
-        else hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 128>), grid, dim3(WG), 0, st, q, e);
-    } else if constexpr (sizeof(T) == 2) {
-        int rc = TT_OK;
-        with_flag(p.way == STREAM_WIDE, [&](auto w) {
-            typedef StreamShape<decltype(w)::value> S;
-            dim3 grid = grid_of(p.tiles_m * p.tiles_n, S::THREADS);
-            grid.z = (unsigned)p.parts;
-            const auto kernel = product_stream_kernel<T, O, AK, BK, decltype(w)::value>;
-            static OncePerDevice once;
-            const hipError_t err = allow_dynamic_lds(once, (const void *)kernel, S::LDS);
-            if (err != hipSuccess) {
-                rc = hip_fail(err, "LDS of a product");
-                return;
-            }
-            hipLaunchKernelGGL(kernel, grid, dim3(S::THREADS), S::LDS, st, q, e);
-        });
-        if (rc) return rc;
-    }
-    if (p.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, O>), grid_of(ceil_div(M * (q.ld_part / 8), WG), WG), dim3(WG), 0, st, q, e, p.parts);
-    return launched("product launch");
-}
 
 int check_product(int64_t M, int64_t K, int64_t N)
 {
@@ -154,7 +50,7 @@ struct GradRoom {
 GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, int32_t act, bool x, bool w, bool b)
 {
     GradRoom r{};
-    const size_t px = x ? parts_bytes(M, K, N, type) : 0, pw = w ? parts_bytes(N, K, M, type) : 0;
+    const size_t px = x ? product_bytes(M, K, N, type) : 0, pw = w ? product_bytes(N, K, M, type) : 0;
     const int64_t cols = 8 * ceil_div(N, 8);
     r.parts = up(px > pw ? px : pw);
     r.dz = act != TT_ACT_NONE && (x || w) ? up((size_t)M * (size_t)cols * element_bytes(type)) : 0;
@@ -165,15 +61,6 @@ GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, int32_t act, b
     return r;
 }
 
-template <typename F>
-void with_output(int32_t type, int32_t out, F f)
-{
-    with_type(type, [&](auto t) {
-        if (out == TT_F32) f(t, float{});
-        else f(t, t);
-    });
-}
-
 }  // namespace
 
 extern "C" {
@@ -181,7 +68,7 @@ extern "C" {
 size_t tt_linear_fwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type)
 {
     if (check_product(n_rows, K, N) || (type != TT_F32 && type != TT_BF16 && type != TT_F16)) return 0;
-    return n_rows <= PF_MOST ? 0 : parts_bytes(n_rows, N, K, type);
+    return n_rows <= PF_MOST ? 0 : product_bytes(n_rows, N, K, type);
 }
 
 int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias, int32_t bias_type, int32_t activation,
@@ -201,10 +88,7 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
     if (activation < 0 || activation >= ACT_COUNT) return fail(TT_ERR_BAD_ARG, "activation %d", (int)activation);
     if ((rc = check_workspace(tt_linear_fwd_workspace_bytes(n_rows, K, N, x->type), workspace, workspace_bytes))) return rc;
     EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
-    with_output(x->type, output->type, [&](auto t, auto o) {
-        rc = product<decltype(t), decltype(o), true, true>(x->data, x->ld, weight->data, weight->ld, n_rows, N, K, e, workspace, (hipStream_t)stream);
-    });
-    return rc;
+    return product(x->type, DENSE_DENSE, output->type, x->data, x->ld, weight->data, weight->ld, n_rows, N, K, e, workspace, (hipStream_t)stream);
 }
 
 size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation)
@@ -280,11 +164,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         EpilogueArgs e{};
         e.out = grad_x->data;
         e.ld_out = grad_x->ld;
-        with_type(type, [&](auto t) {
-            typedef decltype(t) T;
-            rc = product<T, T, true, false>(dz, ld_dz, weight->data, weight->ld, n_rows, K, N, e, ws, st);
-        });
-        if (rc) return rc;
+        if ((rc = product(type, DENSE_STRIDED, type, dz, ld_dz, weight->data, weight->ld, n_rows, K, N, e, ws, st))) return rc;
     }
     if (grad_weight && !(accumulate && n_rows == 0)) {
         EpilogueArgs e{};
@@ -294,9 +174,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
             e.add = e.out;
             e.ld_add = e.ld_out;
         }
-        with_output(type, grad_weight->type, [&](auto t, auto o) {
-            rc = product<decltype(t), decltype(o), false, false>(dz, ld_dz, x->data, x->ld, N, K, n_rows, e, ws, st);
-        });
+        rc = product(type, STRIDED_STRIDED, grad_weight->type, dz, ld_dz, x->data, x->ld, N, K, n_rows, e, ws, st);
     }
     return rc;
 }

@@ -1,0 +1,69 @@
+// The launches behind product_of, for the files that compile the kernels of a type.
+#pragma once
+
+#include "tt_product_launch.h"
+
+namespace tt {
+
+// C = A B^T; AK, BK: the operands' rows are dense in k
+template <typename T, typename O, bool AK, bool BK>
+int launch_product(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st)
+{
+    if (M == 0 || N == 0) return TT_OK;
+    const int32_t type = sizeof(T) == 4 ? TT_F32 : TT_BF16;
+    const bool whole = whole_chunks(a, lda, AK ? K : M, type) && whole_chunks(b, ldb, BK ? K : N, type);
+    const Plan p = plan_of(M, N, K, type, AK && BK, whole);
+    ProductArgs q{a, b, lda, ldb, M, N, K, (int)p.tiles_m, (int)p.tiles_n, p.k_part, p.parts > 1 ? (float *)workspace : nullptr, 8 * ceil_div(N, 8)};
+    if (p.way == FEW) {
+        if constexpr (AK && BK) {
+            const dim3 grid = grid_of(ceil_div(N, BLOCK), PF_WAVES * WAVE);
+            const bool chunks = whole || (type == TT_F32 && K % 4 == 0 && lda % 4 == 0 && ldb % 4 == 0 && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0);
+            with_flag(chunks && K > 0, [&](auto w) {
+                auto launch = [&](auto mb) { hipLaunchKernelGGL((product_few_kernel<T, O, decltype(mb)::value, decltype(w)::value>), grid, dim3(PF_WAVES * WAVE), 0, st, q, e); };
+                if (M <= 16) launch(std::integral_constant<int, 1>{});
+                else if (M <= 32) launch(std::integral_constant<int, 2>{});
+                else launch(std::integral_constant<int, 4>{});
+            });
+        }
+        return launched("product launch");
+    }
+    if (p.way == TILES) {
+        dim3 grid = grid_of(p.tiles_m * p.tiles_n, WG);
+        grid.z = (unsigned)p.parts;
+        if (M <= 32) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 32, 128>), grid, dim3(WG), 0, st, q, e);
+        else hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 128>), grid, dim3(WG), 0, st, q, e);
+    } else if constexpr (sizeof(T) == 2) {
+        int rc = TT_OK;
+        with_flag(p.way == STREAM_WIDE, [&](auto w) {
+            typedef StreamShape<decltype(w)::value> S;
+            dim3 grid = grid_of(p.tiles_m * p.tiles_n, S::THREADS);
+            grid.z = (unsigned)p.parts;
+            const auto kernel = product_stream_kernel<T, O, AK, BK, decltype(w)::value>;
+            static OncePerDevice once;
+            const hipError_t err = allow_dynamic_lds(once, (const void *)kernel, S::LDS);
+            if (err != hipSuccess) {
+                rc = hip_fail(err, "LDS of a product");
+                return;
+            }
+            hipLaunchKernelGGL(kernel, grid, dim3(S::THREADS), S::LDS, st, q, e);
+        });
+        if (rc) return rc;
+    }
+    if (p.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, O>), grid_of(ceil_div(M * (q.ld_part / 8), WG), WG), dim3(WG), 0, st, q, e, p.parts);
+    return launched("product launch");
+}
+
+template <typename T>
+int product_of(Layout layout, int32_t out_type, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e,
+               void *workspace, hipStream_t st)
+{
+    if (layout == DENSE_STRIDED) return launch_product<T, T, true, false>(a, lda, b, ldb, M, N, K, e, workspace, st);
+    if (layout == STRIDED_STRIDED) {
+        if (out_type == TT_F32) return launch_product<T, float, false, false>(a, lda, b, ldb, M, N, K, e, workspace, st);
+        return launch_product<T, T, false, false>(a, lda, b, ldb, M, N, K, e, workspace, st);
+    }
+    if (out_type == TT_F32) return launch_product<T, float, true, true>(a, lda, b, ldb, M, N, K, e, workspace, st);
+    return launch_product<T, T, true, true>(a, lda, b, ldb, M, N, K, e, workspace, st);
+}
+
+}  // namespace tt

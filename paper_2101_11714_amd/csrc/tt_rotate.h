@@ -2,9 +2,11 @@
 //
 // A unit is 16 columns of a head: eight pairs that are turned (eight columns of each half, or eight pairs of neighbours), or 16 columns behind
 // those.  A head is the 1 << lg neighbouring lanes that have a unit each; a lane keeps its columns in registers from the load to the store, so
-// that a head is read once.  A workgroup takes some rows at a time: it leaves the cosines and sines of their pairs in LDS, once for all heads,
-// and goes through the rows' heads, queries' and keys' alike.
+// that a head is read once.  Such a group of lanes takes some heads of one row in turn, queries or keys, with the cosines and sines of its pairs and
+// its part of the weight in registers: nothing goes through LDS, and nothing waits for other groups.
 #pragma once
+
+#include <type_traits>
 
 #include "tt_rows_io.h"
 
@@ -21,14 +23,15 @@ struct RotateArgs {
     Heads oq, ok;                // outputs
     const void *wq, *wk;
     int wq_type, wk_type;
-    int q_heads, heads;          // heads: of queries and keys together
+    int q_heads, k_heads;
     const void *positions;
     int64_t ld_positions;
     const float *freqs;
     int positions64, pairs, ends[4], neighbours;
     int64_t rows;
     int D, units, turned;        // units of a head, of which so many are turned
-    int lg, chunk;               // lanes of a head, rows at a time
+    int lg;                      // lanes of a head
+    int each, q_slices, k_slices;// heads that a group takes, and groups for a row's queries and for its keys
     float eps;
     float *part;                 // backward: [workgroups][2][D] sums of the weights' gradients, null: not wanted
 };
@@ -47,22 +50,9 @@ __device__ __forceinline__ float2 turn_of(double t)
     return make_float2(quarter == 1 || quarter == 2 ? -a : a, quarter >= 2 ? -b : b);
 }
 
-// cosines and sines of `n` rows from `row` on into LDS, [rows][pairs]
-__device__ __forceinline__ void leave_turns(const RotateArgs &a, int64_t row, int n, float2 *turns)
-{
-    for (int i = threadIdx.x; i < n * a.pairs; i += WG) {
-        const int r = i / a.pairs, p = i - r * a.pairs;
-        const int axis = p < a.ends[0] ? 0 : p < a.ends[1] ? 1 : p < a.ends[2] ? 2 : 3;
-        const int64_t at = axis * a.ld_positions + row + r;
-        const double pos = a.positions64 ? (double)((const int64_t *)a.positions)[at] : (double)((const int32_t *)a.positions)[at];
-        turns[i] = turn_of(pos * ((double)a.freqs[p] * 0.15915494309189535));
-    }
-}
-
 // Where a unit's two vectors of eight begin, and how many columns of each there are.
 struct Unit {
     int at[2], n[2];
-    int limit;                   // columns in the part of the head that the vectors lie in
 };
 
 __device__ __forceinline__ Unit unit_of(const RotateArgs &a, int u)
@@ -85,204 +75,272 @@ __device__ __forceinline__ Unit unit_of(const RotateArgs &a, int u)
         r.n[0] = a.D - r.at[0];
         r.n[1] = a.D - r.at[1];
     }
+    if (r.n[0] <= 0) r.at[0] = 0;
+    if (r.n[1] <= 0) r.at[1] = 0;
     return r;
 }
 
-// Up to eight columns of a head from column `at` on, zeros behind the n-th: the vector that ends at the head's end, or begins at its start,
-// is loaded where fewer than eight lie there.  D: the head's columns.
-template <typename T>
-__device__ __forceinline__ void load_unit(const T *head, int at, int n, int D, float (&x)[8])
+// the lane's cosines and sines in row `row`
+__device__ __forceinline__ void turns_of(const RotateArgs &a, int64_t row, int u, float2 (&t)[8])
 {
-    if (at + 8 <= D) {
-        widen8(fetch8<true>(head + at, 8, 8), x);
-    } else {
+    double pos[4];
+    for (int x = 0; x < 4; ++x) pos[x] = 0.0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = (float)head[j < n ? at + j : 0];
+    for (int x = 0; x < 4; ++x) {
+        if (x && a.ends[x] == a.ends[x - 1]) continue;       // (no pair: an axis that may not be there)
+        const int64_t at = x * a.ld_positions + row;
+        pos[x] = a.positions64 ? (double)((const int64_t *)a.positions)[at] : (double)((const int32_t *)a.positions)[at];
     }
+    float freq[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) x[j] = j < n ? x[j] : 0.f;
+    for (int j = 0; j < 8; ++j) freq[j] = a.freqs[min(8 * u + j, a.pairs - 1)];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int p = min(8 * u + j, a.pairs - 1);
+        const double at = p < a.ends[0] ? pos[0] : p < a.ends[1] ? pos[1] : p < a.ends[2] ? pos[2] : pos[3];
+        t[j] = turn_of(at * ((double)freq[j] * 0.15915494309189535));
+        if (j & 1) __builtin_amdgcn_sched_barrier(0);        // (eight at once would take the registers that heads are on their way to)
+    }
 }
 
-template <typename T>
+// Eight columns of a head from column `at` on.  WHOLE: a unit's vectors have eight columns or none (which load the head's first).
+template <typename T, bool WHOLE>
+__device__ __forceinline__ Vec8<T> fetch_unit(const T *head, int at, int D) { return fetch8<WHOLE>(head + at, D - at, D); }
+
+// the first n of them, and zeros behind
+template <bool WHOLE, typename T>
+__device__ __forceinline__ void widen_unit(Vec8<T> r, int at, int n, int D, float (&x)[8])
+{
+    settle8<WHOLE>(r, D - at, D);
+    widen8(r, x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = (WHOLE ? n > 0 : j < n) ? x[j] : 0.f;
+}
+
+template <bool WHOLE, typename T>
 __device__ __forceinline__ void store_unit(T *head, int at, int n, const float (&x)[8])
 {
-    if (n > 0) put8(head + at, n, x);
+    if (n > 0) put8<WHOLE>(head + at, n, x);
 }
 
-__device__ __forceinline__ void load_weight(const void *w, int type, const Unit &u, float (&x)[2][8])
+// the lane's part of a weight (null: ones)
+template <bool WHOLE>
+__device__ __forceinline__ void load_weight(const void *w, int type, const Unit &u, int D, float (&x)[2][8])
 {
+    auto load = [&](auto *p) {
+        typedef std::remove_cv_t<std::remove_pointer_t<decltype(p)>> W;
+        const Vec8<W> r0 = fetch_unit<W, WHOLE>(p, u.at[0], D), r1 = fetch_unit<W, WHOLE>(p, u.at[1], D);
+        widen_unit<WHOLE>(r0, u.at[0], u.n[0], D, x[0]);
+        widen_unit<WHOLE>(r1, u.at[1], u.n[1], D, x[1]);
+    };
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int c = j < u.n[h] ? u.at[h] + j : 0;
-            x[h][j] = !w ? 1.f : type == TT_F32 ? ((const float *)w)[c] : type == TT_BF16 ? (float)((const bf16_t *)w)[c] : (float)((const f16_t *)w)[c];
-        }
+    for (int j = 0; j < 8; ++j) x[0][j] = x[1][j] = 1.f;
+    if (!w) return;
+    if (type == TT_F32) load((const float *)w);
+    else if (type == TT_BF16) load((const bf16_t *)w);
+    else load((const f16_t *)w);
 }
 
 // the unit's pairs turned; BACK: the other way round
-template <bool BACK>
-__device__ __forceinline__ void turn_unit(const RotateArgs &a, const float2 *turns, int u, float (&x)[2][8])
+template <bool BACK, bool NEIGHBOURS>
+__device__ __forceinline__ void turn_unit(const float2 (&t)[8], float (&x)[2][8])
 {
-    float y[2][8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float2 t = turns[min(8 * u + j, a.pairs - 1)];
-        const float s = BACK ? -t.y : t.y;
-        const float v = a.neighbours ? x[j >> 2][2 * j & 7] : x[0][j], w = a.neighbours ? x[j >> 2][(2 * j & 7) + 1] : x[1][j];
-        y[0][j] = v * t.x - w * s;
-        y[1][j] = w * t.x + v * s;
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        x[0][j] = a.neighbours ? y[j & 1][j >> 1] : y[0][j];
-        x[1][j] = a.neighbours ? y[j & 1][4 + (j >> 1)] : y[1][j];
+        float &p = NEIGHBOURS ? x[j >> 2][2 * j & 7] : x[0][j], &q = NEIGHBOURS ? x[j >> 2][(2 * j & 7) + 1] : x[1][j];
+        const float v = p, w = q, s = BACK ? -t[j].y : t[j].y;
+        p = v * t[j].x - w * s;
+        q = w * t[j].x + v * s;
     }
 }
 
 template <typename T>
 __device__ __forceinline__ T *head_at(const Heads &h, int64_t row, int head) { return (T *)h.data + row * h.ld + head * h.ld_head; }
 
-template <typename T, bool NORM>
+// A group's place: its row and the heads [from, to) of queries or keys.
+struct Slice {
+    int64_t row;
+    int from, to;
+};
+
+__device__ __forceinline__ Slice slice_of(int64_t item, int slices, int each, int heads)
+{
+    Slice s;
+    s.row = item / slices;
+    s.from = (int)(item - s.row * slices) * each;
+    s.to = min(s.from + each, heads);
+    return s;
+}
+
+template <typename T, bool NORM, bool WHOLE, bool NEIGHBOURS>
 __global__ __launch_bounds__(WG) void rotate_kernel(RotateArgs a)
 {
-    extern __shared__ float2 turns[];
-    const int g = 1 << a.lg, u = threadIdx.x & (g - 1), group = threadIdx.x >> a.lg, groups = WG >> a.lg;
+    constexpr int U = sizeof(T) == 4 || !WHOLE ? 2 : 4;      // heads whose loads are on their way together
+    const int g = 1 << a.lg, u = threadIdx.x & (g - 1), slices = a.q_slices + a.k_slices;
+    const int64_t item = workgroup() * (WG >> a.lg) + (threadIdx.x >> a.lg);
+    if (item >= a.rows * slices) return;                     // (whole groups)
     const bool in = u < a.units;
-    const Unit unit = unit_of(a, in ? u : 0);
-    const int64_t row0 = workgroup() * a.chunk;
-    if (row0 >= a.rows) return;
-    const int n = a.rows - row0 < a.chunk ? (int)(a.rows - row0) : a.chunk;
-    leave_turns(a, row0, n, turns);
-    __syncthreads();
-    for (int i = group; i < n * a.heads; i += groups) {
-        const int r = i / a.heads, head = i - r * a.heads;
-        const bool key = head >= a.q_heads;
-        const int h = key ? head - a.q_heads : head;
-        const int64_t row = row0 + r;
-        const T *src = head_at<T>(key ? a.k : a.q, row, h);
-        float x[2][8];
-        load_unit(src, unit.at[0], in ? unit.n[0] : 0, a.D, x[0]);
-        load_unit(src, unit.at[1], in ? unit.n[1] : 0, a.D, x[1]);
-        if (NORM) {
-            float s = 0.f, w[2][8];
+    Unit unit = unit_of(a, in ? u : 0);
+    if (!in) unit.n[0] = unit.n[1] = 0;
+    Slice s = slice_of(item, slices, a.each, 1 << 30);
+    const bool key = s.from >= a.q_slices * a.each;
+    if (key) s.from -= a.q_slices * a.each;
+    s.to = min(s.from + a.each, key ? a.k_heads : a.q_heads);
+    const Heads src = key ? a.k : a.q, dst = key ? a.ok : a.oq;
+    float w[2][8];
+    float2 turns[8];
+    Vec8<T> raw[U][2];
+    auto fetch = [&](int h0) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s += x[0][j] * x[0][j] + x[1][j] * x[1][j];
-            s = lanes_reduce(s, a.lg, [](float p, float q) { return p + q; });
-            const float rho = 1.f / sqrtf(s / (float)a.D + a.eps);
-            load_weight(key ? a.wk : a.wq, key ? a.wk_type : a.wq_type, unit, w);
-#pragma unroll
-            for (int c = 0; c < 2; ++c)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[c][j] *= rho * w[c][j];
+        for (int i = 0; i < U; ++i) {
+            const T *p = head_at<T>(src, s.row, min(h0 + i, s.to - 1));
+            raw[i][0] = fetch_unit<T, WHOLE>(p, unit.at[0], a.D);
+            raw[i][1] = fetch_unit<T, WHOLE>(p, unit.at[1], a.D);
         }
-        if (!in) continue;
-        if (u < a.turned) turn_unit<false>(a, turns + r * a.pairs, u, x);
-        T *dst = head_at<T>(key ? a.ok : a.oq, row, h);
-        store_unit(dst, unit.at[0], unit.n[0], x[0]);
-        store_unit(dst, unit.at[1], unit.n[1], x[1]);
+    };
+    fetch(s.from);
+    if (NORM) load_weight<WHOLE>(key ? a.wk : a.wq, key ? a.wk_type : a.wq_type, unit, a.D, w);
+    const bool turned = u < a.turned;
+    if (turned) turns_of(a, s.row, u, turns);
+    for (int h0 = s.from; h0 < s.to; h0 += U) {
+        if (h0 > s.from) fetch(h0);
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            if (h0 + i >= s.to) break;
+            float x[2][8];
+            widen_unit<WHOLE>(raw[i][0], unit.at[0], unit.n[0], a.D, x[0]);
+            widen_unit<WHOLE>(raw[i][1], unit.at[1], unit.n[1], a.D, x[1]);
+            if (NORM) {
+                float sum = 0.f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += x[0][j] * x[0][j] + x[1][j] * x[1][j];
+                sum = lanes_reduce(sum, a.lg, [](float p, float q) { return p + q; });
+                const float rho = 1.f / sqrtf(sum / (float)a.D + a.eps);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[c][j] *= rho * w[c][j];
+            }
+            if (turned) turn_unit<false, NEIGHBOURS>(turns, x);
+            T *p = head_at<T>(dst, s.row, h0 + i);
+            store_unit<WHOLE>(p, unit.at[0], unit.n[0], x[0]);
+            store_unit<WHOLE>(p, unit.at[1], unit.n[1], x[1]);
+        }
     }
 }
 
-template <typename T, bool NORM>
-__global__ __launch_bounds__(WG) void rotate_bwd_kernel(RotateArgs a)
+// Groups go through all queries, then through all keys, so that one weight's sums are in registers at a time.
+template <typename T, bool NORM, bool WHOLE, bool NEIGHBOURS>
+__global__ __launch_bounds__(WG, NORM ? 2 : WHOLE ? 4 : 3) void rotate_bwd_kernel(RotateArgs a)
 {
-    extern __shared__ float2 turns[];
-    const int g = 1 << a.lg, u = threadIdx.x & (g - 1), group = threadIdx.x >> a.lg, groups = WG >> a.lg;
-    const bool in = u < a.units;
-    const Unit unit = unit_of(a, in ? u : 0);
-    float dw[2][2][8] = {};
-    for (int64_t row0 = (int64_t)blockIdx.x * a.chunk; row0 < a.rows; row0 += (int64_t)gridDim.x * a.chunk) {
-        const int n = a.rows - row0 < a.chunk ? (int)(a.rows - row0) : a.chunk;
-        __syncthreads();
-        leave_turns(a, row0, n, turns);
-        __syncthreads();
-        for (int i = group; i < n * a.heads; i += groups) {
-            const int r = i / a.heads, head = i - r * a.heads;
-            const bool key = head >= a.q_heads;
-            const int h = key ? head - a.q_heads : head;
-            const int64_t row = row0 + r;
-            const T *grad = head_at<T>(key ? a.gk : a.gq, row, h);
-            float d[2][8];
-            load_unit(grad, unit.at[0], in ? unit.n[0] : 0, a.D, d[0]);
-            load_unit(grad, unit.at[1], in ? unit.n[1] : 0, a.D, d[1]);
-            if (in && u < a.turned) turn_unit<true>(a, turns + r * a.pairs, u, d);
-            if (NORM) {
-                float x[2][8], w[2][8], s = 0.f, dot = 0.f;
-                const T *src = head_at<T>(key ? a.k : a.q, row, h);
-                load_unit(src, unit.at[0], in ? unit.n[0] : 0, a.D, x[0]);
-                load_unit(src, unit.at[1], in ? unit.n[1] : 0, a.D, x[1]);
-                load_weight(key ? a.wk : a.wq, key ? a.wk_type : a.wq_type, unit, w);
+    extern __shared__ float sums[];
+    const int g = 1 << a.lg, u = threadIdx.x & (g - 1), groups = WG >> a.lg;
+    const bool in = u < a.units, turned = u < a.turned;
+    Unit unit = unit_of(a, in ? u : 0);
+    if (!in) unit.n[0] = unit.n[1] = 0;
+#pragma unroll 1
+    for (int which = 0; which < 2; ++which) {
+        const int slices = which ? a.k_slices : a.q_slices, heads = which ? a.k_heads : a.q_heads;
+        const Heads src = which ? a.k : a.q, grad = which ? a.gk : a.gq, dst = which ? a.ok : a.oq;
+        float w[2][8], dw[2][8] = {};
+        if (NORM) load_weight<WHOLE>(which ? a.wk : a.wq, which ? a.wk_type : a.wq_type, unit, a.D, w);
+        for (int64_t item = (int64_t)blockIdx.x * groups + (threadIdx.x >> a.lg); item < a.rows * slices; item += (int64_t)gridDim.x * groups) {
+            const Slice s = slice_of(item, slices, a.each, heads);
+            float2 turns[8];
+            Vec8<T> rd[2], rx[2], nd[2], nx[2];
+            auto fetch = [&](int h) {
+                const T *p = head_at<T>(grad, s.row, h);
+                nd[0] = fetch_unit<T, WHOLE>(p, unit.at[0], a.D);
+                nd[1] = fetch_unit<T, WHOLE>(p, unit.at[1], a.D);
+                if (NORM) {
+                    const T *x = head_at<T>(src, s.row, h);
+                    nx[0] = fetch_unit<T, WHOLE>(x, unit.at[0], a.D);
+                    nx[1] = fetch_unit<T, WHOLE>(x, unit.at[1], a.D);
+                }
+            };
+            fetch(s.from);
+            if (turned) turns_of(a, s.row, u, turns);
+#pragma unroll 1
+            for (int h = s.from; h < s.to; ++h) {
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < 2; ++c) {
+                    rd[c] = nd[c];
+                    if (NORM) rx[c] = nx[c];
+                }
+                fetch(min(h + 1, s.to - 1));                 // the next head, while this one is worked on
+                float d[2][8];
+                widen_unit<WHOLE>(rd[0], unit.at[0], unit.n[0], a.D, d[0]);
+                widen_unit<WHOLE>(rd[1], unit.at[1], unit.n[1], a.D, d[1]);
+                if (turned) turn_unit<true, NEIGHBOURS>(turns, d);
+                if (NORM) {
+                    float x[2][8], sum = 0.f, dot = 0.f;
+                    widen_unit<WHOLE>(rx[0], unit.at[0], unit.n[0], a.D, x[0]);
+                    widen_unit<WHOLE>(rx[1], unit.at[1], unit.n[1], a.D, x[1]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        s += x[c][j] * x[c][j];
-                        dot += d[c][j] * w[c][j] * x[c][j];
-                    }
-                s = lanes_reduce(s, a.lg, [](float p, float q) { return p + q; });
-                dot = lanes_reduce(dot, a.lg, [](float p, float q) { return p + q; });
-                const float rho = 1.f / sqrtf(s / (float)a.D + a.eps), along = rho * rho * dot / (float)a.D;
+                    for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                        for (int j = 0; j < 8; ++j) {
+                            sum += x[c][j] * x[c][j];
+                            dot += d[c][j] * w[c][j] * x[c][j];
+                        }
+                    sum = lanes_reduce(sum, a.lg, [](float p, float q) { return p + q; });
+                    dot = lanes_reduce(dot, a.lg, [](float p, float q) { return p + q; });
+                    const float rho = 1.f / sqrtf(sum / (float)a.D + a.eps), along = rho * rho * dot / (float)a.D;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float p = d[c][j] * x[c][j] * rho;
-                        dw[0][c][j] += key ? 0.f : p;
-                        dw[1][c][j] += key ? p : 0.f;
-                        d[c][j] = rho * (d[c][j] * w[c][j] - x[c][j] * along);
-                    }
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            dw[c][j] += d[c][j] * x[c][j] * rho;
+                            d[c][j] = rho * (d[c][j] * w[c][j] - x[c][j] * along);
+                        }
+                }
+                T *p = head_at<T>(dst, s.row, h);
+                store_unit<WHOLE>(p, unit.at[0], unit.n[0], d[0]);
+                store_unit<WHOLE>(p, unit.at[1], unit.n[1], d[1]);
             }
-            if (!in) continue;
-            T *dst = head_at<T>(key ? a.ok : a.oq, row, h);
-            store_unit(dst, unit.at[0], unit.n[0], d[0]);
-            store_unit(dst, unit.at[1], unit.n[1], d[1]);
         }
-    }
-    if (!NORM || !a.part) return;
-    // the groups' sums: lanes of a wave, then waves through LDS, in their order
-    float *sums = reinterpret_cast<float *>(turns);
-    const int cols = 16 * a.units, lanes = g < WAVE ? g : WAVE;
-    for (int b = a.lg; b < 6; ++b)
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
+        if (!NORM || !a.part) continue;
+        // the groups' sums: lanes of a wave, then waves through LDS, in their order
+        const int cols = 16 * a.units, lanes = g < WAVE ? g : WAVE;
+        for (int b = a.lg; b < 6; ++b)
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dw[s][c][j] += __shfl_xor(dw[s][c][j], 1 << b);
-    for (int s = 0; s < 2; ++s) {
+                for (int j = 0; j < 8; ++j) dw[c][j] += __shfl_xor(dw[c][j], 1 << b);
         __syncthreads();
         if ((int)(threadIdx.x & 63) < lanes && in)
 #pragma unroll
             for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sums[(threadIdx.x >> 6) * cols + 16 * u + 8 * c + j] = s ? dw[1][c][j] : dw[0][c][j];
+                for (int j = 0; j < 8; ++j) sums[(threadIdx.x >> 6) * cols + 16 * u + 8 * c + j] = dw[c][j];
         __syncthreads();
         for (int i = threadIdx.x; i < cols; i += WG) {
             const Unit x = unit_of(a, i >> 4);
             const int c = i >> 3 & 1, j = i & 7;
-            if (j < (c ? x.n[1] : x.n[0])) a.part[((int64_t)blockIdx.x * 2 + s) * a.D + (c ? x.at[1] : x.at[0]) + j] = (sums[i] + sums[cols + i]) + (sums[2 * cols + i] + sums[3 * cols + i]);
+            if (j < (c ? x.n[1] : x.n[0]))
+                a.part[((int64_t)blockIdx.x * 2 + which) * a.D + (c ? x.at[1] : x.at[0]) + j] = (sums[i] + sums[cols + i]) + (sums[2 * cols + i] + sums[3 * cols + i]);
         }
     }
 }
 
-// the workgroups' sums added in their order: blockIdx.y 0 the queries' weight, 1 the keys'
-__global__ __launch_bounds__(WG) void rotate_weight_kernel(const float *part, int n_part, int D, void *gq, int gq_type, void *gk, int gk_type, int add)
+// the workgroups' sums added in their order, 32 columns a workgroup: blockIdx.y 0 the queries' weight, 1 the keys'
+__global__ __launch_bounds__(1024) void rotate_weight_kernel(const float *part, int n_part, int D, void *gq, int gq_type, void *gk, int gk_type, int add)
 {
-    __shared__ float sums[8][32];
+    __shared__ float sums[32][33];
     const int c = threadIdx.x & 31, q = threadIdx.x >> 5, at = blockIdx.x * 32 + c, which = blockIdx.y;
     void *out = which ? gk : gq;
     if (!out) return;
     const int type = which ? gk_type : gq_type;
     float s = 0.f;
     if (at < D)
-        for (int b = q; b < n_part; b += 8) s += part[((int64_t)b * 2 + which) * D + at];
+#pragma unroll 4
+        for (int b = q; b < n_part; b += 32) s += part[((int64_t)b * 2 + which) * D + at];
     sums[q][c] = s;
     __syncthreads();
     if (q || at >= D) return;
     float y = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) y += sums[i][c];
+    for (int i = 0; i < 32; ++i) y += sums[i][c];
     if (type == TT_F32) ((float *)out)[at] = y + (add ? ((float *)out)[at] : 0.f);
     else if (type == TT_BF16) ((bf16_t *)out)[at] = (bf16_t)(y + (add ? (float)((bf16_t *)out)[at] : 0.f));
     else ((f16_t *)out)[at] = (f16_t)(y + (add ? (float)((f16_t *)out)[at] : 0.f));

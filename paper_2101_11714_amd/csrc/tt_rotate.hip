@@ -11,7 +11,7 @@ using namespace tt;
 namespace {
 
 constexpr int MOST_HEAD = 512;                               // columns of a head: 34 units at most, whatever its pairs
-constexpr int64_t BWD_WORKGROUPS = 1024;
+constexpr int64_t BWD_WORKGROUPS = 512;
 
 int check_heads(const tt_heads_t *h, const char *name, int64_t rows, int64_t D, int32_t type, int32_t heads, int way)
 {
@@ -86,18 +86,25 @@ void shape_of(RotateArgs &a)
     a.lg = lg_ceil(a.units);
 }
 
-// Rows at a time: as many as give every group of lanes a few heads.
-void chunk_of(RotateArgs &a, int rounds)
+// Heads of a group: up to eight, which then share its cosines and sines, where that leaves every compute unit 16 waves.
+void slices_of(RotateArgs &a)
 {
-    const int groups = WG >> a.lg;
-    int64_t n = (int64_t)groups * rounds / a.heads;
-    const int64_t most = a.pairs ? 4096 / a.pairs : 64;
-    if (n > most) n = most;
-    if (n > 64) n = 64;
-    a.chunk = n < 1 ? 1 : (int)n;
+    const int64_t wanted = 256 * 16 * (WAVE >> a.lg), heads = a.rows * ((int64_t)a.q_heads + a.k_heads);
+    int64_t each = heads / wanted;
+    a.each = each < 1 ? 1 : each > 8 ? 8 : (int)each;
+    a.q_slices = (int)ceil_div(a.q_heads, a.each);
+    a.k_slices = (int)ceil_div(a.k_heads, a.each);
 }
 
 int64_t bwd_grid(int64_t rows) { return rows < BWD_WORKGROUPS ? rows : BWD_WORKGROUPS; }
+
+template <typename F>
+void with_shape(const RotateArgs &a, bool norm, F f)
+{
+    with_flag(norm, [&](auto nm) {
+        with_flag(a.pairs % (a.neighbours ? 4 : 8) == 0 && (a.D - 2 * a.pairs) % 8 == 0, [&](auto whole) { with_flag(a.neighbours != 0, [&](auto nb) { f(nm, whole, nb); }); });
+    });
+}
 
 Heads of(const tt_heads_t *h) { return h ? Heads{h->data, h->ld, h->ld_head} : Heads{}; }
 
@@ -129,17 +136,17 @@ int tt_qk_norm_rotate_fwd(const tt_heads_t *q, const tt_heads_t *k, const tt_rot
     a.wq_type = q_weight_type;
     a.wk_type = k_weight_type;
     a.q_heads = q->heads;
-    a.heads = q->heads + (k ? k->heads : 0);
+    a.k_heads = k ? k->heads : 0;
     a.rows = n_rows;
     a.D = (int)D;
     a.eps = eps;
-    if (n_rows == 0 || D == 0 || a.heads == 0) return TT_OK;
+    if (n_rows == 0 || D == 0 || a.q_heads + a.k_heads == 0) return TT_OK;
     shape_of(a);
-    chunk_of(a, 4);
-    const size_t lds = (size_t)a.chunk * a.pairs * sizeof(float2);
+    slices_of(a);
+    const dim3 grid = grid_of(ceil_div(n_rows * ((int64_t)a.q_slices + a.k_slices), WG >> a.lg), WG);
     with_type(q->type, [&](auto t) {
-        with_flag(norm != 0, [&](auto nm) {
-            hipLaunchKernelGGL((rotate_kernel<decltype(t), decltype(nm)::value>), grid_of(ceil_div(n_rows, a.chunk), WG), dim3(WG), lds, (hipStream_t)stream, a);
+        with_shape(a, norm != 0, [&](auto nm, auto whole, auto nb) {
+            hipLaunchKernelGGL((rotate_kernel<decltype(t), decltype(nm)::value, decltype(whole)::value, decltype(nb)::value>), grid, dim3(WG), 0, (hipStream_t)stream, a);
         });
     });
     return launched("rotation launch");
@@ -177,10 +184,9 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
     if (grad_k_weight && !grad_k) return fail(TT_ERR_BAD_ARG, "grad_k_weight without keys");
     if ((rc = check_weight(q_weight, "q_weight", q_weight_type)) || (rc = check_weight(k_weight, "k_weight", k_weight_type)) ||
         (rc = check_weight(grad_q_weight, "grad_q_weight", grad_q_weight_type)) || (rc = check_weight(grad_k_weight, "grad_k_weight", grad_k_weight_type))) return rc;
-    a.heads = q_heads + k_heads;
     if (D == 0) return TT_OK;
     const bool weights = grad_q_weight || grad_k_weight;
-    const bool some = n_rows > 0 && a.heads > 0;
+    const bool some = n_rows > 0 && q_heads + k_heads > 0;
     if (!some && (!weights || accumulate)) return TT_OK;
     const int64_t grid = bwd_grid(n_rows);
     const size_t need = weights && some ? (size_t)grid * 2 * (size_t)D * sizeof(float) : 0;
@@ -197,6 +203,7 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
     a.wq_type = q_weight_type;
     a.wk_type = k_weight_type;
     a.q_heads = q_heads;
+    a.k_heads = k_heads;
     a.rows = n_rows;
     a.D = (int)D;
     a.eps = eps;
@@ -204,18 +211,16 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
     hipStream_t st = (hipStream_t)stream;
     if (some) {
         shape_of(a);
-        chunk_of(a, 2);
-        size_t lds = (size_t)a.chunk * a.pairs * sizeof(float2);
-        const size_t sums = norm ? (size_t)NWAVE * 16 * a.units * sizeof(float) : 0;
-        if (lds < sums) lds = sums;
+        slices_of(a);
+        const size_t lds = weights ? (size_t)NWAVE * 16 * a.units * sizeof(float) : 0;
         with_type(type, [&](auto t) {
-            with_flag(norm != 0, [&](auto nm) {
-                hipLaunchKernelGGL((rotate_bwd_kernel<decltype(t), decltype(nm)::value>), dim3((unsigned)grid), dim3(WG), lds, st, a);
+            with_shape(a, norm != 0, [&](auto nm, auto whole, auto nb) {
+                hipLaunchKernelGGL((rotate_bwd_kernel<decltype(t), decltype(nm)::value, decltype(whole)::value, decltype(nb)::value>), dim3((unsigned)grid), dim3(WG), lds, st, a);
             });
         });
     }
     if (weights)
-        hipLaunchKernelGGL(rotate_weight_kernel, dim3((unsigned)ceil_div(D, 32), 2), dim3(WG), 0, st, (const float *)workspace, some ? (int)grid : 0, (int)D, grad_q_weight, grad_q_weight_type,
+        hipLaunchKernelGGL(rotate_weight_kernel, dim3((unsigned)ceil_div(D, 32), 2), dim3(1024), 0, st, (const float *)workspace, some ? (int)grid : 0, (int)D, grad_q_weight, grad_q_weight_type,
                            grad_k_weight, grad_k_weight_type, accumulate);
     return launched("rotation gradient launch");
 }
