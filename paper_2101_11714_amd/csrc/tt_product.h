@@ -95,11 +95,11 @@ __device__ __forceinline__ void finish8(const EpilogueArgs &e, int64_t m, int64_
 
 // ---- tiles of operands in LDS -------------------------------------------------------------------------------------------
 //
-// A step takes 128 bytes of k: PB_K<T> values.  A matrix instruction 16 x 16 takes of each operand 16 bytes of k per lane from one
+// A step takes 128 bytes of k, PB_K<T> values, or 64.  A matrix instruction 16 x 16 takes of each operand 16 bytes of k per lane from one
 // of 16 rows (8 values of 16 bits: one instruction of k = 32; 4 of 32 bits: four of k = 4 whose k are not neighbours, the same
-// ones in both operands), so that a step is two "halves" of 64 bytes.
-//   dense in k:   the tile is [rows][128 bytes], read by 16 bytes per lane;
-//   strided in k: it is [PB_K][rows], as it lies in memory; 16-bit values are read transposed by the LDS (4 rows of k x 16
+// ones in both operands), so that 64 bytes are a "half".
+//   dense in k:   the tile is [rows][bytes of the step], read by 16 bytes per lane;
+//   strided in k: it is [values of the step][rows], as it lies in memory; 16-bit values are read transposed by the LDS (4 rows of k x 16
 //                 columns to 16 lanes), 32-bit values one by one.
 // In both, 16-byte chunks are permuted along a row by an exclusive or with bits of its number, so that the lanes that read at
 // the same time find different banks.
@@ -111,18 +111,19 @@ constexpr int PB_K = 128 / (int)sizeof(T);
 
 constexpr int BLOCK = 16;
 
-template <typename T, bool KDENSE, int ROWS>
+template <typename T, bool KDENSE, int ROWS, int HALVES>
 struct OperandTile {
     static constexpr int CH = 16 / sizeof(T);                // values of a chunk
-    static constexpr int LINE = KDENSE ? 8 : ROWS / CH;      // chunks of a line
-    static constexpr int LINES = KDENSE ? ROWS : PB_K<T>;
+    static constexpr int LINE = KDENSE ? 4 * HALVES : ROWS / CH;             // chunks of a line
+    static constexpr int LINES = KDENSE ? ROWS : 4 * HALVES * CH;
     static constexpr int CHUNKS = LINE * LINES, BYTES = CHUNKS * 16;
     static_assert((LINE & (LINE - 1)) == 0, "a permutation of the line's chunks");
 
+    // (transposed reads: 32 lanes read four lines each of two groups, eight lines apart)
     static __device__ __forceinline__ int swizzle(int line)
     {
-        const int x = KDENSE ? line : sizeof(T) == 4 ? (line >> 2) << 2 : line << 1;
-        return x & (KDENSE ? 7 : sizeof(T) == 4 ? 12 : 6) & (LINE - 1);
+        const int x = KDENSE ? HALVES == 2 ? line & 7 : line >> 2 & 3 : sizeof(T) == 4 ? (line >> 2 & 3) << 2 : (line & 3) << 1 | (line & 8);
+        return x & (LINE - 1);
     }
     // byte offset of a chunk
     static __device__ __forceinline__ int at(int line, int chunk) { return (line * LINE + (chunk ^ swizzle(line))) * 16; }
@@ -288,8 +289,8 @@ __global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, Epilogue
 template <typename T, typename O, bool AK, bool BK, int TM, int TN>
 __global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArgs e)
 {
-    typedef OperandTile<T, AK, TM> TA;
-    typedef OperandTile<T, BK, TN> TB;
+    typedef OperandTile<T, AK, TM, 2> TA;
+    typedef OperandTile<T, BK, TN, 2> TB;
     constexpr int KB = PB_K<T>, BM = TM / 2 / BLOCK, BN = TN / 2 / BLOCK, PA = TA::CHUNKS / 256, PB = TB::CHUNKS / 256;
     static_assert(BN == 4, "what a wave leaves is 64 columns wide");
     constexpr int SOME = BM < 2 ? 1 : 2;

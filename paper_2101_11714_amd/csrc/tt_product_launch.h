@@ -30,23 +30,50 @@ inline int64_t parts_of(int64_t tiles, int64_t steps)
     return parts < 1 ? 1 : parts;
 }
 
+// Tiles of 256 or of 128, and how many parts of k: whatever should be done first, by what was measured on 256 compute units.  A step of a wide tile,
+// one on a compute unit, takes 1.87 us (8,192 x 16,384 x 4,096: 1,127 TFLOP/s); one of a narrow tile 0.70 us alone on its compute unit and 1.17 beside
+// another one (2,048 x 2,048 x 4,096, one tile each: 48 us, by wide tiles in four parts 41 and the parts' sums 15; 8,192 x 4,096 x 4,096: 293, by
+// wide ones 221).  Parts cost a launch, and their sums a write and a read.
+inline void stream_plan(Plan &p, int64_t M, int64_t N, int64_t K)
+{
+    const int64_t steps = ceil_div(K, PS_K);
+    double best = 0;
+    for (const bool wide : {true, false}) {
+        const int64_t tile = wide ? 256 : 128, tiles_m = ceil_div(M, tile), tiles_n = ceil_div(N, tile), tiles = tiles_m * tiles_n, room = wide ? 256 : MOST_TILES;
+        for (int64_t parts = 1; parts == 1 || (parts * tiles <= room && 4 * parts <= steps); parts *= 2) {
+            const int64_t each = ceil_div(steps, parts), all = tiles * parts, whole = all / room, rest = all % room;
+            double us = wide ? 1.87 * (double)(whole + (rest > 0)) : 1.17 * (double)(whole + (rest > 256)) + (rest > 0 && rest <= 256 ? 0.70 : 0.0);
+            us = us * (double)each + 5.0;
+            if (parts > 1) us += 3.0 + (double)parts * (double)M * (double)N * 8.0 / 5.0e6;
+            if (best == 0 || us < best) {
+                best = us;
+                p.way = wide ? STREAM_WIDE : STREAM;
+                p.tiles_m = tiles_m;
+                p.tiles_n = tiles_n;
+                p.k_part = each * PS_K;
+            }
+        }
+    }
+    p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
+}
+
 inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense, bool whole)
 {
     Plan p{};
-    const int64_t step = 128 / element_bytes(type);
     p.parts = 1;
     p.k_part = K;
     if (dense && M <= PF_MOST) {
         p.way = FEW;
-        return p;
+    } else if (whole && type != TT_F32) {
+        stream_plan(p, M, N, K);
+    } else {
+        p.way = TILES;
+        p.tiles_m = ceil_div(M, M <= 32 ? 32 : 128);
+        p.tiles_n = ceil_div(N, 128);
+        const int64_t step = 128 / element_bytes(type), steps = ceil_div(K, step);
+        p.k_part = ceil_div(steps, parts_of(p.tiles_m * p.tiles_n, steps)) * step;
+        p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
     }
-    p.way = !whole || type == TT_F32 ? TILES : ceil_div(M, 256) * ceil_div(N, 256) >= 128 ? STREAM_WIDE : STREAM;
-    const int64_t tile = p.way == STREAM_WIDE ? 256 : 128, steps = ceil_div(K, step);
-    p.tiles_m = ceil_div(M, p.way == TILES && M <= 32 ? 32 : tile);
-    p.tiles_n = ceil_div(N, tile);
-    const int64_t parts = parts_of(p.tiles_m * p.tiles_n, steps);
-    p.k_part = ceil_div(steps, parts) * step;
-    p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
     return p;
 }
 

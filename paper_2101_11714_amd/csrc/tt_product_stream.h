@@ -8,18 +8,20 @@ namespace tt {
 constexpr uint32_t PS_RECORDS = 0x7ffffff0u, PS_NOWHERE = 0x80000000u;       // a buffer's bytes; an offset behind them: zeros are loaded
 constexpr int64_t PS_MOST_STRIDE = 1 << 22;                  // of rows, so that offsets in a tile stay below PS_RECORDS
 
+constexpr int PS_K = 64, PS_SLOTS = 5;                       // values of k in a step; tiles of operands that LDS holds
+
 template <bool WIDE>
 struct StreamShape {
     static constexpr int TILE = WIDE ? 256 : 128, THREADS = WIDE ? 512 : 256, WAVES = THREADS / WAVE;
     static constexpr int BM = TILE / 2 / BLOCK;              // a wave's blocks along m; along n they are four
-    static constexpr int STAGE = 2 * TILE * 128, LDS = 2 * STAGE;
+    static constexpr int SLOT = TILE * 128, LDS = PS_SLOTS * SLOT;
 };
 
 // What a wave loads of an operand's tile: PIECES times 64 chunks, one per lane, which go to 1 KB of LDS in the lanes' order.
 template <typename T, bool KDENSE, bool WIDE>
 struct Stream {
     typedef StreamShape<WIDE> S;
-    typedef OperandTile<T, KDENSE, S::TILE> Tile;
+    typedef OperandTile<T, KDENSE, S::TILE, 2> Tile;
     static constexpr int PIECES = Tile::CHUNKS / S::THREADS, CH = Tile::CH;
     const char *base;            // of the step's values
     int64_t step;                // bytes to the next one's
@@ -30,7 +32,7 @@ struct Stream {
     __device__ __forceinline__ Stream(const void *data, int64_t ld, int64_t row0, int64_t rows, int64_t k0, int w, int lane) : wave(w)
     {
         base = (const char *)data + (KDENSE ? row0 * ld + k0 : k0 * ld + row0) * (int64_t)sizeof(T);
-        step = (KDENSE ? (int64_t)PB_K<T> : PB_K<T> * ld) * (int64_t)sizeof(T);
+        step = (KDENSE ? PS_K : PS_K * ld) * (int64_t)sizeof(T);
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int s = (i * S::WAVES + wave) * WAVE + lane, line = s / Tile::LINE, chunk = (s % Tile::LINE) ^ Tile::swizzle(line);
@@ -44,9 +46,10 @@ struct Stream {
             }
         }
     }
-    // `left`: values of k from the step's first on.  In assembly, since the compiler takes every read of LDS for one of what is still on its way and waits
-    // for it; nothing but LDS and M0 is written, which nothing else here uses, and the waits are landed()'s.
-    __device__ __forceinline__ void load(char *lds, int64_t left)
+    // The next step's tile; `left`: its values of k that exist.  Behind the last ones zeros are loaded, so that the number of loads does not depend on
+    // it.  In assembly, since the compiler takes every read of LDS for one of what is still on its way and waits for it; nothing but LDS and M0 is
+    // written, which nothing else here uses, and the waits are landed()'s.
+    __device__ __forceinline__ void load(char *lds, int left)
     {
         typedef uint32_t Words __attribute__((ext_vector_type(4)));
         const uint64_t from = (uint64_t)base;
@@ -54,17 +57,21 @@ struct Stream {
         const uint32_t to = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char *)lds + wave * 1024;
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint32_t o = left >= PB_K<T> || k[i] < left ? at[i] : PS_NOWHERE;
+            const uint32_t o = k[i] < left ? at[i] : PS_NOWHERE;
             asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * S::WAVES * 1024), "v"(o), "s"(r) : "memory");
         }
         base += step;
     }
-    static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+    template <int N>
+    static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 };
 
-// WIDE: tiles of 256 x 256 by eight waves of 128 x 64 in two groups of four, one of each group on every SIMD.  A step is two halves, each first
-// read from LDS into registers and then multiplied; the second group is one phase behind, so that a SIMD's matrix core works for one
-// wave while the other one reads.  A barrier ends every phase.
+// Steps of 64 values of k.  LDS holds five tiles of operands, both of the step that is read and of the next one, and a fifth that makes room for
+// one operand's step after that, so that one tile is asked for in every half of a step (both in its first half: products of 8,192^3 zeros at 1,390 instead of 1,600
+// TFLOP/s, since what misses an L2 holds up what follows it).
+// WIDE: tiles of 256 x 256 by eight waves of 128 x 64 in two groups of four, one of each group on every SIMD.  A half is first read from LDS into
+// registers and then multiplied; the second group is one phase behind, so that a SIMD's matrix core works for one wave while the other one
+// reads.  A barrier ends every phase.
 // Else: tiles of 128 x 128 by four waves of 64 x 64, two workgroups on a compute unit, which find their turns by themselves.
 template <typename T, typename O, bool AK, bool BK, bool WIDE>
 __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_kernel(ProductArgs p, EpilogueArgs e)
@@ -72,7 +79,7 @@ __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_
     typedef StreamShape<WIDE> S;
     typedef Stream<T, AK, WIDE> SA;
     typedef Stream<T, BK, WIDE> SB;
-    constexpr int KB = PB_K<T>, BM = S::BM, BN = 4;
+    constexpr int BM = S::BM, BN = 4;
     extern __shared__ __attribute__((aligned(16))) char lds[];
     const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n, id = workgroup();
     if (id >= tiles) return;
@@ -91,12 +98,14 @@ __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_
 #pragma unroll
         for (int j = 0; j < BN; ++j) acc[i][j] = mfma_acc_t{0.f, 0.f, 0.f, 0.f};
     uint4 fa[BM], fb[BN];
-    auto read = [&](const char *stage, int h) {
+    auto read = [&](const char *ta, const char *tb, int h) {
 #pragma unroll
-        for (int j = 0; j < BN; ++j) fb[j] = SB::Tile::fragment(stage + SA::Tile::BYTES, wn, j, h, lane);
+        for (int j = 0; j < BN; ++j) fb[j] = SB::Tile::fragment(tb, wn, j, h, lane);
 #pragma unroll
-        for (int i = 0; i < BM; ++i) fa[i] = SA::Tile::fragment(stage, wm, i, h, lane);
+        for (int i = 0; i < BM; ++i) fa[i] = SA::Tile::fragment(ta, wm, i, h, lane);
     };
+    auto left = [&](int64_t k) { return (int)(k_end - k < PS_K ? k_end - k : PS_K); };
+    auto slot = [&](int first, int n) { return lds + (first + n >= PS_SLOTS ? first + n - PS_SLOTS : first + n) * S::SLOT; };
     auto multiply = [&] {
         __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -111,47 +120,40 @@ __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_
         __builtin_amdgcn_sched_barrier(0);
     };
 
-    if (k0 < k_end) {
-        a.load(lds, k_end - k0);
-        b.load(lds + SA::Tile::BYTES, k_end - k0);
-        SA::landed();
-    }
+    auto have_read = [] { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); };
+
+    // step t's tiles are in slots 2 t and 2 t + 1, modulo their number
+    a.load(slot(0, 0), left(k0));
+    b.load(slot(0, 1), left(k0));
+    a.load(slot(0, 2), left(k0 + PS_K));
+    SA::template landed<SA::PIECES>();
     phase();
-    int stage = 0;
+    int first = 0;
     if (WIDE && group) phase();
-    for (int64_t k = k0; k < k_end; k += KB, stage ^= 1) {
-        const char *now = lds + stage * S::STAGE;
-        char *next = lds + (stage ^ 1) * S::STAGE;
-        const bool more = k + KB < k_end;
+    for (int64_t k = k0; k < k_end; k += PS_K) {
+        read(slot(first, 0), slot(first, 1), 0);
+        b.load(slot(first, 3), left(k + PS_K));              // where the first operand's step before this one was
         if (WIDE) {
-            read(now, 0);
-            if (more) {
-                a.load(next, k_end - k - KB);
-                b.load(next + SA::Tile::BYTES, k_end - k - KB);
-            }
-            phase();
-            multiply();
-            phase();
-            read(now, 1);
-            if (group) SA::landed();
-            phase();
-            multiply();
-            if (!group) SA::landed();
-            phase();
-        } else {
-            if (more) {
-                a.load(next, k_end - k - KB);
-                b.load(next + SA::Tile::BYTES, k_end - k - KB);
-            }
-            read(now, 0);
-            multiply();
-            read(now, 1);
-            multiply();
-            SA::landed();
+            have_read();
             phase();
         }
+        multiply();
+        if (WIDE) phase();
+        read(slot(first, 0), slot(first, 1), 1);
+        a.load(slot(first, 4), left(k + 2 * PS_K));
+        if (WIDE) {
+            have_read();                                     // (what is read now may be written over from the next phase but one on)
+            if (group) SA::template landed<SA::PIECES>();
+            phase();
+        }
+        multiply();
+        if (!WIDE || !group) SA::template landed<SA::PIECES>();
+        phase();
+        first = first + 2 >= PS_SLOTS ? first + 2 - PS_SLOTS : first + 2;
     }
     if (WIDE && !group) phase();
+    SA::template landed<0>();
+    phase();
     leave_tile<T, O, BM, 4>(p, e, m0 + wm, n0 + wn, lane, lds + wave * 4 * LEAVE_BLOCK, acc);
 }
 
