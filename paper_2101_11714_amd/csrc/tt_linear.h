@@ -8,7 +8,7 @@ namespace tt {
 
 struct SlopeArgs {
     const void *dy, *pre;        // pre null: no activation
-    void *dz;                    // null: not wanted (no activation)
+    void *dz;                    // rows of nv vectors, zeros behind the N-th column; null: not wanted
     float *part;                 // [bands][8 nv] sums of columns, null: not wanted
     int64_t ld_dy, ld_pre, ld_dz;
     int64_t rows, band;          // rows of a band
@@ -38,11 +38,11 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
                 widen8(y, z);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], a.act);
-                if (a.dz) put8<true>((T *)a.dz + row_at(r, a.ld_dz) + 8 * v, 8, d);      // (its rows are whole vectors)
             } else {
                 settle8<WHOLE>(x, n, a.N);
                 widen8(x, d);
             }
+            if (a.dz) put8<true>((T *)a.dz + row_at(r, a.ld_dz) + 8 * v, 8, d);
 #pragma unroll
             for (int j = 0; j < 8; ++j) s[j] += d[j];
         }
@@ -59,18 +59,23 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     a.part[(int64_t)blockIdx.y * 8 * a.nv + at] = y;
 }
 
-// the bands' sums added in their order
+// the bands' sums added in their order, 32 columns a workgroup, every 32nd band a thread
 template <typename W>
-__global__ __launch_bounds__(256) void bias_sum_kernel(const float *part, int bands, int N, int cols, W *db, int add)
+__global__ __launch_bounds__(1024) void bias_sum_kernel(const float *part, int bands, int N, int cols, W *db, int add)
 {
-    __shared__ float sums[4][64];
-    const int c = threadIdx.x & 63, q = threadIdx.x >> 6, at = blockIdx.x * 64 + c;
+    __shared__ float sums[32][33];
+    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, at = blockIdx.x * 32 + c;
     float s = 0.f;
     if (at < N)
-        for (int b = q; b < bands; b += 4) s += part[(int64_t)b * cols + at];
+#pragma unroll 8
+        for (int b = q; b < bands; b += 32) s += part[(int64_t)b * cols + at];
     sums[q][c] = s;
     __syncthreads();
-    if (q == 0 && at < N) db[at] = (W)((add ? (float)db[at] : 0.f) + ((sums[0][c] + sums[1][c]) + (sums[2][c] + sums[3][c])));
+    if (q || at >= N) return;
+    float y = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) y += sums[i][c];
+    db[at] = (W)((add ? (float)db[at] : 0.f) + y);
 }
 
 }  // namespace tt

@@ -41,19 +41,19 @@ int check_workspace(size_t need, const void *workspace, size_t bytes)
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where what lies in the workspace of a gradient: parts of sums first (of one product, then of the other), the gradient in front of the
-// activation, the columns' sums of the bands.
+// activation, or a copy of the output's in rows of whole chunks where a product could not load it in these, the columns' sums of the bands.
 struct GradRoom {
     size_t parts, dz, bands, all;
     int64_t band, n_bands;
 };
 
-GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, int32_t act, bool x, bool w, bool b)
+GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, bool x, bool w, bool b)
 {
     GradRoom r{};
     const size_t px = x ? product_bytes(M, K, N, type) : 0, pw = w ? product_bytes(N, K, M, type) : 0;
     const int64_t cols = 8 * ceil_div(N, 8);
     r.parts = up(px > pw ? px : pw);
-    r.dz = act != TT_ACT_NONE && (x || w) ? up((size_t)M * (size_t)cols * element_bytes(type)) : 0;
+    r.dz = copy && (x || w) ? up((size_t)M * (size_t)cols * element_bytes(type)) : 0;
     r.n_bands = M < 64 * 256 ? ceil_div(M, 64) : 256;
     r.band = ceil_div(M, r.n_bands > 0 ? r.n_bands : 1);
     r.bands = b ? up((size_t)r.n_bands * (size_t)cols * sizeof(float)) : 0;
@@ -88,13 +88,13 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
     if (activation < 0 || activation >= ACT_COUNT) return fail(TT_ERR_BAD_ARG, "activation %d", (int)activation);
     if ((rc = check_workspace(tt_linear_fwd_workspace_bytes(n_rows, K, N, x->type), workspace, workspace_bytes))) return rc;
     EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
-    return product(x->type, DENSE_DENSE, output->type, x->data, x->ld, weight->data, weight->ld, n_rows, N, K, e, workspace, (hipStream_t)stream);
+    return product(x->type, DENSE_DENSE, output->type, x->data, x->ld, false, weight->data, weight->ld, n_rows, N, K, e, workspace, (hipStream_t)stream);
 }
 
 size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation)
 {
     if (check_product(n_rows, K, N) || (type != TT_F32 && type != TT_BF16 && type != TT_F16)) return 0;
-    return grad_room(n_rows, K, N, type, activation, true, true, true).all;
+    return grad_room(n_rows, K, N, type, activation != TT_ACT_NONE || type != TT_F32, true, true, true).all;
 }
 
 int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_rows_t *weight, const tt_rows_t *pre, int32_t activation,
@@ -120,12 +120,14 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         if (grad_weight->type != type && grad_weight->type != TT_F32) return fail(TT_ERR_UNSUPPORTED, "grad_weight has grad_output's type or 32 bits");
     }
     if ((rc = check_vector(grad_bias, "grad_bias", grad_bias_type))) return rc;
-    const GradRoom room = grad_room(n_rows, K, N, type, activation, grad_x != nullptr, grad_weight != nullptr, grad_bias != nullptr);
+    const bool copy = activation != TT_ACT_NONE || (type != TT_F32 && !whole_chunks(grad_output->data, grad_output->ld, N, type));
+    const GradRoom room = grad_room(n_rows, K, N, type, copy, grad_x != nullptr, grad_weight != nullptr, grad_bias != nullptr);
     if ((rc = check_workspace(room.all, workspace, workspace_bytes))) return rc;
     hipStream_t st = (hipStream_t)stream;
     char *ws = (char *)workspace;
     const void *dz = grad_output->data;
     int64_t ld_dz = grad_output->ld;
+    const bool padded = room.dz > 0;                         // (the slopes' kernel writes whole vectors)
     if (N > 0 && (room.dz || room.bands) && n_rows > 0) {
         SlopeArgs a{};
         a.dy = grad_output->data;
@@ -155,7 +157,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
     }
     if (grad_bias && N > 0) {
         with_type(grad_bias_type, [&](auto w) {
-            hipLaunchKernelGGL((bias_sum_kernel<decltype(w)>), dim3((unsigned)ceil_div(N, 64)), dim3(WG), 0, st, (const float *)(ws + room.parts + room.dz), (int)room.n_bands, (int)N,
+            hipLaunchKernelGGL((bias_sum_kernel<decltype(w)>), dim3((unsigned)ceil_div(N, 32)), dim3(1024), 0, st, (const float *)(ws + room.parts + room.dz), (int)room.n_bands, (int)N,
                                (int)(8 * ceil_div(N, 8)), (decltype(w) *)grad_bias, accumulate);
         });
         if ((rc = launched("gradient launch"))) return rc;
@@ -164,7 +166,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         EpilogueArgs e{};
         e.out = grad_x->data;
         e.ld_out = grad_x->ld;
-        if ((rc = product(type, DENSE_STRIDED, type, dz, ld_dz, weight->data, weight->ld, n_rows, K, N, e, ws, st))) return rc;
+        if ((rc = product(type, DENSE_STRIDED, type, dz, ld_dz, padded, weight->data, weight->ld, n_rows, K, N, e, ws, st))) return rc;
     }
     if (grad_weight && !(accumulate && n_rows == 0)) {
         EpilogueArgs e{};
@@ -174,7 +176,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
             e.add = e.out;
             e.ld_add = e.ld_out;
         }
-        rc = product(type, STRIDED_STRIDED, grad_weight->type, dz, ld_dz, x->data, x->ld, N, K, n_rows, e, ws, st);
+        rc = product(type, STRIDED_STRIDED, grad_weight->type, dz, ld_dz, padded, x->data, x->ld, N, K, n_rows, e, ws, st);
     }
     return rc;
 }

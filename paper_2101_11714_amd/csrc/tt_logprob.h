@@ -3,9 +3,8 @@
 // One pass over a row holds the largest logit m so far, S = sum of exp(z - m) and T = sum of exp(z - m) (z - m) in 32 bits, and multiplies the two
 // sums when m grows; lse = m + log S, entropy = log S - T / S, both without a difference of large numbers.  Few rows are cut into
 // pieces, a workgroup each, which a second launch joins.
-// The k likeliest: the k-th largest of the threads' largest logits is no larger than the k-th largest of all, so that a second look at the
-// piece, by then in the caches, leaves little more than k to be ranked.  Logits are ordered by a 64-bit key, value first and column
-// after it, so that no two are equal.
+// The k likeliest: the k-th largest of the threads' largest logits is no larger than the k-th largest of all, so that few more than k logits
+// are left to be ranked.  Logits are ordered by a 64-bit key, value first and column after it, so that no two are equal.
 #pragma once
 
 #include "tt_rows_io.h"
@@ -67,6 +66,18 @@ __device__ __forceinline__ uint64_t key_of(float x, uint32_t column)
     return x == -INFINITY ? 0ull : (uint64_t)order_of(x) << 32 | (uint32_t)~column;
 }
 
+// how many of the 256 values are larger, and how many are no smaller
+__device__ __forceinline__ void counts_of(const uint4 *orders, uint32_t own, int &more, int &least)
+{
+    more = least = 0;
+#pragma unroll 8
+    for (int i = 0; i < WG / 4; ++i) {
+        const uint4 o = orders[i];
+        more += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
+        least += (o.x >= own) + (o.y >= own) + (o.z >= own) + (o.w >= own);
+    }
+}
+
 // how many of n keys are larger
 __device__ __forceinline__ int rank_of(const uint64_t *keys, int n, uint64_t key)
 {
@@ -105,55 +116,74 @@ __device__ __forceinline__ void leave_top(const LogprobArgs &a, int64_t row, int
     if (a.top) a.top[at] = key ? a.scale * (value_of((uint32_t)(key >> 32)) - m) - log_s : -INFINITY;
 }
 
-// the vectors [from, to) of a row, U at a time per thread: f(vector's number, its eight logits), -inf where there is no column
-template <typename T, bool WHOLE, typename F>
-__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
-{
-    for (int v0 = from + threadIdx.x; v0 < to; v0 += WG * LP_UNROLL) {
-        Vec8<T> r[LP_UNROLL];
+// Four vectors of eight logits of a row per thread, and the walk over the vectors [from, to): f(vector's number, its logits), -inf where there is no column.
+template <typename T, bool WHOLE>
+struct Vectors {
+    Vec8<T> r[LP_UNROLL];
+
+    __device__ __forceinline__ void fetch(const T *line, int v0, int to, int V)
+    {
 #pragma unroll
         for (int i = 0; i < LP_UNROLL; ++i) {
-            const int v = v0 + i * WG < to ? v0 + i * WG : v0;
+            const int v = v0 + i * WG < to ? v0 + i * WG : to - 1;
             r[i] = fetch8<WHOLE>(line + 8 * (int64_t)v, V - 8 * v, V);
         }
+    }
+    template <typename F>
+    __device__ __forceinline__ void each(int v0, int to, int V, F f) const
+    {
 #pragma unroll
         for (int i = 0; i < LP_UNROLL; ++i) {
             const int v = v0 + i * WG;
             if (v >= to) break;
+            Vec8<T> y = r[i];
             float x[8];
-            settle8<WHOLE>(r[i], V - 8 * v, V);
-            widen8(r[i], x);
-            if (!WHOLE)
+            settle8<WHOLE>(y, V - 8 * v, V);
+            widen8(y, x);
+            if (!WHOLE && 8 * v + 8 > V)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = 8 * v + j < V ? x[j] : -INFINITY;
             f(v, x);
         }
     }
+};
+
+template <typename T, bool WHOLE, typename F>
+__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
+{
+    for (int v0 = from + threadIdx.x; v0 < to; v0 += WG * LP_UNROLL) {
+        Vectors<T, WHOLE> held;
+        held.fetch(line, v0, to, V);
+        held.each(v0, to, V, f);
+    }
 }
 
-// The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  `best`: the thread's largest.
-template <typename T, bool WHOLE>
-__device__ void largest_keys(const T *line, int from, int to, int V, int k, uint64_t best, uint64_t *list, int *count, uint64_t *least, uint64_t *out)
+// The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  order: of the thread's largest logit, 0 where it has none;
+// look(f): calls f(column, logit) for all of the thread's.
+template <typename L>
+__device__ __forceinline__ void largest_keys(int k, uint32_t order, uint64_t *list, int *count, uint64_t *least, uint64_t *out, L look)
 {
-    list[threadIdx.x] = best;
+    uint32_t *orders = reinterpret_cast<uint32_t *>(list);
+    orders[threadIdx.x] = order;
     if (threadIdx.x == 0) {
         *count = 0;
         *least = 1;
     }
     __syncthreads();
-    if (best && rank_of(list, WG, best) == k - 1) *least = best;
+    int more, no_less;
+    counts_of(reinterpret_cast<const uint4 *>(orders), order, more, no_less);
+    if (order && more < k && no_less >= k) *least = (uint64_t)order << 32;               // (whoever has that value writes the same)
     __syncthreads();
     int n;
     for (;;) {
         const uint64_t bound = *least;
-        each_vector<T, WHOLE>(line, from, to, V, [&](int v, float (&x)[8]) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const uint64_t key = key_of(x[j], 8 * v + j);
-                if (key >= bound) {
-                    const int at = atomicAdd(count, 1);
-                    if (at < LP_LIST) list[at] = key;
-                }
+        const float at_least = bound > 1 ? value_of((uint32_t)(bound >> 32)) : -INFINITY;
+        look([&](int column, float x) {
+            if (x < at_least) return;                        // (a NaN is not)
+            const uint64_t key = key_of(x, column);
+            if (key >= bound) {
+                const int at = atomicAdd(count, 1);
+                if (at < LP_LIST) list[at] = key;
             }
         });
         __syncthreads();
@@ -176,7 +206,8 @@ __device__ void largest_keys(const T *line, int from, int to, int V, int k, uint
     for (int i = n + threadIdx.x; i < k; i += WG) out[i] = 0;
 }
 
-template <typename T, bool TOP, bool WHOLE>
+// HELD: a piece is at most four vectors a thread, which stay in registers for the second look.
+template <typename T, bool TOP, bool ENTROPY, bool WHOLE, bool HELD>
 __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
 {
     __shared__ Sums waves[NWAVE];
@@ -189,15 +220,14 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
     const T *line = (const T *)a.logits + row * a.ld;
     const float c = a.scale * LOG2E;
     Sums r{LP_LEAST, 0.f, 0.f};
-    float best = -INFINITY;
-    uint32_t column = 0, order = 0;
-    each_vector<T, WHOLE>(line, from, to, a.V, [&](int v, float (&x)[8]) {
+    uint32_t order = 0;
+    auto add = [&](int v, const float (&x)[8]) {
         float m = r.m;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
         if (m > r.m) {
             const float d = fmaxf(r.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
-            r.t = f == 0.f ? 0.f : f * (r.t + d * r.s);
+            if (ENTROPY) r.t = f == 0.f ? 0.f : f * (r.t + d * r.s);
             r.s *= f;
             r.m = m;
         }
@@ -205,18 +235,17 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
         for (int j = 0; j < 8; ++j) {
             const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * c);
             r.s += e;
-            r.t += e * fmaxf(d, LP_LEAST);
-            if (TOP) {
-                const uint32_t o = order_of(x[j]);
-                if (o > order && x[j] != -INFINITY) {
-                    order = o;
-                    best = x[j];
-                    column = 8 * v + j;
-                }
-            }
+            if (ENTROPY) r.t += e * fmaxf(d, LP_LEAST);
+            if (TOP) order = max(order, x[j] == -INFINITY ? 0u : order_of(x[j]));
         }
-    });
-    const uint64_t key = TOP ? key_of(best, column) : 0;
+    };
+    Vectors<T, WHOLE> held;
+    if (HELD) {
+        held.fetch(line, from + threadIdx.x, to, a.V);
+        held.each(from + threadIdx.x, to, a.V, add);
+    } else {
+        each_vector<T, WHOLE>(line, from, to, a.V, add);
+    }
     // lanes, then waves
 #pragma unroll
     for (int b = 1; b < WAVE; b <<= 1) {
@@ -226,14 +255,17 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = r;
     __syncthreads();
     r = joined(joined(waves[0], waves[1], c), joined(waves[2], waves[3], c), c);
-    if (TOP) largest_keys<T, WHOLE>(line, from, to, a.V, a.k, key, list, &count, &least, found);
+    if (TOP)
+        largest_keys(a.k, order, list, &count, &least, found, [&](auto f) {
+            auto each = [&](int v, const float (&x)[8]) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f(8 * v + j, x[j]);
+            };
+            if (HELD) held.each(from + threadIdx.x, to, a.V, each);
+            else each_vector<T, WHOLE>(line, from, to, a.V, each);
+        });
     if (a.pieces > 1) {
-        if (threadIdx.x == 0) {
-            float *p = a.sums + id * 4;
-            p[0] = r.m;
-            p[1] = r.s;
-            p[2] = r.t;
-        }
+        if (threadIdx.x == 0) *reinterpret_cast<float4 *>(a.sums + id * 4) = make_float4(r.m, r.s, r.t, 0.f);
         if (TOP) {
             __syncthreads();
             for (int i = threadIdx.x; i < a.k; i += WG) a.keys[id * a.k + i] = found[i];
@@ -248,15 +280,24 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
     }
 }
 
-// a row's pieces joined, in their order: a workgroup of one wave per row without alternatives, of four with them
+// A row's pieces joined, in their order: a workgroup of one wave per row without alternatives; with them of LP_JOIN threads, which share out the
+// comparisons of every key with every other.
+constexpr int LP_JOIN = 1024;
+
 template <typename T, bool TOP>
-__global__ __launch_bounds__(WG) void logprob_join_kernel(LogprobArgs a)
+__global__ __launch_bounds__(TOP ? LP_JOIN : WAVE) void logprob_join_kernel(LogprobArgs a)
 {
     __shared__ __attribute__((aligned(16))) uint64_t list[TOP ? LP_LIST : 1];
+    __shared__ int ranks[TOP ? LP_LIST : 1];
     __shared__ float row_m, row_log_s;
     const int64_t row = workgroup();
     if (row >= a.rows) return;
     const float c = a.scale * LOG2E;
+    const int n = a.pieces * a.k;                            // (at most LP_LIST)
+    if (TOP && threadIdx.x < n) {
+        list[threadIdx.x] = a.keys[row * n + threadIdx.x];
+        ranks[threadIdx.x] = 0;
+    }
     if (threadIdx.x < WAVE) {
         Sums r{LP_LEAST, 0.f, 0.f};
         for (int p = threadIdx.x; p < a.pieces; p += WAVE) {
@@ -275,22 +316,22 @@ __global__ __launch_bounds__(WG) void logprob_join_kernel(LogprobArgs a)
         }
     }
     if (!TOP) return;
-    const int n = a.pieces * a.k;                            // (at most LP_LIST)
-    for (int i = threadIdx.x; i < n; i += WG) list[i] = a.keys[row * n + i];
     __syncthreads();
-    int there = 0;
-    for (int i = threadIdx.x; i < n; i += WG) {
-        const uint64_t key = list[i];
-        if (!key) continue;
-        const int r = rank_of(list, n, key);
-        if (r < a.k) leave_top(a, row, r, key, row_m, row_log_s);
+    // a key's rank: in every piece's list, which is in order, the number of larger ones
+    for (int i = threadIdx.x; i < n * a.pieces; i += LP_JOIN) {
+        const int p = i / n, at = i - p * n;
+        const uint64_t key = list[at], *other = list + p * a.k;
+        int lo = 0, hi = a.k;
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (other[mid] > key) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo) atomicAdd(&ranks[at], lo);
     }
-    // places that no key takes
-    for (int i = threadIdx.x; i < a.k; i += WG) {
-        there = 0;
-        for (int j = 0; j < n; ++j) there += list[j] != 0;
-        if (i >= there) leave_top(a, row, i, 0, row_m, row_log_s);
-    }
+    const int there = __syncthreads_count(threadIdx.x < n && list[threadIdx.x] != 0);
+    if (threadIdx.x < n && list[threadIdx.x] != 0 && ranks[threadIdx.x] < a.k) leave_top(a, row, ranks[threadIdx.x], list[threadIdx.x], row_m, row_log_s);
+    if (threadIdx.x < a.k && (int)threadIdx.x >= there) leave_top(a, row, threadIdx.x, 0, row_m, row_log_s);
 }
 
 struct LogprobGradArgs {

@@ -285,82 +285,114 @@ __global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, Epilogue
     finish8<T, O>(e, m, n, have, bias, v);
 }
 
-// A tile of TM x TN per workgroup of 2 x 2 waves, operands through registers into LDS, so that every alignment and edge is right.
-template <typename T, typename O, bool AK, bool BK, int TM, int TN>
+// What a thread loads of an operand's tile through registers: PIECES chunks of 16 bytes.  Steps in the middle load from any address; where the tile or
+// the step ends outside of the operand every chunk is looked at.
+template <typename T, bool KDENSE, int ROWS, int THREADS>
+struct Staged {
+    typedef OperandTile<T, KDENSE, ROWS, 2> Tile;
+    static constexpr int PIECES = Tile::CHUNKS / THREADS, CH = Tile::CH;
+    static_assert(Tile::CHUNKS % THREADS == 0, "every thread has as many");
+    const T *line[PIECES];       // where the thread's lines begin (KDENSE: at k = 0; else at the tile's first row, k = 0)
+    int64_t ld, rows, row0;
+    uint4 reg[PIECES];
+    bool inside;                 // all rows of the tile exist
+
+    static __device__ __forceinline__ int line_of(int i) { return (i * THREADS + threadIdx.x) / Tile::LINE; }
+    static __device__ __forceinline__ int chunk_of(int i) { return (i * THREADS + threadIdx.x) % Tile::LINE; }
+    __device__ __forceinline__ Staged(const void *data, int64_t stride, int64_t first, int64_t n) : ld(stride), rows(n), row0(first), inside(first + ROWS <= n)
+    {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int64_t row = first + line_of(i);
+            if (KDENSE) line[i] = (const T *)data + (row < n ? row : n - 1) * ld + chunk_of(i) * CH;
+            else line[i] = (const T *)data + line_of(i) * ld + first + chunk_of(i) * CH;
+        }
+    }
+    // the step's values from k on, of which those below `end` exist
+    __device__ __forceinline__ void fetch(int64_t k, int64_t end)
+    {
+        if (k + PB_K<T> <= end && (KDENSE || inside)) {
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) reg[i] = __builtin_bit_cast(uint4, *reinterpret_cast<const typename Chunk<T>::Anywhere *>(line[i] + (KDENSE ? k : k * ld)));
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = chunk_of(i) * CH;
+            if (KDENSE) reg[i] = fetch_chunk(line[i] - c, k + c, end);
+            else reg[i] = k + line_of(i) < end ? fetch_chunk(line[i] + k * ld - c - row0, row0 + c, rows) : uint4{0u, 0u, 0u, 0u};
+        }
+    }
+    __device__ __forceinline__ void put(char *lds) const
+    {
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) *reinterpret_cast<uint4 *>(lds + Tile::at(line_of(i), chunk_of(i))) = reg[i];
+    }
+};
+
+// A tile of TM x TN per workgroup of WM x (4 / WM) waves, operands through registers into LDS, so that every alignment and edge is right.  Two tiles of
+// each operand in LDS: while one is multiplied the next one is written, and the one after it is on its way.
+template <typename T, typename O, bool AK, bool BK, int TM, int TN, int WM>
 __global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArgs e)
 {
-    typedef OperandTile<T, AK, TM, 2> TA;
-    typedef OperandTile<T, BK, TN, 2> TB;
-    constexpr int KB = PB_K<T>, BM = TM / 2 / BLOCK, BN = TN / 2 / BLOCK, PA = TA::CHUNKS / 256, PB = TB::CHUNKS / 256;
+    typedef Staged<T, AK, TM, 256> SA;
+    typedef Staged<T, BK, TN, 256> SB;
+    constexpr int KB = PB_K<T>, BM = TM / WM / BLOCK, BN = TN / (4 / WM) / BLOCK, STAGE = SA::Tile::BYTES + SB::Tile::BYTES;
     static_assert(BN == 4, "what a wave leaves is 64 columns wide");
-    constexpr int SOME = BM < 2 ? 1 : 2;
-    static_assert(4 * SOME * LEAVE_BLOCK <= TA::BYTES + TB::BYTES, "room for the sums");
-    __shared__ __attribute__((aligned(16))) char lds[TA::BYTES + TB::BYTES];
+    constexpr int SOME = BM < 4 ? BM : 4;
+    static_assert(4 * SOME * LEAVE_BLOCK <= 2 * STAGE, "room for the sums");
+    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE];
     if (workgroup() >= (int64_t)p.tiles_m * p.tiles_n) return;
     int tm, tn;
     tile_place((int)workgroup(), p.tiles_m, p.tiles_n, tm, tn);
     const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN, k0 = (int64_t)blockIdx.z * p.k_part;
     const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = (wave >> 1) * (TM / 2), wn = (wave & 1) * (TN / 2);
-
-    uint4 ra[PA], rb[PB];
-    auto fetch = [&](int64_t k) {
-#pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int s = i * 256 + threadIdx.x, line = s / TA::LINE, chunk = s % TA::LINE;
-            if (AK) {
-                const int64_t row = m0 + line < p.M ? m0 + line : p.M - 1;
-                ra[i] = fetch_chunk((const T *)p.a + row * p.lda, k + chunk * TA::CH, k_end);
-            } else {
-                ra[i] = k + line < k_end ? fetch_chunk((const T *)p.a + (k + line) * p.lda, m0 + chunk * TA::CH, p.M) : uint4{0u, 0u, 0u, 0u};
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int s = i * 256 + threadIdx.x, line = s / TB::LINE, chunk = s % TB::LINE;
-            if (BK) {
-                const int64_t row = n0 + line < p.N ? n0 + line : p.N - 1;
-                rb[i] = fetch_chunk((const T *)p.b + row * p.ldb, k + chunk * TB::CH, k_end);
-            } else {
-                rb[i] = k + line < k_end ? fetch_chunk((const T *)p.b + (k + line) * p.ldb, n0 + chunk * TB::CH, p.N) : uint4{0u, 0u, 0u, 0u};
-            }
-        }
-    };
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave / (4 / WM) * (TM / WM), wn = wave % (4 / WM) * 64;
+    SA a(p.a, p.lda, m0, p.M);
+    SB b(p.b, p.ldb, n0, p.N);
 
     mfma_acc_t acc[BM][BN];
 #pragma unroll
     for (int i = 0; i < BM; ++i)
 #pragma unroll
         for (int j = 0; j < BN; ++j) acc[i][j] = mfma_acc_t{0.f, 0.f, 0.f, 0.f};
-    if (k0 < k_end) fetch(k0);
-    for (int64_t k = k0; k < k_end; k += KB) {
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < PA; ++i) {
-            const int s = i * 256 + threadIdx.x;
-            *reinterpret_cast<uint4 *>(lds + TA::at(s / TA::LINE, s % TA::LINE)) = ra[i];
+    if (k0 < k_end) {
+        a.fetch(k0, k_end);
+        b.fetch(k0, k_end);
+        a.put(lds);
+        b.put(lds + SA::Tile::BYTES);
+        if (k0 + KB < k_end) {
+            a.fetch(k0 + KB, k_end);
+            b.fetch(k0 + KB, k_end);
         }
-#pragma unroll
-        for (int i = 0; i < PB; ++i) {
-            const int s = i * 256 + threadIdx.x;
-            *reinterpret_cast<uint4 *>(lds + TA::BYTES + TB::at(s / TB::LINE, s % TB::LINE)) = rb[i];
+    }
+    __syncthreads();
+    int stage = 0;
+    for (int64_t k = k0; k < k_end; k += KB, stage ^= 1) {
+        const char *now = lds + stage * STAGE;
+        char *next = lds + (stage ^ 1) * STAGE;
+        if (k + KB < k_end) {
+            a.put(next);
+            b.put(next + SA::Tile::BYTES);
         }
-        __syncthreads();
-        if (k + KB < k_end) fetch(k + KB);
+        if (k + 2 * KB < k_end) {
+            a.fetch(k + 2 * KB, k_end);
+            b.fetch(k + 2 * KB, k_end);
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             uint4 fa[BM], fb[BN];
 #pragma unroll
-            for (int i = 0; i < BM; ++i) fa[i] = TA::fragment(lds, wm, i, h, lane);
+            for (int i = 0; i < BM; ++i) fa[i] = SA::Tile::fragment(now, wm, i, h, lane);
 #pragma unroll
-            for (int j = 0; j < BN; ++j) fb[j] = TB::fragment(lds + TA::BYTES, wn, j, h, lane);
+            for (int j = 0; j < BN; ++j) fb[j] = SB::Tile::fragment(now + SA::Tile::BYTES, wn, j, h, lane);
 #pragma unroll
             for (int i = 0; i < BM; ++i)
 #pragma unroll
                 for (int j = 0; j < BN; ++j) block_product<T>(fb[j], fa[i], acc[i][j]);
         }
+        __syncthreads();
     }
-    __syncthreads();
     leave_tile<T, O, BM, SOME>(p, e, m0 + wm, n0 + wn, lane, lds + wave * SOME * LEAVE_BLOCK, acc);
 }
 

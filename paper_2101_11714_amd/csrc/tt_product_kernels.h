@@ -7,11 +7,11 @@ namespace tt {
 
 // C = A B^T; AK, BK: the operands' rows are dense in k
 template <typename T, typename O, bool AK, bool BK>
-int launch_product(const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st)
+int launch_product(const void *a, int64_t lda, bool a_padded, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st)
 {
     if (M == 0 || N == 0) return TT_OK;
     const int32_t type = sizeof(T) == 4 ? TT_F32 : TT_BF16;
-    const bool whole = whole_chunks(a, lda, AK ? K : M, type) && whole_chunks(b, ldb, BK ? K : N, type);
+    const bool whole = whole_chunks(a, lda, AK ? K : M, type, a_padded) && whole_chunks(b, ldb, BK ? K : N, type);
     const Plan p = plan_of(M, N, K, type, AK && BK, whole);
     ProductArgs q{a, b, lda, ldb, M, N, K, (int)p.tiles_m, (int)p.tiles_n, p.k_part, p.parts > 1 ? (float *)workspace : nullptr, 8 * ceil_div(N, 8)};
     if (p.way == FEW) {
@@ -27,11 +27,12 @@ int launch_product(const void *a, int64_t lda, const void *b, int64_t ldb, int64
         }
         return launched("product launch");
     }
-    if (p.way == TILES) {
+    if (p.way == TILES || p.way == SMALL_TILES) {
         dim3 grid = grid_of(p.tiles_m * p.tiles_n, WG);
         grid.z = (unsigned)p.parts;
-        if (M <= 32) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 32, 128>), grid, dim3(WG), 0, st, q, e);
-        else hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 128>), grid, dim3(WG), 0, st, q, e);
+        if (p.way == TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 128, 2>), grid, dim3(WG), 0, st, q, e);
+        if constexpr (sizeof(T) == 4)
+            if (p.way == SMALL_TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 64, 64, 4>), grid, dim3(WG), 0, st, q, e);
     } else if constexpr (sizeof(T) == 2) {
         int rc = TT_OK;
         with_flag(p.way == STREAM_WIDE, [&](auto w) {
@@ -54,16 +55,16 @@ int launch_product(const void *a, int64_t lda, const void *b, int64_t ldb, int64
 }
 
 template <typename T>
-int product_of(Layout layout, int32_t out_type, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e,
+int product_of(Layout layout, int32_t out_type, const void *a, int64_t lda, bool a_padded, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e,
                void *workspace, hipStream_t st)
 {
-    if (layout == DENSE_STRIDED) return launch_product<T, T, true, false>(a, lda, b, ldb, M, N, K, e, workspace, st);
+    if (layout == DENSE_STRIDED) return launch_product<T, T, true, false>(a, lda, a_padded, b, ldb, M, N, K, e, workspace, st);
     if (layout == STRIDED_STRIDED) {
-        if (out_type == TT_F32) return launch_product<T, float, false, false>(a, lda, b, ldb, M, N, K, e, workspace, st);
-        return launch_product<T, T, false, false>(a, lda, b, ldb, M, N, K, e, workspace, st);
+        if (out_type == TT_F32) return launch_product<T, float, false, false>(a, lda, a_padded, b, ldb, M, N, K, e, workspace, st);
+        return launch_product<T, T, false, false>(a, lda, a_padded, b, ldb, M, N, K, e, workspace, st);
     }
-    if (out_type == TT_F32) return launch_product<T, float, true, true>(a, lda, b, ldb, M, N, K, e, workspace, st);
-    return launch_product<T, T, true, true>(a, lda, b, ldb, M, N, K, e, workspace, st);
+    if (out_type == TT_F32) return launch_product<T, float, true, true>(a, lda, a_padded, b, ldb, M, N, K, e, workspace, st);
+    return launch_product<T, T, true, true>(a, lda, a_padded, b, ldb, M, N, K, e, workspace, st);
 }
 
 }  // namespace tt

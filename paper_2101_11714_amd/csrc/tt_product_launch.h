@@ -11,7 +11,7 @@ namespace tt {
 enum Layout { DENSE_DENSE, DENSE_STRIDED, STRIDED_STRIDED };
 
 // How a product is computed.
-enum Way { FEW, TILES, STREAM, STREAM_WIDE };
+enum Way { FEW, SMALL_TILES, TILES, STREAM, STREAM_WIDE };
 
 struct Plan {
     Way way;
@@ -21,14 +21,6 @@ struct Plan {
 };
 
 constexpr int64_t MOST_TILES = 512;                          // workgroups that parts are made for
-
-// Parts of k, of four steps at least, where the tiles alone are too few for the device.
-inline int64_t parts_of(int64_t tiles, int64_t steps)
-{
-    int64_t parts = tiles < 256 ? MOST_TILES / (tiles > 0 ? tiles : 1) : 1;
-    if (parts > steps / 4) parts = steps / 4;
-    return parts < 1 ? 1 : parts;
-}
 
 // Tiles of 256 or of 128, and how many parts of k: whatever should be done first, by what was measured on 256 compute units.  A step of a wide tile,
 // one on a compute unit, takes 1.87 us (8,192 x 16,384 x 4,096: 1,127 TFLOP/s); one of a narrow tile 0.70 us alone on its compute unit and 1.17 beside
@@ -67,39 +59,44 @@ inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense, b
     } else if (whole && type != TT_F32) {
         stream_plan(p, M, N, K);
     } else {
-        p.way = TILES;
-        p.tiles_m = ceil_div(M, M <= 32 ? 32 : 128);
-        p.tiles_n = ceil_div(N, 128);
-        const int64_t step = 128 / element_bytes(type), steps = ceil_div(K, step);
-        p.k_part = ceil_div(steps, parts_of(p.tiles_m * p.tiles_n, steps)) * step;
+        // 32 bits: the matrix cores take sixteen times as long as for 16 and LDS is no bound, so that small tiles, which share out better, cost nothing
+        // until there are many large ones
+        p.way = type == TT_F32 && ceil_div(M, 128) * ceil_div(N, 128) < 1024 ? SMALL_TILES : TILES;
+        const int64_t tile = p.way == TILES ? 128 : 64, step = 128 / element_bytes(type), steps = ceil_div(K, step);
+        p.tiles_m = ceil_div(M, tile);
+        p.tiles_n = ceil_div(N, tile);
+        int64_t parts = (p.way == TILES ? MOST_TILES : 2 * MOST_TILES) / (p.tiles_m * p.tiles_n > 0 ? p.tiles_m * p.tiles_n : 1);
+        if (parts > steps / 4) parts = steps / 4;
+        p.k_part = ceil_div(steps, parts < 1 ? 1 : parts) * step;
         p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
     }
     return p;
 }
 
-// What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but a part is
-// no larger than its tiles.
+// What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but no more than
+// 256 wide tiles' or MOST_TILES narrow ones' worth of rows, or the same of small ones.
 inline size_t product_bytes(int64_t M, int64_t N, int64_t K, int32_t type)
 {
     if (M <= 0 || N <= 0) return 0;
     const int64_t most = ceil_div(K, 128 / element_bytes(type)) / 4, wide = ceil_div(N, 256);
     if (wide >= 256 || most < 2) return 0;
-    const int64_t rows = M * (most < MOST_TILES ? most : MOST_TILES), tiled = MOST_TILES * 256 / wide;
+    const int64_t rows = M * (most < 2 * MOST_TILES ? most : 2 * MOST_TILES), tiled = MOST_TILES * 256 / wide;
     return (size_t)(rows < tiled ? rows : tiled) * (size_t)(8 * ceil_div(N, 8)) * sizeof(float);
 }
 
-inline bool whole_chunks(const void *p, int64_t ld, int64_t columns, int32_t type)
+// padded: rows end in zeros up to a whole chunk
+inline bool whole_chunks(const void *p, int64_t ld, int64_t columns, int32_t type, bool padded = false)
 {
-    return type != TT_F32 && columns % 8 == 0 && ld % 8 == 0 && (uintptr_t)p % 16 == 0 && ld <= PS_MOST_STRIDE;
+    return type != TT_F32 && (padded || columns % 8 == 0) && ld % 8 == 0 && (uintptr_t)p % 16 == 0 && ld <= PS_MOST_STRIDE;
 }
 
-// C = A B^T, of M x N with sums over K, by the kernels of type T; out_type: T or 32 bits.
+// C = A B^T, of M x N with sums over K, by the kernels of type T; out_type: T or 32 bits.  a_padded: A's rows end in zeros up to a whole chunk.
 template <typename T>
-int product_of(Layout layout, int32_t out_type, const void *a, int64_t lda, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e,
+int product_of(Layout layout, int32_t out_type, const void *a, int64_t lda, bool a_padded, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e,
                void *workspace, hipStream_t st);
-extern template int product_of<float>(Layout, int32_t, const void *, int64_t, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
-extern template int product_of<bf16_t>(Layout, int32_t, const void *, int64_t, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
-extern template int product_of<f16_t>(Layout, int32_t, const void *, int64_t, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+extern template int product_of<float>(Layout, int32_t, const void *, int64_t, bool, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+extern template int product_of<bf16_t>(Layout, int32_t, const void *, int64_t, bool, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+extern template int product_of<f16_t>(Layout, int32_t, const void *, int64_t, bool, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
 
 template <typename... A>
 int product(int32_t type, A... args)
