@@ -7,7 +7,7 @@
 namespace tt {
 
 struct SlopeArgs {
-    const void *dy, *pre;        // pre null: no activation
+    const void *dy, *pre;        // (pre is not looked at without an activation)
     void *dz;                    // rows of nv vectors, zeros behind the N-th column; null: not wanted
     float *part;                 // [bands][8 nv] sums of columns, null: not wanted
     int64_t ld_dy, ld_pre, ld_dz;
@@ -16,7 +16,7 @@ struct SlopeArgs {
 };
 
 // 32 vectors of eight columns x 8 rows per workgroup at a time, down a band of rows.
-template <typename T, bool WHOLE>
+template <typename T, bool WHOLE, bool ACT>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
 {
     __shared__ float sums[8][32][8];
@@ -25,26 +25,34 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     const int64_t first = (int64_t)blockIdx.y * a.band, last = first + a.band < a.rows ? first + a.band : a.rows;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     if (v < a.nv) {
-#pragma unroll 4
-        for (int64_t r = first + lane_row; r < last; r += 8) {
-            float d[8];
-            Vec8<T> x = fetch8<WHOLE>((const T *)a.dy + row_at(r, a.ld_dy) + 8 * v, n, a.N);
-            if (a.pre) {
-                float z[8];
-                Vec8<T> y = fetch8<WHOLE>((const T *)a.pre + row_at(r, a.ld_pre) + 8 * v, n, a.N);
-                settle8<WHOLE>(x, n, a.N);
-                settle8<WHOLE>(y, n, a.N);
-                widen8(x, d);
-                widen8(y, z);
+        constexpr int U = sizeof(T) == 4 ? 2 : 4;            // rows whose loads are on their way together
+#pragma unroll 1
+        for (int64_t r0 = first + lane_row; r0 < last; r0 += 8 * U) {
+            Vec8<T> x[U], y[U];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], a.act);
-            } else {
-                settle8<WHOLE>(x, n, a.N);
-                widen8(x, d);
+            for (int i = 0; i < U; ++i) {
+                const int64_t r = r0 + 8 * i < last ? r0 + 8 * i : r0;
+                x[i] = fetch8<WHOLE>((const T *)a.dy + row_at(r, a.ld_dy) + 8 * v, n, a.N);
+                if (ACT) y[i] = fetch8<WHOLE>((const T *)a.pre + row_at(r, a.ld_pre) + 8 * v, n, a.N);
             }
-            if (a.dz) put8<true>((T *)a.dz + row_at(r, a.ld_dz) + 8 * v, 8, d);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) s[j] += d[j];
+            for (int i = 0; i < U; ++i) {
+                const int64_t r = r0 + 8 * i;
+                if (r >= last) break;
+                float d[8];
+                settle8<WHOLE>(x[i], n, a.N);
+                widen8(x[i], d);
+                if (ACT) {
+                    float z[8];
+                    settle8<WHOLE>(y[i], n, a.N);
+                    widen8(y[i], z);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) d[j] *= act_slope(z[j], a.act);
+                }
+                if (a.dz) put8<true>((T *)a.dz + row_at(r, a.ld_dz) + 8 * v, 8, d);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) s[j] += d[j];
+            }
         }
     }
     if (!a.part) return;

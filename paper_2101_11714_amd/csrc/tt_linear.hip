@@ -150,7 +150,9 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         a.act = activation;
         with_type(type, [&](auto t) {
             with_whole(N, [&](auto whole) {
-                hipLaunchKernelGGL((slope_kernel<decltype(t), decltype(whole)::value>), dim3((unsigned)ceil_div(a.nv, 32), (unsigned)room.n_bands), dim3(WG), 0, st, a);
+                with_flag(activation != TT_ACT_NONE, [&](auto act) {
+                    hipLaunchKernelGGL((slope_kernel<decltype(t), decltype(whole)::value, decltype(act)::value>), dim3((unsigned)ceil_div(a.nv, 32), (unsigned)room.n_bands), dim3(WG), 0, st, a);
+                });
             });
         });
         if ((rc = launched("gradient launch"))) return rc;

@@ -37,19 +37,21 @@ struct Sums {
     float m, s, t;
 };
 
-// the sums about the larger of two maxima; -0 and 0 for what has none
-__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c)
+// the sums about another maximum, no smaller than theirs; 0 for what has none
+__device__ __forceinline__ Sums about(const Sums &a, float m, float c)
 {
-    const float m = fmaxf(a.m, b.m);
-    auto part = [&](const Sums &x, float &s, float &t) {
-        const float d = fmaxf(x.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
-        s += x.s * f;
-        t += f == 0.f ? 0.f : f * (x.t + d * x.s);
-    };
-    Sums r{m, 0.f, 0.f};
-    part(a, r.s, r.t);
-    part(b, r.s, r.t);
-    return r;
+    const float d = fmaxf(a.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
+    return {m, a.s * f, f == 0.f ? a.s * f : f * (a.t + d * a.s)};
+}
+
+// a wave's sums, in every lane
+__device__ __forceinline__ Sums joined(Sums a, float c)
+{
+    auto add = [](float x, float y) { return x + y; };
+    a = about(a, lanes_reduce(a.m, 6, [](float x, float y) { return fmaxf(x, y); }), c);
+    a.s = lanes_reduce(a.s, 6, add);
+    a.t = lanes_reduce(a.t, 6, add);
+    return a;
 }
 
 __device__ __forceinline__ uint32_t order_of(float x)
@@ -66,16 +68,14 @@ __device__ __forceinline__ uint64_t key_of(float x, uint32_t column)
     return x == -INFINITY ? 0ull : (uint64_t)order_of(x) << 32 | (uint32_t)~column;
 }
 
-// how many of the 256 values are larger, and how many are no smaller
-__device__ __forceinline__ void counts_of(const uint4 *orders, uint32_t own, int &more, int &least)
+// the n-th largest of a wave's 64 values (1 <= n <= 64), bit by bit
+__device__ __forceinline__ uint32_t nth_largest(uint32_t x, int n)
 {
-    more = least = 0;
-#pragma unroll 8
-    for (int i = 0; i < WG / 4; ++i) {
-        const uint4 o = orders[i];
-        more += (o.x > own) + (o.y > own) + (o.z > own) + (o.w > own);
-        least += (o.x >= own) + (o.y >= own) + (o.z >= own) + (o.w >= own);
-    }
+    uint32_t t = 0;
+#pragma unroll 1
+    for (uint32_t bit = 0x80000000u; bit; bit >>= 1)
+        if (__popcll(__ballot(x >= (t | bit))) >= n) t |= bit;
+    return t;
 }
 
 // how many of n keys are larger
@@ -89,23 +89,29 @@ __device__ __forceinline__ int rank_of(const uint64_t *keys, int n, uint64_t key
 
 __device__ __forceinline__ int64_t token_at(const LogprobArgs &a, int64_t row) { return a.tokens64 ? ((const int64_t *)a.tokens)[row] : ((const int32_t *)a.tokens)[row]; }
 
+// the logit of a row's token, and whether there is one
+struct Given {
+    float z;
+    bool there;
+};
+
+template <typename T>
+__device__ __forceinline__ Given given_logit(const LogprobArgs &a, int64_t row)
+{
+    if (!a.logprob) return {0.f, false};
+    const int64_t token = token_at(a, row);
+    const bool there = token >= 0 && token < a.V;
+    return {(float)((const T *)a.logits)[row * a.ld + (there ? token : 0)], there};
+}
+
 // What a row's sums say.  Log probabilities are taken from the largest logit and not from lse, which has lost log S in rows of the lowest
 // values of a type.
-template <typename T>
-__device__ __forceinline__ void leave_row(const LogprobArgs &a, int64_t row, const Sums &r, float log_s)
+__device__ __forceinline__ void leave_row(const LogprobArgs &a, int64_t row, const Sums &r, float log_s, const Given &given)
 {
     const bool none = r.s == 0.f;
     if (a.lse) a.lse[row] = none ? -INFINITY : r.m * a.scale + log_s;
     if (a.entropy) a.entropy[row] = none ? 0.f : log_s - a.scale * (r.t / r.s);
-    if (a.logprob) {
-        const int64_t token = token_at(a, row);
-        float y = 0.f;
-        if (token >= 0 && token < a.V) {
-            const float z = (float)((const T *)a.logits)[row * a.ld + token];
-            y = none ? -INFINITY : a.scale * (z - r.m) - log_s;
-        }
-        a.logprob[row] = y;
-    }
+    if (a.logprob) a.logprob[row] = !given.there ? 0.f : none ? -INFINITY : a.scale * (given.z - r.m) - log_s;
 }
 
 __device__ __forceinline__ void leave_top(const LogprobArgs &a, int64_t row, int place, uint64_t key, float m, float log_s)
@@ -116,76 +122,67 @@ __device__ __forceinline__ void leave_top(const LogprobArgs &a, int64_t row, int
     if (a.top) a.top[at] = key ? a.scale * (value_of((uint32_t)(key >> 32)) - m) - log_s : -INFINITY;
 }
 
-// Four vectors of eight logits of a row per thread, and the walk over the vectors [from, to): f(vector's number, its logits), -inf where there is no column.
-template <typename T, bool WHOLE>
-struct Vectors {
-    Vec8<T> r[LP_UNROLL];
-
-    __device__ __forceinline__ void fetch(const T *line, int v0, int to, int V)
-    {
+// the vectors [from, to) of a row, U of a thread's at a time: f(vector's number, its eight logits), -inf where there is no column
+template <typename T, bool WHOLE, int U, typename F>
+__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
+{
+#pragma unroll 1
+    for (int v0 = from + threadIdx.x; v0 < to; v0 += WG * U) {
+        Vec8<T> r[U];
 #pragma unroll
-        for (int i = 0; i < LP_UNROLL; ++i) {
+        for (int i = 0; i < U; ++i) {
             const int v = v0 + i * WG < to ? v0 + i * WG : to - 1;
             r[i] = fetch8<WHOLE>(line + 8 * (int64_t)v, V - 8 * v, V);
         }
-    }
-    template <typename F>
-    __device__ __forceinline__ void each(int v0, int to, int V, F f) const
-    {
+        __builtin_amdgcn_sched_barrier(0);                   // (or the compiler loads them one after the other)
 #pragma unroll
-        for (int i = 0; i < LP_UNROLL; ++i) {
+        for (int i = 0; i < U; ++i) {
             const int v = v0 + i * WG;
             if (v >= to) break;
-            Vec8<T> y = r[i];
             float x[8];
-            settle8<WHOLE>(y, V - 8 * v, V);
-            widen8(y, x);
+            settle8<WHOLE>(r[i], V - 8 * v, V);
+            widen8(r[i], x);
             if (!WHOLE && 8 * v + 8 > V)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) x[j] = 8 * v + j < V ? x[j] : -INFINITY;
             f(v, x);
         }
     }
-};
-
-template <typename T, bool WHOLE, typename F>
-__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
-{
-    for (int v0 = from + threadIdx.x; v0 < to; v0 += WG * LP_UNROLL) {
-        Vectors<T, WHOLE> held;
-        held.fetch(line, v0, to, V);
-        held.each(v0, to, V, f);
-    }
 }
 
-// The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  order: of the thread's largest logit, 0 where it has none;
-// look(f): calls f(column, logit) for all of the thread's.
-template <typename L>
-__device__ __forceinline__ void largest_keys(int k, uint32_t order, uint64_t *list, int *count, uint64_t *least, uint64_t *out, L look)
+// The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  order: of the thread's largest logit (or of a smaller one of its own), 0
+// where it has none; only threads that have one of the candidates look at their logits again (`again`: those whose order may be too small do).
+// The bound that leaves k candidates at least is the smallest over the waves of the k / 4-th largest order of a wave.
+template <typename T, bool WHOLE>
+__device__ __forceinline__ void largest_keys(const T *line, int from, int to, int V, int k, uint32_t order, bool again, uint64_t *list, int *count, uint64_t *least, uint64_t *out)
 {
-    uint32_t *orders = reinterpret_cast<uint32_t *>(list);
-    orders[threadIdx.x] = order;
-    if (threadIdx.x == 0) {
-        *count = 0;
-        *least = 1;
-    }
+    uint32_t *bounds = reinterpret_cast<uint32_t *>(out);
+    const uint32_t nth = nth_largest(order, (k + NWAVE - 1) / NWAVE);
+    if ((threadIdx.x & 63) == 0) bounds[threadIdx.x >> 6] = nth;
+    if (threadIdx.x == 0) *count = 0;
     __syncthreads();
-    int more, no_less;
-    counts_of(reinterpret_cast<const uint4 *>(orders), order, more, no_less);
-    if (order && more < k && no_less >= k) *least = (uint64_t)order << 32;               // (whoever has that value writes the same)
+    if (threadIdx.x == 0) {
+        uint32_t low = bounds[0];
+#pragma unroll
+        for (int w = 1; w < NWAVE; ++w) low = min(low, bounds[w]);
+        *least = low ? (uint64_t)low << 32 : 1;
+    }
     __syncthreads();
     int n;
     for (;;) {
         const uint64_t bound = *least;
-        const float at_least = bound > 1 ? value_of((uint32_t)(bound >> 32)) : -INFINITY;
-        look([&](int column, float x) {
-            if (x < at_least) return;                        // (a NaN is not)
-            const uint64_t key = key_of(x, column);
-            if (key >= bound) {
-                const int at = atomicAdd(count, 1);
-                if (at < LP_LIST) list[at] = key;
-            }
-        });
+        const uint32_t high = (uint32_t)(bound >> 32);
+        if (again || (order && order >= high))
+            each_vector<T, WHOLE, 1>(line, from, to, V, [&](int v, const float (&x)[8]) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const uint64_t key = key_of(x[j], 8 * v + j);
+                    if (key >= bound) {
+                        const int at = atomicAdd(count, 1);
+                        if (at < LP_LIST) list[at] = key;
+                    }
+                }
+            });
         __syncthreads();
         n = *count;
         if (n <= LP_LIST) break;
@@ -206,8 +203,7 @@ __device__ __forceinline__ void largest_keys(int k, uint32_t order, uint64_t *li
     for (int i = n + threadIdx.x; i < k; i += WG) out[i] = 0;
 }
 
-// HELD: a piece is at most four vectors a thread, which stay in registers for the second look.
-template <typename T, bool TOP, bool ENTROPY, bool WHOLE, bool HELD>
+template <typename T, bool TOP, bool ENTROPY, bool WHOLE>
 __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
 {
     __shared__ Sums waves[NWAVE];
@@ -219,9 +215,10 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
     const int piece = (int)(id - row * a.pieces), from = piece * a.piece, to = min(from + a.piece, a.nv);
     const T *line = (const T *)a.logits + row * a.ld;
     const float c = a.scale * LOG2E;
+    Given given{0.f, false};
+    if (a.pieces == 1 && threadIdx.x == 0) given = given_logit<T>(a, row);
     Sums r{LP_LEAST, 0.f, 0.f};
-    uint32_t order = 0;
-    auto add = [&](int v, const float (&x)[8]) {
+    each_vector<T, WHOLE, LP_UNROLL>(line, from, to, a.V, [&](int v, const float (&x)[8]) {
         float m = r.m;
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
@@ -236,34 +233,23 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
             const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * c);
             r.s += e;
             if (ENTROPY) r.t += e * fmaxf(d, LP_LEAST);
-            if (TOP) order = max(order, x[j] == -INFINITY ? 0u : order_of(x[j]));
         }
-    };
-    Vectors<T, WHOLE> held;
-    if (HELD) {
-        held.fetch(line, from + threadIdx.x, to, a.V);
-        held.each(from + threadIdx.x, to, a.V, add);
-    } else {
-        each_vector<T, WHOLE>(line, from, to, a.V, add);
-    }
-    // lanes, then waves
-#pragma unroll
-    for (int b = 1; b < WAVE; b <<= 1) {
-        const Sums o{__shfl_xor(r.m, b), __shfl_xor(r.s, b), __shfl_xor(r.t, b)};
-        r = joined(r, o, c);
-    }
+    });
+    // a sum that is no number: a NaN among the logits, or an infinity (and maybe a NaN beside it)
+    const bool odd = r.s != r.s;
+    const uint32_t order = r.s == 0.f ? 0u : odd && r.m != INFINITY ? 0xffffffffu : order_of(r.m);
+    r = joined(r, c);
     if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = r;
     __syncthreads();
-    r = joined(joined(waves[0], waves[1], c), joined(waves[2], waves[3], c), c);
-    if (TOP)
-        largest_keys(a.k, order, list, &count, &least, found, [&](auto f) {
-            auto each = [&](int v, const float (&x)[8]) {
+    r.m = fmaxf(fmaxf(waves[0].m, waves[1].m), fmaxf(waves[2].m, waves[3].m));
+    r.s = r.t = 0.f;
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f(8 * v + j, x[j]);
-            };
-            if (HELD) held.each(from + threadIdx.x, to, a.V, each);
-            else each_vector<T, WHOLE>(line, from, to, a.V, each);
-        });
+    for (int w = 0; w < NWAVE; ++w) {
+        const Sums o = about(waves[w], r.m, c);
+        r.s += o.s;
+        r.t += o.t;
+    }
+    if (TOP) largest_keys<T, WHOLE>(line, from, to, a.V, a.k, order, odd, list, &count, &least, found);
     if (a.pieces > 1) {
         if (threadIdx.x == 0) *reinterpret_cast<float4 *>(a.sums + id * 4) = make_float4(r.m, r.s, r.t, 0.f);
         if (TOP) {
@@ -273,7 +259,7 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
         return;
     }
     const float log_s = logf(r.s);
-    if (threadIdx.x == 0) leave_row<T>(a, row, r, log_s);
+    if (threadIdx.x == 0) leave_row(a, row, r, log_s, given);
     if (TOP) {
         __syncthreads();
         for (int i = threadIdx.x; i < a.k; i += WG) leave_top(a, row, i, found[i], r.m, log_s);
@@ -299,20 +285,21 @@ __global__ __launch_bounds__(TOP ? LP_JOIN : WAVE) void logprob_join_kernel(Logp
         ranks[threadIdx.x] = 0;
     }
     if (threadIdx.x < WAVE) {
+        Given given{0.f, false};
+        if (threadIdx.x == 0) given = given_logit<T>(a, row);
         Sums r{LP_LEAST, 0.f, 0.f};
         for (int p = threadIdx.x; p < a.pieces; p += WAVE) {
-            const float *s = a.sums + (row * a.pieces + p) * 4;
-            r = joined(r, Sums{s[0], s[1], s[2]}, c);
+            const float4 s = *reinterpret_cast<const float4 *>(a.sums + (row * a.pieces + p) * 4);
+            const Sums x{s.x, s.y, s.z};
+            const float m = fmaxf(r.m, x.m);
+            const Sums y = about(r, m, c), z = about(x, m, c);
+            r = {m, y.s + z.s, y.t + z.t};
         }
-#pragma unroll
-        for (int b = 1; b < WAVE; b <<= 1) {
-            const Sums o{__shfl_xor(r.m, b), __shfl_xor(r.s, b), __shfl_xor(r.t, b)};
-            r = joined(r, o, c);
-        }
+        r = joined(r, c);
         if (threadIdx.x == 0) {
             row_m = r.m;
             row_log_s = logf(r.s);
-            leave_row<T>(a, row, r, row_log_s);
+            leave_row(a, row, r, row_log_s, given);
         }
     }
     if (!TOP) return;
@@ -357,7 +344,7 @@ __global__ __launch_bounds__(WG) void logprob_bwd_kernel(LogprobGradArgs a)
     if (token < 0 || token >= a.V) token = -1;
     const float g = token >= 0 ? a.g[row] : 0.f, ge = a.ge ? a.ge[row] : 0.f, h = a.ge ? a.entropy[row] : 0.f, lse = a.lse[row];
     const bool none = lse == -INFINITY;
-    each_vector<T, WHOLE>(line, from, to, a.V, [&](int v, float (&x)[8]) {
+    each_vector<T, WHOLE, LP_UNROLL>(line, from, to, a.V, [&](int v, float (&x)[8]) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float l = fmaf(x[j], a.scale, -lse), p = __builtin_amdgcn_exp2f(l * LOG2E);

@@ -12,8 +12,7 @@ namespace {
 
 constexpr int64_t MOST_VOCAB = 1ll << 30;
 
-// How a row is cut.  Few rows: into pieces enough for 512 workgroups, of 512 vectors at least, or, with alternatives, into pieces that a workgroup holds in
-// its registers, as long as one workgroup can rank what they leave.
+// How a row is cut: into pieces enough for 512 workgroups, of 512 vectors at least, whose alternatives one workgroup can rank.
 struct Pieces {
     int n, size;
 };
@@ -21,14 +20,10 @@ struct Pieces {
 Pieces pieces_of(int64_t rows, int64_t V, int32_t k)
 {
     const int64_t nv = ceil_div(V, 8);
-    int64_t n = 1;
-    if (rows < 512) {
-        n = ceil_div(512, rows > 0 ? rows : 1);
-        if (n > ceil_div(nv, 512)) n = ceil_div(nv, 512);
-        const int64_t held = ceil_div(nv, WG * LP_UNROLL);
-        if (k > 0 && n < held && held <= 64) n = held;
-        if (k > 0 && n > LP_LIST / k) n = LP_LIST / k;
-    }
+    int64_t n = rows > 0 ? ceil_div(512, rows) : 1;
+    if (n > ceil_div(nv, 512)) n = ceil_div(nv, 512);
+    if (k > 0 && n > LP_LIST / k) n = LP_LIST / k;
+    if (n < 1) n = 1;
     const int64_t size = ceil_div(nv, n);
     return {(int)ceil_div(nv, size), (int)size};
 }
@@ -68,9 +63,9 @@ extern "C" {
 size_t tt_token_logprob_fwd_workspace_bytes(int64_t n_rows, int64_t V, int32_t k)
 {
     if (n_rows <= 0 || V <= 0 || check_logits(n_rows, V) || k < 0 || k > LP_MOST_K) return 0;
-    // pieces of up to 511 rows: 512 + rows at most, or 64 a row with alternatives
-    const int64_t rows = n_rows < 511 ? n_rows : 511, most = ceil_div(ceil_div(V, 8), 512) > 1 ? (k > 0 ? 64 * rows + 1024 : 1024) : 0;
-    return (size_t)(most < rows * 512 ? most : rows * 512) * (4 * sizeof(float) + (size_t)k * sizeof(uint64_t));
+    // (rows times pieces is at most 512 + rows while there are pieces, that is up to 511 rows)
+    const int64_t most = ceil_div(ceil_div(V, 8), 512) > 1 ? 1024 : 0;
+    return (size_t)(most < n_rows * 512 ? most : n_rows * 512) * (4 * sizeof(float) + (size_t)k * sizeof(uint64_t));
 }
 
 int tt_token_logprob_fwd(const tt_rows_t *logits, const tt_tokens_t *tokens, float scale, float *logprob, float *lse, float *entropy,
@@ -116,12 +111,10 @@ int tt_token_logprob_fwd(const tt_rows_t *logits, const tt_tokens_t *tokens, flo
             constexpr bool WHOLE = decltype(w)::value;
             const dim3 grid = grid_of(n_rows * p.n, WG);
             if (k > 0) {
-                with_flag(p.size <= WG * LP_UNROLL, [&](auto held) {
-                    hipLaunchKernelGGL((logprob_kernel<T, true, true, WHOLE, decltype(held)::value>), grid, dim3(WG), 0, (hipStream_t)stream, a);
-                });
+                hipLaunchKernelGGL((logprob_kernel<T, true, true, WHOLE>), grid, dim3(WG), 0, (hipStream_t)stream, a);
             } else {
                 with_flag(entropy != nullptr, [&](auto h) {
-                    hipLaunchKernelGGL((logprob_kernel<T, false, decltype(h)::value, WHOLE, false>), grid, dim3(WG), 0, (hipStream_t)stream, a);
+                    hipLaunchKernelGGL((logprob_kernel<T, false, decltype(h)::value, WHOLE>), grid, dim3(WG), 0, (hipStream_t)stream, a);
                 });
             }
         });

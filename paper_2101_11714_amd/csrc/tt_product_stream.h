@@ -108,10 +108,7 @@ __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_
     auto slot = [&](int first, int n) { return lds + (first + n >= PS_SLOTS ? first + n - PS_SLOTS : first + n) * S::SLOT; };
     auto multiply = [&] {
         __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-        for (int i = 0; i < BM; ++i)
-#pragma unroll
-            for (int j = 0; j < BN; ++j) block_product<T>(fb[j], fa[i], acc[i][j]);
+        block_products<T>(fb, fa, acc);
         __builtin_amdgcn_s_setprio(0);
     };
     auto phase = [] {
