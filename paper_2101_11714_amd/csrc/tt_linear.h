@@ -9,7 +9,9 @@ namespace tt {
 struct SlopeArgs {
     const void *dy, *pre;        // (pre is not looked at without an activation)
     void *dz;                    // rows of nv vectors, zeros behind the N-th column; null: not wanted
-    float *part;                 // [bands][8 nv] sums of columns, null: not wanted
+    float *part;                 // [bands][8 nv] sums of columns, null: not wanted, or
+    void *db;                    // one band's: the bias's gradient
+    int db_type, add;
     int64_t ld_dy, ld_pre, ld_dz;
     int64_t rows, band;          // rows of a band
     int N, nv, act;
@@ -55,7 +57,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             }
         }
     }
-    if (!a.part) return;
+    if (!a.part && !a.db) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[lane_row][threadIdx.x & 31][j] = s[j];
     __syncthreads();
@@ -64,7 +66,12 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
     float y = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) y += sums[q][c >> 3][c & 7];
-    a.part[(int64_t)blockIdx.y * 8 * a.nv + at] = y;
+    if (a.part) a.part[(int64_t)blockIdx.y * 8 * a.nv + at] = y;
+    else if (at < a.N) {
+        if (a.db_type == TT_F32) ((float *)a.db)[at] = y + (a.add ? ((float *)a.db)[at] : 0.f);
+        else if (a.db_type == TT_BF16) ((bf16_t *)a.db)[at] = (bf16_t)(y + (a.add ? (float)((bf16_t *)a.db)[at] : 0.f));
+        else ((f16_t *)a.db)[at] = (f16_t)(y + (a.add ? (float)((f16_t *)a.db)[at] : 0.f));
+    }
 }
 
 // the bands' sums added in their order, 32 columns a workgroup, every 32nd band a thread

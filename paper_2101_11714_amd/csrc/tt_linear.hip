@@ -56,7 +56,7 @@ GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, boo
     r.dz = copy && (x || w) ? up((size_t)M * (size_t)cols * element_bytes(type)) : 0;
     r.n_bands = M < 64 * 256 ? ceil_div(M, 64) : 256;
     r.band = ceil_div(M, r.n_bands > 0 ? r.n_bands : 1);
-    r.bands = b ? up((size_t)r.n_bands * (size_t)cols * sizeof(float)) : 0;
+    r.bands = b && r.n_bands > 1 ? up((size_t)r.n_bands * (size_t)cols * sizeof(float)) : 0;
     r.all = r.parts + r.dz + r.bands;
     return r;
 }
@@ -128,7 +128,8 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
     const void *dz = grad_output->data;
     int64_t ld_dz = grad_output->ld;
     const bool padded = room.dz > 0;                         // (the slopes' kernel writes whole vectors)
-    if (N > 0 && (room.dz || room.bands) && n_rows > 0) {
+    const bool alone = grad_bias && room.n_bands == 1;       // its sums are the gradient
+    if (N > 0 && (room.dz || grad_bias) && n_rows > 0) {
         SlopeArgs a{};
         a.dy = grad_output->data;
         a.ld_dy = grad_output->ld;
@@ -145,6 +146,9 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
             ld_dz = a.ld_dz;
         }
         a.part = room.bands ? (float *)(ws + room.parts + room.dz) : nullptr;
+        a.db = alone ? grad_bias : nullptr;
+        a.db_type = grad_bias_type;
+        a.add = accumulate;
         a.rows = n_rows;
         a.band = room.band;
         a.act = activation;
@@ -157,7 +161,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         });
         if ((rc = launched("gradient launch"))) return rc;
     }
-    if (grad_bias && N > 0) {
+    if (grad_bias && N > 0 && !alone) {
         with_type(grad_bias_type, [&](auto w) {
             hipLaunchKernelGGL((bias_sum_kernel<decltype(w)>), dim3((unsigned)ceil_div(N, 32)), dim3(1024), 0, st, (const float *)(ws + room.parts + room.dz), (int)room.n_bands, (int)N,
                                (int)(8 * ceil_div(N, 8)), (decltype(w) *)grad_bias, accumulate);

@@ -152,19 +152,25 @@ __device__ __forceinline__ void each_vector(const T *line, int from, int to, int
 
 // The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  order: of the thread's largest logit (or of a smaller one of its own), 0
 // where it has none; only threads that have one of the candidates look at their logits again (`again`: those whose order may be too small do).
-// The bound that leaves k candidates at least is the smallest over the waves of the k / 4-th largest order of a wave.
+// Two bounds leave k candidates at least: the smallest over the waves of the k / 4-th largest order of a wave, and the largest over the waves of the
+// k-th largest (which alone says something where the logits are too few for all waves).
 template <typename T, bool WHOLE>
 __device__ __forceinline__ void largest_keys(const T *line, int from, int to, int V, int k, uint32_t order, bool again, uint64_t *list, int *count, uint64_t *least, uint64_t *out)
 {
     uint32_t *bounds = reinterpret_cast<uint32_t *>(out);
-    const uint32_t nth = nth_largest(order, (k + NWAVE - 1) / NWAVE);
-    if ((threadIdx.x & 63) == 0) bounds[threadIdx.x >> 6] = nth;
+    const uint32_t nth = nth_largest(order, (k + NWAVE - 1) / NWAVE), kth = nth_largest(order, k);
+    if ((threadIdx.x & 63) == 0) {
+        bounds[threadIdx.x >> 6] = nth;
+        bounds[NWAVE + (threadIdx.x >> 6)] = kth;
+    }
     if (threadIdx.x == 0) *count = 0;
     __syncthreads();
     if (threadIdx.x == 0) {
         uint32_t low = bounds[0];
 #pragma unroll
         for (int w = 1; w < NWAVE; ++w) low = min(low, bounds[w]);
+#pragma unroll
+        for (int w = 0; w < NWAVE; ++w) low = max(low, bounds[NWAVE + w]);
         *least = low ? (uint64_t)low << 32 : 1;
     }
     __syncthreads();
@@ -209,6 +215,7 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
     __shared__ Sums waves[NWAVE];
     __shared__ __attribute__((aligned(16))) uint64_t list[TOP ? LP_LIST : 1];
     __shared__ uint64_t found[TOP ? LP_MOST_K : 1], least;
+    static_assert(!TOP || LP_MOST_K >= NWAVE, "the bounds' room");
     __shared__ int count;
     const int64_t id = workgroup(), row = id / a.pieces;
     if (row >= a.rows) return;

@@ -16,14 +16,18 @@ int launch_product(const void *a, int64_t lda, bool a_padded, const void *b, int
     ProductArgs q{a, b, lda, ldb, M, N, K, (int)p.tiles_m, (int)p.tiles_n, p.k_part, p.parts > 1 ? (float *)workspace : nullptr, 8 * ceil_div(N, 8)};
     if (p.way == FEW) {
         if constexpr (AK && BK) {
-            const dim3 grid = grid_of(ceil_div(N, BLOCK), PF_WAVES * WAVE);
-            const bool chunks = whole || (type == TT_F32 && K % 4 == 0 && lda % 4 == 0 && ldb % 4 == 0 && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0);
-            with_flag(chunks && K > 0, [&](auto w) {
-                auto launch = [&](auto mb) { hipLaunchKernelGGL((product_few_kernel<T, O, decltype(mb)::value, decltype(w)::value>), grid, dim3(PF_WAVES * WAVE), 0, st, q, e); };
-                if (M <= 16) launch(std::integral_constant<int, 1>{});
-                else if (M <= 32) launch(std::integral_constant<int, 2>{});
-                else launch(std::integral_constant<int, 4>{});
-            });
+            // two blocks of columns share a reading of x where that leaves a workgroup for every compute unit
+            auto launch = [&](auto mb, auto nb) {
+                hipLaunchKernelGGL((product_few_kernel<T, O, decltype(mb)::value, decltype(nb)::value>), grid_of(ceil_div(N, BLOCK * decltype(nb)::value), PF_WAVES * WAVE), dim3(PF_WAVES * WAVE), 0, st, q, e);
+            };
+            constexpr std::integral_constant<int, 1> one{};
+            constexpr std::integral_constant<int, 2> two{};
+            constexpr std::integral_constant<int, 4> four{};
+            if (M <= 16) launch(one, one);
+            else if (M <= 32 && N < 256 * 32) launch(two, one);
+            else if (M <= 32) launch(two, two);
+            else if (N < 256 * 32) launch(four, one);
+            else launch(four, two);
         }
         return launched("product launch");
     }
@@ -32,7 +36,7 @@ int launch_product(const void *a, int64_t lda, bool a_padded, const void *b, int
         grid.z = (unsigned)p.parts;
         if (p.way == TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 128, 2>), grid, dim3(WG), 0, st, q, e);
         if constexpr (sizeof(T) == 4)
-            if (p.way == SMALL_TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 64, 64, 4>), grid, dim3(WG), 0, st, q, e);
+            if (p.way == SMALL_TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 64, 4>), grid, dim3(WG), 0, st, q, e);
     } else if constexpr (sizeof(T) == 2) {
         int rc = TT_OK;
         with_flag(p.way == STREAM_WIDE, [&](auto w) {

@@ -59,12 +59,11 @@ inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense, b
     } else if (whole && type != TT_F32) {
         stream_plan(p, M, N, K);
     } else {
-        // 32 bits: the matrix cores take sixteen times as long as for 16 and LDS is no bound, so that small tiles, which share out better, cost nothing
-        // until there are many large ones
+        // 32 bits: tiles of 128 x 64 share out better until there are many of 128 x 128
         p.way = type == TT_F32 && ceil_div(M, 128) * ceil_div(N, 128) < 1024 ? SMALL_TILES : TILES;
-        const int64_t tile = p.way == TILES ? 128 : 64, step = 128 / element_bytes(type), steps = ceil_div(K, step);
-        p.tiles_m = ceil_div(M, tile);
-        p.tiles_n = ceil_div(N, tile);
+        const int64_t step = 128 / element_bytes(type), steps = ceil_div(K, step);
+        p.tiles_m = ceil_div(M, 128);
+        p.tiles_n = ceil_div(N, p.way == TILES ? 128 : 64);
         int64_t parts = (p.way == TILES ? MOST_TILES : 2 * MOST_TILES) / (p.tiles_m * p.tiles_n > 0 ? p.tiles_m * p.tiles_n : 1);
         if (parts > steps / 4) parts = steps / 4;
         p.k_part = ceil_div(steps, parts < 1 ? 1 : parts) * step;

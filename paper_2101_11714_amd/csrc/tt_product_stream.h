@@ -151,7 +151,7 @@ __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_
     if (WIDE && !group) phase();
     SA::template landed<0>();
     phase();
-    leave_tile<T, O, BM, 4>(p, e, m0 + wm, n0 + wn, lane, lds + wave * 4 * LEAVE_BLOCK, acc);
+    leave_tile<T, O, BM, 4, AK && BK>(p, e, m0 + wm, n0 + wn, lane, lds + wave * 4 * LEAVE_BLOCK, acc);
 }
 
 }  // namespace tt

@@ -33,7 +33,11 @@ struct RotateArgs {
     int lg;                      // lanes of a head
     int each, q_slices, k_slices;// heads that a group takes, and groups for a row's queries and for its keys
     float eps;
-    float *part;                 // backward: [workgroups][2][D] sums of the weights' gradients, null: not wanted
+    // backward
+    int q_workgroups;            // the first ones, which take the queries
+    void *gwq, *gwk;             // the weights' gradients, null: not wanted
+    int gwq_type, gwk_type, add;
+    float *part;                 // [workgroups][D] sums of theirs; null: one workgroup has them all
 };
 
 // cos and sin of 2 pi t.  The fraction of a turn is taken in 64 bits; from the nearest quarter it is an eighth at most, pi / 4 as an angle, where
@@ -157,6 +161,15 @@ __device__ __forceinline__ void turn_unit(const float2 (&t)[8], float (&x)[2][8]
 template <typename T>
 __device__ __forceinline__ T *head_at(const Heads &h, int64_t row, int head) { return (T *)h.data + row * h.ld + head * h.ld_head; }
 
+// a weight's gradient, null: not wanted
+__device__ __forceinline__ void put_weight(void *w, int type, int at, float y, int add)
+{
+    if (!w) return;
+    if (type == TT_F32) ((float *)w)[at] = y + (add ? ((float *)w)[at] : 0.f);
+    else if (type == TT_BF16) ((bf16_t *)w)[at] = (bf16_t)(y + (add ? (float)((bf16_t *)w)[at] : 0.f));
+    else ((f16_t *)w)[at] = (f16_t)(y + (add ? (float)((f16_t *)w)[at] : 0.f));
+}
+
 // A group's place: its row and the heads [from, to) of queries or keys.
 struct Slice {
     int64_t row;
@@ -229,7 +242,7 @@ __global__ __launch_bounds__(WG) void rotate_kernel(RotateArgs a)
     }
 }
 
-// Groups go through all queries, then through all keys, so that one weight's sums are in registers at a time.
+// Queries and keys have workgroups of their own, each of which has the sums of one weight in its registers.
 template <typename T, bool NORM, bool WHOLE, bool NEIGHBOURS>
 __global__ __launch_bounds__(WG, NORM ? 2 : WHOLE ? 4 : 3) void rotate_bwd_kernel(RotateArgs a)
 {
@@ -238,112 +251,110 @@ __global__ __launch_bounds__(WG, NORM ? 2 : WHOLE ? 4 : 3) void rotate_bwd_kerne
     const bool in = u < a.units, turned = u < a.turned;
     Unit unit = unit_of(a, in ? u : 0);
     if (!in) unit.n[0] = unit.n[1] = 0;
-#pragma unroll 1
-    for (int which = 0; which < 2; ++which) {
-        const int slices = which ? a.k_slices : a.q_slices, heads = which ? a.k_heads : a.q_heads;
-        const Heads src = which ? a.k : a.q, grad = which ? a.gk : a.gq, dst = which ? a.ok : a.oq;
-        float w[2][8], dw[2][8] = {};
-        if (NORM) load_weight<WHOLE>(which ? a.wk : a.wq, which ? a.wk_type : a.wq_type, unit, a.D, w);
-        for (int64_t item = (int64_t)blockIdx.x * groups + (threadIdx.x >> a.lg); item < a.rows * slices; item += (int64_t)gridDim.x * groups) {
-            const Slice s = slice_of(item, slices, a.each, heads);
-            float2 turns[8];
-            Vec8<T> rd[2], rx[2], nd[2], nx[2];
-            auto fetch = [&](int h) {
-                const T *p = head_at<T>(grad, s.row, h);
-                nd[0] = fetch_unit<T, WHOLE>(p, unit.at[0], a.D);
-                nd[1] = fetch_unit<T, WHOLE>(p, unit.at[1], a.D);
-                if (NORM) {
-                    const T *x = head_at<T>(src, s.row, h);
-                    nx[0] = fetch_unit<T, WHOLE>(x, unit.at[0], a.D);
-                    nx[1] = fetch_unit<T, WHOLE>(x, unit.at[1], a.D);
-                }
-            };
-            fetch(s.from);
-            if (turned) turns_of(a, s.row, u, turns);
-#pragma unroll 1
-            for (int h = s.from; h < s.to; ++h) {
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    rd[c] = nd[c];
-                    if (NORM) rx[c] = nx[c];
-                }
-                fetch(min(h + 1, s.to - 1));                 // the next head, while this one is worked on
-                float d[2][8];
-                widen_unit<WHOLE>(rd[0], unit.at[0], unit.n[0], a.D, d[0]);
-                widen_unit<WHOLE>(rd[1], unit.at[1], unit.n[1], a.D, d[1]);
-                if (turned) turn_unit<true, NEIGHBOURS>(turns, d);
-                if (NORM) {
-                    float x[2][8], sum = 0.f, dot = 0.f;
-                    widen_unit<WHOLE>(rx[0], unit.at[0], unit.n[0], a.D, x[0]);
-                    widen_unit<WHOLE>(rx[1], unit.at[1], unit.n[1], a.D, x[1]);
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            sum += x[c][j] * x[c][j];
-                            dot += d[c][j] * w[c][j] * x[c][j];
-                        }
-                    sum = lanes_reduce(sum, a.lg, [](float p, float q) { return p + q; });
-                    dot = lanes_reduce(dot, a.lg, [](float p, float q) { return p + q; });
-                    const float rho = 1.f / sqrtf(sum / (float)a.D + a.eps), along = rho * rho * dot / (float)a.D;
-#pragma unroll
-                    for (int c = 0; c < 2; ++c)
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            dw[c][j] += d[c][j] * x[c][j] * rho;
-                            d[c][j] = rho * (d[c][j] * w[c][j] - x[c][j] * along);
-                        }
-                }
-                T *p = head_at<T>(dst, s.row, h);
-                store_unit<WHOLE>(p, unit.at[0], unit.n[0], d[0]);
-                store_unit<WHOLE>(p, unit.at[1], unit.n[1], d[1]);
+    const bool which = (int)blockIdx.x >= a.q_workgroups;
+    const int first = which ? blockIdx.x - a.q_workgroups : blockIdx.x, workgroups = which ? gridDim.x - a.q_workgroups : a.q_workgroups;
+    const int slices = which ? a.k_slices : a.q_slices, heads = which ? a.k_heads : a.q_heads;
+    const Heads src = which ? a.k : a.q, grad = which ? a.gk : a.gq, dst = which ? a.ok : a.oq;
+    float w[2][8], dw[2][8] = {};
+    if (NORM) load_weight<WHOLE>(which ? a.wk : a.wq, which ? a.wk_type : a.wq_type, unit, a.D, w);
+    for (int64_t item = (int64_t)first * groups + (threadIdx.x >> a.lg); item < a.rows * slices; item += (int64_t)workgroups * groups) {
+        const Slice s = slice_of(item, slices, a.each, heads);
+        float2 turns[8];
+        Vec8<T> rd[2], rx[2], nd[2], nx[2];
+        auto fetch = [&](int h) {
+            const T *p = head_at<T>(grad, s.row, h);
+            nd[0] = fetch_unit<T, WHOLE>(p, unit.at[0], a.D);
+            nd[1] = fetch_unit<T, WHOLE>(p, unit.at[1], a.D);
+            if (NORM) {
+                const T *x = head_at<T>(src, s.row, h);
+                nx[0] = fetch_unit<T, WHOLE>(x, unit.at[0], a.D);
+                nx[1] = fetch_unit<T, WHOLE>(x, unit.at[1], a.D);
             }
+        };
+        fetch(s.from);
+        if (turned) turns_of(a, s.row, u, turns);
+#pragma unroll 1
+        for (int h = s.from; h < s.to; ++h) {
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                rd[c] = nd[c];
+                if (NORM) rx[c] = nx[c];
+            }
+            fetch(min(h + 1, s.to - 1));                 // the next head, while this one is worked on
+            float d[2][8];
+            widen_unit<WHOLE>(rd[0], unit.at[0], unit.n[0], a.D, d[0]);
+            widen_unit<WHOLE>(rd[1], unit.at[1], unit.n[1], a.D, d[1]);
+            if (turned) turn_unit<true, NEIGHBOURS>(turns, d);
+            if (NORM) {
+                float x[2][8], sum = 0.f, dot = 0.f;
+                widen_unit<WHOLE>(rx[0], unit.at[0], unit.n[0], a.D, x[0]);
+                widen_unit<WHOLE>(rx[1], unit.at[1], unit.n[1], a.D, x[1]);
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        sum += x[c][j] * x[c][j];
+                        dot += d[c][j] * w[c][j] * x[c][j];
+                    }
+                sum = lanes_reduce(sum, a.lg, [](float p, float q) { return p + q; });
+                dot = lanes_reduce(dot, a.lg, [](float p, float q) { return p + q; });
+                const float rho = 1.f / sqrtf(sum / (float)a.D + a.eps), along = rho * rho * dot / (float)a.D;
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        dw[c][j] += d[c][j] * x[c][j] * rho;
+                        d[c][j] = rho * (d[c][j] * w[c][j] - x[c][j] * along);
+                    }
+            }
+            T *p = head_at<T>(dst, s.row, h);
+            store_unit<WHOLE>(p, unit.at[0], unit.n[0], d[0]);
+            store_unit<WHOLE>(p, unit.at[1], unit.n[1], d[1]);
         }
-        if (!NORM || !a.part) continue;
-        // the groups' sums: lanes of a wave, then waves through LDS, in their order
-        const int cols = 16 * a.units, lanes = g < WAVE ? g : WAVE;
-        for (int b = a.lg; b < 6; ++b)
+    }
+    if (!NORM || !(which ? a.gwk : a.gwq)) return;
+    // the groups' sums: lanes of a wave, then waves through LDS, in their order
+    const int cols = 16 * a.units, lanes = g < WAVE ? g : WAVE;
+    for (int b = a.lg; b < 6; ++b)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) dw[c][j] += __shfl_xor(dw[c][j], 1 << b);
-        __syncthreads();
-        if ((int)(threadIdx.x & 63) < lanes && in)
+            for (int j = 0; j < 8; ++j) dw[c][j] += __shfl_xor(dw[c][j], 1 << b);
+    __syncthreads();
+    if ((int)(threadIdx.x & 63) < lanes && in)
 #pragma unroll
-            for (int c = 0; c < 2; ++c)
+        for (int c = 0; c < 2; ++c)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) sums[(threadIdx.x >> 6) * cols + 16 * u + 8 * c + j] = dw[c][j];
-        __syncthreads();
-        for (int i = threadIdx.x; i < cols; i += WG) {
-            const Unit x = unit_of(a, i >> 4);
-            const int c = i >> 3 & 1, j = i & 7;
-            if (j < (c ? x.n[1] : x.n[0]))
-                a.part[((int64_t)blockIdx.x * 2 + which) * a.D + (c ? x.at[1] : x.at[0]) + j] = (sums[i] + sums[cols + i]) + (sums[2 * cols + i] + sums[3 * cols + i]);
-        }
+            for (int j = 0; j < 8; ++j) sums[(threadIdx.x >> 6) * cols + 16 * u + 8 * c + j] = dw[c][j];
+    __syncthreads();
+    for (int i = threadIdx.x; i < cols; i += WG) {
+        const Unit x = unit_of(a, i >> 4);
+        const int c = i >> 3 & 1, j = i & 7, at = (c ? x.at[1] : x.at[0]) + j;
+        if (j >= (c ? x.n[1] : x.n[0])) continue;
+        const float y = (sums[i] + sums[cols + i]) + (sums[2 * cols + i] + sums[3 * cols + i]);
+        if (a.part) a.part[(int64_t)blockIdx.x * a.D + at] = y;
+        else put_weight(which ? a.gwk : a.gwq, which ? a.gwk_type : a.gwq_type, at, y, a.add);
     }
 }
 
 // the workgroups' sums added in their order, 32 columns a workgroup: blockIdx.y 0 the queries' weight, 1 the keys'
-__global__ __launch_bounds__(1024) void rotate_weight_kernel(const float *part, int n_part, int D, void *gq, int gq_type, void *gk, int gk_type, int add)
+__global__ __launch_bounds__(1024) void rotate_weight_kernel(RotateArgs a, int workgroups)
 {
     __shared__ float sums[32][33];
-    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, at = blockIdx.x * 32 + c, which = blockIdx.y;
-    void *out = which ? gk : gq;
-    if (!out) return;
-    const int type = which ? gk_type : gq_type;
+    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, at = blockIdx.x * 32 + c;
+    const bool which = blockIdx.y;
+    const int first = which ? a.q_workgroups : 0, last = which ? workgroups : a.q_workgroups;
     float s = 0.f;
-    if (at < D)
+    if (at < a.D)
 #pragma unroll 4
-        for (int b = q; b < n_part; b += 32) s += part[((int64_t)b * 2 + which) * D + at];
+        for (int b = first + q; b < last; b += 32) s += a.part[(int64_t)b * a.D + at];
     sums[q][c] = s;
     __syncthreads();
-    if (q || at >= D) return;
+    if (q || at >= a.D) return;
     float y = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) y += sums[i][c];
-    if (type == TT_F32) ((float *)out)[at] = y + (add ? ((float *)out)[at] : 0.f);
-    else if (type == TT_BF16) ((bf16_t *)out)[at] = (bf16_t)(y + (add ? (float)((bf16_t *)out)[at] : 0.f));
-    else ((f16_t *)out)[at] = (f16_t)(y + (add ? (float)((f16_t *)out)[at] : 0.f));
+    put_weight(which ? a.gwk : a.gwq, which ? a.gwk_type : a.gwq_type, at, y, a.add);
 }
 
 }  // namespace tt

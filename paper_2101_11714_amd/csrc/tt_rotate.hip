@@ -96,7 +96,13 @@ void slices_of(RotateArgs &a)
     a.k_slices = (int)ceil_div(a.k_heads, a.each);
 }
 
-int64_t bwd_grid(int64_t rows) { return rows < BWD_WORKGROUPS ? rows : BWD_WORKGROUPS; }
+// Workgroups of the backward pass: no more than have heads to take, BWD_WORKGROUPS shared out by the numbers of heads.
+int64_t bwd_workgroups(const RotateArgs &a, bool keys)
+{
+    const int64_t heads = keys ? a.k_heads : a.q_heads, items = a.rows * (keys ? a.k_slices : a.q_slices);
+    const int64_t most = BWD_WORKGROUPS * heads / ((int64_t)a.q_heads + a.k_heads), all = ceil_div(items, WG >> a.lg);
+    return all < most || most < 1 ? (most < 1 && all > 1 ? 1 : all) : most;
+}
 
 template <typename F>
 void with_shape(const RotateArgs &a, bool norm, F f)
@@ -155,7 +161,8 @@ int tt_qk_norm_rotate_fwd(const tt_heads_t *q, const tt_heads_t *k, const tt_rot
 size_t tt_qk_norm_rotate_bwd_workspace_bytes(int64_t n_rows, int64_t q_heads, int64_t k_heads, int64_t D)
 {
     if (n_rows <= 0 || D <= 0 || q_heads < 0 || k_heads < 0 || check_sizes_of(n_rows, D, q_heads + k_heads)) return 0;
-    return (size_t)bwd_grid(n_rows) * 2 * (size_t)D * sizeof(float);
+    const int64_t heads = n_rows * (q_heads + k_heads);      // (a workgroup has one at least)
+    return (size_t)(heads < BWD_WORKGROUPS + 2 ? heads : BWD_WORKGROUPS + 2) * (size_t)D * sizeof(float);
 }
 
 int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *grad_k_output, const tt_heads_t *q, const tt_heads_t *k,
@@ -188,10 +195,6 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
     const bool weights = grad_q_weight || grad_k_weight;
     const bool some = n_rows > 0 && q_heads + k_heads > 0;
     if (!some && (!weights || accumulate)) return TT_OK;
-    const int64_t grid = bwd_grid(n_rows);
-    const size_t need = weights && some ? (size_t)grid * 2 * (size_t)D * sizeof(float) : 0;
-    if (need && (!workspace || workspace_bytes < need)) return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
-    if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
     a.q = of(q);
     a.k = of(k);
     a.gq = of(grad_q_output);
@@ -207,11 +210,25 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
     a.rows = n_rows;
     a.D = (int)D;
     a.eps = eps;
-    a.part = weights ? (float *)workspace : nullptr;
+    a.gwq = grad_q_weight;
+    a.gwk = grad_k_weight;
+    a.gwq_type = grad_q_weight_type;
+    a.gwk_type = grad_k_weight_type;
+    a.add = accumulate;
     hipStream_t st = (hipStream_t)stream;
+    int64_t grid = 0;
     if (some) {
         shape_of(a);
         slices_of(a);
+        a.q_workgroups = (int)bwd_workgroups(a, false);
+        const int64_t k_workgroups = bwd_workgroups(a, true);
+        grid = a.q_workgroups + k_workgroups;
+        // (a weight whose heads are none has a gradient of zeros, which only the second launch writes)
+        const bool alone = a.q_workgroups == 1 && k_workgroups == (grad_k_weight ? 1 : k_workgroups);
+        const size_t need = weights && !alone ? (size_t)grid * (size_t)D * sizeof(float) : 0;
+        if (need && (!workspace || workspace_bytes < need)) return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
+        if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
+        a.part = need ? (float *)workspace : nullptr;
         const size_t lds = weights ? (size_t)NWAVE * 16 * a.units * sizeof(float) : 0;
         with_type(type, [&](auto t) {
             with_shape(a, norm != 0, [&](auto nm, auto whole, auto nb) {
@@ -219,9 +236,7 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
             });
         });
     }
-    if (weights)
-        hipLaunchKernelGGL(rotate_weight_kernel, dim3((unsigned)ceil_div(D, 32), 2), dim3(1024), 0, st, (const float *)workspace, some ? (int)grid : 0, (int)D, grad_q_weight, grad_q_weight_type,
-                           grad_k_weight, grad_k_weight_type, accumulate);
+    if (weights && (a.part || !some)) hipLaunchKernelGGL(rotate_weight_kernel, dim3((unsigned)ceil_div(D, 32), 2), dim3(1024), 0, st, a, (int)grid);
     return launched("rotation gradient launch");
 }
 

@@ -89,13 +89,13 @@ def test_rotation_calls_check_their_arguments():
         assert len(l.tt_last_error()) > 0
     for k in (dict(rows=0), dict(D=0, rot=None), dict(q=heads(n=0), qo=heads(n=0), k=None, ko=None)):
         assert l.tt_qk_norm_rotate_fwd(*fwd(**k)) == 0, k
-    need = l.tt_qk_norm_rotate_bwd_workspace_bytes(5, 4, 4, 16)
+    need = l.tt_qk_norm_rotate_bwd_workspace_bytes(50, 4, 4, 16)
     assert need > 0
     bwd = lambda **k: (k.get("gqo", heads()), k.get("gko", heads()), k.get("q", heads()), k.get("k", heads()), k.get("rot", rot()), k.get("norm", 1), k.get("eps", 1e-6), k.get("qw"), k.get("qt", F32),  # noqa: E731
-                       k.get("kw"), k.get("kt", F32), k.get("gq", heads()), k.get("gk", heads()), k.get("gqw", 64), k.get("gqt", F32), k.get("gkw", 64), k.get("gkt", F32), 0, k.get("rows", 5), k.get("D", 16),
+                       k.get("kw"), k.get("kt", F32), k.get("gq", heads()), k.get("gk", heads()), k.get("gqw", 64), k.get("gqt", F32), k.get("gkw", 64), k.get("gkt", F32), 0, k.get("rows", 5000), k.get("D", 16),
                        k.get("ws", 256), k.get("bytes", need), None)
     for code, k in [(-1, dict(gqo=None)), (-1, dict(gko=None)), (-1, dict(q=None)), (-1, dict(k=None)), (-1, dict(gq=None)), (-2, dict(gq=heads(n=3))), (-2, dict(k=heads(n=3))), (-6, dict(gq=heads(type=BF16))),
-                    (-6, dict(q=heads(type=BF16))), (-3, dict(norm=0)), (-3, dict(gko=None, gk=None)), (-6, dict(gqt=E4M3)), (-3, dict(gkw=66)), (-4, dict(ws=None)), (-4, dict(bytes=need - 4)), (-3, dict(ws=24)),
+                    (-6, dict(q=heads(type=BF16))), (-3, dict(norm=0)), (-3, dict(gko=None, gk=None)), (-6, dict(gqt=E4M3)), (-3, dict(gkw=66)), (-4, dict(ws=None)), (-4, dict(bytes=64)), (-3, dict(ws=24)),
                     (-3, dict(rot=rot(sections=(7,)))), (-6, dict(D=513))]:
         assert l.tt_qk_norm_rotate_bwd(*bwd(**k)) == code, k
     assert l.tt_qk_norm_rotate_bwd(*bwd(rows=0, gqw=None, gkw=None)) == 0
