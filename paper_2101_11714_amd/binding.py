@@ -143,9 +143,9 @@ def lib():
         i32, size = C.c_int32, C.c_size_t
         for name in ("tt_linear_fwd", "tt_linear_bwd", "tt_qk_norm_rotate_bwd", "tt_token_logprob_fwd"):
             getattr(l, name + "_workspace_bytes").restype = size
-        l.tt_linear_fwd_workspace_bytes.argtypes = [i64, i64, i64, i32]
+        l.tt_linear_fwd_workspace_bytes.argtypes = [i64, i64, i64, i32, C.c_int]
         l.tt_linear_fwd.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, i64, i64, i64, vp, size, vp]
-        l.tt_linear_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+        l.tt_linear_bwd_workspace_bytes.argtypes = [i64, i64, i64, i32, i32, C.c_int]
         l.tt_linear_bwd.argtypes = [vp, vp, vp, vp, i32, vp, vp, vp, i32, C.c_int, i64, i64, i64, vp, size, vp]
         l.tt_qk_norm_rotate_fwd.argtypes = [vp, vp, vp, C.c_int, f32, vp, i32, vp, i32, vp, vp, i64, i64, vp]
         l.tt_qk_norm_rotate_bwd_workspace_bytes.argtypes = [i64, i64, i64, i64]
@@ -764,8 +764,9 @@ def _activation(a: Union[str, int]) -> int:
     return int(a)
 
 
-def linear_fwd_workspace_bytes(n_rows: int, K: int, N: int, dtype: torch.dtype) -> int:
-    return int(lib().tt_linear_fwd_workspace_bytes(int(n_rows), int(K), int(N), _TYPES[dtype]))
+def linear_fwd_workspace_bytes(n_rows: int, K: int, N: int, dtype: torch.dtype, whole: bool = False) -> int:
+    """whole: K and all strides are multiples of 8 and the addresses of 16 bytes (16-bit values: what is not is copied)."""
+    return int(lib().tt_linear_fwd_workspace_bytes(int(n_rows), int(K), int(N), _TYPES[dtype], whole))
 
 
 def tt_linear_fwd(x: torch.Tensor, weight: torch.Tensor, output: torch.Tensor, bias: Optional[torch.Tensor] = None, activation: Union[str, int] = ACT_NONE,
@@ -778,8 +779,9 @@ def tt_linear_fwd(x: torch.Tensor, weight: torch.Tensor, output: torch.Tensor, b
     return output
 
 
-def linear_bwd_workspace_bytes(n_rows: int, K: int, N: int, dtype: torch.dtype, activation: Union[str, int] = ACT_NONE) -> int:
-    return int(lib().tt_linear_bwd_workspace_bytes(int(n_rows), int(K), int(N), _TYPES[dtype], _activation(activation)))
+def linear_bwd_workspace_bytes(n_rows: int, K: int, N: int, dtype: torch.dtype, activation: Union[str, int] = ACT_NONE, whole: bool = False) -> int:
+    """whole: as above, of N too."""
+    return int(lib().tt_linear_bwd_workspace_bytes(int(n_rows), int(K), int(N), _TYPES[dtype], _activation(activation), whole))
 
 
 def tt_linear_bwd(grad_output: torch.Tensor, x: Optional[torch.Tensor], weight: Optional[torch.Tensor], grad_x: Optional[torch.Tensor], grad_weight: Optional[torch.Tensor],

@@ -11,8 +11,7 @@ using namespace tt;
 
 namespace {
 
-
-constexpr int64_t MOST_COLUMNS = 1ll << 24;                  // of x, weight and output
+constexpr int64_t MOST_COLUMNS = PS_MOST_STRIDE;             // of x, weight and output, so that copies in whole chunks can be loaded
 
 int check_product(int64_t M, int64_t K, int64_t N)
 {
@@ -20,7 +19,7 @@ int check_product(int64_t M, int64_t K, int64_t N)
     if (!rc) rc = check_sizes(M, N);
     if (!rc) rc = check_sizes(N, K);
     if (rc) return rc;
-    if (K > MOST_COLUMNS || N > MOST_COLUMNS) return fail(TT_ERR_UNSUPPORTED, "more than 2^24 columns");
+    if (K > MOST_COLUMNS || N > MOST_COLUMNS) return fail(TT_ERR_UNSUPPORTED, "more than 2^22 columns");
     return TT_OK;
 }
 
@@ -40,24 +39,41 @@ int check_workspace(size_t need, const void *workspace, size_t bytes)
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Where what lies in the workspace of a gradient: parts of sums first (of one product, then of the other), the gradient in front of the
-// activation, or a copy of the output's in rows of whole chunks where a product could not load it in these, the columns' sums of the bands.
+// Where what lies in the workspace of a product: parts of sums, copies of x and of the weight in whole chunks where they are not.
+struct Room {
+    size_t parts, x, w, all;
+};
+
+Room product_room(int64_t M, int64_t K, int64_t N, int32_t type, bool whole_x, bool whole_w)
+{
+    Room r{};
+    if (M <= PF_MOST) return r;                              // few rows are loaded as they lie
+    r.parts = up(product_bytes(M, N, K, type));
+    r.x = whole_x ? 0 : up(packed_bytes(M, K, type));
+    r.w = whole_w ? 0 : up(packed_bytes(N, K, type));
+    r.all = r.parts + r.x + r.w;
+    return r;
+}
+
+// The same of a gradient: parts of sums first (of one product, then of the other), the gradient in front of the activation, or a copy of the output's in
+// rows of whole chunks, a copy of the weight (then of x), the columns' sums of the bands.
 struct GradRoom {
-    size_t parts, dz, bands, all;
+    size_t parts, dz, copy, bands, all;
     int64_t band, n_bands;
 };
 
-GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, bool x, bool w, bool b)
+GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, bool copy_x, bool copy_w, bool x, bool w, bool b)
 {
     GradRoom r{};
     const size_t px = x ? product_bytes(M, K, N, type) : 0, pw = w ? product_bytes(N, K, M, type) : 0;
-    const int64_t cols = 8 * ceil_div(N, 8);
+    const size_t cx = copy_x ? packed_bytes(M, K, type) : 0, cw = copy_w ? packed_bytes(N, K, type) : 0;
     r.parts = up(px > pw ? px : pw);
-    r.dz = copy && (x || w) ? up((size_t)M * (size_t)cols * element_bytes(type)) : 0;
+    r.dz = copy && (x || w) ? up(packed_bytes(M, N, type)) : 0;
+    r.copy = up(cx > cw ? cx : cw);
     r.n_bands = M < 64 * 256 ? ceil_div(M, 64) : 256;
     r.band = ceil_div(M, r.n_bands > 0 ? r.n_bands : 1);
-    r.bands = b && r.n_bands > 1 ? up((size_t)r.n_bands * (size_t)cols * sizeof(float)) : 0;
-    r.all = r.parts + r.dz + r.bands;
+    r.bands = b && r.n_bands > 1 ? up((size_t)r.n_bands * (size_t)(8 * ceil_div(N, 8)) * sizeof(float)) : 0;
+    r.all = r.parts + r.dz + r.copy + r.bands;
     return r;
 }
 
@@ -65,10 +81,11 @@ GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, boo
 
 extern "C" {
 
-size_t tt_linear_fwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type)
+size_t tt_linear_fwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int whole)
 {
     if (check_product(n_rows, K, N) || (type != TT_F32 && type != TT_BF16 && type != TT_F16)) return 0;
-    return n_rows <= PF_MOST ? 0 : product_bytes(n_rows, N, K, type);
+    whole = whole || type == TT_F32;
+    return product_room(n_rows, K, N, type, whole, whole).all;
 }
 
 int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias, int32_t bias_type, int32_t activation,
@@ -86,15 +103,19 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
     if (residual && residual->type != output->type) return fail(TT_ERR_UNSUPPORTED, "residual has the output's type");
     if (pre && pre->type != x->type) return fail(TT_ERR_UNSUPPORTED, "pre has x's type");
     if (activation < 0 || activation >= ACT_COUNT) return fail(TT_ERR_BAD_ARG, "activation %d", (int)activation);
-    if ((rc = check_workspace(tt_linear_fwd_workspace_bytes(n_rows, K, N, x->type), workspace, workspace_bytes))) return rc;
+    const Room room = product_room(n_rows, K, N, x->type, whole_chunks(*x, K), whole_chunks(*weight, K));
+    if ((rc = check_workspace(room.all, workspace, workspace_bytes))) return rc;
+    char *ws = (char *)workspace;
+    const Operand a{x->data, x->ld, n_rows, K, room.x ? ws + room.parts : nullptr}, b{weight->data, weight->ld, N, K, room.w ? ws + room.parts + room.x : nullptr};
     EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
-    return product(x->type, DENSE_DENSE, output->type, x->data, x->ld, false, weight->data, weight->ld, n_rows, N, K, e, workspace, (hipStream_t)stream);
+    return product(x->type, DENSE_DENSE, output->type, a, b, n_rows, N, K, e, workspace, (hipStream_t)stream);
 }
 
-size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation)
+size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation, int whole)
 {
     if (check_product(n_rows, K, N) || (type != TT_F32 && type != TT_BF16 && type != TT_F16)) return 0;
-    return grad_room(n_rows, K, N, type, activation != TT_ACT_NONE || type != TT_F32, true, true, true).all;
+    const bool copy = !whole && type != TT_F32;
+    return grad_room(n_rows, K, N, type, copy || activation != TT_ACT_NONE, copy, copy, true, true, true).all;
 }
 
 int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_rows_t *weight, const tt_rows_t *pre, int32_t activation,
@@ -120,14 +141,14 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         if (grad_weight->type != type && grad_weight->type != TT_F32) return fail(TT_ERR_UNSUPPORTED, "grad_weight has grad_output's type or 32 bits");
     }
     if ((rc = check_vector(grad_bias, "grad_bias", grad_bias_type))) return rc;
-    const bool copy = activation != TT_ACT_NONE || (type != TT_F32 && !whole_chunks(grad_output->data, grad_output->ld, N, type));
-    const GradRoom room = grad_room(n_rows, K, N, type, copy, grad_x != nullptr, grad_weight != nullptr, grad_bias != nullptr);
+    const bool copy = activation != TT_ACT_NONE || !whole_chunks(*grad_output, N);
+    const bool copy_x = grad_weight && !whole_chunks(*x, K), copy_w = grad_x && !whole_chunks(*weight, K);
+    const GradRoom room = grad_room(n_rows, K, N, type, copy, copy_x, copy_w, grad_x != nullptr, grad_weight != nullptr, grad_bias != nullptr);
     if ((rc = check_workspace(room.all, workspace, workspace_bytes))) return rc;
     hipStream_t st = (hipStream_t)stream;
     char *ws = (char *)workspace;
     const void *dz = grad_output->data;
     int64_t ld_dz = grad_output->ld;
-    const bool padded = room.dz > 0;                         // (the slopes' kernel writes whole vectors)
     const bool alone = grad_bias && room.n_bands == 1;       // its sums are the gradient
     if (N > 0 && (room.dz || grad_bias) && n_rows > 0) {
         SlopeArgs a{};
@@ -145,7 +166,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
             dz = a.dz;
             ld_dz = a.ld_dz;
         }
-        a.part = room.bands ? (float *)(ws + room.parts + room.dz) : nullptr;
+        a.part = room.bands ? (float *)(ws + room.parts + room.dz + room.copy) : nullptr;
         a.db = alone ? grad_bias : nullptr;
         a.db_type = grad_bias_type;
         a.add = accumulate;
@@ -163,7 +184,7 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
     }
     if (grad_bias && N > 0 && !alone) {
         with_type(grad_bias_type, [&](auto w) {
-            hipLaunchKernelGGL((bias_sum_kernel<decltype(w)>), dim3((unsigned)ceil_div(N, 32)), dim3(1024), 0, st, (const float *)(ws + room.parts + room.dz), (int)room.n_bands, (int)N,
+            hipLaunchKernelGGL((bias_sum_kernel<decltype(w)>), dim3((unsigned)ceil_div(N, 32)), dim3(1024), 0, st, (const float *)(ws + room.parts + room.dz + room.copy), (int)room.n_bands, (int)N,
                                (int)(8 * ceil_div(N, 8)), (decltype(w) *)grad_bias, accumulate);
         });
         if ((rc = launched("gradient launch"))) return rc;
@@ -172,7 +193,8 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         EpilogueArgs e{};
         e.out = grad_x->data;
         e.ld_out = grad_x->ld;
-        if ((rc = product(type, DENSE_STRIDED, type, dz, ld_dz, padded, weight->data, weight->ld, n_rows, K, N, e, ws, st))) return rc;
+        const Operand a{dz, ld_dz, n_rows, N, nullptr}, b{weight->data, weight->ld, N, K, copy_w ? ws + room.parts + room.dz : nullptr};
+        if ((rc = product(type, DENSE_STRIDED, type, a, b, n_rows, K, N, e, ws, st))) return rc;
     }
     if (grad_weight && !(accumulate && n_rows == 0)) {
         EpilogueArgs e{};
@@ -182,7 +204,8 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
             e.add = e.out;
             e.ld_add = e.ld_out;
         }
-        rc = product(type, STRIDED_STRIDED, grad_weight->type, dz, ld_dz, padded, x->data, x->ld, N, K, n_rows, e, ws, st);
+        const Operand a{dz, ld_dz, n_rows, N, nullptr}, b{x->data, x->ld, n_rows, K, copy_x ? ws + room.parts + room.dz : nullptr};
+        rc = product(type, STRIDED_STRIDED, grad_weight->type, a, b, N, K, n_rows, e, ws, st);
     }
     return rc;
 }

@@ -201,38 +201,99 @@ __device__ __forceinline__ void block_products(const uint4 (&b)[BN], const uint4
 
 // ---- loads that bear any alignment and any edge ---------------------------------------------------------------------------
 
-template <typename T>
+// 16 bytes from a place of 4-byte alignment or (HALVES: 16-bit values) of 2: there the words around them, of which each has one of the values, are loaded
+// and shifted.  (The device loads 16 bytes from any address, but from odd ones at a third of the rate: few rows, 14 x 3,065 x 512, 20 us instead of 10.)
+template <typename T, bool HALVES>
 struct Chunk {
-    static constexpr int W = 16 / sizeof(T) * sizeof(T) / 4;                 // words
-    typedef uint32_t Words __attribute__((ext_vector_type(W)));
-    typedef Words Anywhere __attribute__((aligned(sizeof(T))));
-};
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    typedef Words Aligned __attribute__((aligned(4)));
+    Words w;
+    uint32_t next, shift;        // HALVES: the word behind them, 16 at odd places
 
-// 16 bytes of a line of N values from value c on; zeros behind the line's end.  The last 16 bytes of the line are loaded where
-// fewer are left, and moved into place; lines of less than 16 bytes value by value.
-template <typename T>
-__device__ __forceinline__ uint4 fetch_chunk(const T *line, int64_t c, int64_t N)
-{
-    constexpr int CH = 16 / sizeof(T);
-    typedef typename Chunk<T>::Words Words;
-    Words w = {0u, 0u, 0u, 0u};
-    if (N >= CH) {
-        const int64_t last = N - CH, from = c < last ? c : last;
-        w = *reinterpret_cast<const typename Chunk<T>::Anywhere *>(line + from);
-        const int64_t d = c - from;
-        if (d > 0) {
-            if (d >= CH) return uint4{0u, 0u, 0u, 0u};
-            unsigned __int128 all = __builtin_bit_cast(unsigned __int128, w);
-            all >>= 8 * (int)sizeof(T) * (int)d;
-            w = __builtin_bit_cast(Words, all);
+    __device__ __forceinline__ void load(const T *p)
+    {
+        if (HALVES) {
+            const uintptr_t at = (uintptr_t)p;
+            const char *from = (const char *)(at & ~(uintptr_t)3);
+            shift = (uint32_t)(at & 2) * 8;
+            w = *reinterpret_cast<const Aligned *>(from);
+            next = *reinterpret_cast<const uint32_t *>(from + 12 + (at & 2) * 2);
+        } else {
+            w = *reinterpret_cast<const Aligned *>(p);
         }
-    } else if (c == 0) {
+    }
+    __device__ __forceinline__ uint4 get() const
+    {
+        if (!HALVES) return {w.x, w.y, w.z, w.w};
+        return {__builtin_amdgcn_alignbit(w.y, w.x, shift), __builtin_amdgcn_alignbit(w.z, w.y, shift), __builtin_amdgcn_alignbit(w.w, w.z, shift), __builtin_amdgcn_alignbit(next, w.w, shift)};
+    }
+
+    // From value c on of a line of N values (one at least): the line's last 16 bytes where fewer are left; lines of less than 16 bytes value by value.
+    __device__ __forceinline__ void load(const T *line, int64_t c, int64_t N)
+    {
+        constexpr int CH = 16 / sizeof(T);
+        if (N >= CH) return load(line + (c < N - CH ? c : N - CH));
         struct { T v[CH]; } x;
 #pragma unroll
-        for (int j = 0; j < CH; ++j) x.v[j] = j < N ? line[j] : (T)0.f;
+        for (int j = 0; j < CH; ++j) x.v[j] = line[j < N ? j : N - 1];
         w = __builtin_bit_cast(Words, x);
+        next = shift = 0;
     }
-    return __builtin_bit_cast(uint4, w);
+    // what load() brought, moved into place, with zeros behind the line's end
+    __device__ __forceinline__ uint4 get(int64_t c, int64_t N) const { return settled(get(), c, N); }
+
+    static __device__ __forceinline__ uint4 settled(uint4 w, int64_t c, int64_t N)
+    {
+        constexpr int CH = 16 / sizeof(T), PER = 4 / sizeof(T);
+        const int n = N - c >= CH ? CH : N > c ? (int)(N - c) : 0;           // values that exist
+        const int d = N >= CH ? (CH - n) * (int)sizeof(T) : 0;               // bytes to move down by
+        auto pick = [](bool yes, uint32_t x, uint32_t y) { return yes ? x : y; };
+        w = {pick(d & 8, w.z, w.x), pick(d & 8, w.w, w.y), pick(d & 8, 0u, w.z), pick(d & 8, 0u, w.w)};
+        w = {pick(d & 4, w.y, w.x), pick(d & 4, w.z, w.y), pick(d & 4, w.w, w.z), pick(d & 4, 0u, w.w)};
+        if (sizeof(T) == 2)
+            w = {pick(d & 2, w.x >> 16 | w.y << 16, w.x), pick(d & 2, w.y >> 16 | w.z << 16, w.y), pick(d & 2, w.z >> 16 | w.w << 16, w.z), pick(d & 2, w.w >> 16, w.w)};
+        if (N < CH || n == 0) {
+            auto word = [&](uint32_t x, int k) {
+                const int left = n - k * PER;                // values of this word
+                return left >= PER ? x : left == 1 && PER == 2 ? x & 0xffffu : 0u;
+            };
+            w = {word(w.x, 0), word(w.y, 1), word(w.z, 2), word(w.w, 3)};
+        }
+        return w;
+    }
+};
+
+// Operands of 16 bits whose rows are not whole chunks, copied into rows that are, with zeros behind their ends: two of them in one launch.  (Loaded through
+// registers as they lie, with shifts and edges: 4,096 x 4,096 x 4,096 from rows of 4,099 values 223 us; copied and then by chunks 123.)
+struct PackArgs {
+    const void *from[2];
+    void *to[2];
+    int64_t ld[2], columns[2], chunks[2];                    // chunks: of the operand (0: none)
+    int row[2];                                              // chunks of a row
+};
+constexpr int PACK_U = 4;
+
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs p)
+{
+    const int64_t first_wgs = (p.chunks[0] + 256 * PACK_U - 1) / (256 * PACK_U);
+    const int which = workgroup() >= first_wgs;
+    const int64_t base = (workgroup() - (which ? first_wgs : 0)) * 256 * PACK_U, left = p.chunks[which] - base;
+    if (left <= 0) return;
+    const int64_t row0 = base / p.row[which], columns = p.columns[which];
+    const uint32_t per = (uint32_t)p.row[which], rest = (uint32_t)(base - row0 * per) + threadIdx.x;
+    Chunk<T, true> x[PACK_U];
+    int64_t c[PACK_U];
+#pragma unroll
+    for (int u = 0; u < PACK_U; ++u) {
+        const uint32_t at = rest + ((int64_t)threadIdx.x + u * 256 < left ? u * 256 : 0), row = at / per;
+        c[u] = 8 * (int64_t)(at - row * per);
+        if ((int64_t)threadIdx.x < left) x[u].load((const T *)p.from[which] + (row0 + row) * p.ld[which], c[u], columns);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < PACK_U; ++u)
+        if ((int64_t)threadIdx.x + u * 256 < left) reinterpret_cast<uint4 *>(p.to[which])[base + threadIdx.x + u * 256] = x[u].get(c[u], columns);
 }
 
 struct ProductArgs {
@@ -338,16 +399,24 @@ __global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, Epilogue
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bias[8];
     const int have = p.N - n < 8 ? (int)(p.N - n) : 8;
     load_bias(e, n, have, bias);
-    for (int s = 0; s < parts; ++s) {
-        float x[8];
-        widen8(fetch8<true>(p.part + ((int64_t)s * p.M + m) * p.ld_part + n, 8, 8), x);
+    constexpr int U = 8;                                     // parts whose loads are on their way together
+    for (int s0 = 0; s0 < parts; s0 += U) {
+        Vec8<float> x[U];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += x[j];
+        for (int u = 0; u < U; ++u) x[u] = fetch8<true>(p.part + ((int64_t)(s0 + u < parts ? s0 + u : s0) * p.M + m) * p.ld_part + n, 8, 8);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float y[8];
+            widen8(x[u], y);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += s0 + u < parts ? y[j] : 0.f;
+        }
     }
     finish8<T, O>(e, m, n, have, bias, v);
 }
 
-// What a thread loads of an operand's tile through registers: PIECES chunks of 16 bytes.  Steps in the middle load from any address; where the tile or
+// What a thread loads of an operand's tile of 32-bit values through registers: PIECES chunks of 16 bytes.  Steps in the middle load from any address; where the tile or
 // the step ends outside of the operand every chunk is looked at.
 template <typename T, bool KDENSE, int ROWS, int THREADS>
 struct Staged {
@@ -356,12 +425,13 @@ struct Staged {
     static_assert(Tile::CHUNKS % THREADS == 0, "every thread has as many");
     const T *line[PIECES];       // where the thread's lines begin (KDENSE: at k = 0; else at the tile's first row, k = 0)
     int64_t ld, rows, row0;
-    uint4 reg[PIECES];
+    Chunk<T, false> reg[PIECES];
     bool inside;                 // all rows of the tile exist
+    bool edge;                   // what is in reg was not all there
 
     static __device__ __forceinline__ int line_of(int i) { return (i * THREADS + threadIdx.x) / Tile::LINE; }
     static __device__ __forceinline__ int chunk_of(int i) { return (i * THREADS + threadIdx.x) % Tile::LINE; }
-    __device__ __forceinline__ Staged(const void *data, int64_t stride, int64_t first, int64_t n) : ld(stride), rows(n), row0(first), inside(first + ROWS <= n)
+    __device__ __forceinline__ Staged(const void *data, int64_t stride, int64_t first, int64_t n) : ld(stride), rows(n), row0(first), inside(first + ROWS <= n), edge(false)
     {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
@@ -373,29 +443,36 @@ struct Staged {
     // the step's values from k on, of which those below `end` exist
     __device__ __forceinline__ void fetch(int64_t k, int64_t end)
     {
-        if (k + PB_K<T> <= end && (KDENSE || inside)) {
+        edge = k + PB_K<T> > end || (!KDENSE && !inside);
+        if (!edge) {
 #pragma unroll
-            for (int i = 0; i < PIECES; ++i) reg[i] = __builtin_bit_cast(uint4, *reinterpret_cast<const typename Chunk<T>::Anywhere *>(line[i] + (KDENSE ? k : k * ld)));
+            for (int i = 0; i < PIECES; ++i) reg[i].load(line[i] + (KDENSE ? k : k * ld));
             return;
         }
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const int c = chunk_of(i) * CH;
-            if (KDENSE) reg[i] = fetch_chunk(line[i] - c, k + c, end);
-            else reg[i] = k + line_of(i) < end ? fetch_chunk(line[i] + k * ld - c - row0, row0 + c, rows) : uint4{0u, 0u, 0u, 0u};
+            if (KDENSE) reg[i].load(line[i] - c, k + c, end);
+            else reg[i].load(line[i] + (k + line_of(i) < end ? k : end - 1 - line_of(i)) * ld - c - row0, row0 + c, rows);
         }
     }
-    __device__ __forceinline__ void put(char *lds) const
+    // (k, end: as they were fetched)
+    __device__ __forceinline__ void put(char *lds, int64_t k, int64_t end) const
     {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) *reinterpret_cast<uint4 *>(lds + Tile::at(line_of(i), chunk_of(i))) = reg[i];
+        for (int i = 0; i < PIECES; ++i) {
+            const int c = chunk_of(i) * CH;
+            uint4 x = reg[i].get();
+            if (edge) x = KDENSE ? Chunk<T, false>::settled(x, k + c, end) : Chunk<T, false>::settled(x, row0 + c, k + line_of(i) < end ? rows : 0);
+            *reinterpret_cast<uint4 *>(lds + Tile::at(line_of(i), chunk_of(i))) = x;
+        }
     }
 };
 
 // A tile of TM x TN per workgroup of WM x (4 / WM) waves, operands through registers into LDS, so that every alignment and edge is right.  Two tiles of
 // each operand in LDS: while one is multiplied the next one is written, and the one after it is on its way.
 template <typename T, typename O, bool AK, bool BK, int TM, int TN, int WM>
-__global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArgs e)
+__global__ __launch_bounds__(256, 2) void product_kernel(ProductArgs p, EpilogueArgs e)
 {
     typedef Staged<T, AK, TM, 256> SA;
     typedef Staged<T, BK, TN, 256> SB;
@@ -421,8 +498,8 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArg
     if (k0 < k_end) {
         a.fetch(k0, k_end);
         b.fetch(k0, k_end);
-        a.put(lds);
-        b.put(lds + SA::Tile::BYTES);
+        a.put(lds, k0, k_end);
+        b.put(lds + SA::Tile::BYTES, k0, k_end);
         if (k0 + KB < k_end) {
             a.fetch(k0 + KB, k_end);
             b.fetch(k0 + KB, k_end);
@@ -434,8 +511,8 @@ __global__ __launch_bounds__(256) void product_kernel(ProductArgs p, EpilogueArg
         const char *now = lds + stage * STAGE;
         char *next = lds + (stage ^ 1) * STAGE;
         if (k + KB < k_end) {
-            a.put(next);
-            b.put(next + SA::Tile::BYTES);
+            a.put(next, k + KB, k_end);
+            b.put(next + SA::Tile::BYTES, k + KB, k_end);
         }
         if (k + 2 * KB < k_end) {
             a.fetch(k + 2 * KB, k_end);

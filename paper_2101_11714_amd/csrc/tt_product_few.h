@@ -9,8 +9,8 @@ constexpr int PF_WAVES = 8, PF_MOST = 64;                    // waves of a workg
 
 // A workgroup takes 16 * NB columns of C and all of k, every wave an eighth of k (in turns of FLIGHT steps of 64 bytes, all of whose loads are on their
 // way together, from any address; the last turn looks at every chunk); the waves' sums are added through LDS, in their order.
-// MB: blocks of 16 rows.
-template <typename T, typename O, int MB, int NB>
+// MB: blocks of 16 rows.  ODD: rows of 16-bit values begin at places that are no multiples of 4 bytes.
+template <typename T, typename O, int MB, int NB, bool ODD>
 __global__ __launch_bounds__(PF_WAVES *WAVE) void product_few_kernel(ProductArgs p, EpilogueArgs e)
 {
     constexpr int CH = 16 / sizeof(T), STEP = 4 * CH, FLIGHT = MB + NB <= 2 ? 8 : MB + NB <= 4 ? 4 : 3, TURN = FLIGHT * STEP;
@@ -28,25 +28,31 @@ __global__ __launch_bounds__(PF_WAVES *WAVE) void product_few_kernel(ProductArgs
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = mfma_acc_t{0.f, 0.f, 0.f, 0.f};
-    auto turn = [&](int64_t k0, auto chunk) {
-        uint4 w[FLIGHT][NB], x[FLIGHT][MB];
+    auto turn = [&](int64_t k0, auto load, auto get) {
+        Chunk<T, ODD> w[FLIGHT][NB], x[FLIGHT][MB];
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f)
 #pragma unroll
-            for (int j = 0; j < NB; ++j) w[f][j] = chunk(wrow[j], k0 + f * STEP + q * CH);
+            for (int j = 0; j < NB; ++j) load(w[f][j], wrow[j], k0 + f * STEP + q * CH);
 #pragma unroll
         for (int f = 0; f < FLIGHT; ++f)
 #pragma unroll
-            for (int i = 0; i < MB; ++i) x[f][i] = chunk(xrow[i], k0 + f * STEP + q * CH);
+            for (int i = 0; i < MB; ++i) load(x[f][i], xrow[i], k0 + f * STEP + q * CH);
         __builtin_amdgcn_sched_barrier(0);                   // (or the compiler loads them one after the other)
 #pragma unroll
-        for (int f = 0; f < FLIGHT; ++f) block_products<T>(w[f], x[f], acc);
+        for (int f = 0; f < FLIGHT; ++f) {
+            uint4 a[MB], b[NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) b[j] = get(w[f][j], k0 + f * STEP + q * CH);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) a[i] = get(x[f][i], k0 + f * STEP + q * CH);
+            block_products<T>(b, a, acc);
+        }
     };
     int64_t k0 = (int64_t)wave * TURN;
 #pragma unroll 1
-    for (; k0 + TURN <= p.K; k0 += PF_WAVES * TURN)
-        turn(k0, [](const T *line, int64_t k) { return __builtin_bit_cast(uint4, *reinterpret_cast<const typename Chunk<T>::Anywhere *>(line + k)); });
-    if (k0 < p.K) turn(k0, [&](const T *line, int64_t k) { return fetch_chunk(line, k, p.K); });
+    for (; k0 + TURN <= p.K; k0 += PF_WAVES * TURN) turn(k0, [](Chunk<T, ODD> &c, const T *line, int64_t k) { c.load(line + k); }, [](const Chunk<T, ODD> &c, int64_t) { return c.get(); });
+    if (k0 < p.K) turn(k0, [&](Chunk<T, ODD> &c, const T *line, int64_t k) { c.load(line, k, p.K); }, [&](const Chunk<T, ODD> &c, int64_t k) { return c.get(k, p.K); });
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll

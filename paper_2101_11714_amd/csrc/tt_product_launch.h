@@ -11,7 +11,7 @@ namespace tt {
 enum Layout { DENSE_DENSE, DENSE_STRIDED, STRIDED_STRIDED };
 
 // How a product is computed.
-enum Way { FEW, SMALL_TILES, TILES, STREAM, STREAM_WIDE };
+enum Way { FEW, SMALL_TILES, TILES, STREAM, STREAM_WIDE };       // (tiles: 32 bits; streams: 16)
 
 struct Plan {
     Way way;
@@ -49,19 +49,19 @@ inline void stream_plan(Plan &p, int64_t M, int64_t N, int64_t K)
     p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
 }
 
-inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense, bool whole)
+inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense)
 {
     Plan p{};
     p.parts = 1;
     p.k_part = K;
     if (dense && M <= PF_MOST) {
         p.way = FEW;
-    } else if (whole && type != TT_F32) {
+    } else if (type != TT_F32) {
         stream_plan(p, M, N, K);
     } else {
         // 32 bits: tiles of 128 x 64 share out better until there are many of 128 x 128
-        p.way = type == TT_F32 && ceil_div(M, 128) * ceil_div(N, 128) < 1024 ? SMALL_TILES : TILES;
-        const int64_t step = 128 / element_bytes(type), steps = ceil_div(K, step);
+        p.way = ceil_div(M, 128) * ceil_div(N, 128) < 1024 ? SMALL_TILES : TILES;
+        const int64_t step = PB_K<float>, steps = ceil_div(K, step);
         p.tiles_m = ceil_div(M, 128);
         p.tiles_n = ceil_div(N, p.way == TILES ? 128 : 64);
         int64_t parts = (p.way == TILES ? MOST_TILES : 2 * MOST_TILES) / (p.tiles_m * p.tiles_n > 0 ? p.tiles_m * p.tiles_n : 1);
@@ -83,19 +83,29 @@ inline size_t product_bytes(int64_t M, int64_t N, int64_t K, int32_t type)
     return (size_t)(rows < tiled ? rows : tiled) * (size_t)(8 * ceil_div(N, 8)) * sizeof(float);
 }
 
-// padded: rows end in zeros up to a whole chunk
-inline bool whole_chunks(const void *p, int64_t ld, int64_t columns, int32_t type, bool padded = false)
+// rows of whole 16-byte chunks, at strides that a buffer's offsets can bear
+inline bool whole_chunks(const tt_rows_t &r, int64_t columns)
 {
-    return type != TT_F32 && (padded || columns % 8 == 0) && ld % 8 == 0 && (uintptr_t)p % 16 == 0 && ld <= PS_MOST_STRIDE;
+    return r.type == TT_F32 || (columns % 8 == 0 && r.ld % 8 == 0 && (uintptr_t)r.data % 16 == 0 && r.ld <= PS_MOST_STRIDE);
 }
 
-// C = A B^T, of M x N with sums over K, by the kernels of type T; out_type: T or 32 bits.  a_padded: A's rows end in zeros up to a whole chunk.
+// bytes of a copy in whole chunks
+inline size_t packed_bytes(int64_t rows, int64_t columns, int32_t type) { return (size_t)rows * (size_t)(8 * ceil_div(columns, 8)) * (size_t)element_bytes(type); }
+
+// An operand: rows, dense along their columns; packed: where its copy in whole chunks goes where it needs one, null: it is not to be copied (few rows
+// bear any alignment).
+struct Operand {
+    const void *data;
+    int64_t ld, rows, columns;
+    void *packed;
+};
+
+// C = A B^T, of M x N with sums over K, by the kernels of type T; out_type: T or 32 bits.
 template <typename T>
-int product_of(Layout layout, int32_t out_type, const void *a, int64_t lda, bool a_padded, const void *b, int64_t ldb, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e,
-               void *workspace, hipStream_t st);
-extern template int product_of<float>(Layout, int32_t, const void *, int64_t, bool, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
-extern template int product_of<bf16_t>(Layout, int32_t, const void *, int64_t, bool, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
-extern template int product_of<f16_t>(Layout, int32_t, const void *, int64_t, bool, const void *, int64_t, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+int product_of(Layout layout, int32_t out_type, const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st);
+extern template int product_of<float>(Layout, int32_t, const Operand &, const Operand &, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+extern template int product_of<bf16_t>(Layout, int32_t, const Operand &, const Operand &, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+extern template int product_of<f16_t>(Layout, int32_t, const Operand &, const Operand &, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
 
 template <typename... A>
 int product(int32_t type, A... args)

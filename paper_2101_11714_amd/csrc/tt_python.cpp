@@ -932,6 +932,15 @@ struct Room {
     }
 };
 
+// what the products load as it lies
+static int whole_chunks(int64_t columns, std::initializer_list<const tt_rows_t *> arrays)
+{
+    int64_t odd = columns;
+    for (const tt_rows_t *r : arrays)
+        if (r) odd |= r->ld | (int64_t)((uintptr_t)r->data / 2) | (r->ld > (1 << 22));
+    return odd % 8 == 0;
+}
+
 // x weight output bias activation residual pre workspace
 TT_FUNCTION(linear_fwd)
 {
@@ -950,7 +959,7 @@ TT_FUNCTION(linear_fwd)
     void *ws = g.bytes_or_null(7, &wsb);
     for (int i : {0, 1, 2, 3, 5, 6}) g.here(i);
     if (!g.ok) return nullptr;
-    const Room room(ws, wsb, tt_linear_fwd_workspace_bytes(n, K, N, x.type));
+    const Room room(ws, wsb, tt_linear_fwd_workspace_bytes(n, K, N, x.type, whole_chunks(K, {&x, &w})));
     return call([&](void *st) { return tt_linear_fwd(&x, &w, b, bt, (int32_t)act, r, p, o, n, K, N, room.data, room.bytes, st); });
 }
 
@@ -981,7 +990,7 @@ TT_FUNCTION(linear_bwd)
     for (int i : {0, 1, 2, 3, 5, 6, 7}) g.here(i);
     if (!g.ok) return nullptr;
     if (K < 0) K = 0;
-    const Room room(ws, wsb, tt_linear_bwd_workspace_bytes(n, K, N, go.type, (int32_t)act));
+    const Room room(ws, wsb, tt_linear_bwd_workspace_bytes(n, K, N, go.type, (int32_t)act, whole_chunks(K | N, {&go, x, w})));
     return call([&](void *st) { return tt_linear_bwd(&go, x, w, p, (int32_t)act, gx, gw, gb, bt, add ? 1 : 0, n, K, N, room.data, room.bytes, st); });
 }
 

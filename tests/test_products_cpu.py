@@ -45,19 +45,19 @@ def test_linear_calls_check_their_arguments():
                     (-6, dict(out=rows(type=BF16))), (-6, dict(x=rows(type=BF16), w=rows(type=BF16), out=rows(type=F16))), (-6, dict(res=rows(type=BF16))),
                     (-6, dict(x=rows(type=F16), w=rows(type=F16), out=rows(), res=rows(type=F16))), (-6, dict(x=rows(type=F16), w=rows(type=F16), pre=rows())), (-3, dict(act=5)), (-3, dict(act=-1)),
                     (-6, dict(b=64, bt=E4M3)), (-3, dict(b=66)), (-3, dict(out=rows(ld=15))), (-3, dict(pre=rows(ld=15))), (-3, dict(rows=-1)), (-3, dict(K=-1)), (-3, dict(N=-1)),
-                    (-6, dict(K=2**24 + 1)), (-6, dict(N=2**24 + 1, out=rows(ld=2**25))), (-6, dict(rows=2**31)), (-3, dict(x=rows(data=66))), (-6, dict(x=rows(ld=2**31 + 1))),
+                    (-6, dict(K=2**22 + 1)), (-6, dict(N=2**22 + 1, out=rows(ld=2**25))), (-6, dict(rows=2**31)), (-3, dict(x=rows(data=66))), (-6, dict(x=rows(ld=2**31 + 1))),
                     (-4, dict(rows=100, K=4096, ws=None)), (-4, dict(rows=100, K=4096, ws=256, bytes=16)), (-3, dict(ws=8))]:
         assert l.tt_linear_fwd(*fwd(**k)) == code, k
         assert len(l.tt_last_error()) > 0
     assert l.tt_linear_fwd(*fwd(rows=0)) == 0
     assert l.tt_linear_fwd(*fwd(N=0)) == 0
-    need = l.tt_linear_bwd_workspace_bytes(5, 16, 16, F32, 1)
+    need = l.tt_linear_bwd_workspace_bytes(5, 16, 16, F32, 1, 0)
     assert need > 0
     bwd = lambda **k: (k.get("dy", rows()), k.get("x", rows()), k.get("w", rows()), k.get("pre", rows()), k.get("act", 1), k.get("dx", rows()), k.get("dw", rows()), k.get("db", 64),  # noqa: E731
                        k.get("dbt", F32), k.get("add", 0), k.get("rows", 5), k.get("K", 16), k.get("N", 16), k.get("ws", 256), k.get("bytes", need), None)
     for code, k in [(-1, dict(dy=None)), (-1, dict(x=None)), (-1, dict(w=None)), (-1, dict(pre=None)), (-3, dict(act=9)), (-6, dict(pre=rows(type=BF16))), (-6, dict(w=rows(type=BF16))),
                     (-6, dict(x=rows(type=F16))), (-6, dict(dx=rows(type=F16))), (-6, dict(dw=rows(type=BF16))), (-6, dict(dbt=E4M3)), (-3, dict(db=65)), (-4, dict(ws=None)), (-4, dict(bytes=need - 256)),
-                    (-3, dict(ws=24)), (-3, dict(dx=rows(ld=15))), (-3, dict(dw=rows(ld=0))), (-6, dict(K=2**24 + 1))]:
+                    (-3, dict(ws=24)), (-3, dict(dx=rows(ld=15))), (-3, dict(dw=rows(ld=0))), (-6, dict(K=2**22 + 1))]:
         assert l.tt_linear_bwd(*bwd(**k)) == code, k
     assert l.tt_linear_bwd(*bwd(dx=None, dw=None, db=None)) == 0
     assert l.tt_linear_bwd(*bwd(rows=0, add=1, db=None)) == 0
@@ -68,10 +68,23 @@ def test_linear_workspaces_are_enough_for_fewer_rows():
     counts = [1, 2, 31, 32, 33, 127, 128, 129, 255, 256, 257, 1000, 1024, 4096, 16384, 20_000]
     for K, N in [(16, 16), (4096, 4096), (777, 1283), (8192, 64), (64, 8192), (50_000, 10), (1024, 131072)]:
         for type in (F32, BF16):
-            for f in (lambda n: l.tt_linear_fwd_workspace_bytes(n, K, N, type), lambda n: l.tt_linear_bwd_workspace_bytes(n, K, N, type, 1)):
-                sizes = [f(n) for n in counts]
-                assert sizes == sorted(sizes), (K, N, type, sizes)
-    assert l.tt_linear_fwd_workspace_bytes(5, 16, 2**25, F32) == 0 and l.tt_linear_fwd_workspace_bytes(5, 16, 16, 7) == 0
+            for whole in (0, 1):
+                for f in (lambda n: l.tt_linear_fwd_workspace_bytes(n, K, N, type, whole), lambda n: l.tt_linear_bwd_workspace_bytes(n, K, N, type, 1, whole)):
+                    sizes = [f(n) for n in counts]
+                    assert sizes == sorted(sizes), (K, N, type, sizes)
+    assert l.tt_linear_fwd_workspace_bytes(5, 16, 2**22 + 1, F32, 0) == 0 and l.tt_linear_fwd_workspace_bytes(5, 16, 16, 7, 0) == 0
+    # 32 bits need no copies, nor do few rows
+    assert l.tt_linear_fwd_workspace_bytes(300, 16, 16, F32, 0) == l.tt_linear_fwd_workspace_bytes(300, 16, 16, F32, 1)
+    assert l.tt_linear_fwd_workspace_bytes(64, 15, 16, BF16, 0) == 0 and l.tt_linear_fwd_workspace_bytes(65, 15, 16, BF16, 0) >= (65 + 16) * 32
+
+
+def test_copies_are_asked_for_where_they_are_needed():
+    l = B.lib()
+    size = l.tt_linear_fwd_workspace_bytes(65, 16, 16, BF16, 1)
+    call = lambda x, w, K: l.tt_linear_fwd(x, w, None, 0, 0, None, None, rows(type=BF16), 65, K, 16, 256, size, None)  # noqa: E731
+    for x, w, K in [(rows(type=BF16, ld=17), rows(type=BF16), 16), (rows(type=BF16), rows(type=BF16, ld=20), 16), (rows(type=BF16, data=72), rows(type=BF16), 16),
+                    (rows(type=BF16), rows(type=BF16), 15), (rows(type=BF16, ld=2**22 + 8), rows(type=BF16), 16)]:
+        assert call(x, w, K) == -4
 
 
 def test_rotation_calls_check_their_arguments():
