@@ -57,8 +57,8 @@ int launch_product(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const 
     dim3 grid = grid_of(p.tiles_m * p.tiles_n, WG);
     grid.z = (unsigned)p.parts;
     if constexpr (sizeof(T) == 4) {
-        if (p.way == TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 128, 2>), grid, dim3(WG), 0, st, q, e);
-        else hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128, 64, 4>), grid, dim3(WG), 0, st, q, e);
+        if (p.way == TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 64>), grid, dim3(WG), 0, st, q, e);
+        else hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128>), grid, dim3(WG), 0, st, q, e);
     } else {
         int rc = TT_OK;
         with_flag(p.way == STREAM_WIDE, [&](auto w) {

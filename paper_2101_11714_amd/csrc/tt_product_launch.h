@@ -11,7 +11,7 @@ namespace tt {
 enum Layout { DENSE_DENSE, DENSE_STRIDED, STRIDED_STRIDED };
 
 // How a product is computed.
-enum Way { FEW, SMALL_TILES, TILES, STREAM, STREAM_WIDE };       // (tiles: 32 bits; streams: 16)
+enum Way { FEW, TILES, TALL_TILES, STREAM, STREAM_WIDE };        // (tiles: 32 bits; streams: 16)
 
 struct Plan {
     Way way;
@@ -49,31 +49,45 @@ inline void stream_plan(Plan &p, int64_t M, int64_t N, int64_t K)
     p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
 }
 
+// The same for 32 bits, by tiles of 64 x 64 or of 128 x 64: a step takes 0.60 us of a compute unit or 1.13 (2,048^3 by the one 158, by the other 152 us,
+// one or two workgroups alike; 4,096^3 1,128 and 1,075), a launch for the parts' sums 6.  1,001 x 1,283 x 777: 37 us by both, as one part or as three;
+// 256 x 1,024 x 1,024: 24 us as 64 workgroups, in four parts 14.
+inline void tiles_plan(Plan &p, int64_t M, int64_t N, int64_t K)
+{
+    const int64_t steps = ceil_div(K, PB_K<float>);
+    double best = 0;
+    for (const bool tall : {true, false}) {
+        const int64_t tiles_m = ceil_div(M, tall ? 128 : 64), tiles_n = ceil_div(N, 64), tiles = tiles_m * tiles_n;
+        for (int64_t parts = 1; parts == 1 || (parts * tiles <= 2 * MOST_TILES && 4 * parts <= steps); ++parts) {
+            const int64_t each = ceil_div(steps, parts);
+            if (parts > 1 && ceil_div(steps, each) < parts) continue;
+            double us = (double)ceil_div(tiles * parts, 256) * (double)each * (tall ? 1.13 : 0.60);
+            if (parts > 1) us += 6.0 + (double)parts * (double)M * (double)N * 8.0 / 5.0e6;
+            if (best == 0 || us < best) {
+                best = us;
+                p.way = tall ? TALL_TILES : TILES;
+                p.tiles_m = tiles_m;
+                p.tiles_n = tiles_n;
+                p.k_part = each * PB_K<float>;
+            }
+        }
+    }
+    p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
+}
+
 inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense)
 {
     Plan p{};
     p.parts = 1;
     p.k_part = K;
-    if (dense && M <= PF_MOST) {
-        p.way = FEW;
-    } else if (type != TT_F32) {
-        stream_plan(p, M, N, K);
-    } else {
-        // 32 bits: tiles of 128 x 64 share out better until there are many of 128 x 128
-        p.way = ceil_div(M, 128) * ceil_div(N, 128) < 1024 ? SMALL_TILES : TILES;
-        const int64_t step = PB_K<float>, steps = ceil_div(K, step);
-        p.tiles_m = ceil_div(M, 128);
-        p.tiles_n = ceil_div(N, p.way == TILES ? 128 : 64);
-        int64_t parts = (p.way == TILES ? MOST_TILES : 2 * MOST_TILES) / (p.tiles_m * p.tiles_n > 0 ? p.tiles_m * p.tiles_n : 1);
-        if (parts > steps / 4) parts = steps / 4;
-        p.k_part = ceil_div(steps, parts < 1 ? 1 : parts) * step;
-        p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
-    }
+    if (dense && M <= PF_MOST) p.way = FEW;
+    else if (type != TT_F32) stream_plan(p, M, N, K);
+    else tiles_plan(p, M, N, K);
     return p;
 }
 
 // What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but no more than
-// 256 wide tiles' or MOST_TILES narrow ones' worth of rows, or the same of small ones.
+// 256 wide tiles' or MOST_TILES narrow ones' worth of rows, or twice as many of 64 columns.
 inline size_t product_bytes(int64_t M, int64_t N, int64_t K, int32_t type)
 {
     if (M <= 0 || N <= 0) return 0;
