@@ -10,8 +10,7 @@ struct SlopeArgs {
     const void *dy, *pre;        // (pre is not looked at without an activation)
     void *dz;                    // rows of nv vectors, zeros behind the N-th column; null: not wanted
     float *part;                 // [bands][8 nv] sums of columns, null: not wanted, or
-    void *db;                    // one band's: the bias's gradient
-    int db_type, add;
+    BiasSum one;                 // of one band: the bias's gradient
     int64_t ld_dy, ld_pre, ld_dz;
     int64_t rows, band;          // rows of a band
     int N, nv, act;
@@ -57,7 +56,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
             }
         }
     }
-    if (!a.part && !a.db) return;
+    if (!a.part && !a.one.db) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[lane_row][threadIdx.x & 31][j] = s[j];
     __syncthreads();
@@ -67,30 +66,7 @@ __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
 #pragma unroll
     for (int q = 0; q < 8; ++q) y += sums[q][c >> 3][c & 7];
     if (a.part) a.part[(int64_t)blockIdx.y * 8 * a.nv + at] = y;
-    else if (at < a.N) {
-        if (a.db_type == TT_F32) ((float *)a.db)[at] = y + (a.add ? ((float *)a.db)[at] : 0.f);
-        else if (a.db_type == TT_BF16) ((bf16_t *)a.db)[at] = (bf16_t)(y + (a.add ? (float)((bf16_t *)a.db)[at] : 0.f));
-        else ((f16_t *)a.db)[at] = (f16_t)(y + (a.add ? (float)((f16_t *)a.db)[at] : 0.f));
-    }
-}
-
-// the bands' sums added in their order, 32 columns a workgroup, every 32nd band a thread
-template <typename W>
-__global__ __launch_bounds__(1024) void bias_sum_kernel(const float *part, int bands, int N, int cols, W *db, int add)
-{
-    __shared__ float sums[32][33];
-    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, at = blockIdx.x * 32 + c;
-    float s = 0.f;
-    if (at < N)
-#pragma unroll 8
-        for (int b = q; b < bands; b += 32) s += part[(int64_t)b * cols + at];
-    sums[q][c] = s;
-    __syncthreads();
-    if (q || at >= N) return;
-    float y = 0.f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) y += sums[i][c];
-    db[at] = (W)((add ? (float)db[at] : 0.f) + y);
+    else if (at < a.N) leave_bias(a.one, at, y);
 }
 
 }  // namespace tt

@@ -55,25 +55,25 @@ Room product_room(int64_t M, int64_t K, int64_t N, int32_t type, bool whole_x, b
     return r;
 }
 
-// The same of a gradient: parts of sums first (of one product, then of the other), the gradient in front of the activation, or a copy of the output's in
-// rows of whole chunks, a copy of the weight (then of x), the columns' sums of the bands.
+// The same of a gradient: parts of sums of both products, the gradient in front of the activation, or a copy of the output's in rows of whole chunks,
+// copies of x and of the weight, the columns' sums of the bands.
 struct GradRoom {
-    size_t parts, dz, copy, bands, all;
+    size_t parts_x, parts_w, dz, x, w, bands, all;
     int64_t band, n_bands;
 };
 
 GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, bool copy_x, bool copy_w, bool x, bool w, bool b)
 {
     GradRoom r{};
-    const size_t px = x ? product_bytes(M, K, N, type) : 0, pw = w ? product_bytes(N, K, M, type) : 0;
-    const size_t cx = copy_x ? packed_bytes(M, K, type) : 0, cw = copy_w ? packed_bytes(N, K, type) : 0;
-    r.parts = up(px > pw ? px : pw);
+    r.parts_x = x ? up(product_bytes(M, K, N, type)) : 0;
+    r.parts_w = w ? up(product_bytes(N, K, M, type)) : 0;
     r.dz = copy && (x || w) ? up(packed_bytes(M, N, type)) : 0;
-    r.copy = up(cx > cw ? cx : cw);
+    r.x = copy_x ? up(packed_bytes(M, K, type)) : 0;
+    r.w = copy_w ? up(packed_bytes(N, K, type)) : 0;
     r.n_bands = M < 64 * 256 ? ceil_div(M, 64) : 256;
     r.band = ceil_div(M, r.n_bands > 0 ? r.n_bands : 1);
     r.bands = b && r.n_bands > 1 ? up((size_t)r.n_bands * (size_t)(8 * ceil_div(N, 8)) * sizeof(float)) : 0;
-    r.all = r.parts + r.dz + r.copy + r.bands;
+    r.all = r.parts_x + r.parts_w + r.dz + r.x + r.w + r.bands;
     return r;
 }
 
@@ -107,8 +107,10 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
     if ((rc = check_workspace(room.all, workspace, workspace_bytes))) return rc;
     char *ws = (char *)workspace;
     const Operand a{x->data, x->ld, n_rows, K, room.x ? ws + room.parts : nullptr}, b{weight->data, weight->ld, N, K, room.w ? ws + room.parts + room.x : nullptr};
-    EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
-    return product(x->type, DENSE_DENSE, output->type, a, b, n_rows, N, K, e, workspace, (hipStream_t)stream);
+    const EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
+    const Product p{a, b, {n_rows, N, K}, e, (float *)ws};
+    with_type(x->type, [&](auto t) { rc = product_of<decltype(t)>(output->type, p, (hipStream_t)stream); });
+    return rc;
 }
 
 size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation, int whole)
@@ -149,7 +151,8 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
     char *ws = (char *)workspace;
     const void *dz = grad_output->data;
     int64_t ld_dz = grad_output->ld;
-    const bool alone = grad_bias && room.n_bands == 1;       // its sums are the gradient
+    char *const at_dz = ws + room.parts_x + room.parts_w, *const at_x = at_dz + room.dz, *const at_w = at_x + room.x;
+    BiasSum bias{nullptr, grad_bias, grad_bias_type, accumulate, (int)room.n_bands, (int)N, (int)(8 * ceil_div(N, 8))};
     if (N > 0 && (room.dz || grad_bias) && n_rows > 0) {
         SlopeArgs a{};
         a.dy = grad_output->data;
@@ -161,15 +164,13 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         a.N = (int)N;
         a.nv = (int)ceil_div(N, 8);
         if (room.dz) {
-            a.dz = ws + room.parts;
+            a.dz = at_dz;
             a.ld_dz = 8 * a.nv;
             dz = a.dz;
             ld_dz = a.ld_dz;
         }
-        a.part = room.bands ? (float *)(ws + room.parts + room.dz + room.copy) : nullptr;
-        a.db = alone ? grad_bias : nullptr;
-        a.db_type = grad_bias_type;
-        a.add = accumulate;
+        if (room.bands) bias.part = a.part = (float *)(at_w + room.w);
+        else a.one = bias;
         a.rows = n_rows;
         a.band = room.band;
         a.act = activation;
@@ -182,31 +183,29 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         });
         if ((rc = launched("gradient launch"))) return rc;
     }
-    if (grad_bias && N > 0 && !alone) {
-        with_type(grad_bias_type, [&](auto w) {
-            hipLaunchKernelGGL((bias_sum_kernel<decltype(w)>), dim3((unsigned)ceil_div(N, 32)), dim3(1024), 0, st, (const float *)(ws + room.parts + room.dz + room.copy), (int)room.n_bands, (int)N,
-                               (int)(8 * ceil_div(N, 8)), (decltype(w) *)grad_bias, accumulate);
-        });
-        if ((rc = launched("gradient launch"))) return rc;
-    }
+    if (grad_bias && n_rows == 0) bias.part = (const float *)grad_bias;          // (no bands: nothing of it is read)
+    Product dx{}, dw{};
     if (grad_x) {
-        EpilogueArgs e{};
-        e.out = grad_x->data;
-        e.ld_out = grad_x->ld;
-        const Operand a{dz, ld_dz, n_rows, N, nullptr}, b{weight->data, weight->ld, N, K, copy_w ? ws + room.parts + room.dz : nullptr};
-        if ((rc = product(type, DENSE_STRIDED, type, a, b, n_rows, K, N, e, ws, st))) return rc;
+        dx.a = {dz, ld_dz, n_rows, N, nullptr};
+        dx.b = {weight->data, weight->ld, N, K, copy_w ? at_w : nullptr};
+        dx.d = {n_rows, K, N};
+        dx.e.out = grad_x->data;
+        dx.e.ld_out = grad_x->ld;
+        dx.parts = (float *)ws;
     }
     if (grad_weight && !(accumulate && n_rows == 0)) {
-        EpilogueArgs e{};
-        e.out = grad_weight->data;
-        e.ld_out = grad_weight->ld;
+        dw.a = {dz, ld_dz, n_rows, N, nullptr};
+        dw.b = {x->data, x->ld, n_rows, K, copy_x ? at_x : nullptr};
+        dw.d = {N, K, n_rows};
+        dw.e.out = grad_weight->data;
+        dw.e.ld_out = grad_weight->ld;
         if (accumulate) {
-            e.add = e.out;
-            e.ld_add = e.ld_out;
+            dw.e.add = dw.e.out;
+            dw.e.ld_add = dw.e.ld_out;
         }
-        const Operand a{dz, ld_dz, n_rows, N, nullptr}, b{x->data, x->ld, n_rows, K, copy_x ? ws + room.parts + room.dz : nullptr};
-        rc = product(type, STRIDED_STRIDED, grad_weight->type, a, b, N, K, n_rows, e, ws, st);
+        dw.parts = (float *)(ws + room.parts_x);
     }
+    with_type(type, [&](auto t) { rc = gradients_of<decltype(t)>(grad_weight ? grad_weight->type : type, dx, dw, bias, st); });
     return rc;
 }
 

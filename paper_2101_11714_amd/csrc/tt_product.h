@@ -300,7 +300,7 @@ struct ProductArgs {
     const void *a, *b;
     int64_t lda, ldb;            // between rows of a tile that is dense in k, between values of k otherwise
     int64_t M, N, K;
-    int tiles_m, tiles_n;
+    int tiles_m, tiles_n, parts;
     int64_t k_part;              // values of k of one part (a multiple of the step's)
     float *part;                 // sums of parts, [parts][M][ld_part]; null: one part, whose sums go through the epilogue
     int64_t ld_part;
@@ -329,7 +329,7 @@ __device__ __forceinline__ int xcd_tile(int id, int tiles)
 constexpr int LEAVE_BLOCK = BLOCK * 64 * 4;
 
 template <typename T, typename O, int BM, int SOME, bool FULL>
-__device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueArgs &e, int64_t m0, int64_t n0, int lane, char *lds, mfma_acc_t (&acc)[BM][4])
+__device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueArgs &e, int part, int64_t m0, int64_t n0, int lane, char *lds, mfma_acc_t (&acc)[BM][4])
 {
     constexpr int U = SOME == 1 ? 2 : FULL ? 2 : 4;
     const int c = lane & 7;
@@ -367,7 +367,7 @@ __device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueA
                 *reinterpret_cast<float4 *>(v) = *reinterpret_cast<const float4 *>(lds + r * 256 + ((2 * c) ^ row) * 16);
                 *reinterpret_cast<float4 *>(v + 4) = *reinterpret_cast<const float4 *>(lds + r * 256 + ((2 * c + 1) ^ row) * 16);
                 if (p.part) {
-                    put8<true>(p.part + ((int64_t)blockIdx.z * p.M + m) * p.ld_part + n, 8, v);
+                    put8<true>(p.part + ((int64_t)part * p.M + m) * p.ld_part + n, 8, v);
                 } else if (have < 8) {
                     finish8<T, O>(e, m, n, have, bias, v);
                 } else {
@@ -390,30 +390,36 @@ __device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueA
     }
 }
 
-// The parts' sums added in their order, and the epilogue: eight columns per thread.
+// The parts' sums added in their order, and the epilogue: eight columns, the at-th of them.
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, EpilogueArgs e, int parts)
+__device__ __forceinline__ void join_parts(const ProductArgs &p, const EpilogueArgs &e, int64_t at)
 {
-    const int64_t nv = p.ld_part / 8, at = workgroup() * 256 + threadIdx.x, m = at / nv, n = 8 * (at - m * nv);
+    const int64_t nv = p.ld_part / 8, m = at / nv, n = 8 * (at - m * nv);
     if (m >= p.M) return;
     float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, bias[8];
     const int have = p.N - n < 8 ? (int)(p.N - n) : 8;
     load_bias(e, n, have, bias);
     constexpr int U = 8;                                     // parts whose loads are on their way together
-    for (int s0 = 0; s0 < parts; s0 += U) {
+    for (int s0 = 0; s0 < p.parts; s0 += U) {
         Vec8<float> x[U];
 #pragma unroll
-        for (int u = 0; u < U; ++u) x[u] = fetch8<true>(p.part + ((int64_t)(s0 + u < parts ? s0 + u : s0) * p.M + m) * p.ld_part + n, 8, 8);
+        for (int u = 0; u < U; ++u) x[u] = fetch8<true>(p.part + ((int64_t)(s0 + u < p.parts ? s0 + u : s0) * p.M + m) * p.ld_part + n, 8, 8);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             float y[8];
             widen8(x[u], y);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] += s0 + u < parts ? y[j] : 0.f;
+            for (int j = 0; j < 8; ++j) v[j] += s0 + u < p.parts ? y[j] : 0.f;
         }
     }
     finish8<T, O>(e, m, n, have, bias, v);
+}
+
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, EpilogueArgs e)
+{
+    join_parts<T, O>(p, e, workgroup() * 256 + threadIdx.x);
 }
 
 // What a thread loads of an operand's tile of 32-bit values through registers: PIECES chunks of 16 bytes.
@@ -482,19 +488,22 @@ struct Staged {
 // steps' tiles of each operand in LDS: what a half of a step multiplies has been read from LDS in the half before, over the step's end, too; the step after
 // the next one is written, from what two steps ago was asked for.  (Two steps' tiles, read when they are multiplied, one step ahead: 256 x 1,024 x 1,024
 // 16.5 instead of 14.4 us, a step alone on its compute unit 0.98 instead of 0.60.)
+template <int TM>
+struct TileShape {
+    static constexpr int THREADS = 256, EACH = TM > 64 ? 2 : 3, STAGE = (TM + 64) * 128, LDS = 3 * STAGE;            // EACH: waves of a SIMD
+};
+
 template <typename T, typename O, bool AK, bool BK, int TM>
-__global__ __launch_bounds__(256, TM > 64 ? 2 : 3) void product_kernel(ProductArgs p, EpilogueArgs e)
+__device__ __forceinline__ void product_tile(const ProductArgs &p, const EpilogueArgs &e, int tile, int part, char *lds)
 {
     constexpr int TN = 64, KB = PB_K<T>, BM = TM / 4 / BLOCK, BN = TN / BLOCK, SOME = BM;
     typedef Staged<T, AK, TM, 256> SA;
     typedef Staged<T, BK, TN, 256> SB;
-    constexpr int STAGE = SA::Tile::BYTES + SB::Tile::BYTES;
-    static_assert(4 * SOME * LEAVE_BLOCK <= 3 * STAGE, "room for the sums");
-    __shared__ __attribute__((aligned(16))) char lds[3 * STAGE];
-    if (workgroup() >= (int64_t)p.tiles_m * p.tiles_n) return;
+    constexpr int STAGE = TileShape<TM>::STAGE;
+    static_assert(STAGE == SA::Tile::BYTES + SB::Tile::BYTES && 4 * SOME * LEAVE_BLOCK <= 3 * STAGE, "room for the tiles and for the sums");
     int tm, tn;
-    tile_place((int)workgroup(), p.tiles_m, p.tiles_n, tm, tn);
-    const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN, k0 = (int64_t)blockIdx.z * p.k_part;
+    tile_place(tile, p.tiles_m, p.tiles_n, tm, tn);
+    const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN, k0 = part * p.k_part;
     const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave * (TM / 4);
     const SA a(p.a, p.lda, m0, p.M, p.K);
@@ -564,7 +573,84 @@ __global__ __launch_bounds__(256, TM > 64 ? 2 : 3) void product_kernel(ProductAr
         step(std::false_type{}, 0, k);
         if (k + KB < k_end) step(std::false_type{}, 1, k + KB);
     }
-    leave_tile<T, O, BM, SOME, AK && BK>(p, e, m0 + wm, n0, lane, lds + wave * SOME * LEAVE_BLOCK, acc);
+    leave_tile<T, O, BM, SOME, AK && BK>(p, e, part, m0 + wm, n0, lane, lds + wave * SOME * LEAVE_BLOCK, acc);
+}
+
+template <typename T, typename O, int TM>
+__global__ __launch_bounds__(256, TileShape<TM>::EACH) void product_kernel(ProductArgs p, EpilogueArgs e)
+{
+    __shared__ __attribute__((aligned(16))) char lds[TileShape<TM>::LDS];
+    if (workgroup() < (int64_t)p.tiles_m * p.tiles_n) product_tile<T, O, true, true, TM>(p, e, (int)workgroup(), blockIdx.z, lds);
+}
+
+// The gradients' products, dx = dz w and dw = dz^T x, in one launch, so that the one with longer sums goes first and the other one fills up behind it.
+struct PairArgs {
+    ProductArgs p[2];
+    EpilogueArgs e[2];
+    int first;                   // of the two, which has the first workgroups
+    int64_t wgs[2];              // of which it has so many
+};
+
+// -> which of the two, its tile and its part
+__device__ __forceinline__ int place_of(const PairArgs &g, int64_t id, int &tile, int &part)
+{
+    int which = g.first;
+    if (id >= g.wgs[which]) {
+        id -= g.wgs[which];
+        which ^= 1;
+        if (id >= g.wgs[which]) return -1;
+    }
+    const int tiles = g.p[which].tiles_m * g.p[which].tiles_n;
+    part = (int)id / tiles;
+    tile = (int)id - part * tiles;
+    return which;
+}
+
+template <typename T, typename W, int TM>
+__global__ __launch_bounds__(256, TileShape<TM>::EACH) void pair_kernel(PairArgs g)
+{
+    __shared__ __attribute__((aligned(16))) char lds[TileShape<TM>::LDS];
+    int tile, part;
+    const int which = place_of(g, workgroup(), tile, part);
+    if (which == 0) product_tile<T, T, true, false, TM>(g.p[0], g.e[0], tile, part, lds);
+    else if (which == 1) product_tile<T, W, false, false, TM>(g.p[1], g.e[1], tile, part, lds);
+}
+
+// What is left to be done behind the pair: parts' sums of either, and the bias's gradient from bands of rows, in their order.
+struct BiasSum {
+    const float *part;           // null: there is none
+    void *db;
+    int type, add, bands, N, cols;
+};
+
+__device__ __forceinline__ void leave_bias(const BiasSum &b, int at, float y)
+{
+    if (b.type == TT_F32) ((float *)b.db)[at] = y + (b.add ? ((float *)b.db)[at] : 0.f);
+    else if (b.type == TT_BF16) ((bf16_t *)b.db)[at] = (bf16_t)(y + (b.add ? (float)((bf16_t *)b.db)[at] : 0.f));
+    else ((f16_t *)b.db)[at] = (f16_t)(y + (b.add ? (float)((f16_t *)b.db)[at] : 0.f));
+}
+
+// 32 columns of the bias, every eighth band a thread, or 256 times eight columns of a product
+template <typename T, typename W>
+__global__ __launch_bounds__(256) void finish_pair_kernel(PairArgs g, BiasSum b, int64_t wgs0, int64_t wgs1)
+{
+    __shared__ float sums[8][33];
+    int64_t id = workgroup();
+    if (id < wgs0) return join_parts<T, T>(g.p[0], g.e[0], id * 256 + threadIdx.x);
+    if ((id -= wgs0) < wgs1) return join_parts<T, W>(g.p[1], g.e[1], id * 256 + threadIdx.x);
+    if (!b.part || (id -= wgs1) >= (b.N + 31) / 32) return;
+    const int c = threadIdx.x & 31, q = threadIdx.x >> 5, at = (int)id * 32 + c;
+    float s = 0.f;
+    if (at < b.N)
+#pragma unroll 8
+        for (int i = q; i < b.bands; i += 8) s += b.part[(int64_t)i * b.cols + at];
+    sums[q][c] = s;
+    __syncthreads();
+    if (q || at >= b.N) return;
+    float y = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y += sums[i][c];
+    leave_bias(b, at, y);
 }
 
 }  // namespace tt

@@ -4,4 +4,4 @@
 
 #include "tt_product_kernels.h"
 
-template int tt::product_of<tt::f16_t>(tt::Layout, int32_t, const tt::Operand &, const tt::Operand &, int64_t, int64_t, int64_t, const tt::EpilogueArgs &, void *, hipStream_t);
+TT_PRODUCTS(, tt::f16_t)

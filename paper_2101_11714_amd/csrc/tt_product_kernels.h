@@ -5,89 +5,122 @@
 
 namespace tt {
 
-// C = A B^T; AK, BK: the operands' rows are dense in k
-template <typename T, typename O, bool AK, bool BK>
-int launch_product(Operand a, Operand b, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st)
+// copies the operands that are to be copied
+template <typename T>
+void pack(Operand &a, Operand &b, hipStream_t st)
 {
-    if (M == 0 || N == 0) return TT_OK;
-    const Plan p = plan_of(M, N, K, sizeof(T) == 4 ? TT_F32 : TT_BF16, AK && BK);
-    if constexpr (sizeof(T) == 2)
-        if (K > 0 && (a.packed || b.packed)) {
-            PackArgs q{};
-            int64_t wgs = 0;
-            auto pack = [&](int i, Operand &o) {
-                if (!o.packed) return;
-                q.from[i] = o.data;
-                q.to[i] = o.packed;
-                q.ld[i] = o.ld;
-                q.columns[i] = o.columns;
-                q.row[i] = (int)ceil_div(o.columns, 8);
-                q.chunks[i] = o.rows * q.row[i];
-                wgs += ceil_div(q.chunks[i], WG * PACK_U);
-                o.data = o.packed;
-                o.ld = 8 * q.row[i];
+    PackArgs q{};
+    int64_t wgs = 0;
+    auto add = [&](int i, Operand &o) {
+        if (!o.packed || o.rows == 0 || o.columns == 0) return;
+        q.from[i] = o.data;
+        q.to[i] = o.packed;
+        q.ld[i] = o.ld;
+        q.columns[i] = o.columns;
+        q.row[i] = (int)ceil_div(o.columns, 8);
+        q.chunks[i] = o.rows * q.row[i];
+        wgs += ceil_div(q.chunks[i], WG * PACK_U);
+        o.data = o.packed;
+        o.ld = 8 * q.row[i];
+    };
+    add(0, a);
+    add(1, b);
+    if (wgs) hipLaunchKernelGGL((pack_kernel<T>), grid_of(wgs, WG), dim3(WG), 0, st, q);
+}
+
+inline ProductArgs args_of(const Product &x, const Plan &p)
+{
+    return {x.a.data, x.b.data, x.a.ld, x.b.ld, x.d.M, x.d.N, x.d.K, (int)p.tiles_m, (int)p.tiles_n, p.parts, p.k_part, p.parts > 1 ? x.parts : nullptr, 8 * ceil_div(x.d.N, 8)};
+}
+
+inline int64_t join_workgroups(const ProductArgs &q) { return q.parts > 1 ? ceil_div(q.M * (q.ld_part / 8), WG) : 0; }
+
+// a kernel whose LDS is given with its launch
+template <auto KERNEL, typename... A>
+int launch_stream(dim3 grid, int threads, int lds, hipStream_t st, const A &...args)
+{
+    static OncePerDevice once;
+    const hipError_t err = allow_dynamic_lds(once, (const void *)KERNEL, lds);
+    if (err != hipSuccess) return hip_fail(err, "LDS of a product");
+    hipLaunchKernelGGL(KERNEL, grid, dim3(threads), lds, st, args...);
+    return TT_OK;
+}
+
+template <typename T, typename O>
+int launch_product(Product x, hipStream_t st)
+{
+    const Size &d = x.d;
+    if (d.M == 0 || d.N == 0) return TT_OK;
+    if (d.M <= PF_MOST) {
+        const ProductArgs q = args_of(x, Plan{0, 0, 1, d.K});
+        const bool odd = sizeof(T) == 2 && (x.a.ld % 2 || x.b.ld % 2 || (uintptr_t)x.a.data % 4 || (uintptr_t)x.b.data % 4);
+        with_flag(odd, [&](auto o) {
+            constexpr bool ODD = sizeof(T) == 2 && decltype(o)::value;
+            auto launch = [&](auto mb, auto nb) {
+                constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value;
+                hipLaunchKernelGGL((product_few_kernel<T, O, MB, NB, ODD>), grid_of(ceil_div(d.N, BLOCK * NB), PF_WAVES * WAVE), dim3(PF_WAVES * WAVE), 0, st, q, x.e);
             };
-            pack(0, a);
-            pack(1, b);
-            hipLaunchKernelGGL((pack_kernel<T>), grid_of(wgs, WG), dim3(WG), 0, st, q);
-        }
-    ProductArgs q{a.data, b.data, a.ld, b.ld, M, N, K, (int)p.tiles_m, (int)p.tiles_n, p.k_part, p.parts > 1 ? (float *)workspace : nullptr, 8 * ceil_div(N, 8)};
-    if (p.way == FEW) {
-        if constexpr (AK && BK) {
-            const bool odd = sizeof(T) == 2 && (a.ld % 2 || b.ld % 2 || (uintptr_t)a.data % 4 || (uintptr_t)b.data % 4);
-            with_flag(odd, [&](auto o) {
-                constexpr bool ODD = sizeof(T) == 2 && decltype(o)::value;
-                auto launch = [&](auto mb, auto nb) {
-                    constexpr int MB = decltype(mb)::value, NB = decltype(nb)::value;
-                    hipLaunchKernelGGL((product_few_kernel<T, O, MB, NB, ODD>), grid_of(ceil_div(N, BLOCK * NB), PF_WAVES * WAVE), dim3(PF_WAVES * WAVE), 0, st, q, e);
-                };
-                constexpr std::integral_constant<int, 1> one{};
-                constexpr std::integral_constant<int, 2> two{};
-                constexpr std::integral_constant<int, 4> four{};
-                // two blocks of columns share a reading of x where that leaves a workgroup for every compute unit
-                if (M <= 16) launch(one, one);
-                else if (M <= 32 && N < 256 * 32) launch(two, one);
-                else if (M <= 32) launch(two, two);
-                else if (N < 256 * 32) launch(four, one);
-                else launch(four, two);
-            });
-        }
+            constexpr std::integral_constant<int, 1> one{};
+            constexpr std::integral_constant<int, 2> two{};
+            constexpr std::integral_constant<int, 4> four{};
+            // two blocks of columns share a reading of x where that leaves a workgroup for every compute unit
+            if (d.M <= 16) launch(one, one);
+            else if (d.M <= 32 && d.N < 256 * 32) launch(two, one);
+            else if (d.M <= 32) launch(two, two);
+            else if (d.N < 256 * 32) launch(four, one);
+            else launch(four, two);
+        });
         return launched("product launch");
     }
-    dim3 grid = grid_of(p.tiles_m * p.tiles_n, WG);
-    grid.z = (unsigned)p.parts;
-    if constexpr (sizeof(T) == 4) {
-        if (p.way == TILES) hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 64>), grid, dim3(WG), 0, st, q, e);
-        else hipLaunchKernelGGL((product_kernel<T, O, AK, BK, 128>), grid, dim3(WG), 0, st, q, e);
-    } else {
-        int rc = TT_OK;
-        with_flag(p.way == STREAM_WIDE, [&](auto w) {
-            typedef StreamShape<decltype(w)::value> S;
-            const auto kernel = product_stream_kernel<T, O, AK, BK, decltype(w)::value>;
-            static OncePerDevice once;
-            const hipError_t err = allow_dynamic_lds(once, (const void *)kernel, S::LDS);
-            if (err != hipSuccess) {
-                rc = hip_fail(err, "LDS of a product");
-                return;
-            }
-            hipLaunchKernelGGL(kernel, grid, dim3(S::THREADS), S::LDS, st, q, e);
-        });
-        if (rc) return rc;
-    }
-    if (p.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, O>), grid_of(ceil_div(M * (q.ld_part / 8), WG), WG), dim3(WG), 0, st, q, e, p.parts);
+    if constexpr (sizeof(T) == 2) pack<T>(x.a, x.b, st);
+    Plan p;
+    const int kind = plan_of(&d, 1, sizeof(T) == 4 ? TT_F32 : TT_BF16, &p);
+    const ProductArgs q = args_of(x, p);
+    int rc = TT_OK;
+    with_flag(kind == 0, [&](auto large) {
+        constexpr bool LARGE = decltype(large)::value;
+        dim3 grid = grid_of(p.tiles_m * p.tiles_n, 512);
+        grid.z = (unsigned)p.parts;
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((product_kernel<T, O, LARGE ? 128 : 64>), grid, dim3(WG), 0, st, q, x.e);
+        else rc = launch_stream<product_stream_kernel<T, O, LARGE>>(grid, StreamShape<LARGE>::THREADS, StreamShape<LARGE>::LDS, st, q, x.e);
+    });
+    if (rc) return rc;
+    if (p.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, O>), grid_of(join_workgroups(q), WG), dim3(WG), 0, st, q, x.e);
     return launched("product launch");
 }
 
-template <typename T>
-int product_of(Layout layout, int32_t out_type, const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st)
+template <typename T, typename W>
+int launch_gradients(Product dx, Product dw, const BiasSum &b, hipStream_t st)
 {
-    if (layout == DENSE_STRIDED) return launch_product<T, T, true, false>(a, b, M, N, K, e, workspace, st);
-    if (layout == STRIDED_STRIDED) {
-        if (out_type == TT_F32) return launch_product<T, float, false, false>(a, b, M, N, K, e, workspace, st);
-        return launch_product<T, T, false, false>(a, b, M, N, K, e, workspace, st);
-    }
-    if (out_type == TT_F32) return launch_product<T, float, true, true>(a, b, M, N, K, e, workspace, st);
-    return launch_product<T, T, true, true>(a, b, M, N, K, e, workspace, st);
+    if constexpr (sizeof(T) == 2) pack<T>(dx.b, dw.b, st);
+    const Size d[2] = {dx.d, dw.d};
+    Plan p[2];
+    const int kind = plan_of(d, 2, sizeof(T) == 4 ? TT_F32 : TT_BF16, p);
+    PairArgs g{{args_of(dx, p[0]), args_of(dw, p[1])}, {dx.e, dw.e}, p[1].k_part > p[0].k_part, {p[0].tiles_m * p[0].tiles_n * p[0].parts, p[1].tiles_m * p[1].tiles_n * p[1].parts}};
+    int rc = TT_OK;
+    if (g.wgs[0] + g.wgs[1] > 0)
+        with_flag(kind == 0, [&](auto large) {
+            constexpr bool LARGE = decltype(large)::value;
+            const dim3 grid = grid_of(g.wgs[0] + g.wgs[1], 512);
+            if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((pair_kernel<T, W, LARGE ? 128 : 64>), grid, dim3(WG), 0, st, g);
+            else rc = launch_stream<pair_stream_kernel<T, W, LARGE>>(grid, StreamShape<LARGE>::THREADS, StreamShape<LARGE>::LDS, st, g);
+        });
+    if (rc) return rc;
+    const int64_t wgs0 = g.wgs[0] ? join_workgroups(g.p[0]) : 0, wgs1 = g.wgs[1] ? join_workgroups(g.p[1]) : 0, all = wgs0 + wgs1 + (b.part ? ceil_div(b.N, 32) : 0);
+    if (all) hipLaunchKernelGGL((finish_pair_kernel<T, W>), grid_of(all, WG), dim3(WG), 0, st, g, b, wgs0, wgs1);
+    return g.wgs[0] + g.wgs[1] + all > 0 ? launched("gradient launch") : TT_OK;
+}
+
+template <typename T>
+int product_of(int32_t out_type, const Product &x, hipStream_t st)
+{
+    return out_type == TT_F32 ? launch_product<T, float>(x, st) : launch_product<T, T>(x, st);
+}
+
+template <typename T>
+int gradients_of(int32_t w_type, const Product &dx, const Product &dw, const BiasSum &b, hipStream_t st)
+{
+    return w_type == TT_F32 ? launch_gradients<T, float>(dx, dw, b, st) : launch_gradients<T, T>(dx, dw, b, st);
 }
 
 }  // namespace tt

@@ -7,14 +7,12 @@
 
 namespace tt {
 
-// which operands' rows are dense in k: x W^T, dz W, dz^T x
-enum Layout { DENSE_DENSE, DENSE_STRIDED, STRIDED_STRIDED };
-
-// How a product is computed.
-enum Way { FEW, TILES, TALL_TILES, STREAM, STREAM_WIDE };        // (tiles: 32 bits; streams: 16)
+// C = A B^T, of M x N with sums over K, by tiles and parts of k.
+struct Size {
+    int64_t M, N, K;
+};
 
 struct Plan {
-    Way way;
     int64_t tiles_m, tiles_n;
     int parts;
     int64_t k_part;
@@ -22,68 +20,74 @@ struct Plan {
 
 constexpr int64_t MOST_TILES = 512;                          // workgroups that parts are made for
 
-// Tiles of 256 or of 128, and how many parts of k: whatever should be done first, by what was measured on 256 compute units.  A step of a wide tile,
-// one on a compute unit, takes 1.87 us (8,192 x 16,384 x 4,096: 1,127 TFLOP/s); one of a narrow tile 0.70 us alone on its compute unit and 1.17 beside
-// another one (2,048 x 2,048 x 4,096, one tile each: 48 us, by wide tiles in four parts 41 and the parts' sums 15; 8,192 x 4,096 x 4,096: 293, by
-// wide ones 221).  Parts cost a launch, and their sums a write and a read.
-inline void stream_plan(Plan &p, int64_t M, int64_t N, int64_t K)
-{
-    const int64_t steps = ceil_div(K, PS_K);
-    double best = 0;
-    for (const bool wide : {true, false}) {
-        const int64_t tile = wide ? 256 : 128, tiles_m = ceil_div(M, tile), tiles_n = ceil_div(N, tile), tiles = tiles_m * tiles_n, room = wide ? 256 : MOST_TILES;
-        for (int64_t parts = 1; parts == 1 || (parts * tiles <= room && 4 * parts <= steps); parts *= 2) {
-            const int64_t each = ceil_div(steps, parts), all = tiles * parts, whole = all / room, rest = all % room;
-            double us = wide ? 1.87 * (double)(whole + (rest > 0)) : 1.17 * (double)(whole + (rest > 256)) + (rest > 0 && rest <= 256 ? 0.70 : 0.0);
-            us = us * (double)each + 5.0;
-            if (parts > 1) us += 3.0 + (double)parts * (double)M * (double)N * 8.0 / 5.0e6;
-            if (best == 0 || us < best) {
-                best = us;
-                p.way = wide ? STREAM_WIDE : STREAM;
-                p.tiles_m = tiles_m;
-                p.tiles_n = tiles_n;
-                p.k_part = each * PS_K;
-            }
-        }
-    }
-    p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
-}
+// Kinds of tiles, and what a step of 128 bytes of k takes, in us, as measured on 256 compute units.
+// 16 bits.  256 x 256, one on a compute unit: 1.87 (8,192 x 16,384 x 4,096: 1,127 TFLOP/s).  128 x 128: 0.70 alone on its compute unit and 1.17 beside another
+// one (2,048 x 2,048 x 4,096, one tile each: 48 us, by the others in four parts 41 and the parts' sums 15; 8,192 x 4,096 x 4,096: 293, by the others 221).
+// 32 bits.  128 x 64 takes 1.13 of a compute unit and 64 x 64 0.60, alone or beside others (2,048^3 152 and 158 us, 4,096^3 1,075 and 1,128; 256 x 1,024 x
+// 1,024 24 us as 64 small tiles, in four parts 14).
+struct TileKind {
+    int64_t m, n, room;          // room: how many tiles run together
+    double step, alone;
+};
+constexpr TileKind KINDS[2][2] = {{{128, 64, 256, 1.13, 1.13}, {64, 64, 256, 0.60, 0.60}}, {{256, 256, 256, 1.87, 1.87}, {128, 128, 512, 1.17, 0.70}}};
 
-// The same for 32 bits, by tiles of 64 x 64 or of 128 x 64: a step takes 0.60 us of a compute unit or 1.13 (2,048^3 by the one 158, by the other 152 us,
-// one or two workgroups alike; 4,096^3 1,128 and 1,075), a launch for the parts' sums 6.  1,001 x 1,283 x 777: 37 us by both, as one part or as three;
-// 256 x 1,024 x 1,024: 24 us as 64 workgroups, in four parts 14.
-inline void tiles_plan(Plan &p, int64_t M, int64_t N, int64_t K)
+// Which kind (large: 0) and how many parts of each of n products that run together: whatever should be done first.  Parts cost a launch, and their sums
+// a write and a read.
+inline int plan_of(const Size *d, int n, int32_t type, Plan *p)
 {
-    const int64_t steps = ceil_div(K, PB_K<float>);
+    const int64_t step = 128 / element_bytes(type);
+    const bool f32 = type == TT_F32;
+    int best_kind = 0;
     double best = 0;
-    for (const bool tall : {true, false}) {
-        const int64_t tiles_m = ceil_div(M, tall ? 128 : 64), tiles_n = ceil_div(N, 64), tiles = tiles_m * tiles_n;
-        for (int64_t parts = 1; parts == 1 || (parts * tiles <= 2 * MOST_TILES && 4 * parts <= steps); ++parts) {
-            const int64_t each = ceil_div(steps, parts);
-            if (parts > 1 && ceil_div(steps, each) < parts) continue;
-            double us = (double)ceil_div(tiles * parts, 256) * (double)each * (tall ? 1.13 : 0.60);
-            if (parts > 1) us += 6.0 + (double)parts * (double)M * (double)N * 8.0 / 5.0e6;
-            if (best == 0 || us < best) {
-                best = us;
-                p.way = tall ? TALL_TILES : TILES;
-                p.tiles_m = tiles_m;
-                p.tiles_n = tiles_n;
-                p.k_part = each * PB_K<float>;
-            }
+    for (int kind = 0; kind < 2; ++kind) {
+        const TileKind &t = KINDS[!f32][kind];
+        const int64_t most = f32 ? 2 * MOST_TILES : t.room;
+        int64_t tiles[2] = {}, steps[2] = {};
+        for (int i = 0; i < n; ++i) {
+            tiles[i] = ceil_div(d[i].M, t.m) * ceil_div(d[i].N, t.n);
+            steps[i] = tiles[i] ? ceil_div(d[i].K, step) : 0;
         }
+        auto can = [&](int i, int64_t parts) { return parts == 1 || (i < n && parts * tiles[i] <= most && 4 * parts <= steps[i]); };
+        int64_t parts[2];
+        for (parts[0] = 1; can(0, parts[0]); parts[0] *= 2)
+            for (parts[1] = 1; can(1, parts[1]); parts[1] *= 2) {
+                int64_t wgs = 0, work = 0, longest = 0, shortest = 0;
+                double us = 0;
+                bool joins = false;
+                for (int i = 0; i < n; ++i) {
+                    if (!tiles[i]) continue;
+                    const int64_t each = ceil_div(steps[i], parts[i]);
+                    if (wgs == 0 || each < shortest) shortest = each;
+                    if (each > longest) longest = each;
+                    wgs += tiles[i] * parts[i];
+                    work += tiles[i] * parts[i] * each;
+                    if (parts[i] > 1) us += (double)parts[i] * (double)d[i].M * (double)d[i].N * 8.0 / 5.0e6;
+                    joins |= parts[i] > 1;
+                }
+                if (joins) us += f32 ? 6.0 : 3.0;
+                if (wgs <= 256) {
+                    us += t.alone * (double)longest;
+                } else if (n == 1 || shortest == longest) {
+                    const int64_t whole = wgs / t.room, rest = wgs % t.room;
+                    us += (double)longest * (t.step * (double)(whole + (rest > 256 || (rest && t.room == 256))) + (rest && rest <= 256 && t.room > 256 ? t.alone : 0.0));
+                } else {
+                    const double all = (double)work / (double)t.room + 0.5 * (double)shortest;
+                    us += t.step * (all > (double)longest ? all : (double)longest);
+                }
+                if (best == 0 || us < best) {
+                    best = us;
+                    best_kind = kind;
+                    for (int i = 0; i < n; ++i) {
+                        const int64_t each = ceil_div(steps[i], parts[i]);
+                        p[i].tiles_m = tiles[i] ? ceil_div(d[i].M, t.m) : 0;
+                        p[i].tiles_n = ceil_div(d[i].N, t.n);
+                        p[i].k_part = (each > 0 ? each : 1) * step;
+                        p[i].parts = steps[i] > 0 ? (int)ceil_div(d[i].K, p[i].k_part) : 1;
+                    }
+                }
+            }
     }
-    p.parts = K > 0 ? (int)ceil_div(K, p.k_part) : 1;
-}
-
-inline Plan plan_of(int64_t M, int64_t N, int64_t K, int32_t type, bool dense)
-{
-    Plan p{};
-    p.parts = 1;
-    p.k_part = K;
-    if (dense && M <= PF_MOST) p.way = FEW;
-    else if (type != TT_F32) stream_plan(p, M, N, K);
-    else tiles_plan(p, M, N, K);
-    return p;
+    return best_kind;
 }
 
 // What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but no more than
@@ -114,17 +118,24 @@ struct Operand {
     void *packed;
 };
 
-// C = A B^T, of M x N with sums over K, by the kernels of type T; out_type: T or 32 bits.
-template <typename T>
-int product_of(Layout layout, int32_t out_type, const Operand &a, const Operand &b, int64_t M, int64_t N, int64_t K, const EpilogueArgs &e, void *workspace, hipStream_t st);
-extern template int product_of<float>(Layout, int32_t, const Operand &, const Operand &, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
-extern template int product_of<bf16_t>(Layout, int32_t, const Operand &, const Operand &, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
-extern template int product_of<f16_t>(Layout, int32_t, const Operand &, const Operand &, int64_t, int64_t, int64_t, const EpilogueArgs &, void *, hipStream_t);
+// A product: A and B (null: there is none), and what is done with its sums; parts: room for the parts' ones.
+struct Product {
+    Operand a, b;
+    Size d;
+    EpilogueArgs e;
+    float *parts;
+};
 
-template <typename... A>
-int product(int32_t type, A... args)
-{
-    return type == TT_F32 ? product_of<float>(args...) : type == TT_BF16 ? product_of<bf16_t>(args...) : product_of<f16_t>(args...);
-}
+// x W^T by the kernels of type T (out_type: T or 32 bits), and the gradients dz W and dz^T x with what is left to do for the bias (w_type: of the second).
+template <typename T>
+int product_of(int32_t out_type, const Product &x, hipStream_t st);
+template <typename T>
+int gradients_of(int32_t w_type, const Product &dx, const Product &dw, const BiasSum &b, hipStream_t st);
+#define TT_PRODUCTS(prefix, T)                                             \
+    prefix template int tt::product_of<T>(int32_t, const tt::Product &, hipStream_t); \
+    prefix template int tt::gradients_of<T>(int32_t, const tt::Product &, const tt::Product &, const tt::BiasSum &, hipStream_t);
+TT_PRODUCTS(extern, float)
+TT_PRODUCTS(extern, bf16_t)
+TT_PRODUCTS(extern, f16_t)
 
 }  // namespace tt
