@@ -315,11 +315,14 @@ __device__ __forceinline__ void tile_place(int tile, int tiles_m, int tiles_n, i
     tm = band * BAND + rest - tn * rows;
 }
 
-// The workgroups of one XCD, which have every eighth number, take neighbouring tiles, whose operands its L2 then holds.
-__device__ __forceinline__ int xcd_tile(int id, int tiles)
+// A workgroup's tile and part of k: the workgroups of one XCD, which have every eighth number, take neighbouring tiles of one part, whose operands its L2
+// then holds.
+__device__ __forceinline__ void tile_of(int id, const ProductArgs &p, int &tm, int &tn, int &part)
 {
-    const int each = tiles / 8, more = tiles % 8, xcd = id % 8, nth = id / 8;
-    return xcd * each + min(xcd, more) + nth;
+    const int tiles = p.tiles_m * p.tiles_n, all = tiles * p.parts, each = all / 8, more = all % 8, xcd = id % 8, nth = id / 8;
+    const int at = xcd * each + min(xcd, more) + nth;
+    part = at / tiles;
+    tile_place(at - part * tiles, p.tiles_m, p.tiles_n, tm, tn);
 }
 
 // A wave's sums on their way out, 16 * BM rows of 64: SOME blocks of 16 rows at a time through LDS of the wave's own (4 KB a block), from where a
@@ -494,15 +497,15 @@ struct TileShape {
 };
 
 template <typename T, typename O, bool AK, bool BK, int TM>
-__device__ __forceinline__ void product_tile(const ProductArgs &p, const EpilogueArgs &e, int tile, int part, char *lds)
+__device__ __forceinline__ void product_tile(const ProductArgs &p, const EpilogueArgs &e, int id, char *lds)
 {
     constexpr int TN = 64, KB = PB_K<T>, BM = TM / 4 / BLOCK, BN = TN / BLOCK, SOME = BM;
     typedef Staged<T, AK, TM, 256> SA;
     typedef Staged<T, BK, TN, 256> SB;
     constexpr int STAGE = TileShape<TM>::STAGE;
     static_assert(STAGE == SA::Tile::BYTES + SB::Tile::BYTES && 4 * SOME * LEAVE_BLOCK <= 3 * STAGE, "room for the tiles and for the sums");
-    int tm, tn;
-    tile_place(tile, p.tiles_m, p.tiles_n, tm, tn);
+    int tm, tn, part;
+    tile_of(id, p, tm, tn, part);
     const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN, k0 = part * p.k_part;
     const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave * (TM / 4);
@@ -580,10 +583,11 @@ template <typename T, typename O, int TM>
 __global__ __launch_bounds__(256, TileShape<TM>::EACH) void product_kernel(ProductArgs p, EpilogueArgs e)
 {
     __shared__ __attribute__((aligned(16))) char lds[TileShape<TM>::LDS];
-    if (workgroup() < (int64_t)p.tiles_m * p.tiles_n) product_tile<T, O, true, true, TM>(p, e, (int)workgroup(), blockIdx.z, lds);
+    if (workgroup() < (int64_t)p.tiles_m * p.tiles_n * p.parts) product_tile<T, O, true, true, TM>(p, e, (int)workgroup(), lds);
 }
 
 // The gradients' products, dx = dz w and dw = dz^T x, in one launch, so that the one with longer sums goes first and the other one fills up behind it.
+// (Both by turns, eight workgroups each: 8,192 x 4,096 x 4,096 559 instead of 451 us, since an L2 then holds neither's operands.)
 struct PairArgs {
     ProductArgs p[2];
     EpilogueArgs e[2];
@@ -591,8 +595,8 @@ struct PairArgs {
     int64_t wgs[2];              // of which it has so many
 };
 
-// -> which of the two, its tile and its part
-__device__ __forceinline__ int place_of(const PairArgs &g, int64_t id, int &tile, int &part)
+// which of the two, and its how manieth workgroup
+__device__ __forceinline__ int which_of(const PairArgs &g, int64_t &id)
 {
     int which = g.first;
     if (id >= g.wgs[which]) {
@@ -600,9 +604,6 @@ __device__ __forceinline__ int place_of(const PairArgs &g, int64_t id, int &tile
         which ^= 1;
         if (id >= g.wgs[which]) return -1;
     }
-    const int tiles = g.p[which].tiles_m * g.p[which].tiles_n;
-    part = (int)id / tiles;
-    tile = (int)id - part * tiles;
     return which;
 }
 
@@ -610,10 +611,10 @@ template <typename T, typename W, int TM>
 __global__ __launch_bounds__(256, TileShape<TM>::EACH) void pair_kernel(PairArgs g)
 {
     __shared__ __attribute__((aligned(16))) char lds[TileShape<TM>::LDS];
-    int tile, part;
-    const int which = place_of(g, workgroup(), tile, part);
-    if (which == 0) product_tile<T, T, true, false, TM>(g.p[0], g.e[0], tile, part, lds);
-    else if (which == 1) product_tile<T, W, false, false, TM>(g.p[1], g.e[1], tile, part, lds);
+    int64_t id = workgroup();
+    const int which = which_of(g, id);
+    if (which == 0) product_tile<T, T, true, false, TM>(g.p[0], g.e[0], (int)id, lds);
+    else if (which == 1) product_tile<T, W, false, false, TM>(g.p[1], g.e[1], (int)id, lds);
 }
 
 // What is left to be done behind the pair: parts' sums of either, and the bias's gradient from bands of rows, in their order.

@@ -79,8 +79,7 @@ int launch_product(Product x, hipStream_t st)
     int rc = TT_OK;
     with_flag(kind == 0, [&](auto large) {
         constexpr bool LARGE = decltype(large)::value;
-        dim3 grid = grid_of(p.tiles_m * p.tiles_n, 512);
-        grid.z = (unsigned)p.parts;
+        const dim3 grid = grid_of(p.tiles_m * p.tiles_n * p.parts, 512);
         if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((product_kernel<T, O, LARGE ? 128 : 64>), grid, dim3(WG), 0, st, q, x.e);
         else rc = launch_stream<product_stream_kernel<T, O, LARGE>>(grid, StreamShape<LARGE>::THREADS, StreamShape<LARGE>::LDS, st, q, x.e);
     });

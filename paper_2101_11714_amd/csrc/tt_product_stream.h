@@ -74,14 +74,14 @@ struct Stream {
 // reads.  A barrier ends every phase.
 // Else: tiles of 128 x 128 by four waves of 64 x 64, two workgroups on a compute unit, which find their turns by themselves.
 template <typename T, typename O, bool AK, bool BK, bool WIDE>
-__device__ __forceinline__ void stream_tile(const ProductArgs &p, const EpilogueArgs &e, int id, int part, char *lds)
+__device__ __forceinline__ void stream_tile(const ProductArgs &p, const EpilogueArgs &e, int id, char *lds)
 {
     typedef StreamShape<WIDE> S;
     typedef Stream<T, AK, WIDE> SA;
     typedef Stream<T, BK, WIDE> SB;
     constexpr int BM = S::BM, BN = 4;
-    int tm, tn;
-    tile_place(xcd_tile(id, p.tiles_m * p.tiles_n), p.tiles_m, p.tiles_n, tm, tn);
+    int tm, tn, part;
+    tile_of(id, p, tm, tn, part);
     const int64_t m0 = (int64_t)tm * S::TILE, n0 = (int64_t)tn * S::TILE, k0 = part * p.k_part;
     const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> (WIDE ? 2 : 1);
@@ -155,17 +155,17 @@ template <typename T, typename O, bool WIDE>
 __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void product_stream_kernel(ProductArgs p, EpilogueArgs e)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    if (workgroup() < (int64_t)p.tiles_m * p.tiles_n) stream_tile<T, O, true, true, WIDE>(p, e, (int)workgroup(), blockIdx.z, lds);
+    if (workgroup() < (int64_t)p.tiles_m * p.tiles_n * p.parts) stream_tile<T, O, true, true, WIDE>(p, e, (int)workgroup(), lds);
 }
 
 template <typename T, typename W, bool WIDE>
 __global__ __launch_bounds__(StreamShape<WIDE>::THREADS, 2) void pair_stream_kernel(PairArgs g)
 {
     extern __shared__ __attribute__((aligned(16))) char lds[];
-    int tile, part;
-    const int which = place_of(g, workgroup(), tile, part);
-    if (which == 0) stream_tile<T, T, true, false, WIDE>(g.p[0], g.e[0], tile, part, lds);
-    else if (which == 1) stream_tile<T, W, false, false, WIDE>(g.p[1], g.e[1], tile, part, lds);
+    int64_t id = workgroup();
+    const int which = which_of(g, id);
+    if (which == 0) stream_tile<T, T, true, false, WIDE>(g.p[0], g.e[0], (int)id, lds);
+    else if (which == 1) stream_tile<T, W, false, false, WIDE>(g.p[1], g.e[1], (int)id, lds);
 }
 
 }  // namespace tt
