@@ -41,13 +41,15 @@ size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // Where what lies in the workspace of a product: parts of sums, copies of x and of the weight in whole chunks where they are not.
 struct Room {
+    bool few;                    // (few rows are loaded as they lie)
     size_t parts, x, w, all;
 };
 
 Room product_room(int64_t M, int64_t K, int64_t N, int32_t type, bool whole_x, bool whole_w)
 {
     Room r{};
-    if (M <= PF_MOST) return r;                              // few rows are loaded as they lie
+    r.few = few_rows(M, N, K, type, whole_x && whole_w);
+    if (r.few) return r;
     r.parts = up(product_bytes(M, N, K, type));
     r.x = whole_x ? 0 : up(packed_bytes(M, K, type));
     r.w = whole_w ? 0 : up(packed_bytes(N, K, type));
@@ -84,8 +86,14 @@ extern "C" {
 size_t tt_linear_fwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int whole)
 {
     if (check_product(n_rows, K, N) || (type != TT_F32 && type != TT_BF16 && type != TT_F16)) return 0;
-    whole = whole || type == TT_F32;
-    return product_room(n_rows, K, N, type, whole, whole).all;
+    // fewer rows may go another way, and so may arrays that are whole after all
+    size_t most = 0;
+    for (const bool w : {true, whole || type == TT_F32})
+        for (const int64_t up_to : {PF_CLASS[0], PF_CLASS[1], PF_CLASS[2], n_rows}) {
+            const size_t need = product_room(n_rows < up_to ? n_rows : up_to, K, N, type, w, w).all;
+            if (need > most) most = need;
+        }
+    return most;
 }
 
 int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias, int32_t bias_type, int32_t activation,
@@ -108,7 +116,7 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
     char *ws = (char *)workspace;
     const Operand a{x->data, x->ld, n_rows, K, room.x ? ws + room.parts : nullptr}, b{weight->data, weight->ld, N, K, room.w ? ws + room.parts + room.x : nullptr};
     const EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
-    const Product p{a, b, {n_rows, N, K}, e, (float *)ws};
+    const Product p{a, b, {n_rows, N, K}, e, (float *)ws, room.few};
     with_type(x->type, [&](auto t) { rc = product_of<decltype(t)>(output->type, p, (hipStream_t)stream); });
     return rc;
 }

@@ -334,7 +334,7 @@ constexpr int LEAVE_BLOCK = BLOCK * 64 * 4;
 template <typename T, typename O, int BM, int SOME, bool FULL>
 __device__ __forceinline__ void leave_tile(const ProductArgs &p, const EpilogueArgs &e, int part, int64_t m0, int64_t n0, int lane, char *lds, mfma_acc_t (&acc)[BM][4])
 {
-    constexpr int U = SOME == 1 ? 2 : FULL ? 2 : 4;
+    constexpr int U = SOME == 1 || (FULL && BM > 4) ? 2 : 4;
     const int c = lane & 7;
     const int64_t n = n0 + 8 * c;
     const int have = p.N - n < 8 ? (int)(p.N - n) : 8;

@@ -51,7 +51,7 @@ int launch_product(Product x, hipStream_t st)
 {
     const Size &d = x.d;
     if (d.M == 0 || d.N == 0) return TT_OK;
-    if (d.M <= PF_MOST) {
+    if (x.few) {
         const ProductArgs q = args_of(x, Plan{0, 0, 1, d.K});
         const bool odd = sizeof(T) == 2 && (x.a.ld % 2 || x.b.ld % 2 || (uintptr_t)x.a.data % 4 || (uintptr_t)x.b.data % 4);
         with_flag(odd, [&](auto o) {
@@ -74,7 +74,8 @@ int launch_product(Product x, hipStream_t st)
     }
     if constexpr (sizeof(T) == 2) pack<T>(x.a, x.b, st);
     Plan p;
-    const int kind = plan_of(&d, 1, sizeof(T) == 4 ? TT_F32 : TT_BF16, &p);
+    double us;
+    const int kind = plan_of(&d, 1, sizeof(T) == 4 ? TT_F32 : TT_BF16, &p, us);
     const ProductArgs q = args_of(x, p);
     int rc = TT_OK;
     with_flag(kind == 0, [&](auto large) {
@@ -94,7 +95,8 @@ int launch_gradients(Product dx, Product dw, const BiasSum &b, hipStream_t st)
     if constexpr (sizeof(T) == 2) pack<T>(dx.b, dw.b, st);
     const Size d[2] = {dx.d, dw.d};
     Plan p[2];
-    const int kind = plan_of(d, 2, sizeof(T) == 4 ? TT_F32 : TT_BF16, p);
+    double us;
+    const int kind = plan_of(d, 2, sizeof(T) == 4 ? TT_F32 : TT_BF16, p, us);
     PairArgs g{{args_of(dx, p[0]), args_of(dw, p[1])}, {dx.e, dw.e}, p[1].k_part > p[0].k_part, {p[0].tiles_m * p[0].tiles_n * p[0].parts, p[1].tiles_m * p[1].tiles_n * p[1].parts}};
     int rc = TT_OK;
     if (g.wgs[0] + g.wgs[1] > 0)

@@ -33,12 +33,12 @@ constexpr TileKind KINDS[2][2] = {{{128, 64, 256, 1.13, 1.13}, {64, 64, 256, 0.6
 
 // Which kind (large: 0) and how many parts of each of n products that run together: whatever should be done first.  Parts cost a launch, and their sums
 // a write and a read.
-inline int plan_of(const Size *d, int n, int32_t type, Plan *p)
+inline int plan_of(const Size *d, int n, int32_t type, Plan *p, double &best)
 {
     const int64_t step = 128 / element_bytes(type);
     const bool f32 = type == TT_F32;
     int best_kind = 0;
-    double best = 0;
+    best = 0;
     for (int kind = 0; kind < 2; ++kind) {
         const TileKind &t = KINDS[!f32][kind];
         const int64_t most = f32 ? 2 * MOST_TILES : t.room;
@@ -90,6 +90,27 @@ inline int plan_of(const Size *d, int n, int32_t type, Plan *p)
     return best_kind;
 }
 
+// Whether the kernel of few rows takes a product of up to 64, as one of 16, 32 or 64: it needs no parts and no copies, but every workgroup goes through all of k,
+// which takes (1.6 to 7.3) ns for a value of 16 bits, and twice as long for one of 32.  bf16: 17 x 4,096 x 4,096 12 us instead of 15 by tiles, 48 x 1,024 x
+// 4,096 8.6 instead of 12, but 64 x 8,192 x 1,024 39 instead of 17 and 8 x 16,384 x 256 26 instead of 16; fp32: 32 x 4,096 x 4,096 27 and 31, 64 x 8,192 x 1,024
+// 77 and 20.
+constexpr int64_t PF_CLASS[3] = {16, 32, 64};
+
+inline bool few(int rows_class, int64_t N, int64_t K, int32_t type, bool whole)
+{
+    const int64_t M = PF_CLASS[rows_class];
+    const bool two = M > 16 && N >= 256 * 32;                // two blocks of columns a workgroup
+    const double ns = M == 16 ? 1.6 : M == 32 ? (two ? 4.3 : 2.8) : (two ? 7.3 : 4.6), wgs = (double)ceil_div(N, two ? 32 : 16) / 256.0;
+    const double us = 3.0 + (double)K * ns * 1e-3 * (type == TT_F32 ? 2.0 : 1.0) * (wgs > 1.0 ? wgs : 1.0);
+    Plan p;
+    double tiles;
+    const Size d{M, N, K};
+    plan_of(&d, 1, type, &p, tiles);
+    return us <= tiles + 6.0 + (whole ? 0.0 : 8.0);
+}
+
+inline bool few_rows(int64_t M, int64_t N, int64_t K, int32_t type, bool whole) { return M <= PF_MOST && few(M <= 16 ? 0 : M <= 32 ? 1 : 2, N, K, type, whole); }
+
 // What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but no more than
 // 256 wide tiles' or MOST_TILES narrow ones' worth of rows, or twice as many of 64 columns.
 inline size_t product_bytes(int64_t M, int64_t N, int64_t K, int32_t type)
@@ -124,6 +145,7 @@ struct Product {
     Size d;
     EpilogueArgs e;
     float *parts;
+    bool few;                    // by the kernel of few rows
 };
 
 // x W^T by the kernels of type T (out_type: T or 32 bits), and the gradients dz W and dz^T x with what is left to do for the bias (w_type: of the second).
