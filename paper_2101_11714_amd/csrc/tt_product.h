@@ -21,11 +21,27 @@ constexpr float GELU_TANH_SCALE = 0.7978845608028654f, GELU_TANH_CUBE = 0.044715
 // 8,192 x 4,096, 52 instead of 38 us).  Where the exponential passes 2^128 its reciprocal is 0, as it should be.  (1 + tanh(u)) / 2 is this function of 2 u.
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
+// The normal distribution up to z, and exp(-z^2 / 2): for -|z| that is exp(-z^2 / 2) u P(u), u = 1 / (1 + |z| / 4), with a polynomial of degree 9 whose
+// largest error relative to u P(u) = exp(z^2 / 2) erfc(|z| / sqrt 2) / 2 is 0.6 times 2^-24 (fitted by least squares that were weighted until the errors' peaks
+// were alike).  In 32 bits 4 times 2^-24 of the whole, most of it from the polynomial's sum; no branches, which the library's error function has.
+__device__ __forceinline__ float normal_to(float z, float &e)
+{
+    constexpr float P[10] = {0.0997355655f, 0.0997364372f, 0.0934662372f, 0.0816042423f, 0.0589695089f, 0.0637153611f, -0.0317454860f, 0.0956253558f, -0.0808927864f, 0.0197855458f};
+    const float u = __builtin_amdgcn_rcpf(__builtin_fmaf(0.25f, fabsf(z), 1.f));
+    float p = P[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i) p = __builtin_fmaf(p, u, P[i]);
+    e = __builtin_amdgcn_exp2f(-0.7213475204444817f * z * z);
+    const float q = e * (u * p);
+    return z > 0.f ? 1.f - q : q;
+}
+
 __device__ __forceinline__ float act_of(float z, int act)
 {
+    float e;
     switch (act) {
     case ACT_RELU: return z > 0.f || z != z ? z : 0.f;
-    case ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.7071067811865476f));
+    case ACT_GELU: return z * normal_to(z, e);
     case ACT_GELU_TANH: return z * logistic(2.f * GELU_TANH_SCALE * (z + GELU_TANH_CUBE * z * z * z));
     case ACT_SILU: return z * logistic(z);
     default: return z;
@@ -53,7 +69,11 @@ __device__ __forceinline__ float act_slope(float z, int act)
 {
     switch (act) {
     case ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
-    case ACT_GELU: return 0.5f * (1.f + erff(z * 0.7071067811865476f)) + z * __builtin_amdgcn_exp2f(-0.7213475204444817f * z * z) * 0.3989422804014327f;
+    case ACT_GELU: {
+        float e;
+        const float p = normal_to(z, e);
+        return p + z * e * 0.3989422804014327f;
+    }
     case ACT_GELU_TANH: {
         const float p = logistic(2.f * GELU_TANH_SCALE * (z + GELU_TANH_CUBE * z * z * z));
         return p + 2.f * GELU_TANH_SCALE * z * p * (1.f - p) * (1.f + 3.f * GELU_TANH_CUBE * z * z);
