@@ -21,6 +21,14 @@ constexpr float GELU_TANH_SCALE = 0.7978845608028654f, GELU_TANH_CUBE = 0.044715
 // 8,192 x 4,096, 52 instead of 38 us).  Where the exponential passes 2^128 its reciprocal is 0, as it should be.  (1 + tanh(u)) / 2 is this function of 2 u.
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
+// its slope p (1 - p), without the difference (which is off by 2^-24 as such: 35 times that in the other functions' slopes), and p itself
+__device__ __forceinline__ float logistic_slope(float z, float &p)
+{
+    const float e = __builtin_amdgcn_exp2f(-1.4426950408889634f * fabsf(z)), r = __builtin_amdgcn_rcpf(1.f + e);
+    p = z < 0.f ? e * r : r;
+    return e * r * r;
+}
+
 // The normal distribution up to z, and exp(-z^2 / 2): for -|z| that is exp(-z^2 / 2) u P(u), u = 1 / (1 + |z| / 4), with a polynomial of degree 9 whose
 // largest error relative to u P(u) = exp(z^2 / 2) erfc(|z| / sqrt 2) / 2 is 0.6 times 2^-24 (fitted by least squares that were weighted until the errors' peaks
 // were alike).  In 32 bits 4 times 2^-24 of the whole, most of it from the polynomial's sum; no branches, which the library's error function has.
@@ -75,12 +83,14 @@ __device__ __forceinline__ float act_slope(float z, int act)
         return p + z * e * 0.3989422804014327f;
     }
     case ACT_GELU_TANH: {
-        const float p = logistic(2.f * GELU_TANH_SCALE * (z + GELU_TANH_CUBE * z * z * z));
-        return p + 2.f * GELU_TANH_SCALE * z * p * (1.f - p) * (1.f + 3.f * GELU_TANH_CUBE * z * z);
+        float p;
+        const float q = logistic_slope(2.f * GELU_TANH_SCALE * (z + GELU_TANH_CUBE * z * z * z), p);
+        return q == 0.f ? p : p + 2.f * GELU_TANH_SCALE * z * q * (1.f + 3.f * GELU_TANH_CUBE * z * z);           // (z z can pass what 32 bits hold)
     }
     case ACT_SILU: {
-        const float p = logistic(z);
-        return p * (1.f + z * (1.f - p));
+        float p;
+        const float q = logistic_slope(z, p);
+        return p + z * q;
     }
     default: return 1.f;
     }
