@@ -6,7 +6,10 @@ under dropout.  The sum is normalised.  Training fits the result to a fixed vect
 updates the table's used rows, the cores and the norm's weight; serving takes one token of each sequence and leaves the result in
 8 bits with a scale per row, as a following matrix product in 8 bits reads it.
 
-    python -m paper_2101_11714_amd.token_block [steps]
+With the loss "likelihood" the result is multiplied with a row per token of the vocabulary instead, and training raises the log probability of
+the token that follows.
+
+    python -m paper_2101_11714_amd.token_block [steps] [squares | likelihood]
 """
 
 from __future__ import annotations
@@ -72,9 +75,46 @@ class Block:
         return out, scales
 
 
-def train(steps: int = 200, vocab: int = 2000, L: int = 4096, lr: float = 5.0, lr_shared: float = 0.05, seed: int = 1, device: str = "cuda"):
-    """(block, mean loss of the first and of the last ten steps)."""
+class Answer:
+    """The way out, for L tokens at a time: logits, and log probabilities of tokens under them."""
+
+    def __init__(self, vocab: int, L: int, N: int = PAIRS.dim, seed: int = 1, device: str = "cuda"):
+        gen = torch.Generator(device=device).manual_seed(seed)
+        self.head = torch.randn((vocab, N), generator=gen, device=device) * N ** -0.5
+        self.logits = torch.empty((L, vocab), device=device)
+        self.g_y, self.g_head = torch.empty((L, N), device=device), torch.empty_like(self.head)
+        self.logprob, self.lse = torch.empty(L, device=device), torch.empty(L, device=device)
+        self.g_logprob = torch.full((L,), -1.0 / L, device=device)              # of the mean of -logprob
+
+    def forward(self, y: torch.Tensor, following: torch.Tensor) -> torch.Tensor:
+        B.tt_linear_fwd(y, self.head, self.logits)
+        B.tt_token_logprob_fwd(self.logits, following, self.logprob, self.lse)
+        return self.logprob
+
+    def backward(self, y: torch.Tensor, following: torch.Tensor) -> torch.Tensor:
+        """The gradient of y; the head's stays here.  The logits' takes their place."""
+        B.tt_token_logprob_bwd(self.logits, following, self.lse, self.g_logprob, self.logits)
+        B.tt_linear_bwd(self.logits, y, self.head, self.g_y, self.g_head)
+        return self.g_y
+
+    def likeliest(self, y: torch.Tensor, k: int):
+        """(tokens, log probabilities) of the k likeliest for each row of y."""
+        n = y.shape[0]
+        logits, lse, best = torch.empty((n, self.head.shape[0]), device=y.device), torch.empty(n, device=y.device), torch.empty((n, k), device=y.device)
+        ids = torch.empty((n, k), dtype=torch.int64, device=y.device)
+        B.tt_linear_fwd(y, self.head, logits)
+        B.tt_token_logprob_fwd(logits, None, None, lse, top_ids=ids, top_logprobs=best)
+        return ids, best
+
+
+def train(steps: int = 200, vocab: int = 2000, L: int = 4096, lr: float = 5.0, lr_shared: float = 0.05, seed: int = 1, device: str = "cuda",
+          loss: str = "squares"):
+    """(block, mean loss of the first and of the last ten steps); with the loss "likelihood" block.answer has the way out."""
     block = Block(vocab, L, seed=seed, device=device)
+    if loss == "likelihood":
+        block.answer = Answer(vocab, L, block.N, seed, device)
+    elif loss != "squares":
+        raise ValueError("loss %r" % loss)
     gen = torch.Generator(device=device).manual_seed(seed + 1)
     target = torch.randn((vocab, block.N), generator=gen, device=device)
     successor = torch.randint(0, vocab, (vocab,), generator=gen, device=device)             # the text: each token has one that mostly follows it
@@ -85,18 +125,30 @@ def train(steps: int = 200, vocab: int = 2000, L: int = 4096, lr: float = 5.0, l
         tokens, following = chain, successor[chain]
         pairs = block.pairs(tokens)
         y = block.forward(tokens, pairs)
-        off = y - target[following]
-        losses.append(off.square().mean())
-        block.backward_and_step(tokens, pairs, off / L, lr, lr_shared)
+        if loss == "likelihood":
+            losses.append(-block.answer.forward(y, following).mean())
+            g_y = block.answer.backward(y, following)
+            block.answer.head.sub_(block.answer.g_head, alpha=lr)
+        else:
+            off = y - target[following]
+            losses.append(off.square().mean())
+            g_y = off / L
+        block.backward_and_step(tokens, pairs, g_y, lr, lr_shared)
     losses = torch.stack(losses).cpu()
     return block, float(losses[:10].mean()), float(losses[-10:].mean())
 
 
 def main() -> None:
     steps = int(sys.argv[1]) if len(sys.argv) > 1 else 200
-    block, first, last = train(steps)
-    print("mean squared error: first ten steps %.4f, last ten %.4f" % (first, last))
+    loss = sys.argv[2] if len(sys.argv) > 2 else "squares"
+    block, first, last = train(steps, loss=loss)
+    print("%s: first ten steps %.4f, last ten %.4f" % ("mean squared error" if loss == "squares" else "mean of -log p", first, last))
     tokens = torch.arange(8, device="cuda")
+    if loss == "likelihood":
+        y = block.forward(tokens.repeat(block.L // 8), block.pairs(tokens.repeat(block.L // 8)))[:8]
+        ids, best = block.answer.likeliest(y, 3)
+        for t, row, p in zip(tokens.tolist(), ids.tolist(), best.exp().tolist()):
+            print("after %d: %s" % (t, ", ".join("%d (%.3f)" % x for x in zip(row, p))))
     out, scales = block.serve(tokens, block.pairs(tokens))
     print("8 tokens served: values %s %s, scales %s" % (tuple(out.shape), out.dtype, [round(float(s), 5) for s in scales[:, 0]]))
 

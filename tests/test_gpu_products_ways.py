@@ -224,3 +224,32 @@ def test_alternatives_of_pieces(rows, V, k, kind):
     # the sum is off by 2^-24 for each of the additions in a row, of which a thread, a wave and the pieces have few hundred, and 16 for the exponentials' arguments
     assert (np.abs(got[there] - wbest[there]) <= 1000 * U32 + 4 * U32 * np.abs(wbest[there])).all()
     assert bool((behind == 255).all())
+
+
+def test_the_way_out_of_the_example():
+    from paper_2101_11714_amd import token_block
+    vocab, L = 300, 96
+    answer = token_block.Answer(vocab, L, seed=3)
+    g = gen(6)
+    N = answer.head.shape[1]
+    y, following = rows_of(g, L, N, F32), torch.randint(0, vocab, (L,), generator=g).to(DEV)
+    lp = answer.forward(y, following)
+    x, head = y.double().cpu().requires_grad_(True), answer.head.double().cpu().requires_grad_(True)
+    want = torch.log_softmax(x @ head.t(), 1)[torch.arange(L), following.cpu()]
+    (-want.mean()).backward()
+    # logits of N products of about 1 / sqrt(N) and 1 are off by less than 2 N 2^-24, probabilities by that of themselves, and so are the gradients' terms; sums of L or vocab
+    off = 2 * (N + 40) * U32 * float((x.detach().abs() @ head.detach().abs().t()).max())
+    assert (lp.double().cpu() - want.detach()).abs().max() <= 2 * off + 16 * U32
+    g_y = answer.backward(y, following)
+    p = torch.softmax(x.detach() @ head.detach().t(), 1)
+    terms = (p + torch.nn.functional.one_hot(following.cpu(), vocab)) / L
+    for got, ref, mag in ((g_y, x.grad, terms @ head.detach().abs()), (answer.g_head, head.grad, terms.t() @ x.detach().abs())):
+        assert_within(got, ref.numpy(), (mag * (2 * off + 2 * (vocab + 30) * U32)).numpy(), "gradient")
+    ids, best = answer.likeliest(y[:7], 5)
+    ref = torch.log_softmax(x[:7].detach() @ head.detach().t(), 1)
+    assert (best.double().cpu() - ref.gather(1, ids.cpu())).abs().max() <= 2 * off + 16 * U32
+    assert (best[:, :-1] >= best[:, 1:]).all() and (ref.max(1).values - best[:, 0].double().cpu()).abs().max() <= 2 * off + 16 * U32
+    block, first, last = token_block.train(steps=12, vocab=200, L=512, loss="likelihood")
+    assert block.answer.logprob.isfinite().all() and block.answer.head.isfinite().all()
+    with pytest.raises(ValueError):
+        token_block.train(steps=1, loss="other")
