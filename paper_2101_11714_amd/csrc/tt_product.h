@@ -143,7 +143,7 @@ __device__ __forceinline__ void finish8(const EpilogueArgs &e, int64_t m, int64_
 
 // ---- tiles of operands in LDS -------------------------------------------------------------------------------------------
 //
-// A step takes 128 bytes of k, PB_K<T> values, or 64.  A matrix instruction 16 x 16 takes of each operand 16 bytes of k per lane from one
+// A step takes 128 bytes of k, PB_K<T> values.  A matrix instruction 16 x 16 takes of each operand 16 bytes of k per lane from one
 // of 16 rows (8 values of 16 bits: one instruction of k = 32; 4 of 32 bits: four of k = 4 whose k are not neighbours, the same
 // ones in both operands), so that 64 bytes are a "half".
 //   dense in k:   the tile is [rows][bytes of the step], read by 16 bytes per lane;
@@ -159,18 +159,18 @@ constexpr int PB_K = 128 / (int)sizeof(T);
 
 constexpr int BLOCK = 16;
 
-template <typename T, bool KDENSE, int ROWS, int HALVES>
+template <typename T, bool KDENSE, int ROWS>
 struct OperandTile {
     static constexpr int CH = 16 / sizeof(T);                // values of a chunk
-    static constexpr int LINE = KDENSE ? 4 * HALVES : ROWS / CH;             // chunks of a line
-    static constexpr int LINES = KDENSE ? ROWS : 4 * HALVES * CH;
+    static constexpr int LINE = KDENSE ? 8 : ROWS / CH;      // chunks of a line
+    static constexpr int LINES = KDENSE ? ROWS : 8 * CH;
     static constexpr int CHUNKS = LINE * LINES, BYTES = CHUNKS * 16;
     static_assert((LINE & (LINE - 1)) == 0, "a permutation of the line's chunks");
 
     // (transposed reads: 32 lanes read four lines each of two groups, eight lines apart)
     static __device__ __forceinline__ int swizzle(int line)
     {
-        const int x = KDENSE ? HALVES == 2 ? line & 7 : line >> 2 & 3 : sizeof(T) == 4 ? (line >> 2 & 3) << 2 : (line & 3) << 1 | (line & 8);
+        const int x = KDENSE ? line & 7 : sizeof(T) == 4 ? (line >> 2 & 3) << 2 : (line & 3) << 1 | (line & 8);
         return x & (LINE - 1);
     }
     // byte offset of a chunk
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(256) void join_parts_kernel(ProductArgs p, Epilogue
 template <typename T, bool KDENSE, int ROWS, int THREADS>
 struct Staged {
     static_assert(sizeof(T) == 4, "");
-    typedef OperandTile<T, KDENSE, ROWS, 2> Tile;
+    typedef OperandTile<T, KDENSE, ROWS> Tile;
     static constexpr int PIECES = Tile::CHUNKS / THREADS, CH = Tile::CH;
     static_assert(Tile::CHUNKS % THREADS == 0, "every thread has as many");
     typedef uint32_t Set __attribute__((ext_vector_type(4)));            // (PIECES of them: a step's values on their way)

@@ -21,7 +21,7 @@ struct StreamShape {
 template <typename T, bool KDENSE, bool WIDE>
 struct Stream {
     typedef StreamShape<WIDE> S;
-    typedef OperandTile<T, KDENSE, S::TILE, 2> Tile;
+    typedef OperandTile<T, KDENSE, S::TILE> Tile;
     static constexpr int PIECES = Tile::CHUNKS / S::THREADS, CH = Tile::CH;
     const char *base;            // of the step's values
     int64_t step;                // bytes to the next one's

@@ -13,8 +13,6 @@ from lm_util import f64
 ACTS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
 C, CUBE = math.sqrt(2 / math.pi), 0.044715
 
-_erf = np.vectorize(math.erf, otypes=[np.float64])
-
 
 def erf(z):
     return torch.erf(torch.from_numpy(np.ascontiguousarray(z))).numpy()
