@@ -517,19 +517,19 @@ struct Staged {
     }
 };
 
-// A tile of TM x 64 per workgroup of four waves below each other, operands through registers into LDS, so that every alignment and edge is right.  Three
+// A tile of TM x 64 per workgroup of four waves below each other (32 x 64: of two times two, of which two take each half of a step), operands through registers into LDS, so that every alignment and edge is right.  Three
 // steps' tiles of each operand in LDS: what a half of a step multiplies has been read from LDS in the half before, over the step's end, too; the step after
 // the next one is written, from what two steps ago was asked for.  (Two steps' tiles, read when they are multiplied, one step ahead: 256 x 1,024 x 1,024
 // 16.5 instead of 14.4 us, a step alone on its compute unit 0.98 instead of 0.60.)
 template <int TM>
 struct TileShape {
-    static constexpr int THREADS = 256, EACH = TM > 64 ? 2 : 3, STAGE = (TM + 64) * 128, LDS = 3 * STAGE;            // EACH: waves of a SIMD
+    static constexpr int THREADS = 256, EACH = TM > 64 ? 2 : TM > 32 ? 3 : 4, STAGE = (TM + 64) * 128, LDS = 3 * STAGE;            // EACH: waves of a SIMD
 };
 
 template <typename T, typename O, bool AK, bool BK, int TM>
 __device__ __forceinline__ void product_tile(const ProductArgs &p, const EpilogueArgs &e, int id, char *lds)
 {
-    constexpr int TN = 64, KB = PB_K<T>, BM = TM / 4 / BLOCK, BN = TN / BLOCK, SOME = BM;
+    constexpr int TN = 64, KB = PB_K<T>, KS = TM == 32 ? 2 : 1, BM = TM * KS / 4 / BLOCK, BN = TN / BLOCK, SOME = BM;
     typedef Staged<T, AK, TM, 256> SA;
     typedef Staged<T, BK, TN, 256> SB;
     constexpr int STAGE = TileShape<TM>::STAGE;
@@ -538,7 +538,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs &p, const Epilogu
     tile_of(id, p, tm, tn, part);
     const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * TN, k0 = part * p.k_part;
     const int64_t k_end = k0 + p.k_part < p.K ? k0 + p.k_part : p.K;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, wm = wave * (TM / 4);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, half = KS == 2 ? wave >> 1 : 0, wm = (KS == 2 ? wave & 1 : wave) * (BM * BLOCK);
     const SA a(p.a, p.lda, m0, p.M, p.K);
     const SB b(p.b, p.ldb, n0, p.N, p.K);
 
@@ -566,12 +566,12 @@ __device__ __forceinline__ void product_tile(const ProductArgs &p, const Epilogu
         b.template put<decltype(middle)::value>(sb[set], lds + stage * STAGE + SA::Tile::BYTES, k, k_end);
     };
     uint4 fa[2][BM], fb[2][BN];
-    auto read = [&](int stage, int h) {
+    auto read = [&](int stage, int h, int to) {
         const char *now = lds + stage * STAGE;
 #pragma unroll
-        for (int i = 0; i < BM; ++i) fa[h][i] = SA::Tile::fragment(now, wm, i, h, lane);
+        for (int i = 0; i < BM; ++i) fa[to][i] = SA::Tile::fragment(now, wm, i, h, lane);
 #pragma unroll
-        for (int j = 0; j < BN; ++j) fb[h][j] = SB::Tile::fragment(now + SA::Tile::BYTES, 0, j, h, lane);
+        for (int j = 0; j < BN; ++j) fb[to][j] = SB::Tile::fragment(now + SA::Tile::BYTES, 0, j, h, lane);
     };
     auto first = [&](auto middle) {
         fetch(middle, 0, k0);
@@ -584,20 +584,23 @@ __device__ __forceinline__ void product_tile(const ProductArgs &p, const Epilogu
     int stage = 0;
     auto after = [](int s, int n) { return s + n >= 3 ? s + n - 3 : s + n; };
     auto step = [&](auto middle, int set, int64_t k) {
-        read(stage, 1);
+        if (KS == 1) read(stage, 1, 1);
         put(middle, set, after(stage, 2), k + 2 * KB);
         fetch(middle, set, k + 4 * KB);
-        block_products<T>(fb[0], fa[0], acc);
         stage = after(stage, 1);
-        read(stage, 0);
-        block_products<T>(fb[1], fa[1], acc);
+        if (KS == 2) read(stage, half, set ^ 1);
+        block_products<T>(fb[KS == 1 ? 0 : set], fa[KS == 1 ? 0 : set], acc);
+        if (KS == 1) {
+            read(stage, 0, 0);
+            block_products<T>(fb[1], fa[1], acc);
+        }
         __syncthreads();
     };
     int64_t k = k0;
     if (k0 + 4 * KB <= inside) first(std::true_type{});
     else first(std::false_type{});
     __syncthreads();
-    read(0, 0);
+    read(0, half, 0);
     for (; k + 6 * KB <= inside; k += 2 * KB) {
         step(std::true_type{}, 0, k);
         step(std::true_type{}, 1, k + KB);
@@ -605,6 +608,16 @@ __device__ __forceinline__ void product_tile(const ProductArgs &p, const Epilogu
     for (; k < k_end; k += 2 * KB) {
         step(std::false_type{}, 0, k);
         if (k + KB < k_end) step(std::false_type{}, 1, k + KB);
+    }
+    if (KS == 2) {                                           // the second half's sums to the waves that have the first's
+        mfma_acc_t *other = reinterpret_cast<mfma_acc_t *>(lds + (wave & 1) * LEAVE_BLOCK) + lane;
+        if (half)
+#pragma unroll
+            for (int j = 0; j < BN; ++j) other[64 * j] = acc[0][j];
+        __syncthreads();
+        if (half) return;
+#pragma unroll
+        for (int j = 0; j < BN; ++j) acc[0][j] += other[64 * j];
     }
     leave_tile<T, O, BM, SOME, AK && BK>(p, e, part, m0 + wm, n0, lane, lds + wave * SOME * LEAVE_BLOCK, acc);
 }
@@ -638,7 +651,7 @@ __device__ __forceinline__ int which_of(const PairArgs &g, int64_t &id)
 }
 
 template <typename T, typename W, int TM>
-__global__ __launch_bounds__(256, TileShape<TM>::EACH) void pair_kernel(PairArgs g)
+__global__ __launch_bounds__(256, TM > 64 ? 2 : 3) /* (with four the smallest spills: 132 x 7,040 x 256 27 instead of 22 us) */ void pair_kernel(PairArgs g)
 {
     __shared__ __attribute__((aligned(16))) char lds[TileShape<TM>::LDS];
     int64_t id = workgroup();

@@ -35,6 +35,20 @@ inline ProductArgs args_of(const Product &x, const Plan &p)
 
 inline int64_t join_workgroups(const ProductArgs &q) { return q.parts > 1 ? ceil_div(q.M * (q.ld_part / 8), WG) : 0; }
 
+// calls f with the rows of a kind's tiles
+template <typename T, typename F>
+void with_kind(int kind, F f)
+{
+    if constexpr (sizeof(T) == 4) {
+        if (kind == 0) f(std::integral_constant<int, 128>{});
+        else if (kind == 1) f(std::integral_constant<int, 64>{});
+        else f(std::integral_constant<int, 32>{});
+    } else {
+        if (kind == 0) f(std::integral_constant<int, 256>{});
+        else f(std::integral_constant<int, 128>{});
+    }
+}
+
 // a kernel whose LDS is given with its launch
 template <auto KERNEL, typename... A>
 int launch_stream(dim3 grid, int threads, int lds, hipStream_t st, const A &...args)
@@ -78,11 +92,11 @@ int launch_product(Product x, hipStream_t st)
     const int kind = plan_of(&d, 1, sizeof(T) == 4 ? TT_F32 : TT_BF16, &p, us);
     const ProductArgs q = args_of(x, p);
     int rc = TT_OK;
-    with_flag(kind == 0, [&](auto large) {
-        constexpr bool LARGE = decltype(large)::value;
-        const dim3 grid = grid_of(p.tiles_m * p.tiles_n * p.parts, 512);
-        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((product_kernel<T, O, LARGE ? 128 : 64>), grid, dim3(WG), 0, st, q, x.e);
-        else rc = launch_stream<product_stream_kernel<T, O, LARGE>>(grid, StreamShape<LARGE>::THREADS, StreamShape<LARGE>::LDS, st, q, x.e);
+    const dim3 grid = grid_of(p.tiles_m * p.tiles_n * p.parts, 512);
+    with_kind<T>(kind, [&](auto size) {
+        constexpr int TILE = decltype(size)::value;
+        if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((product_kernel<T, O, TILE>), grid, dim3(WG), 0, st, q, x.e);
+        else rc = launch_stream<product_stream_kernel<T, O, TILE == 256>>(grid, StreamShape<TILE == 256>::THREADS, StreamShape<TILE == 256>::LDS, st, q, x.e);
     });
     if (rc) return rc;
     if (p.parts > 1) hipLaunchKernelGGL((join_parts_kernel<T, O>), grid_of(join_workgroups(q), WG), dim3(WG), 0, st, q, x.e);
@@ -99,12 +113,12 @@ int launch_gradients(Product dx, Product dw, const BiasSum &b, hipStream_t st)
     const int kind = plan_of(d, 2, sizeof(T) == 4 ? TT_F32 : TT_BF16, p, us);
     PairArgs g{{args_of(dx, p[0]), args_of(dw, p[1])}, {dx.e, dw.e}, p[1].k_part > p[0].k_part, {p[0].tiles_m * p[0].tiles_n * p[0].parts, p[1].tiles_m * p[1].tiles_n * p[1].parts}};
     int rc = TT_OK;
+    const dim3 grid = grid_of(g.wgs[0] + g.wgs[1], 512);
     if (g.wgs[0] + g.wgs[1] > 0)
-        with_flag(kind == 0, [&](auto large) {
-            constexpr bool LARGE = decltype(large)::value;
-            const dim3 grid = grid_of(g.wgs[0] + g.wgs[1], 512);
-            if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((pair_kernel<T, W, LARGE ? 128 : 64>), grid, dim3(WG), 0, st, g);
-            else rc = launch_stream<pair_stream_kernel<T, W, LARGE>>(grid, StreamShape<LARGE>::THREADS, StreamShape<LARGE>::LDS, st, g);
+        with_kind<T>(kind, [&](auto size) {
+            constexpr int TILE = decltype(size)::value;
+            if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((pair_kernel<T, W, TILE>), grid, dim3(WG), 0, st, g);
+            else rc = launch_stream<pair_stream_kernel<T, W, TILE == 256>>(grid, StreamShape<TILE == 256>::THREADS, StreamShape<TILE == 256>::LDS, st, g);
         });
     if (rc) return rc;
     const int64_t wgs0 = g.wgs[0] ? join_workgroups(g.p[0]) : 0, wgs1 = g.wgs[1] ? join_workgroups(g.p[1]) : 0, all = wgs0 + wgs1 + (b.part ? ceil_div(b.N, 32) : 0);

@@ -23,15 +23,15 @@ constexpr int64_t MOST_TILES = 512;                          // workgroups that 
 // Kinds of tiles, and what a step of 128 bytes of k takes, in us, as measured on 256 compute units.
 // 16 bits.  256 x 256, one on a compute unit: 1.87 (8,192 x 16,384 x 4,096: 1,127 TFLOP/s).  128 x 128: 0.70 alone on its compute unit and 1.17 beside another
 // one (2,048 x 2,048 x 4,096, one tile each: 48 us, by the others in four parts 41 and the parts' sums 15; 8,192 x 4,096 x 4,096: 293, by the others 221).
-// 32 bits.  128 x 64 takes 1.13 of a compute unit and 64 x 64 0.60, alone or beside others (2,048^3 152 and 158 us, 4,096^3 1,075 and 1,128; 256 x 1,024 x
-// 1,024 24 us as 64 small tiles, in four parts 14).
+// 32 bits.  128 x 64 takes 1.13 of a compute unit, 64 x 64 0.60 and 32 x 64 0.32, alone or beside others (2,048^3 149, 148 and 152 us; 512^3 14.7, 14.7 and 10.1,
+// 1,001 x 777 x 1,283 41, 37 and 32, 1,024 x 4,096 x 4,096 280, 280 and 291; 256 x 1,024 x 1,024 24 us as 64 tiles of 64 x 64, in four parts 15).
 struct TileKind {
     int64_t m, n, room;          // room: how many tiles run together
     double step, alone;
 };
-constexpr TileKind KINDS[2][2] = {{{128, 64, 256, 1.13, 1.13}, {64, 64, 256, 0.60, 0.60}}, {{256, 256, 256, 1.87, 1.87}, {128, 128, 512, 1.17, 0.70}}};
+constexpr TileKind KINDS[2][3] = {{{128, 64, 256, 1.13, 1.13}, {64, 64, 256, 0.60, 0.60}, {32, 64, 256, 0.32, 0.32}}, {{256, 256, 256, 1.87, 1.87}, {128, 128, 512, 1.17, 0.70}, {}}};
 
-// Which kind (large: 0) and how many parts of each of n products that run together: whatever should be done first.  Parts cost a launch, and their sums
+// Which kind and how many parts of each of n products that run together: whatever should be done first.  Parts cost a launch, and their sums
 // a write and a read.
 inline int plan_of(const Size *d, int n, int32_t type, Plan *p, double &best)
 {
@@ -39,7 +39,7 @@ inline int plan_of(const Size *d, int n, int32_t type, Plan *p, double &best)
     const bool f32 = type == TT_F32;
     int best_kind = 0;
     best = 0;
-    for (int kind = 0; kind < 2; ++kind) {
+    for (int kind = 0; kind < (f32 ? 3 : 2); ++kind) {
         const TileKind &t = KINDS[!f32][kind];
         const int64_t most = f32 ? 2 * MOST_TILES : t.room;
         int64_t tiles[2] = {}, steps[2] = {};
@@ -65,6 +65,7 @@ inline int plan_of(const Size *d, int n, int32_t type, Plan *p, double &best)
                     joins |= parts[i] > 1;
                 }
                 if (joins) us += f32 ? 6.0 : 3.0;
+                if (n == 2 && kind == 2) us *= 1.15;         // (gradients' operands: 354 x 4,096 x 4,480 294 us, by larger tiles 270)
                 if (wgs <= 256) {
                     us += t.alone * (double)longest;
                 } else if (n == 1 || shortest == longest) {
