@@ -14,12 +14,15 @@ struct SlopeArgs {
     int64_t ld_dy, ld_pre, ld_dz;
     int64_t rows, band;          // rows of a band
     int N, nv, act;
+    int groups;                  // workgroups of a band; those behind them copy the products' other operands
 };
 
 // 32 vectors of eight columns x 8 rows per workgroup at a time, down a band of rows; bound by memory (8,192 x 4,096 in 16 bits with SiLU 45 us, 4.5 TB/s).
 template <typename T, bool WHOLE, bool ACT>
-__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a)
+__global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, PackArgs p)
 {
+    if constexpr (sizeof(T) == 2)
+        if ((int)blockIdx.x >= a.groups) return pack_rows<T>(p, (int64_t)(blockIdx.x - a.groups) * gridDim.y + blockIdx.y);
     __shared__ float sums[8][32][8];
     const int v = blockIdx.x * 32 + (threadIdx.x & 31), lane_row = threadIdx.x >> 5;
     const int n = a.N - 8 * v;

@@ -161,37 +161,11 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
     int64_t ld_dz = grad_output->ld;
     char *const at_dz = ws + room.parts_x + room.parts_w, *const at_x = at_dz + room.dz, *const at_w = at_x + room.x;
     BiasSum bias{nullptr, grad_bias, grad_bias_type, accumulate, (int)room.n_bands, (int)N, (int)(8 * ceil_div(N, 8))};
-    if (N > 0 && (room.dz || grad_bias) && n_rows > 0) {
-        SlopeArgs a{};
-        a.dy = grad_output->data;
-        a.ld_dy = grad_output->ld;
-        if (activation != TT_ACT_NONE) {
-            a.pre = pre->data;
-            a.ld_pre = pre->ld;
-        }
-        a.N = (int)N;
-        a.nv = (int)ceil_div(N, 8);
-        if (room.dz) {
-            a.dz = at_dz;
-            a.ld_dz = 8 * a.nv;
-            dz = a.dz;
-            ld_dz = a.ld_dz;
-        }
-        if (room.bands) bias.part = a.part = (float *)(at_w + room.w);
-        else a.one = bias;
-        a.rows = n_rows;
-        a.band = room.band;
-        a.act = activation;
-        with_type(type, [&](auto t) {
-            with_whole(N, [&](auto whole) {
-                with_flag(activation != TT_ACT_NONE, [&](auto act) {
-                    hipLaunchKernelGGL((slope_kernel<decltype(t), decltype(whole)::value, decltype(act)::value>), dim3((unsigned)ceil_div(a.nv, 32), (unsigned)room.n_bands), dim3(WG), 0, st, a);
-                });
-            });
-        });
-        if ((rc = launched("gradient launch"))) return rc;
-    }
     if (grad_bias && n_rows == 0) bias.part = (const float *)grad_bias;          // (no bands: nothing of it is read)
+    if (room.dz) {
+        dz = at_dz;
+        ld_dz = 8 * ceil_div(N, 8);
+    }
     Product dx{}, dw{};
     if (grad_x) {
         dx.a = {dz, ld_dz, n_rows, N, nullptr};
@@ -212,6 +186,38 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
             dw.e.ld_add = dw.e.ld_out;
         }
         dw.parts = (float *)(ws + room.parts_x);
+    }
+    if (N > 0 && (room.dz || grad_bias) && n_rows > 0) {
+        SlopeArgs a{};
+        a.dy = grad_output->data;
+        a.ld_dy = grad_output->ld;
+        if (activation != TT_ACT_NONE) {
+            a.pre = pre->data;
+            a.ld_pre = pre->ld;
+        }
+        a.N = (int)N;
+        a.nv = (int)ceil_div(N, 8);
+        a.groups = (int)ceil_div(a.nv, 32);
+        if (room.dz) {
+            a.dz = at_dz;
+            a.ld_dz = ld_dz;
+        }
+        if (room.bands) bias.part = a.part = (float *)(at_w + room.w);
+        else a.one = bias;
+        a.rows = n_rows;
+        a.band = room.band;
+        a.act = activation;
+        int64_t copies;
+        const PackArgs pack = pack_args(dx.b, dw.b, copies);
+        const dim3 grid((unsigned)(a.groups + ceil_div(copies, room.n_bands)), (unsigned)room.n_bands);
+        with_type(type, [&](auto t) {
+            with_whole(N, [&](auto whole) {
+                with_flag(activation != TT_ACT_NONE, [&](auto act) {
+                    hipLaunchKernelGGL((slope_kernel<decltype(t), decltype(whole)::value, decltype(act)::value>), grid, dim3(WG), 0, st, a, pack);
+                });
+            });
+        });
+        if ((rc = launched("gradient launch"))) return rc;
     }
     with_type(type, [&](auto t) { rc = gradients_of<decltype(t)>(grad_weight ? grad_weight->type : type, dx, dw, bias, st); });
     return rc;

@@ -304,11 +304,11 @@ struct PackArgs {
 constexpr int PACK_U = 4;
 
 template <typename T>
-__global__ __launch_bounds__(256) void pack_kernel(PackArgs p)
+__device__ __forceinline__ void pack_rows(const PackArgs &p, int64_t id)
 {
     const int64_t first_wgs = (p.chunks[0] + 256 * PACK_U - 1) / (256 * PACK_U);
-    const int which = workgroup() >= first_wgs;
-    const int64_t base = (workgroup() - (which ? first_wgs : 0)) * 256 * PACK_U, left = p.chunks[which] - base;
+    const int which = id >= first_wgs;
+    const int64_t base = (id - (which ? first_wgs : 0)) * 256 * PACK_U, left = p.chunks[which] - base;
     if (left <= 0) return;
     const int64_t row0 = base / p.row[which], columns = p.columns[which];
     const uint32_t per = (uint32_t)p.row[which], rest = (uint32_t)(base - row0 * per) + threadIdx.x;
@@ -324,6 +324,12 @@ __global__ __launch_bounds__(256) void pack_kernel(PackArgs p)
 #pragma unroll
     for (int u = 0; u < PACK_U; ++u)
         if ((int64_t)threadIdx.x + u * 256 < left) reinterpret_cast<uint4 *>(p.to[which])[base + threadIdx.x + u * 256] = x[u].get(c[u], columns);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void pack_kernel(PackArgs p)
+{
+    pack_rows<T>(p, workgroup());
 }
 
 struct ProductArgs {

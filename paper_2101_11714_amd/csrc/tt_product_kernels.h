@@ -5,26 +5,11 @@
 
 namespace tt {
 
-// copies the operands that are to be copied
 template <typename T>
 void pack(Operand &a, Operand &b, hipStream_t st)
 {
-    PackArgs q{};
-    int64_t wgs = 0;
-    auto add = [&](int i, Operand &o) {
-        if (!o.packed || o.rows == 0 || o.columns == 0) return;
-        q.from[i] = o.data;
-        q.to[i] = o.packed;
-        q.ld[i] = o.ld;
-        q.columns[i] = o.columns;
-        q.row[i] = (int)ceil_div(o.columns, 8);
-        q.chunks[i] = o.rows * q.row[i];
-        wgs += ceil_div(q.chunks[i], WG * PACK_U);
-        o.data = o.packed;
-        o.ld = 8 * q.row[i];
-    };
-    add(0, a);
-    add(1, b);
+    int64_t wgs;
+    const PackArgs q = pack_args(a, b, wgs);
     if (wgs) hipLaunchKernelGGL((pack_kernel<T>), grid_of(wgs, WG), dim3(WG), 0, st, q);
 }
 

@@ -140,6 +140,29 @@ struct Operand {
     void *packed;
 };
 
+// what copies the operands that are to be copied, by so many workgroups; the operands then are the copies
+inline PackArgs pack_args(Operand &a, Operand &b, int64_t &workgroups)
+{
+    PackArgs q{};
+    workgroups = 0;
+    auto add = [&](int i, Operand &o) {
+        if (!o.packed || o.rows == 0 || o.columns == 0) return;
+        q.from[i] = o.data;
+        q.to[i] = o.packed;
+        q.ld[i] = o.ld;
+        q.columns[i] = o.columns;
+        q.row[i] = (int)ceil_div(o.columns, 8);
+        q.chunks[i] = o.rows * q.row[i];
+        workgroups += ceil_div(q.chunks[i], WG * PACK_U);
+        o.data = o.packed;
+        o.ld = 8 * q.row[i];
+        o.packed = nullptr;
+    };
+    add(0, a);
+    add(1, b);
+    return q;
+}
+
 // A product: A and B (null: there is none), and what is done with its sums; parts: room for the parts' ones.
 struct Product {
     Operand a, b;
