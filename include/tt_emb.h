@@ -719,7 +719,7 @@ enum {
  * z = x weight^T + bias,  output = act(z) + residual:  x [n_rows][K], weight [N][K] (a token table as the way out among them), output,
  * residual and pre [n_rows][N].
  * bias: N values of any type, NULL for none.  residual: NULL for none.  pre: z, stored for the gradient (NULL: not).
- * Types: weight and pre x's; output x's or 32 bits; residual the output's.  output may be residual, at the same stride.
+ * Types: weight and pre x's; output x's or 32 bits; residual the output's.  output may be residual, at the same stride; else neither output nor pre may overlap another array.
  * workspace: tt_linear_fwd_workspace_bytes(n_rows, K, N, x's type, whole) bytes, 16-byte aligned (0: none is needed; enough for fewer rows too).
  * whole != 0: x and the weight have K and strides of multiples of 8 (strides up to 2^22) and 16-byte aligned addresses, or 32 bits; others may be copied.
  * K and N up to 2^22.  K == 0 is valid: z = bias.

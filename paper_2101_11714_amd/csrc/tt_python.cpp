@@ -957,7 +957,7 @@ TT_FUNCTION(linear_fwd)
     const void *b = g.vector_or_null(3, N, &bt);
     const int64_t act = g.integer(4);
     void *ws = g.bytes_or_null(7, &wsb);
-    for (int i : {0, 1, 2, 3, 5, 6}) g.here(i);
+    for (int i : {0, 1, 2, 3, 5, 6, 7}) g.here(i);
     if (!g.ok) return nullptr;
     const Room room(ws, wsb, tt_linear_fwd_workspace_bytes(n, K, N, x.type, whole_chunks(K, {&x, &w})));
     return call([&](void *st) { return tt_linear_fwd(&x, &w, b, bt, (int32_t)act, r, p, o, n, K, N, room.data, room.bytes, st); });
@@ -987,7 +987,7 @@ TT_FUNCTION(linear_bwd)
     void *gb = g.vector_or_null(7, N, &bt);
     const bool add = g.truth(8);
     void *ws = g.bytes_or_null(9, &wsb);
-    for (int i : {0, 1, 2, 3, 5, 6, 7}) g.here(i);
+    for (int i : {0, 1, 2, 3, 5, 6, 7, 9}) g.here(i);
     if (!g.ok) return nullptr;
     if (K < 0) K = 0;
     const Room room(ws, wsb, tt_linear_bwd_workspace_bytes(n, K, N, go.type, (int32_t)act, whole_chunks(K | N, {&go, x, w})));
@@ -1032,7 +1032,7 @@ TT_FUNCTION(qk_norm_rotate_bwd)
     const float eps = g.real(12);
     const bool add = g.truth(13);
     void *ws = g.bytes_or_null(14, &wsb);
-    for (int i : {0, 1, 2, 3, 4, 5, 8, 9, 10, 11}) g.here(i);
+    for (int i : {0, 1, 2, 3, 4, 5, 8, 9, 10, 11, 14}) g.here(i);
     if (!g.ok) return nullptr;
     const Room room(ws, wsb, gqw || gkw ? tt_qk_norm_rotate_bwd_workspace_bytes(n, pgqo ? gqo.heads : 0, pgko ? gko.heads : 0, D) : 0);
     return call([&](void *st) {
@@ -1064,7 +1064,7 @@ TT_FUNCTION(token_logprob_fwd)
     float *top = g.f32_or_null(6, &nt);
     const float scale = g.real(7);
     void *ws = g.bytes_or_null(8, &wsb);
-    for (int i = 0; i < 7; ++i) g.here(i);
+    for (int i : {0, 1, 2, 3, 4, 5, 6, 8}) g.here(i);
     if (g.ok && ((args[2] != Py_None && nl != n) || (args[3] != Py_None && ns != n) || (args[4] != Py_None && ne != n))) g.fail("logprob, lse and entropy have one value per row");
     if (g.ok && (k > 64 || ni != n * k || (args[6] != Py_None && nt != ni))) g.fail("top_ids and top_logprobs are [rows, k], k up to 64");
     if (!g.ok) return nullptr;
