@@ -48,7 +48,8 @@ struct Stream {
     }
     // The next step's tile; `left`: its values of k that exist.  Behind the last ones zeros are loaded, so that the number of loads does not depend on
     // it.  In assembly, since the compiler takes every read of LDS for one of what is still on its way and waits for it; nothing but LDS and M0 is
-    // written, which nothing else here uses, and the waits are landed()'s.
+    // written, which nothing else here uses, and the waits are landed()'s.  A load into LDS reads M0 a wait state after it is written at the earliest, which
+    // the compiler sees to around its own instructions and not in here: the s_nop.
     __device__ __forceinline__ void load(char *lds, int left)
     {
         typedef uint32_t Words __attribute__((ext_vector_type(4)));
@@ -58,7 +59,7 @@ struct Stream {
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
             const uint32_t o = k[i] < left ? at[i] : PS_NOWHERE;
-            asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * S::WAVES * 1024), "v"(o), "s"(r) : "memory");
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to + i * S::WAVES * 1024), "v"(o), "s"(r) : "memory");
         }
         base += step;
     }
