@@ -367,7 +367,7 @@ __global__ __launch_bounds__(WG) void logprob_bwd_kernel(LogprobGradArgs a)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const float l = fmaf(x[j], a.scale, -lse), p = __builtin_amdgcn_exp2f(l * LOG2E);
-            float d = -p * (g + (ge != 0.f ? ge * (l + h) : 0.f));
+            float d = -p * (g + (ge != 0.f && p != 0.f ? ge * (l + h) : 0.f));       // (p log p is 0 where p is, however large the log: masks of a type's lowest value)
             if (8 * v + j == token) d += g;
             x[j] = none || x[j] == -INFINITY ? 0.f : d * a.scale;
         }
