@@ -801,7 +801,7 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
  * Log probabilities of tokens under z = scale * logits (0 < scale <= 1e30), logits [n_rows][V] of 32 or 16 bits:
  *   lse[r] = log(sum over the row of exp(z)),  logprob[r] = z[r][token r] - lse[r],  entropy[r] = lse[r] - sum of exp(z - lse) z.
  * A logit of -inf has no probability and adds nothing.  A row of nothing else: lse and logprob -inf, entropy 0.  A row with a NaN or +inf: NaN in
- * all three.  A token outside [0, V) is no token: its logprob is 0.  tokens->L == n_rows.
+ * all three.  An lse that 32 bits do not hold is infinite; nothing else is taken from it.  A token outside [0, V) is no token: its logprob is 0.  tokens->L == n_rows.
  * lse, logprob, entropy: fp32 [n_rows]; any of them may be NULL, and tokens if logprob is.
  * k > 0: the k likeliest columns, equal ones by their number (NaN before all others), ids [n_rows][k] of 32 or 64 bits and their log probabilities
  * fp32 [n_rows][k] (NULL: not wanted); columns of logit -inf are no alternatives, and places for which there is none get -1 and -inf.
@@ -815,7 +815,10 @@ int tt_token_logprob_fwd(const tt_rows_t *logits, const tt_tokens_t *tokens, flo
 
 /*
  * grad_logits = scale (g (1[column = token] - p) - ge p (log p + entropy)),  p = exp(z - lse), with g = grad_logprob[r] (0 for a row without a token;
- * NULL: 0) and ge = grad_entropy[r] (NULL: 0; else entropy is needed).  Columns of logit -inf, and rows whose lse is -inf, have no gradient (0).
+ * NULL: 0) and ge = grad_entropy[r] (NULL: 0; else entropy is needed).  Columns of logit -inf, and rows of nothing else, have no gradient (0).
+ * An lse over 2^12 in size, infinite ones among them, has lost some of the row's sum, or all of it (rows of a type's lowest value).  Where it is what the
+ * row's logits give, p is taken from these instead, and is as exact as in other rows; where it is not (the lse of more columns than the row has) it is
+ * taken as it is, and a row whose lse then is -inf has no gradient.
  * grad_logits: the logits' type; it may be logits.
  */
 int tt_token_logprob_bwd(const tt_rows_t *logits, const tt_tokens_t *tokens, float scale, const float *lse, const float *entropy,

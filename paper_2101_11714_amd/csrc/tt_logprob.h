@@ -125,9 +125,10 @@ __device__ __forceinline__ void leave_top(const LogprobArgs &a, int64_t row, int
     if (a.top) a.top[at] = key ? a.scale * (value_of((uint32_t)(key >> 32)) - m) - log_s : -INFINITY;
 }
 
-// the vectors [from, to) of a row, U of a thread's at a time: f(vector's number, its eight logits), -inf where there is no column
-template <typename T, bool WHOLE, int U, typename F>
-__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
+// the vectors [from, to) of a row, U of a thread's at a time: f(vector's number, its eight logits), -inf where there is no column.
+// go(): whether to go on, asked when U loads are on their way.
+template <typename T, bool WHOLE, int U, typename F, typename G>
+__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f, G go)
 {
 #pragma unroll 1
     for (int v0 = from + threadIdx.x; v0 < to; v0 += WG * U) {
@@ -138,6 +139,7 @@ __device__ __forceinline__ void each_vector(const T *line, int from, int to, int
             r[i] = fetch8<WHOLE>(line + 8 * (int64_t)v, V - 8 * v, V);
         }
         __builtin_amdgcn_sched_barrier(0);                   // (or the compiler loads them one after the other)
+        if (!go()) return;
 #pragma unroll
         for (int i = 0; i < U; ++i) {
             const int v = v0 + i * WG;
@@ -151,6 +153,54 @@ __device__ __forceinline__ void each_vector(const T *line, int from, int to, int
             f(v, x);
         }
     }
+}
+
+template <typename T, bool WHOLE, int U, typename F>
+__device__ __forceinline__ void each_vector(const T *line, int from, int to, int V, F f)
+{
+    each_vector<T, WHOLE, U>(line, from, to, V, f, [] { return true; });
+}
+
+// a thread's sums over its vectors of [from, to)
+template <typename T, bool ENTROPY, bool WHOLE, int U = LP_UNROLL>
+__device__ __forceinline__ Sums thread_sums(const T *line, int from, int to, int V, float c)
+{
+    Sums r{LP_LEAST, 0.f, 0.f};
+    each_vector<T, WHOLE, U>(line, from, to, V, [&](int v, const float (&x)[8]) {
+        float m = r.m;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
+        if (m > r.m) {
+            const float d = fmaxf(r.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
+            if (ENTROPY) r.t = f == 0.f ? 0.f : f * (r.t + d * r.s);
+            r.s *= f;
+            r.m = m;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * c);
+            r.s += e;
+            if (ENTROPY) r.t += e * fmaxf(d, LP_LEAST);
+        }
+    });
+    return r;
+}
+
+// the workgroup's, in every thread
+__device__ __forceinline__ Sums workgroup_sums(Sums r, Sums *waves, float c)
+{
+    r = joined(r, c);
+    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = r;
+    __syncthreads();
+    r.m = fmaxf(fmaxf(waves[0].m, waves[1].m), fmaxf(waves[2].m, waves[3].m));
+    r.s = r.t = 0.f;
+#pragma unroll
+    for (int w = 0; w < NWAVE; ++w) {
+        const Sums o = about(waves[w], r.m, c);
+        r.s += o.s;
+        r.t += o.t;
+    }
+    return r;
 }
 
 // The workgroup's k largest keys into out[0 .. k), 0 where there are fewer.  order: of the thread's largest logit (or of a smaller one of its own), 0
@@ -228,38 +278,11 @@ __global__ __launch_bounds__(WG) void logprob_kernel(LogprobArgs a)
     const float c = a.scale * LOG2E;
     Given given{0.f, false};
     if (a.pieces == 1 && threadIdx.x == 0) given = given_logit<T>(a, row);
-    Sums r{LP_LEAST, 0.f, 0.f};
-    each_vector<T, WHOLE, LP_UNROLL>(line, from, to, a.V, [&](int v, const float (&x)[8]) {
-        float m = r.m;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
-        if (m > r.m) {
-            const float d = fmaxf(r.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
-            if (ENTROPY) r.t = f == 0.f ? 0.f : f * (r.t + d * r.s);
-            r.s *= f;
-            r.m = m;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * c);
-            r.s += e;
-            if (ENTROPY) r.t += e * fmaxf(d, LP_LEAST);
-        }
-    });
+    Sums r = thread_sums<T, ENTROPY, WHOLE>(line, from, to, a.V, c);
     // a sum that is no number: a NaN among the logits, or an infinity (and maybe a NaN beside it)
     const bool odd = r.s != r.s;
     const uint32_t order = r.s == 0.f ? 0u : odd && r.m != INFINITY ? 0xffffffffu : order_of(r.m);
-    r = joined(r, c);
-    if ((threadIdx.x & 63) == 0) waves[threadIdx.x >> 6] = r;
-    __syncthreads();
-    r.m = fmaxf(fmaxf(waves[0].m, waves[1].m), fmaxf(waves[2].m, waves[3].m));
-    r.s = r.t = 0.f;
-#pragma unroll
-    for (int w = 0; w < NWAVE; ++w) {
-        const Sums o = about(waves[w], r.m, c);
-        r.s += o.s;
-        r.t += o.t;
-    }
+    r = workgroup_sums(r, waves, c);
     if (TOP) largest_keys<T, WHOLE>(line, from, to, a.V, a.k, order, odd, list, &count, &least, found);
     if (a.pieces > 1) {
         if (threadIdx.x == 0) *reinterpret_cast<float4 *>(a.sums + id * 4) = make_float4(r.m, r.s, r.t, 0.f);
@@ -350,29 +373,47 @@ struct LogprobGradArgs {
     float scale;
 };
 
+// An lse beyond LP_FAR has lost 2^-12 of the sum that it holds, or more, and all of it where the row has nothing but its type's lowest value (which under a
+// scale above 1 make it -inf).  There the row's first workgroup takes all of the row: it finds the largest logit and the sum once more and goes by these, if
+// they are what the lse was made of; an lse of more columns than the row has is taken as it is.  The row's other workgroups do nothing, since out may be
+// the logits, which are read as a whole before the first of them is written (4,096 x 50,257 in bfloat16 148 us, with a tenth of the rows of lowest values 178, with half of them 235).
+constexpr float LP_FAR = 4096.f;
+
 template <typename T, bool WHOLE>
 __global__ __launch_bounds__(WG) void logprob_bwd_kernel(LogprobGradArgs a)
 {
+    __shared__ Sums waves[NWAVE];
     const int64_t id = workgroup(), row = id / a.pieces;
     if (row >= a.rows) return;
-    const int from = (int)(id - row * a.pieces) * a.piece, to = min(from + a.piece, a.nv);
+    const int piece = (int)(id - row * a.pieces), from = piece * a.piece, to = min(from + a.piece, a.nv);
     const T *line = (const T *)a.logits + row * a.ld;
     T *out = (T *)a.out + row * a.ld_out;
+    // (what a row has is loaded together, whether it is there or not: one after the other they took as long as a short row's logits)
+    const float lse = a.lse[row], at_g = (a.g ? a.g : a.lse)[row], at_ge = (a.ge ? a.ge : a.lse)[row], at_h = (a.ge ? a.entropy : a.lse)[row];
     int64_t token = -1;
     if (a.tokens && a.g) token = a.tokens64 ? ((const int64_t *)a.tokens)[row] : ((const int32_t *)a.tokens)[row];
     if (token < 0 || token >= a.V) token = -1;
-    const float g = token >= 0 ? a.g[row] : 0.f, ge = a.ge ? a.ge[row] : 0.f, h = a.ge ? a.entropy[row] : 0.f, lse = a.lse[row];
-    const bool none = lse == -INFINITY;
-    each_vector<T, WHOLE, LP_UNROLL>(line, from, to, a.V, [&](int v, float (&x)[8]) {
+    const float g = token >= 0 ? at_g : 0.f, ge = a.ge ? at_ge : 0.f, h = a.ge ? at_h : 0.f;
+    // log p = scale (logit - m) - log_s
+    auto leave = [&](int v, float (&x)[8], float m, float log_s, bool none) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float l = fmaf(x[j], a.scale, -lse), p = __builtin_amdgcn_exp2f(l * LOG2E);
+            const float l = fmaf(x[j] - m, a.scale, -log_s), p = __builtin_amdgcn_exp2f(l * LOG2E);
             float d = -p * (g + (ge != 0.f && p != 0.f ? ge * (l + h) : 0.f));       // (p log p is 0 where p is, however large the log: masks of a type's lowest value)
             if (8 * v + j == token) d += g;
             x[j] = none || x[j] == -INFINITY ? 0.f : d * a.scale;
         }
         put8<WHOLE>(out + 8 * (int64_t)v, a.V - 8 * v, x);
-    });
+    };
+    const bool far = fabsf(lse) > LP_FAR;
+    each_vector<T, WHOLE, LP_UNROLL>(line, from, to, a.V, [&](int v, float (&x)[8]) { leave(v, x, 0.f, lse, false); }, [&] { return !far; });
+    if (!far || piece) return;
+    const float c = a.scale * LOG2E;
+    const Sums r = workgroup_sums(thread_sums<T, false, WHOLE, 1>(line, 0, a.nv, a.V, c), waves, c);
+    const float log_r = logf(r.s), own = r.m * a.scale + log_r;
+    const bool same = r.s > 0.f && (own == lse || fabsf(own - lse) <= fabsf(lse) * 0x1p-22f);            // (sums in another order: a unit of the last place)
+    const float m = same ? r.m : 0.f, log_s = same ? log_r : lse;
+    each_vector<T, WHOLE, 1>(line, 0, a.nv, a.V, [&](int v, float (&x)[8]) { leave(v, x, m, log_s, !same && lse == -INFINITY); });
 }
 
 }  // namespace tt

@@ -100,3 +100,76 @@ def test_columns_of_the_lowest_value_have_no_gradient_of_the_entropy(rows, V, ty
         want, off = Rows(x, scale).gradient(tokens, g, ge)
         got, _, _, _ = run(x, tokens, g, ge, scale, in_place)
         assert_within(got, want, off + UNIT[type] * (np.abs(want) + off) + TINY[type], (scale, in_place))
+
+
+def special_rows(gr, V, type):
+    """Rows whose lse has lost the logarithm of the sum, or is no finite number, and others between them."""
+    low, high = torch.finfo(type).min, torch.finfo(type).max
+    x = torch.randn((11, V), generator=gr) * 2
+    x[0] = low
+    x[1] = low
+    x[1, ::2] = -math.inf
+    x[1, -1] = low
+    x[2] = low
+    x[2, V // 3] = low / 2
+    x[3] += 30000.0                                          # (values as the type holds them)
+    x[4] = high
+    x[5] = -math.inf
+    x[7] = -math.inf
+    x[7, V // 2] = low
+    x[8] = -x[3]
+    x[9] = high
+    x[9, V // 2:] = low
+    return x.to(type).to(DEV)
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 64, 1000, 4097, 8192, 50257])
+@pytest.mark.parametrize("type", TYPES)
+def test_rows_of_the_lowest_value_have_even_probabilities(V, type):
+    gr = gen(V)
+    for scale, in_place in [(1.0, False), (1.3, False), (1.3, True), (0.7, True), (100.0, False)]:
+        scale = float(np.float32(scale))
+        x = special_rows(gr, V, type)
+        rows = x.shape[0]
+        tokens = torch.randint(0, V, (rows,), generator=gr).to(DEV)
+        tokens[0] = 0
+        g, ge = (torch.randn(rows, generator=gr).to(DEV) * 4 for _ in range(2))
+        r = Rows(x, scale)
+        want, off = r.gradient(tokens, g, ge)
+        got, _, lse, ent = run(x, tokens, g, ge, scale, in_place)
+        assert_within(got, want, off + UNIT[type] * (np.abs(want) + off) + TINY[type], (scale, in_place))
+        assert (np.abs(f64(ent) - r.entropy) <= r.entropy_bound()).all()
+
+
+@pytest.mark.parametrize("type", TYPES)
+def test_many_rows_of_the_lowest_value(type):
+    # as in a padded batch: half of the rows, each beside another one's pieces
+    gr, rows, V = gen(1), 400, 9001
+    x = rows_of(gr, rows, V, type, 0, 0, 2.0)
+    x[::2] = torch.finfo(type).min
+    x[::8] = -math.inf
+    tokens = torch.randint(0, V, (rows,), generator=gr).to(DEV)
+    g, ge = (torch.randn(rows, generator=gr).to(DEV) for _ in range(2))
+    want, off = Rows(x, 1.0).gradient(tokens, g, ge)
+    first, _, _, _ = run(x, tokens, g, ge, 1.0, False)
+    got, _, _, _ = run(x, tokens, g, ge, 1.0, True)
+    assert_within(got, want, off + UNIT[type] * (np.abs(want) + off) + TINY[type], "in place")
+    assert torch.equal(first, got)
+
+
+def test_an_lse_of_more_columns_than_the_row_has_is_taken_as_it_is():
+    # halves of a vocabulary: p = exp(z - lse) with the lse of both
+    gr, rows, V = gen(2), 12, 3001
+    for offset, scale in [(0.0, 1.0), (20000.0, 1.0), (-30000.0, 1.3)]:
+        scale = float(np.float32(scale))
+        x = (torch.randn((rows, 2 * V), generator=gr) * 2 + offset).to(DEV)
+        tokens = torch.randint(0, V, (rows,), generator=gr).to(DEV)
+        g, ge = torch.randn(rows, generator=gr).to(DEV), torch.zeros(rows, device=DEV)
+        whole = Rows(x, scale)
+        lse = torch.from_numpy(whole.lse).float().to(DEV)
+        out, _, _, _ = run(x[:, :V].contiguous(), tokens, g, ge, scale, False, lse)
+        want, off = whole.gradient(tokens, g, ge)
+        want, off = want[:, :V], off[:, :V]
+        # (what the lse has lost as it is stored, and as much again for the product that it is taken from)
+        off = off + 2 * U32 * np.abs(whole.lse)[:, None] * np.abs(f64(g))[:, None] * whole.p[:, :V] * scale * 1.01
+        assert_within(out, want, off + UNIT[F32] * (np.abs(want) + off), offset)
