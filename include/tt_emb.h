@@ -798,7 +798,7 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
                           void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * Log probabilities of tokens under z = scale * logits (0 < scale <= 1e30), logits [n_rows][V] of 32 or 16 bits:
+ * Log probabilities of tokens under z = scale * logits (1e-36 <= scale <= 1e30), logits [n_rows][V] of 32 or 16 bits:
  *   lse[r] = log(sum over the row of exp(z)),  logprob[r] = z[r][token r] - lse[r],  entropy[r] = lse[r] - sum of exp(z - lse) z.
  * A logit of -inf has no probability and adds nothing.  A row of nothing else: lse and logprob -inf, entropy 0.  A row with a NaN or +inf: NaN in
  * all three.  An lse that 32 bits do not hold is infinite; nothing else is taken from it.  A token outside [0, V) is no token: its logprob is 0.  tokens->L == n_rows.

@@ -1,7 +1,7 @@
 // Log probabilities of tokens under rows of logits, with entropy and the likeliest alternatives, and the gradient.
 //
-// One pass over a row holds the largest logit m so far, S = sum of exp(z - m) and T = sum of exp(z - m) (z - m) in 32 bits, and multiplies the two
-// sums when m grows; lse = m + log S, entropy = log S - T / S, both without a difference of large numbers.  Few rows are cut into
+// One pass over a row holds the largest logit m so far, S = sum of exp(z - m) and T = sum of exp(z - m) (z - m) / log 2 in 32 bits, and multiplies the two
+// sums when m grows; lse = m + log S, entropy = log S - T log 2 / S, both without a difference of large numbers.  Few rows are cut into
 // pieces, a workgroup each, which a second launch joins.
 // The k likeliest: the k-th largest of the threads' largest logits is no larger than the k-th largest of all, so that few more than k logits
 // are left to be ranked.  Logits are ordered by a 64-bit key, value first and column after it, so that no two are equal.
@@ -14,7 +14,7 @@ namespace tt {
 constexpr int LP_UNROLL = 4;                                 // vectors of eight logits a thread loads at a time
 constexpr int LP_LIST = 1024;                                // candidates that a workgroup can rank
 constexpr int LP_MOST_K = 64;
-constexpr float LP_LEAST = -3.402823466e38f, LOG2E = 1.4426950408889634f;
+constexpr float LP_LEAST = -3.402823466e38f, LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 struct LogprobArgs {
     const void *logits;
@@ -40,7 +40,7 @@ struct Sums {
 // the sums about another maximum, no smaller than theirs; 0 for what has none
 __device__ __forceinline__ Sums about(const Sums &a, float m, float c)
 {
-    const float d = fmaxf(a.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
+    const float d = fmaxf((a.m - m) * c, LP_LEAST), f = __builtin_amdgcn_exp2f(d);
     return {m, a.s * f, f == 0.f ? a.s * f : f * (a.t + d * a.s)};
 }
 
@@ -113,7 +113,7 @@ __device__ __forceinline__ void leave_row(const LogprobArgs &a, int64_t row, con
 {
     const bool none = r.s == 0.f;
     if (a.lse) a.lse[row] = none ? -INFINITY : r.m * a.scale + log_s;
-    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - a.scale * (r.t / r.s);
+    if (a.entropy) a.entropy[row] = none ? 0.f : log_s - LN2 * (r.t / r.s);
     if (a.logprob) a.logprob[row] = !given.there ? 0.f : none ? -INFINITY : a.scale * (given.z - r.m) - log_s;
 }
 
@@ -171,14 +171,14 @@ __device__ __forceinline__ Sums thread_sums(const T *line, int from, int to, int
 #pragma unroll
         for (int j = 0; j < 8; ++j) m = fmaxf(m, x[j]);
         if (m > r.m) {
-            const float d = fmaxf(r.m - m, LP_LEAST), f = __builtin_amdgcn_exp2f(d * c);
+            const float d = fmaxf((r.m - m) * c, LP_LEAST), f = __builtin_amdgcn_exp2f(d);
             if (ENTROPY) r.t = f == 0.f ? 0.f : f * (r.t + d * r.s);
             r.s *= f;
             r.m = m;
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const float d = x[j] - m, e = __builtin_amdgcn_exp2f(d * c);
+            const float d = (x[j] - m) * c, e = __builtin_amdgcn_exp2f(d);
             r.s += e;
             if (ENTROPY) r.t += e * fmaxf(d, LP_LEAST);
         }

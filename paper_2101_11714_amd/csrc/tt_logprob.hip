@@ -53,7 +53,8 @@ int check_floats(const float *p, const char *name) { return (uintptr_t)p % 4 ? f
 
 int check_scale(float scale)
 {
-    return scale > 0.f && scale <= 1e30f ? TT_OK : fail(TT_ERR_BAD_ARG, "scale must be positive, and 1e30 at most");
+    // (with less, logits whose difference 32 bits do not hold could both have a probability)
+    return scale >= 1e-36f && scale <= 1e30f ? TT_OK : fail(TT_ERR_BAD_ARG, "scale must be 1e-36 at least, and 1e30 at most");
 }
 
 }  // namespace

@@ -173,3 +173,20 @@ def test_an_lse_of_more_columns_than_the_row_has_is_taken_as_it_is():
         # (what the lse has lost as it is stored, and as much again for the product that it is taken from)
         off = off + 2 * U32 * np.abs(whole.lse)[:, None] * np.abs(f64(g))[:, None] * whole.p[:, :V] * scale * 1.01
         assert_within(out, want, off + UNIT[F32] * (np.abs(want) + off), offset)
+
+
+@pytest.mark.parametrize("scale", [1e-36, 1e-30, 1e-20, 1e30])
+@pytest.mark.parametrize("top", [0, 5])
+def test_scales_at_the_ends_of_their_range(scale, top):
+    # logits as far apart as that takes to tell them from each other
+    gr, scale = gen(3), float(np.float32(scale))
+    for rows, V, wide in [(3, 5, 3), (2, 1000, 3), (2, 20001, 3), (2, 20001, 0.5)]:
+        x = torch.randn((rows, V), generator=gr).double() * wide / scale
+        x = x.clamp(-3e38, 3e38).float().to(DEV)
+        tokens = torch.randint(0, V, (rows,), generator=gr).to(DEV)
+        lp, lse, ent = (torch.empty(rows, device=DEV) for _ in range(3))
+        ids = torch.empty((rows, top), dtype=torch.int64, device=DEV) if top else None
+        B.tt_token_logprob_fwd(x, tokens, lp, lse, entropy=ent, scale=scale, top_ids=ids)
+        r = Rows(x, scale)
+        for got, want, by in ((lse, r.lse, r.lse_bound()), (lp, r.log_p[np.arange(rows), tokens.cpu().numpy()], r.sum_bound()), (ent, r.entropy, r.entropy_bound())):
+            assert_within(got, want, by + 8 * U32 * np.abs(want), (rows, V))
