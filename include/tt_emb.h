@@ -775,7 +775,7 @@ typedef struct tt_rotation_t {
  * Norm of every head and rotation, of queries and keys in one call (k == NULL: of q alone):
  *   u = x * w / sqrt(mean of x^2 over the head + eps) (norm == 0: u = x),  output = u turned by its row's position (rotation == NULL: u).
  * weights: D values of any type, NULL for ones.  All arrays of heads have one type; heads may lie apart (parts of a product's wider
- * rows).  An output may be its input.  D up to 512.
+ * rows).  An output may be its input; else it may not overlap another array.  D up to 512.
  */
 int tt_qk_norm_rotate_fwd(const tt_heads_t *q, const tt_heads_t *k, const tt_rotation_t *rotation, int norm, float eps,
                           const void *q_weight, int32_t q_weight_type, const void *k_weight, int32_t k_weight_type,
@@ -785,7 +785,7 @@ int tt_qk_norm_rotate_fwd(const tt_heads_t *q, const tt_heads_t *k, const tt_rot
  * Gradients from the inputs q and k (not read where norm == 0; NULL then will do) and the outputs' gradients.  With g the gradient turned back and
  * r = 1 / sqrt(mean x^2 + eps):
  *   grad_x = r (g w - x r^2 mean(g w x)),   grad_weight = sum over rows and heads of g x r   (norm == 0: grad_x = g).
- * grad_q and grad_k may be the outputs' gradients.  grad_q_weight, grad_k_weight: D values of any type, NULL: not wanted; accumulate != 0 adds to them.
+ * grad_q and grad_k may be the outputs' gradients; the weights' gradients may not overlap each other.  grad_q_weight, grad_k_weight: D values of any type, NULL: not wanted; accumulate != 0 adds to them.
  * workspace: tt_qk_norm_rotate_bwd_workspace_bytes(n_rows, heads of q, heads of k, D) bytes, 16-byte aligned, if a weight's gradient is asked for
  * (enough for fewer rows and heads too).
  */

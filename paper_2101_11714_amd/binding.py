@@ -812,7 +812,7 @@ def tt_qk_norm_rotate_bwd(grad_q_output: torch.Tensor, grad_k_output: Optional[t
                           k_weight: Optional[torch.Tensor] = None, grad_q_weight: Optional[torch.Tensor] = None, grad_k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
                           accumulate: bool = False, workspace: Optional[torch.Tensor] = None) -> None:
     """Gradients from the forward pass's inputs q and k (None will do without a norm).  grad_q may be grad_q_output, grad_k grad_k_output;
-    accumulate adds to the weights' gradients."""
+    accumulate adds to the weights' gradients, which may not overlap each other."""
     rc = _call.qk_norm_rotate_bwd(grad_q_output, grad_k_output, q, k, grad_q, grad_k, rotation, norm, q_weight, k_weight, grad_q_weight, grad_k_weight, eps, accumulate, workspace)
     if rc:
         _check(rc)

@@ -217,6 +217,10 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
     a.add = accumulate;
     hipStream_t st = (hipStream_t)stream;
     int64_t grid = 0;
+    // (queries and keys have sums of their own, and of two that go to one place one would be lost)
+    const char *const gwq = (const char *)grad_q_weight, *const gwk = (const char *)grad_k_weight;
+    const bool apart = !gwq || !gwk || gwq + D * element_bytes(grad_q_weight_type) <= gwk || gwk + D * element_bytes(grad_k_weight_type) <= gwq;
+    auto overlap = [] { return fail(TT_ERR_BAD_ARG, "grad_q_weight and grad_k_weight overlap"); };
     if (some) {
         shape_of(a);
         slices_of(a);
@@ -228,6 +232,7 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
         const size_t need = weights && !alone ? (size_t)grid * (size_t)D * sizeof(float) : 0;
         if (need && (!workspace || workspace_bytes < need)) return fail(TT_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, workspace_bytes);
         if ((uintptr_t)workspace & 15) return fail(TT_ERR_BAD_ARG, "workspace must be 16-byte aligned");
+        if (!apart) return overlap();
         a.part = need ? (float *)workspace : nullptr;
         const size_t lds = weights ? (size_t)NWAVE * 16 * a.units * sizeof(float) : 0;
         with_type(type, [&](auto t) {
@@ -235,6 +240,8 @@ int tt_qk_norm_rotate_bwd(const tt_heads_t *grad_q_output, const tt_heads_t *gra
                 hipLaunchKernelGGL((rotate_bwd_kernel<decltype(t), decltype(nm)::value, decltype(whole)::value, decltype(nb)::value>), dim3((unsigned)grid), dim3(WG), lds, st, a);
             });
         });
+    } else if (!apart) {
+        return overlap();
     }
     if (weights && (a.part || !some)) hipLaunchKernelGGL(rotate_weight_kernel, dim3((unsigned)ceil_div(D, 32), 2), dim3(1024), 0, st, a, (int)grid);
     return launched("rotation gradient launch");
