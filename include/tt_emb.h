@@ -758,7 +758,7 @@ typedef struct tt_heads_t {
  * (one axis: text; time, height, width: images and video); the sections' sum is `pairs`, and a section may be 0.  Pair i is columns i and
  * pairs + i, or 2 i and 2 i + 1 (neighbours != 0).  A pair (u, v) becomes (u cos - v sin, v cos + u sin).
  * positions: axes x n_rows whole numbers of 32 or 64 bits (signed, any value up to 2^52 in size), row stride ld_positions between axes.
- * freqs: fp32 [pairs].  Angles are held in 64 bits.  Host struct, device data.
+ * freqs: fp32 [pairs].  An angle's fraction of a turn is exact to 2^-50, also of the farthest positions (freqs up to 1 in size).  Host struct, device data.
  */
 typedef struct tt_rotation_t {
     const void *positions;
