@@ -721,6 +721,7 @@ enum {
  * bias: N values of any type, NULL for none.  residual: NULL for none.  pre: z, stored for the gradient (NULL: not).
  * Types: weight and pre x's; output x's or 32 bits; residual the output's.  output may be residual, at the same stride; else neither output nor pre may overlap another array.
  * workspace: tt_linear_fwd_workspace_bytes(n_rows, K, N, x's type, whole) bytes, 16-byte aligned (0: none is needed; enough for fewer rows too).
+ * A call is content with what it uses itself, which may be less or nothing.
  * whole != 0: x and the weight have K and strides of multiples of 8 (strides up to 2^22) and 16-byte aligned addresses, or 32 bits; others may be copied.
  * K and N up to 2^22.  K == 0 is valid: z = bias.
  */
@@ -736,8 +737,8 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
  * needs it.  Types: x, weight, pre and grad_x grad_output's; grad_weight that or 32 bits; grad_bias any.  dz is rounded to that type
  * before the products where there is an activation (not before its sums over the rows).  accumulate != 0 adds to grad_weight and grad_bias.
  * No output may overlap another array.
- * workspace: tt_linear_bwd_workspace_bytes(n_rows, K, N, type, activation, whole) bytes, 16-byte aligned (enough for fewer rows and fewer gradients too).
- * whole: as above, of N and of grad_output's rows too.
+ * workspace: tt_linear_bwd_workspace_bytes(n_rows, K, N, type, activation, whole) bytes, 16-byte aligned (enough for fewer rows and fewer gradients too;
+ * a call is content with what it uses itself).  whole: as above, of N and of grad_output's rows too.
  */
 size_t tt_linear_bwd_workspace_bytes(int64_t n_rows, int64_t K, int64_t N, int32_t type, int32_t activation, int whole);
 int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_rows_t *weight, const tt_rows_t *pre, int32_t activation,

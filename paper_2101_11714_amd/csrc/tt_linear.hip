@@ -39,18 +39,26 @@ int check_workspace(size_t need, const void *workspace, size_t bytes)
 
 size_t up(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// Where what lies in the workspace of a product: parts of sums, copies of x and of the weight in whole chunks where they are not.
+// Where what lies in the workspace of a product: parts of sums, copies of x and of the weight in whole chunks where they are not.  The parts' room is the
+// call's own by its plan; a query's, which is to do for fewer rows and so for any plan, is product_bytes.
 struct Room {
     bool few;                    // (few rows are loaded as they lie)
     size_t parts, x, w, all;
 };
 
-Room product_room(int64_t M, int64_t K, int64_t N, int32_t type, bool whole_x, bool whole_w)
+Room product_room(int64_t M, int64_t K, int64_t N, int32_t type, bool whole_x, bool whole_w, Product *call = nullptr)
 {
     Room r{};
     r.few = few_rows(M, N, K, type, whole_x && whole_w);
     if (r.few) return r;
-    r.parts = up(product_bytes(M, N, K, type));
+    if (call) {
+        double us;
+        const Size d{M, N, K};
+        call->kind = plan_of(&d, 1, type, &call->plan, us);
+        r.parts = up(parts_bytes(d, call->plan));
+    } else {
+        r.parts = up(product_bytes(M, N, K, type));
+    }
     r.x = whole_x ? 0 : up(packed_bytes(M, K, type));
     r.w = whole_w ? 0 : up(packed_bytes(N, K, type));
     r.all = r.parts + r.x + r.w;
@@ -64,11 +72,11 @@ struct GradRoom {
     int64_t band, n_bands;
 };
 
-GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, bool copy_x, bool copy_w, bool x, bool w, bool b)
+GradRoom grad_room(int64_t M, int64_t K, int64_t N, int32_t type, bool copy, bool copy_x, bool copy_w, bool x, bool w, bool b, const Product *dx = nullptr, const Product *dw = nullptr)
 {
     GradRoom r{};
-    r.parts_x = x ? up(product_bytes(M, K, N, type)) : 0;
-    r.parts_w = w ? up(product_bytes(N, K, M, type)) : 0;
+    r.parts_x = dx ? up(parts_bytes(dx->d, dx->plan)) : x ? up(product_bytes(M, K, N, type)) : 0;
+    r.parts_w = dw ? up(parts_bytes(dw->d, dw->plan)) : w ? up(product_bytes(N, K, M, type)) : 0;
     r.dz = copy && (x || w) ? up(packed_bytes(M, N, type)) : 0;
     r.x = copy_x ? up(packed_bytes(M, K, type)) : 0;
     r.w = copy_w ? up(packed_bytes(N, K, type)) : 0;
@@ -111,12 +119,16 @@ int tt_linear_fwd(const tt_rows_t *x, const tt_rows_t *weight, const void *bias,
     if (residual && residual->type != output->type) return fail(TT_ERR_UNSUPPORTED, "residual has the output's type");
     if (pre && pre->type != x->type) return fail(TT_ERR_UNSUPPORTED, "pre has x's type");
     if (activation < 0 || activation >= ACT_COUNT) return fail(TT_ERR_BAD_ARG, "activation %d", (int)activation);
-    const Room room = product_room(n_rows, K, N, x->type, whole_chunks(*x, K), whole_chunks(*weight, K));
+    Product p{};
+    const Room room = product_room(n_rows, K, N, x->type, whole_chunks(*x, K), whole_chunks(*weight, K), &p);
     if ((rc = check_workspace(room.all, workspace, workspace_bytes))) return rc;
     char *ws = (char *)workspace;
-    const Operand a{x->data, x->ld, n_rows, K, room.x ? ws + room.parts : nullptr}, b{weight->data, weight->ld, N, K, room.w ? ws + room.parts + room.x : nullptr};
-    const EpilogueArgs e{bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
-    const Product p{a, b, {n_rows, N, K}, e, (float *)ws, room.few};
+    p.a = {x->data, x->ld, n_rows, K, room.x ? ws + room.parts : nullptr};
+    p.b = {weight->data, weight->ld, N, K, room.w ? ws + room.parts + room.x : nullptr};
+    p.d = {n_rows, N, K};
+    p.e = {bias, bias_type, activation, residual ? residual->data : nullptr, pre ? pre->data : nullptr, output->data, residual ? residual->ld : 0, pre ? pre->ld : 0, output->ld};
+    p.parts = (float *)ws;
+    p.few = room.few;
     with_type(x->type, [&](auto t) { rc = product_of<decltype(t)>(output->type, p, (hipStream_t)stream); });
     return rc;
 }
@@ -153,7 +165,17 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
     if ((rc = check_vector(grad_bias, "grad_bias", grad_bias_type))) return rc;
     const bool copy = activation != TT_ACT_NONE || !whole_chunks(*grad_output, N);
     const bool copy_x = grad_weight && !whole_chunks(*x, K), copy_w = grad_x && !whole_chunks(*weight, K);
-    const GradRoom room = grad_room(n_rows, K, N, type, copy, copy_x, copy_w, grad_x != nullptr, grad_weight != nullptr, grad_bias != nullptr);
+    Product dx{}, dw{};
+    const bool some_w = grad_weight && !(accumulate && n_rows == 0);             // (else there is nothing to add)
+    if (grad_x) dx.d = {n_rows, K, N};
+    if (some_w) dw.d = {N, K, n_rows};
+    const Size sizes[2] = {dx.d, dw.d};
+    Plan plans[2];
+    double us;
+    dx.kind = dw.kind = plan_of(sizes, 2, type, plans, us);
+    dx.plan = plans[0];
+    dw.plan = plans[1];
+    const GradRoom room = grad_room(n_rows, K, N, type, copy, copy_x, copy_w, grad_x != nullptr, grad_weight != nullptr, grad_bias != nullptr, &dx, &dw);
     if ((rc = check_workspace(room.all, workspace, workspace_bytes))) return rc;
     hipStream_t st = (hipStream_t)stream;
     char *ws = (char *)workspace;
@@ -166,19 +188,16 @@ int tt_linear_bwd(const tt_rows_t *grad_output, const tt_rows_t *x, const tt_row
         dz = at_dz;
         ld_dz = 8 * ceil_div(N, 8);
     }
-    Product dx{}, dw{};
     if (grad_x) {
         dx.a = {dz, ld_dz, n_rows, N, nullptr};
         dx.b = {weight->data, weight->ld, N, K, copy_w ? at_w : nullptr};
-        dx.d = {n_rows, K, N};
         dx.e.out = grad_x->data;
         dx.e.ld_out = grad_x->ld;
         dx.parts = (float *)ws;
     }
-    if (grad_weight && !(accumulate && n_rows == 0)) {
+    if (some_w) {
         dw.a = {dz, ld_dz, n_rows, N, nullptr};
         dw.b = {x->data, x->ld, n_rows, K, copy_x ? at_x : nullptr};
-        dw.d = {N, K, n_rows};
         dw.e.out = grad_weight->data;
         dw.e.ld_out = grad_weight->ld;
         if (accumulate) {

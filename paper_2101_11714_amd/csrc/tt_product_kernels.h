@@ -72,13 +72,11 @@ int launch_product(Product x, hipStream_t st)
         return launched("product launch");
     }
     if constexpr (sizeof(T) == 2) pack<T>(x.a, x.b, st);
-    Plan p;
-    double us;
-    const int kind = plan_of(&d, 1, sizeof(T) == 4 ? TT_F32 : TT_BF16, &p, us);
+    const Plan &p = x.plan;
     const ProductArgs q = args_of(x, p);
     int rc = TT_OK;
     const dim3 grid = grid_of(p.tiles_m * p.tiles_n * p.parts, 512);
-    with_kind<T>(kind, [&](auto size) {
+    with_kind<T>(x.kind, [&](auto size) {
         constexpr int TILE = decltype(size)::value;
         if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((product_kernel<T, O, TILE>), grid, dim3(WG), 0, st, q, x.e);
         else rc = launch_stream<product_stream_kernel<T, O, TILE == 256>>(grid, StreamShape<TILE == 256>::THREADS, StreamShape<TILE == 256>::LDS, st, q, x.e);
@@ -92,15 +90,12 @@ template <typename T, typename W>
 int launch_gradients(Product dx, Product dw, const BiasSum &b, hipStream_t st)
 {
     if constexpr (sizeof(T) == 2) pack<T>(dx.b, dw.b, st);
-    const Size d[2] = {dx.d, dw.d};
-    Plan p[2];
-    double us;
-    const int kind = plan_of(d, 2, sizeof(T) == 4 ? TT_F32 : TT_BF16, p, us);
-    PairArgs g{{args_of(dx, p[0]), args_of(dw, p[1])}, {dx.e, dw.e}, p[1].k_part > p[0].k_part, {p[0].tiles_m * p[0].tiles_n * p[0].parts, p[1].tiles_m * p[1].tiles_n * p[1].parts}};
+    const Plan &px = dx.plan, &pw = dw.plan;
+    PairArgs g{{args_of(dx, px), args_of(dw, pw)}, {dx.e, dw.e}, pw.k_part > px.k_part, {px.tiles_m * px.tiles_n * px.parts, pw.tiles_m * pw.tiles_n * pw.parts}};
     int rc = TT_OK;
     const dim3 grid = grid_of(g.wgs[0] + g.wgs[1], 512);
     if (g.wgs[0] + g.wgs[1] > 0)
-        with_kind<T>(kind, [&](auto size) {
+        with_kind<T>(dx.kind, [&](auto size) {
             constexpr int TILE = decltype(size)::value;
             if constexpr (sizeof(T) == 4) hipLaunchKernelGGL((pair_kernel<T, W, TILE>), grid, dim3(WG), 0, st, g);
             else rc = launch_stream<pair_stream_kernel<T, W, TILE == 256>>(grid, StreamShape<TILE == 256>::THREADS, StreamShape<TILE == 256>::LDS, st, g);

@@ -112,7 +112,10 @@ inline bool few(int rows_class, int64_t N, int64_t K, int32_t type, bool whole)
 
 inline bool few_rows(int64_t M, int64_t N, int64_t K, int32_t type, bool whole) { return M <= PF_MOST && few(M <= 16 ? 0 : M <= 32 ? 1 : 2, N, K, type, whole); }
 
-// What the parts' sums of a product of M rows, or of fewer, take at most, whatever its way: with more rows there are fewer parts, but no more than
+// What the parts' sums of a product take: nothing where it has one part, whose sums go through the epilogue.
+inline size_t parts_bytes(const Size &d, const Plan &p) { return p.parts > 1 ? (size_t)p.parts * (size_t)d.M * (size_t)(8 * ceil_div(d.N, 8)) * sizeof(float) : 0; }
+
+// What they take at most for M rows, or for fewer, whatever the product's way: with more rows there are fewer parts, but no more than
 // 256 wide tiles' or MOST_TILES narrow ones' worth of rows, or twice as many of 64 columns.
 inline size_t product_bytes(int64_t M, int64_t N, int64_t K, int32_t type)
 {
@@ -169,7 +172,9 @@ struct Product {
     Size d;
     EpilogueArgs e;
     float *parts;
-    bool few;                    // by the kernel of few rows
+    bool few;                    // by the kernel of few rows, else
+    int kind;                    // by tiles of this kind (a gradient's two products: the same), as planned
+    Plan plan;
 };
 
 // x W^T by the kernels of type T (out_type: T or 32 bits), and the gradients dz W and dz^T x with what is left to do for the bias (w_type: of the second).
