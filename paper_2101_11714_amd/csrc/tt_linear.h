@@ -17,6 +17,9 @@ struct SlopeArgs {
     int groups;                  // workgroups of a band; those behind them copy the products' other operands
 };
 
+// dz is rounded to the operands' type, which the matrix cores take for both operands alike; the bias's sums take it as it is.  In 16 bits that makes the gradients'
+// relative error 0.0023 where their own last rounding alone is 0.0017 (bfloat16, 8,192 x 4,096 x 4,096); dz as the sum of two such numbers would double the
+// products, 424 of 456 us.  Who needs more has the call in 32 bits.
 // 32 vectors of eight columns x 8 rows per workgroup at a time, down a band of rows; bound by memory (8,192 x 4,096 in 16 bits with SiLU 45 us, 4.5 TB/s).
 template <typename T, bool WHOLE, bool ACT>
 __global__ __launch_bounds__(256) void slope_kernel(SlopeArgs a, PackArgs p)

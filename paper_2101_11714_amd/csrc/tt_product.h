@@ -30,8 +30,9 @@ __device__ __forceinline__ float logistic_slope(float z, float &p)
 }
 
 // The normal distribution up to z, and exp(-z^2 / 2): for -|z| that is exp(-z^2 / 2) u P(u), u = 1 / (1 + |z| / 4), with a polynomial of degree 9 whose
-// largest error relative to u P(u) = exp(z^2 / 2) erfc(|z| / sqrt 2) / 2 is 0.6 times 2^-24 (fitted by least squares that were weighted until the errors' peaks
-// were alike).  In 32 bits 4 times 2^-24 of the whole, most of it from the polynomial's sum; no branches, which the library's error function has.
+// largest error relative to u P(u) = exp(z^2 / 2) erfc(|z| / sqrt 2) / 2 is 0.75 times 2^-24 with its coefficients in 32 bits (fitted by least squares that were
+// weighted until the errors' peaks were alike).  Computed in 32 bits it is off by up to 3.4 times 2^-24 as such, most of it from the polynomial's sum, and in the
+// tail by up to (z^2 + 8) 2^-24 of itself, since the exponential's argument is rounded; no branches, which the library's error function has.
 __device__ __forceinline__ float normal_to(float z, float &e)
 {
     constexpr float P[10] = {0.0997355655f, 0.0997364372f, 0.0934662372f, 0.0816042423f, 0.0589695089f, 0.0637153611f, -0.0317454860f, 0.0956253558f, -0.0808927864f, 0.0197855458f};

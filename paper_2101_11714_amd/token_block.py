@@ -4,7 +4,7 @@ Tokens go two ways.  An uncompressed table gives each token its row, scaled and 
 10 M rows in TT format gives a row to each pair of neighbouring tokens (their numbers, hashed): a branch that is added to the stream
 under dropout.  The sum is normalised.  Training fits the result to a fixed vector per following token by least squares, and
 updates the table's used rows, the cores and the norm's weight; serving takes one token of each sequence and leaves the result in
-8 bits with a scale per row, as a following matrix product in 8 bits reads it.
+8 bits with a scale per row, as matrix products in 8 bits take it (those of this package take 32 and 16 bits).
 
 With the loss "likelihood" the result is multiplied with a row per token of the vocabulary instead, and training raises the log probability of
 the token that follows.
