@@ -18,7 +18,7 @@ constexpr float GELU_TANH_SCALE = 0.7978845608028654f, GELU_TANH_CUBE = 0.044715
 
 // By the device's exponential of 2 and reciprocal, which are off by a unit in the last place: the product z log2(e) is rounded, so that exp(-z) is off by
 // |z| 2^-24 of itself and the result by a third of 2^-24 for that (a library's exponential and a true quotient: gradients through an activation,
-// 8,192 x 4,096, 52 instead of 38 us).  Where the exponential passes 2^128 its reciprocal is 0, as it should be.  (1 + tanh(u)) / 2 is this function of 2 u.
+// 8,192 x 4,096, 52 instead of 38 us).  Where the exponential passes 2^128, below z = -88.7, its reciprocal is 0, and SiLU, which is above -3e-37 there, too.  (1 + tanh(u)) / 2 is this function of 2 u.
 __device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-1.4426950408889634f * z)); }
 
 // its slope p (1 - p), without the difference (which is off by 2^-24 as such: 35 times that in the other functions' slopes), and p itself
