@@ -411,7 +411,7 @@ __global__ __launch_bounds__(WG) void logprob_bwd_kernel(LogprobGradArgs a)
     const float c = a.scale * LOG2E;
     const Sums r = workgroup_sums(thread_sums<T, false, WHOLE, 1>(line, 0, a.nv, a.V, c), waves, c);
     const float log_r = logf(r.s), own = r.m * a.scale + log_r;
-    const bool same = r.s > 0.f && (own == lse || fabsf(own - lse) <= fabsf(lse) * 0x1p-22f);            // (sums in another order: a unit of the last place)
+    const bool same = r.s > 0.f && (own == lse || fabsf(own - lse) < fabsf(lse) * 0x1p-22f);            // (sums in another order: a unit of the last place; < is false of infinities)
     const float m = same ? r.m : 0.f, log_s = same ? log_r : lse;
     each_vector<T, WHOLE, 1>(line, 0, a.nv, a.V, [&](int v, float (&x)[8]) { leave(v, x, m, log_s, !same && lse == -INFINITY); });
 }

@@ -190,3 +190,19 @@ def test_scales_at_the_ends_of_their_range(scale, top):
         r = Rows(x, scale)
         for got, want, by in ((lse, r.lse, r.lse_bound()), (lp, r.log_p[np.arange(rows), tokens.cpu().numpy()], r.sum_bound()), (ent, r.entropy, r.entropy_bound())):
             assert_within(got, want, by + 8 * U32 * np.abs(want), (rows, V))
+
+
+@pytest.mark.parametrize("V", [5, 1000, 9001])
+def test_an_infinite_lse_that_is_not_the_row_s_is_taken_as_it_is(V):
+    # +inf: no column has a probability; -inf: no gradient
+    gr, rows = gen(V), 6
+    x = (torch.randn((rows, V), generator=gr) * 2).to(DEV)
+    x[3:] += 30000.0
+    tokens = torch.randint(0, V, (rows,), generator=gr).to(DEV)
+    g, ge = torch.randn(rows, generator=gr).to(DEV), torch.ones(rows, device=DEV)
+    for value in (math.inf, -math.inf):
+        out, _, _, _ = run(x, tokens, g, ge, 1.5, False, torch.full((rows,), value, device=DEV))
+        want = torch.zeros_like(x)
+        if value > 0:
+            want[torch.arange(rows, device=DEV), tokens] = g * 1.5
+        assert torch.equal(out, want), value
